@@ -18,6 +18,7 @@
 
 #include "bct_device.h"
 #include "bct_linear.h"
+#include "bct_model_internal.h"
 
 namespace bct {
 
@@ -312,15 +313,6 @@ __global__ __launch_bounds__(256) void argmax_kernel(const uint16_t* logits, int
 
 thread_local char g_merr[256] = "";
 
-bct_status mfail(bct_status s, const char* msg) {
-  snprintf(g_merr, sizeof(g_merr), "%s", msg);
-  return s;
-}
-bct_status launched(const char* what, hipError_t e = hipGetLastError()) {
-  if (e == hipSuccess) return BCT_OK;
-  snprintf(g_merr, sizeof(g_merr), "%s launch failed: %s", what, hipGetErrorString(e));
-  return BCT_ERR_HIP;
-}
 // The form of a size, by what it measured: us, kGainsWithRow | kGainsLate | kChunkByChunk, the same buffers again and again
 // (x and out in the last-level cache where they fit) / buffers from memory.
 // Row-major outputs: 4096 x 4096 11.5 | 12.0 | 12.2 / 14.1 | 14.6 | 14.8; 16384 x 2048 20.8 | 21.3 | - / 24.2 | 25.2 | -; 16384 x
@@ -341,8 +333,6 @@ RmsForm rmsnorm_form(uint32_t rows, uint32_t dim, bool out_tiled) {
   return dim <= 6144 && n >= (dim <= 5120 ? 48 : 128) * M ? kChunkByChunk : kGainsWithRow;
 }
 
-bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
 bct_status check_linear(const void* x, const void* w, const void* out, uint32_t rows, uint32_t K, uint32_t N) {
   if (!x || !w || !out || rows == 0 || K == 0 || N == 0) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
   if (K % 32 != 0 || N % 16 != 0) return mfail(BCT_ERR_UNSUPPORTED, "K must be a multiple of 32 and N of 16");
@@ -351,6 +341,17 @@ bct_status check_linear(const void* x, const void* w, const void* out, uint32_t 
 }
 
 }  // namespace
+
+bct_status mfail(bct_status s, const char* msg) {
+  snprintf(g_merr, sizeof(g_merr), "%s", msg);
+  return s;
+}
+bct_status launched(const char* what, hipError_t e) {
+  if (e == hipSuccess) return BCT_OK;
+  snprintf(g_merr, sizeof(g_merr), "%s launch failed: %s", what, hipGetErrorString(e));
+  return BCT_ERR_HIP;
+}
+
 }  // namespace bct
 
 using namespace bct;

@@ -15,7 +15,7 @@ from . import binding
 from .binding import BCT_OK, BctCache, BctError, _dptr, _launch, _torch
 
 MODEL_EXPORTS = ["bctm_embed", "bctm_rmsnorm", "bctm_pack_weight", "bctm_pack_rows", "bctm_linear", "bctm_linear_split",
-                 "bctm_swiglu", "bctm_linear_plan", "bctm_linear_tile",
+                 "bctm_swiglu", "bctm_linear_plan", "bctm_linear_tile", "bctm_qk_norm_rope",
                  "bctm_argmax", "bctm_last_error"]
 
 BCTM_KERNEL_STREAMING, BCTM_KERNEL_STREAMING_WIDE, BCTM_KERNEL_TILE128, BCTM_KERNEL_TILE256 = 0, 1, 2, 3
@@ -23,6 +23,8 @@ BCTM_KERNEL_STREAMING_TRIPLE = 4
 
 BCTM_X_TILED = 1
 BCTM_OUT_TILED = 2
+BCTM_HEAD_NORM = 4
+BCTM_ROPE_INTERLEAVED = 8
 
 _ready = False
 
@@ -43,6 +45,8 @@ def mlib() -> ctypes.CDLL:
     L.bctm_swiglu.argtypes = [vp, vp, vp, vp, u32, u32, u32, u32, vp]
     L.bctm_linear_plan.argtypes = [u32, u32, u32, u32, ctypes.POINTER(u32)]
     L.bctm_linear_tile.argtypes = [u32, u32, u32, u32, u32] + [ctypes.POINTER(u32)] * 3
+    L.bctm_qk_norm_rope.argtypes = [vp, vp, vp, u32, u32, u32] * 2 + [vp, vp, u32, u32, u32, ctypes.c_float, ctypes.c_int32, u32,
+                                                                      vp]
     L.bctm_argmax.argtypes = [vp, vp, u32, u32, vp]
     for n in MODEL_EXPORTS[:-1]:
         getattr(L, n).restype = ctypes.c_int
@@ -152,6 +156,63 @@ def bctm_rmsnorm(x, gain, eps, out=None, tiled=False):
     _ck(_launch(mlib().bctm_rmsnorm, x.device, _dptr(x), _dptr(gain), _dptr(dst), x.shape[0], x.shape[1],
                 eps, BCTM_OUT_TILED if tiled else 0), "bctm_rmsnorm")
     return out
+
+
+def _heads(t, name, like=None):
+    """t [rows][heads][d] with contiguous heads, its rows at any distance (a part of a wider row)."""
+    torch = _torch()
+    want = (torch.float32, torch.bfloat16) if like is None else (like.dtype,)
+    if t.dtype not in want or t.dim() != 3 or not t.is_cuda or t.stride(2) != 1 or \
+            (t.shape[1] > 1 and t.stride(1) != t.shape[2]) or (like is not None and t.device != like.device):
+        raise ValueError(f"{name}: expected [rows][heads][d] heads side by side"
+                         + (", float32 or bf16, on the GPU" if like is None else f", {like.dtype} on {like.device}")
+                         + f", got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+    # the distance of a single row is not looked at
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
+
+
+def bctm_qk_norm_rope(q, k=None, q_gain=None, k_gain=None, eps=None, positions=None, inv_freq=None, interleaved=False,
+                      q_out=None, k_out=None):
+    """Queries [rows][Hq][d] and write queries [rows][Hkv][d] (or None): each head normalised (eps given) and turned by its
+    row's position (positions int32 [rows] with inv_freq float64 [rotary_dim / 2], radians per position) -> (q_out, k_out).
+    q and k may be parts of wider rows; q_out=q and k_out=k work in place."""
+    torch = _torch()
+    ldq = _heads(q, "q")
+    rows, hq, d = q.shape
+    if q_out is None:
+        q_out = torch.empty((rows, hq, d), dtype=q.dtype, device=q.device)
+    ldqo = _heads(q_out, "q_out", q)
+    hk = ldk = ldko = 0
+    if k is not None:
+        ldk = _heads(k, "k", q)
+        if k.shape[0] != rows or k.shape[2] != d:
+            raise ValueError("k: one row per row of q, heads of the same size")
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+        ldko = _heads(k_out, "k_out", q)
+        hk = k.shape[1]
+    if q_out.shape != q.shape or (k is None) != (k_out is None) or (k is not None and k_out.shape != k.shape):
+        raise ValueError("q_out / k_out: the shapes of q / k")
+    for g, n in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+        if g is not None and (g.dtype != q.dtype or g.shape != (d,) or not g.is_contiguous() or g.device != q.device):
+            raise ValueError(f"{n}: expected a contiguous {q.dtype} vector of {d} on {q.device}")
+    if (positions is None) != (inv_freq is None):
+        raise ValueError("positions and inv_freq: both or neither")
+    rot = 0
+    if positions is not None:
+        if positions.dtype != torch.int32 or positions.shape != (rows,) or not positions.is_contiguous() or \
+                positions.device != q.device:
+            raise ValueError(f"positions: expected a contiguous int32 vector of {rows} on {q.device}")
+        if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.device != q.device:
+            raise ValueError(f"inv_freq: expected a contiguous float64 vector on {q.device}")
+        rot = 2 * inv_freq.numel()
+    if eps is not None and not eps >= 0:
+        raise ValueError("eps must not be negative")
+    flags = (BCTM_HEAD_NORM if eps is not None else 0) | (BCTM_ROPE_INTERLEAVED if interleaved else 0)
+    _ck(_launch(mlib().bctm_qk_norm_rope, q.device, _dptr(q), _dptr(q_out), _dptr(q_gain), hq, ldq, ldqo, _dptr(k), _dptr(k_out),
+                _dptr(k_gain), hk, ldk, ldko, _dptr(positions), _dptr(inv_freq), rot, rows, d, eps or 0.0,
+                binding.BCT_F32 if q.dtype == torch.float32 else binding.BCT_BF16, flags), "bctm_qk_norm_rope")
+    return q_out, k_out
 
 
 class PackedWeight:

@@ -1,0 +1,186 @@
+"""bctm_qk_norm_rope against its formula in 64 bits (angles in numpy's longdouble).
+
+Tolerance of an element y of the pair (a, b) before the turn: one rounding to the storage type, eps / 2 * |y| (bf16 2^-8, fp32
+2^-24); and the fp32 arithmetic, in units of 2^-24 * (|a| + |b|): the sum of squares of at most 256 elements adds 2 E <= 16 terms
+in a chain and up to five levels of a butterfly, 21, halved by the root, 11; division, addition, root and reciprocal 4; times
+r and gain 2; sine and cosine 2 (their series' last step and 2e-9 of its rest); product and sum 2: 21.  The angle: 3 roundings of
+2^-53 of its own size.  32 for all of it."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def M():
+    from paper_2411_15785_amd import model
+    model.mlib()
+    return model
+
+
+def freqs(rot, base=10000.0):
+    return torch.tensor([base ** (-2.0 * j / rot) for j in range(rot // 2)], dtype=torch.float64)
+
+
+def reference(x, gain, eps, pos, freq, interleaved):
+    """x [rows][H][d] float64 -> (y, its error allowance of fp32 arithmetic)."""
+    y = np.array(x, dtype=np.longdouble)
+    if eps is not None:
+        y = y / np.sqrt(np.mean(y * y, axis=-1, keepdims=True) + np.longdouble(np.float32(eps)))
+        if gain is not None:
+            y = y * gain
+    slack = np.abs(y) * 32 * 2.0 ** -24
+    if pos is not None:
+        n = len(freq)
+        t = np.asarray(pos, np.longdouble)[:, None, None] * np.asarray(freq, np.longdouble)
+        c, s = np.cos(t), np.sin(t)
+        ia, ib = (np.arange(0, 2 * n, 2), np.arange(1, 2 * n, 2)) if interleaved else (np.arange(n), np.arange(n) + n)
+        a, b = y[..., ia].copy(), y[..., ib].copy()
+        y[..., ia], y[..., ib] = a * c - b * s, a * s + b * c
+        both = (np.abs(a) + np.abs(b)) * (32 * 2.0 ** -24 + 3 * 2.0 ** -53 * np.abs(t))
+        slack[..., ia] = both
+        slack[..., ib] = both
+    return y, slack
+
+
+def check(got, x, gain, eps, pos, freq, interleaved, dtype, what):
+    f = lambda t: None if t is None else t.detach().cpu().double().numpy()
+    y, slack = reference(f(x), f(gain), eps, f(pos), f(freq), interleaved)
+    err = np.abs(f(got).astype(np.longdouble) - y)
+    tol = HALF[dtype] * np.abs(y) * 1.001 + slack
+    assert np.all(err <= tol), f"{what}: worst {np.max(err / np.maximum(tol, 1e-30)):.2f} of the tolerance"
+
+
+def draw(shape, dtype, seed, std=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * std).to(DT[dtype]).cuda()
+
+
+SHAPES = [  # rows, Hq, Hkv, d, rotary_dim
+    (1, 1, 1, 16, 16), (1, 32, 32, 128, 128), (3, 4, 1, 64, 64), (33, 32, 8, 128, 64), (257, 12, 4, 64, 32), (5, 3, 3, 80, 80),
+    (7, 5, 1, 96, 48), (130, 8, 2, 256, 256), (2, 7, 7, 112, 16), (1000, 16, 16, 128, 128), (40, 2, 1, 176, 160),
+    (4100, 8, 8, 64, 64),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rows,Hq,Hkv,d,rot", SHAPES)
+def test_norm_and_rotation(M, rows, Hq, Hkv, d, rot, interleaved, dtype):
+    q, k = draw((rows, Hq, d), dtype, 1), draw((rows, Hkv, d), dtype, 2, 3.0)
+    gq, gk = draw((d,), dtype, 3), draw((d,), dtype, 4)
+    pos = torch.randint(0, 40000, (rows,), generator=torch.Generator().manual_seed(5), dtype=torch.int32).cuda()
+    fr = freqs(rot).cuda()
+    q0, k0 = q.clone(), k.clone()
+    qo, ko = M.bctm_qk_norm_rope(q, k, gq, gk, 1e-6, pos, fr, interleaved)
+    check(qo, q0, gq, 1e-6, pos, fr, interleaved, dtype, "q")
+    check(ko, k0, gk, 1e-6, pos, fr, interleaved, dtype, "k")
+    assert torch.equal(q, q0) and torch.equal(k, k0)
+    again = M.bctm_qk_norm_rope(q, k, gq, gk, 1e-6, pos, fr, interleaved, q_out=q, k_out=k)   # in place: the same bits
+    assert again[0] is q and torch.equal(q, qo) and torch.equal(k, ko)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_each_part_alone(M, dtype):
+    q, k = draw((19, 6, 128), dtype, 1), draw((19, 2, 128), dtype, 2)
+    g, pos, fr = draw((128,), dtype, 3), torch.arange(19, dtype=torch.int32).cuda() * 1000, freqs(128).cuda()
+    for interleaved in (False, True):     # a rotation alone
+        qo, ko = M.bctm_qk_norm_rope(q, k, positions=pos, inv_freq=fr, interleaved=interleaved)
+        check(qo, q, None, None, pos, fr, interleaved, dtype, "rotation q")
+        check(ko, k, None, None, pos, fr, interleaved, dtype, "rotation k")
+    qo, ko = M.bctm_qk_norm_rope(q, k, q_gain=g, eps=1e-5)     # a norm alone, k without a gain
+    check(qo, q, g, 1e-5, None, None, False, dtype, "norm q")
+    check(ko, k, None, 1e-5, None, None, False, dtype, "norm k")
+    qo, ko = M.bctm_qk_norm_rope(q, None, q_gain=g, eps=1e-5, positions=pos, inv_freq=fr)   # queries alone
+    assert ko is None
+    check(qo, q, g, 1e-5, pos, fr, False, dtype, "q alone")
+
+
+def test_far_and_negative_positions(M):
+    """Angles of any int32 position: what 32 bits would lose."""
+    at = [0, 1, -1, 4095, 1 << 20, (1 << 20) + 1, -(1 << 24) - 3, (1 << 31) - 1, -(1 << 31), 123456789]
+    pos, fr = torch.tensor(at, dtype=torch.int32).cuda(), freqs(128, 500000.0).cuda()
+    q = draw((len(at), 2, 128), "f32", 7)
+    qo, _ = M.bctm_qk_norm_rope(q, positions=pos, inv_freq=fr)
+    check(qo, q, None, None, pos, fr, False, "f32", "far positions")
+    assert torch.equal(qo[0], q[0])      # position 0: nothing is turned
+
+
+def test_quarter_turns_and_zero_heads(M):
+    """Angles on and next to the borders of the quarter turns; heads of zeros stay zeros; an infinity or a NaN stays in its head."""
+    quarter = np.pi / 2
+    fr = torch.tensor([quarter, quarter / 2, quarter * (1 + 2.0 ** -40), quarter * 1.5, 3 * quarter, 4 * quarter, 1e-9, 0.0],
+                      dtype=torch.float64).cuda()
+    pos = torch.arange(-4, 13, dtype=torch.int32).cuda()
+    q = draw((17, 3, 16), "f32", 8)
+    q[:, 1] = 0
+    qo, _ = M.bctm_qk_norm_rope(q, eps=1e-6, positions=pos, inv_freq=fr)
+    check(qo, q, None, 1e-6, pos, fr, False, "f32", "quarter turns")
+    assert torch.count_nonzero(qo[:, 1]) == 0
+    bad = q.clone()
+    bad[3, 2, 5] = float("inf")
+    bad[4, 0, 0] = float("nan")
+    got, _ = M.bctm_qk_norm_rope(bad, eps=1e-6, positions=pos, inv_freq=fr)
+    keep = torch.ones((17, 3), dtype=torch.bool)
+    keep[3, 2] = keep[4, 0] = False
+    assert torch.equal(got[keep.cuda()], qo[keep.cuda()])
+    # an infinity behind the rotated part makes no NaN of what is turned, nor the other way round
+    part, _ = M.bctm_qk_norm_rope(torch.cat([q, torch.full_like(q, float("inf"))], 2), positions=pos, inv_freq=fr)
+    check(part[..., :16], q, None, None, pos, fr, False, "f32", "beside infinities")
+    assert torch.all(torch.isinf(part[..., 16:]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_parts_of_wider_rows(M, dtype):
+    """Heads taken out of a projection's rows where they lie, written into rows of another width; what lies between stays."""
+    rows, Hq, Hkv, d = 37, 8, 2, 64
+    x = draw((rows, Hq + 2 * Hkv, d), dtype, 9)
+    q, k = x[:, :Hq], x[:, Hq:Hq + Hkv]
+    pos, fr = torch.arange(rows, dtype=torch.int32).cuda(), freqs(d).cuda()
+    out = torch.full((rows, Hq + Hkv + 1, d), 7.0, dtype=DT[dtype], device="cuda")
+    M.bctm_qk_norm_rope(q, k, eps=1e-6, positions=pos, inv_freq=fr, q_out=out[:, Hkv + 1:], k_out=out[:, :Hkv])
+    check(out[:, Hkv + 1:], q, None, 1e-6, pos, fr, False, dtype, "q of wider rows")
+    check(out[:, :Hkv], k, None, 1e-6, pos, fr, False, dtype, "k of wider rows")
+    assert torch.all(out[:, Hkv] == 7.0)
+    before = x.clone()
+    M.bctm_qk_norm_rope(q, k, eps=1e-6, positions=pos, inv_freq=fr, q_out=q, k_out=k)     # in place, in the wider rows
+    assert torch.equal(q, out[:, Hkv + 1:]) and torch.equal(k, out[:, :Hkv]) and torch.equal(x[:, Hq + Hkv:], before[:, Hq + Hkv:])
+
+
+def test_any_share_of_heads_gives_the_same_bits(M):
+    """One row and many rows go to different launches: a row's result does not depend on the others."""
+    rows = 6000
+    q, k = draw((rows, 32, 128), "bf16", 1), draw((rows, 32, 128), "bf16", 2)
+    g, pos, fr = draw((128,), "bf16", 3), torch.arange(rows, dtype=torch.int32).cuda(), freqs(128).cuda()
+    qo, ko = M.bctm_qk_norm_rope(q, k, g, g, 1e-6, pos, fr)
+    for n in (1, 17, 300, 1500):
+        for at in (0, rows - n):
+            s = slice(at, at + n)
+            a, b = M.bctm_qk_norm_rope(q[s], k[s], g, g, 1e-6, pos[s].contiguous(), fr)
+            assert torch.equal(a, qo[s]) and torch.equal(b, ko[s]), (n, at)
+
+
+def test_another_stream_and_a_captured_graph(M):
+    rows = 64
+    q, k = draw((rows, 32, 128), "bf16", 1), draw((rows, 8, 128), "bf16", 2)
+    pos, fr = torch.arange(rows, dtype=torch.int32).cuda(), freqs(128).cuda()
+    want = M.bctm_qk_norm_rope(q, k, eps=1e-6, positions=pos, inv_freq=fr)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = M.bctm_qk_norm_rope(q, k, eps=1e-6, positions=pos, inv_freq=fr)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    qo, ko, g = torch.empty_like(q), torch.empty_like(k), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        M.bctm_qk_norm_rope(q, k, eps=1e-6, positions=pos, inv_freq=fr, q_out=qo, k_out=ko)
+    for step in range(3):     # the positions are read at each replay
+        pos.add_(100)
+        want = M.bctm_qk_norm_rope(q, k, eps=1e-6, positions=pos, inv_freq=fr)
+        qo.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(qo, want[0]) and torch.equal(ko, want[1]), step

@@ -1,0 +1,50 @@
+"""Refusals of the per-request operators (head norms with rotation, adapters, sampling): the C entry points check their
+arguments before the first HIP call, so no GPU is needed."""
+import ctypes
+
+import pytest
+
+import paper_2411_15785_amd as P
+from paper_2411_15785_amd import model
+
+
+@pytest.fixture(scope="module")
+def ML():
+    return model.mlib()
+
+
+A, B, C, D, E = (ctypes.c_void_p(0x1000000 * i) for i in range(1, 6))
+BF16, F32, NORM, PAIRS = 1, 0, model.BCTM_HEAD_NORM, model.BCTM_ROPE_INTERLEAVED
+
+
+def rope(ML, **kw):
+    a = dict(q=A, qo=B, qg=None, hq=4, ldq=512, ldqo=512, k=C, ko=D, kg=None, hk=2, ldk=256, ldko=256, pos=E, freq=E, rot=128, rows=3,
+             d=128, eps=1e-6, dtype=BF16, flags=NORM)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return ML.bctm_qk_norm_rope(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(rows=0), P.BCT_ERR_INVALID_ARG), (dict(q=None), P.BCT_ERR_INVALID_ARG), (dict(qo=None), P.BCT_ERR_INVALID_ARG),
+    (dict(hq=0), P.BCT_ERR_INVALID_ARG), (dict(hk=0), P.BCT_ERR_INVALID_ARG), (dict(k=None), P.BCT_ERR_INVALID_ARG),
+    (dict(ko=None), P.BCT_ERR_INVALID_ARG), (dict(dtype=2), P.BCT_ERR_UNSUPPORTED), (dict(flags=NORM | 1), P.BCT_ERR_INVALID_ARG),
+    (dict(flags=0, rot=0, pos=None, freq=None), P.BCT_ERR_INVALID_ARG), (dict(flags=0, qg=E), P.BCT_ERR_INVALID_ARG),
+    (dict(eps=-1.0), P.BCT_ERR_INVALID_ARG), (dict(eps=float("nan")), P.BCT_ERR_INVALID_ARG),
+    (dict(d=120), P.BCT_ERR_UNSUPPORTED), (dict(d=272, ldq=1088, ldqo=1088, ldk=544, ldko=544), P.BCT_ERR_UNSUPPORTED),
+    (dict(rot=144), P.BCT_ERR_UNSUPPORTED), (dict(rot=24), P.BCT_ERR_UNSUPPORTED), (dict(pos=None), P.BCT_ERR_INVALID_ARG),
+    (dict(freq=None), P.BCT_ERR_INVALID_ARG), (dict(rot=0), P.BCT_ERR_INVALID_ARG), (dict(ldq=504), P.BCT_ERR_INVALID_ARG),
+    (dict(ldko=248), P.BCT_ERR_INVALID_ARG), (dict(ldq=516), P.BCT_ERR_MISALIGNED), (dict(q=ctypes.c_void_p(0x1000008)), P.BCT_ERR_MISALIGNED),
+    (dict(freq=ctypes.c_void_p(0x5000008)), P.BCT_ERR_MISALIGNED),
+    # outputs over inputs: half a row further, another distance, the other input, each other
+    (dict(qo=ctypes.c_void_p(0x1000000 + 512)), P.BCT_ERR_INVALID_ARG), (dict(qo=A, ldqo=640), P.BCT_ERR_INVALID_ARG),
+    (dict(qo=C), P.BCT_ERR_INVALID_ARG), (dict(ko=A), P.BCT_ERR_INVALID_ARG), (dict(ko=B), P.BCT_ERR_INVALID_ARG),
+    (dict(ko=ctypes.c_void_p(0x2000000 + 2 * 512 * 2 + 768)), P.BCT_ERR_INVALID_ARG),
+    # side by side in one row, but one head too far to the left
+    (dict(qo=A, k=ctypes.c_void_p(0x1000000 + 768), ko=ctypes.c_void_p(0x1000000 + 768), ldq=1024, ldqo=1024, ldk=1024, ldko=1024),
+     P.BCT_ERR_INVALID_ARG),
+    (dict(rows=0xFFFFFFFF, hq=0xFFFF0, ldq=0x7FFFF00, ldqo=0x7FFFF00, q=A, qo=A, k=None, ko=None, hk=0), P.BCT_ERR_UNSUPPORTED),
+])
+def test_rope_refusals(ML, kw, status):
+    assert rope(ML, **kw) == status
+    assert ML.bctm_last_error() != b""
