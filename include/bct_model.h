@@ -122,6 +122,23 @@ bct_status bctm_linear_tile(uint32_t rows, uint32_t K, uint32_t N, uint32_t swig
 /* ids[r] = index of the largest logits[r][:] (the lowest index among equal maxima). */
 bct_status bctm_argmax(const void* logits, int32_t* ids, uint32_t rows, uint32_t N, void* hip_stream);
 
+/* The next token of each sequence drawn from its logits, with settings of its own and one uniform number
+ * (bctm_argmax is the greedy choice).  logits [rows], N tokens each, ld >= N elements from row to row, float32 or
+ * bf16 (dtype; aligned to their type, fastest where rows are 16-byte aligned).  Tokens in descending order of their logit, equal
+ * ones by index; a logit of NaN or -inf is never drawn.  With w = exp((l - max) / temperature) and cum(j) the sum of the first j:
+ *   kept   the first n: the least of top_k (0 or less: all), the fewest with cum(n) >= top_p * cum(top_k) (1 or more: all) and
+ *          how many have w >= min_p (0 or less: all); at least 1
+ *   drawn  the first j with cum(j) > u * cum(n)
+ * temperature, top_p, min_p: float32 [rows], top_k int32 [rows], each NULL = 1, 1, 0, 0 for all; u float32 [rows] in [0, 1), below
+ * taken as 0, above as the last number before 1; all device memory.  A temperature of 0 (or below, or NaN) draws the most likely
+ * token, bctm_argmax's but for NaN; NaN elsewhere switches that setting off.  Infinite logits share the draw equally.
+ * ids int32 [rows]: the tokens, -1 in a row that has none left; prob float32 [rows] or NULL: w / cum(n) of each, 0 with -1.
+ * Weights and sums have 40 to 46 bits behind the binary point of the largest weight, added as integers: equal calls draw
+ * equal tokens.  N at most 4194304. */
+bct_status bctm_sample(const void* logits, size_t ld, const float* temperature, const int32_t* top_k, const float* top_p,
+                       const float* min_p, const float* u, int32_t* ids, float* prob, uint32_t rows, uint32_t N,
+                       int32_t dtype, void* hip_stream);
+
 /* Thread-local detail of the last failure of a bctm_ call. */
 const char* bctm_last_error(void);
 

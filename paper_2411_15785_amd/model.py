@@ -16,7 +16,7 @@ from .binding import BCT_OK, BctCache, BctError, _dptr, _launch, _torch
 
 MODEL_EXPORTS = ["bctm_embed", "bctm_rmsnorm", "bctm_pack_weight", "bctm_pack_rows", "bctm_linear", "bctm_linear_split",
                  "bctm_swiglu", "bctm_linear_plan", "bctm_linear_tile", "bctm_qk_norm_rope",
-                 "bctm_argmax", "bctm_last_error"]
+                 "bctm_argmax", "bctm_sample", "bctm_last_error"]
 
 BCTM_KERNEL_STREAMING, BCTM_KERNEL_STREAMING_WIDE, BCTM_KERNEL_TILE128, BCTM_KERNEL_TILE256 = 0, 1, 2, 3
 BCTM_KERNEL_STREAMING_TRIPLE = 4
@@ -48,6 +48,7 @@ def mlib() -> ctypes.CDLL:
     L.bctm_qk_norm_rope.argtypes = [vp, vp, vp, u32, u32, u32] * 2 + [vp, vp, u32, u32, u32, ctypes.c_float, ctypes.c_int32, u32,
                                                                       vp]
     L.bctm_argmax.argtypes = [vp, vp, u32, u32, vp]
+    L.bctm_sample.argtypes = [vp, ctypes.c_size_t] + [vp] * 7 + [u32, u32, ctypes.c_int32, vp]
     for n in MODEL_EXPORTS[:-1]:
         getattr(L, n).restype = ctypes.c_int
     L.bctm_last_error.argtypes = []
@@ -322,6 +323,32 @@ def bctm_argmax(logits, out=None):
         raise ValueError("out: a contiguous int32 vector, one entry per row")
     _ck(_launch(mlib().bctm_argmax, logits.device, _dptr(logits), _dptr(out), logits.shape[0], logits.shape[1]), "bctm_argmax")
     return out
+
+
+def bctm_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, out=None, prob=None):
+    """Draws a token from each row of logits [rows][N] (float32 or bf16, rows at any distance) with its uniform number, float32
+    [rows] in [0, 1), and its settings: temperature, top_p, min_p float32 [rows], top_k int32 [rows], None = off.
+    -> (ids int32 [rows], prob): prob the probability of each drawn token among those kept, into a float32 [rows] given or
+    made (True), else None."""
+    torch = _torch()
+    if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or not logits.is_cuda or \
+            (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise ValueError(f"logits: expected [rows][N] of float32 or bf16 on the GPU, each row contiguous, got {logits.dtype} "
+                         f"{tuple(logits.shape)} strides {logits.stride()} on {logits.device}")
+    rows, N = logits.shape
+    if out is None:
+        out = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    if prob is True:
+        prob = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    f32, i32 = torch.float32, torch.int32
+    for t, n, want in ((uniform, "uniform", f32), (temperature, "temperature", f32), (top_k, "top_k", i32), (top_p, "top_p", f32),
+                       (min_p, "min_p", f32), (out, "out", i32), (prob, "prob", f32)):
+        if t is not None and (t.dtype is not want or t.shape != (rows,) or not t.is_contiguous() or t.device != logits.device):
+            raise ValueError(f"{n}: expected a contiguous {want} vector of {rows} on {logits.device}")
+    _ck(_launch(mlib().bctm_sample, logits.device, _dptr(logits), logits.stride(0) if rows > 1 else max(logits.stride(0), N),
+                _dptr(temperature), _dptr(top_k), _dptr(top_p), _dptr(min_p), _dptr(uniform), _dptr(out), _dptr(prob), rows, N,
+                binding.BCT_F32 if logits.dtype is f32 else binding.BCT_BF16), "bctm_sample")
+    return out, prob
 
 
 # ------------------------------------------------------------------ the stack

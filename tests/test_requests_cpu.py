@@ -48,3 +48,22 @@ def rope(ML, **kw):
 def test_rope_refusals(ML, kw, status):
     assert rope(ML, **kw) == status
     assert ML.bctm_last_error() != b""
+
+
+def sample(ML, **kw):
+    a = dict(x=A, ld=1000, t=None, k=None, p=None, m=None, u=B, ids=C, prob=None, rows=4, N=1000, dtype=BF16)
+    assert set(kw) <= set(a)
+    a.update(kw)
+    return ML.bctm_sample(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(x=None), P.BCT_ERR_INVALID_ARG), (dict(u=None), P.BCT_ERR_INVALID_ARG), (dict(ids=None), P.BCT_ERR_INVALID_ARG),
+    (dict(rows=0), P.BCT_ERR_INVALID_ARG), (dict(N=0), P.BCT_ERR_INVALID_ARG), (dict(dtype=7), P.BCT_ERR_UNSUPPORTED),
+    (dict(ld=999), P.BCT_ERR_INVALID_ARG), (dict(N=(1 << 22) + 1, ld=1 << 23), P.BCT_ERR_UNSUPPORTED),
+    (dict(ld=1 << 60), P.BCT_ERR_UNSUPPORTED), (dict(rows=1 << 31), P.BCT_ERR_UNSUPPORTED),
+    (dict(x=ctypes.c_void_p(0x1000001)), P.BCT_ERR_MISALIGNED), (dict(x=ctypes.c_void_p(0x1000002), dtype=F32), P.BCT_ERR_MISALIGNED),
+])
+def test_sample_refusals(ML, kw, status):
+    assert sample(ML, **kw) == status
+    assert ML.bctm_last_error() != b""
