@@ -103,6 +103,46 @@ bct_status bctm_linear_split(const void* x, const void* w_packed, void* out0, ui
 bct_status bctm_swiglu(const void* x, const void* w_gate_packed, const void* w_up_packed, void* out, uint32_t rows,
                        uint32_t K, uint32_t N, uint32_t flags, void* hip_stream);
 
+/* Low-rank adapters of many requests beside one shared projection: row r belongs to a request with the adapter
+ * a = adapter[r], and its output has scale_a (x[r] A_a^T) B_a^T added before the one rounding.  Rows whose adapter is outside
+ * [0, n_adapters) are those of the plain projection, bit for bit.
+ *   a       the matrices A of all adapters, one below the other: [n_adapters][segments][rank][K], packed by one bctm_pack_weight of
+ *           n_adapters * segments * rank features.  segments: 1 (bctm_linear_lora), the number of outputs (bctm_linear_split_lora:
+ *           each output has an A of its own) or 2 (bctm_swiglu_lora: gate, then up)
+ *   b       the matrices B, [n_adapters][N][rank], packed by one bctm_lora_pack of n_adapters * N features; N all features of
+ *           the projection (all outputs together).  b_up: those of the up matrix in bctm_swiglu_lora, else NULL
+ *   scale   float32 [n_adapters], NULL = 1;  adapter: int32 [rows]
+ *   rank    a multiple of 16, at most 256; adapters of fewer ranks are filled up with zeros
+ * workspace: 16-byte aligned, at least bctm_lora_workspace bytes, holds nothing between calls; it must not be in use by a call
+ * on another stream.  All but the struct is device memory.  x A^T is summed in fp32 and enters the second product with 16 bits.
+ * A NaN or an infinity in one adapter reaches the rows of that adapter alone. */
+typedef struct {
+  const void* a;
+  const void* b;
+  const void* b_up;
+  const float* scale;
+  const int32_t* adapter;
+  uint32_t n_adapters, rank;
+  void* workspace;
+  size_t workspace_bytes;
+} bctm_lora;
+
+/* Bytes of workspace a call of these sizes needs (host call, no GPU needed). */
+bct_status bctm_lora_workspace(uint32_t rows, uint32_t K, uint32_t rank, uint32_t segments, size_t* bytes);
+
+/* Repacks row-major b [N][rank] into 16-byte chunks of 8 ranks of one feature, chunk (n / 16 * rank / 8 + k / 8) * 16 + n % 16.
+ * Done once when adapters are loaded.  N and rank multiples of 16; packed holds N * rank bf16 and must not be b. */
+bct_status bctm_lora_pack(const void* b, void* packed, uint32_t N, uint32_t rank, void* hip_stream);
+
+/* bctm_linear, bctm_linear_split and bctm_swiglu with adapters; everything else as in those. */
+bct_status bctm_linear_lora(const void* x, const void* w_packed, const void* residual, void* out, uint32_t rows, uint32_t K,
+                            uint32_t N, uint32_t flags, const bctm_lora* lora, void* hip_stream);
+bct_status bctm_linear_split_lora(const void* x, const void* w_packed, void* out0, uint32_t N0, void* out1, uint32_t N1,
+                                  void* out2, uint32_t N2, uint32_t rows, uint32_t K, uint32_t flags, const bctm_lora* lora,
+                                  void* hip_stream);
+bct_status bctm_swiglu_lora(const void* x, const void* w_gate_packed, const void* w_up_packed, void* out, uint32_t rows,
+                            uint32_t K, uint32_t N, uint32_t flags, const bctm_lora* lora, void* hip_stream);
+
 /* Which kernel bctm_linear / bctm_linear_split (swiglu = 0, N their widths together) or bctm_swiglu (swiglu = 1) launches
  * for a shape: host logic only, no GPU call.  *kernel receives one of the values below.  The last two of them
  * name the same matrix-core kernel in two ranges of shapes; which tile it gives a workgroup there is

@@ -35,10 +35,12 @@ namespace {
 // KS groups of WR x WC wavefronts; a wavefront owns 16 * MI token rows x 16 * NJ B-tile columns (SwiGLU: gate and
 // up tiles alternate, so half as many output features); group g sums the K steps [KT * g / KS, ...).
 // PAIR (row-major activations): the two K steps of a line are requested together, see request_rows.
-template <bool SWIGLU, bool XT, bool PAIR, int MI, int NJ, int WR, int WC, int KS>
+// LORA: none, or a LoraTerm: the rows' low-rank term is added to the accumulators.  (A pack, so that the kernels without one
+// are compiled as if there were none with it.)
+template <bool SWIGLU, bool XT, bool PAIR, int MI, int NJ, int WR, int WC, int KS, typename... LORA>
 __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
     const uint16_t* __restrict__ x, const u32x4* __restrict__ w, const u32x4* __restrict__ w2, const uint16_t* residual,
-    LinearOut dst, uint32_t rows, uint32_t K, uint32_t NT, uint32_t out_tiled) {
+    LinearOut dst, uint32_t rows, uint32_t K, uint32_t NT, uint32_t out_tiled, LORA... lora) {
   constexpr int NW = WR * WC;                      // wavefronts of a group
   constexpr int TA = MI * WR, TB = NJ * WC, TT = TA + TB;  // 1 KB tiles of a K step: activations, weights
   constexpr int ND = TT / NW, NA = TA / NW, NB = TB / NW;  // of them per wavefront
@@ -208,6 +210,22 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   __builtin_amdgcn_s_waitcnt(wait_vm(0));   // the stages are free once the last requests have arrived
   __syncthreads();
 
+  if constexpr (sizeof...(LORA) > 0) {
+    // B tile j of the wavefront: features past the end take the last tile's, as their weights do
+    const uint32_t most = dst.start[3] / 16 - 1;
+    auto tile = [&](int j) -> uint32_t {
+      const uint32_t bt = NJ * wc + j;
+      return SWIGLU ? min(nt * (TB / 2) + bt / 2, most) : min(nt * TB + bt, most);
+    };
+    auto segment = [&](int j) -> uint32_t {
+      if (SWIGLU) return j % 2;   // a wavefront's tiles begin with a gate tile
+      const uint32_t n = 16 * tile(j);
+      return n >= dst.start[2] ? 2 : n >= dst.start[1] ? 1 : 0;
+    };
+    lora_add<MI, NJ, SWIGLU ? 2 : 1>(lora..., r0 + wr * (16 * MI), rows, dst.start[3], grp, KS, segment, tile,
+                                     [&](int i, int j) -> f32x4& { return acc[i][j]; });
+  }
+
   // the row tiles this wavefront writes out: with two groups, the first half is summed and written by group 0,
   // the second by group 1
   constexpr int MO = MI / KS;
@@ -360,16 +378,20 @@ RowsShape rows_shape(uint32_t rows, uint32_t bcols, uint32_t K, bool x_tiled) {
 
 template <bool SWIGLU, bool XT, int MI, int NJ, int WR, int WC, int KS, bool PAIR = false>
 void launch_shape(const void* x, const void* w, const void* w2, const void* residual, const LinearOut& dst, uint32_t rows,
-                  uint32_t K, uint32_t bcols, bool out_tiled, hipStream_t s) {
+                  uint32_t K, uint32_t bcols, bool out_tiled, const LoraTerm* lora, hipStream_t s) {
   const uint32_t NT = (bcols + 16 * NJ * WC - 1) / (16 * NJ * WC), RT = (rows + 16 * MI * WR - 1) / (16 * MI * WR);
-  hipLaunchKernelGGL((linear_rows_kernel<SWIGLU, XT, PAIR, MI, NJ, WR, WC, KS>), dim3(8 * ((RT * NT + 7) / 8)),
-                     dim3(64 * WR * WC * KS), 0, s, (const uint16_t*)x, (const u32x4*)w, (const u32x4*)w2,
-                     (const uint16_t*)residual, dst, rows, K, NT, out_tiled ? 1u : 0u);
+  const dim3 grid(8 * ((RT * NT + 7) / 8)), block(64 * WR * WC * KS);
+  if (lora)
+    hipLaunchKernelGGL((linear_rows_kernel<SWIGLU, XT, PAIR, MI, NJ, WR, WC, KS, LoraTerm>), grid, block, 0, s,
+                       (const uint16_t*)x, (const u32x4*)w, (const u32x4*)w2, (const uint16_t*)residual, dst, rows, K, NT, out_tiled ? 1u : 0u, *lora);
+  else
+    hipLaunchKernelGGL((linear_rows_kernel<SWIGLU, XT, PAIR, MI, NJ, WR, WC, KS>), grid, block, 0, s, (const uint16_t*)x,
+                       (const u32x4*)w, (const u32x4*)w2, (const uint16_t*)residual, dst, rows, K, NT, out_tiled ? 1u : 0u);
 }
 
 template <bool SWIGLU, bool XT>
 void launch_rows(const void* x, const void* w, const void* w2, const void* residual, const LinearOut& dst, uint32_t rows,
-                 uint32_t K, uint32_t N, bool out_tiled, hipStream_t s) {
+                 uint32_t K, uint32_t N, bool out_tiled, const LoraTerm* lora, hipStream_t s) {
   const uint32_t bcols = SWIGLU ? 2 * N : N;
   const RowsShape shape = rows_shape(rows, bcols, K, XT);
   if constexpr (!SWIGLU && !XT) {
@@ -380,16 +402,16 @@ void launch_rows(const void* x, const void* w, const void* w2, const void* resid
     // tiles (the activations of odd steps come later): 677, 10688 -> 11392 328 | 301.
     const uint64_t tiles = (uint64_t)((rows + 127) / 128) * ((N + 127) / 128);
     if (shape == kTile128 && (uint64_t)K * N >= (100u << 20) && tiles >= 850)
-      return launch_shape<false, false, 4, 4, 2, 2, 1, true>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, s);
+      return launch_shape<false, false, 4, 4, 2, 2, 1, true>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, lora, s);
   }
   switch (shape) {
-    case kTile256: return launch_shape<SWIGLU, XT, 8, 4, 2, 4, 1>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, s);
-    case kTile128x512: return launch_shape<SWIGLU, XT, 4, 8, 2, 4, 1>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, s);
-    case kTile128x256: return launch_shape<SWIGLU, XT, 4, 4, 2, 4, 1>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, s);
-    case kTile128: return launch_shape<SWIGLU, XT, 4, 4, 2, 2, 1>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, s);
-    case kTile128K2: return launch_shape<SWIGLU, XT, 4, 4, 2, 2, 2>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, s);
-    case kTile128x64K2: return launch_shape<SWIGLU, XT, 2, 4, 4, 1, 2>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, s);
-    case kTile64K2: return launch_shape<SWIGLU, XT, 2, 2, 2, 2, 2>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, s);
+    case kTile256: return launch_shape<SWIGLU, XT, 8, 4, 2, 4, 1>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, lora, s);
+    case kTile128x512: return launch_shape<SWIGLU, XT, 4, 8, 2, 4, 1>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, lora, s);
+    case kTile128x256: return launch_shape<SWIGLU, XT, 4, 4, 2, 4, 1>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, lora, s);
+    case kTile128: return launch_shape<SWIGLU, XT, 4, 4, 2, 2, 1>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, lora, s);
+    case kTile128K2: return launch_shape<SWIGLU, XT, 4, 4, 2, 2, 2>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, lora, s);
+    case kTile128x64K2: return launch_shape<SWIGLU, XT, 2, 4, 4, 1, 2>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, lora, s);
+    case kTile64K2: return launch_shape<SWIGLU, XT, 2, 2, 2, 2, 2>(x, w, w2, residual, dst, rows, K, bcols, out_tiled, lora, s);
   }
 }
 
@@ -410,13 +432,14 @@ LinearTile linear_rows_tile(uint32_t rows, uint32_t K, uint32_t N, bool swiglu, 
 }
 
 hipError_t launch_linear_rows(const void* x, const void* w, const void* w2, const void* residual, const LinearOut& dst,
-                              uint32_t rows, uint32_t K, uint32_t N, bool x_tiled, bool out_tiled, hipStream_t s) {
+                              uint32_t rows, uint32_t K, uint32_t N, bool x_tiled, bool out_tiled, hipStream_t s,
+                              const LoraTerm* lora) {
   if (w2) {
-    if (x_tiled) launch_rows<true, true>(x, w, w2, residual, dst, rows, K, N, out_tiled, s);
-    else launch_rows<true, false>(x, w, w2, residual, dst, rows, K, N, out_tiled, s);
+    if (x_tiled) launch_rows<true, true>(x, w, w2, residual, dst, rows, K, N, out_tiled, lora, s);
+    else launch_rows<true, false>(x, w, w2, residual, dst, rows, K, N, out_tiled, lora, s);
   } else {
-    if (x_tiled) launch_rows<false, true>(x, w, w2, residual, dst, rows, K, N, out_tiled, s);
-    else launch_rows<false, false>(x, w, w2, residual, dst, rows, K, N, out_tiled, s);
+    if (x_tiled) launch_rows<false, true>(x, w, w2, residual, dst, rows, K, N, out_tiled, lora, s);
+    else launch_rows<false, false>(x, w, w2, residual, dst, rows, K, N, out_tiled, lora, s);
   }
   return hipGetLastError();
 }

@@ -18,6 +18,7 @@
 
 #include "bct_device.h"
 #include "bct_linear.h"
+#include "bct_lora.h"
 #include "bct_model_internal.h"
 
 namespace bct {
@@ -65,12 +66,13 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const uint16_t* __restri
 // two row tiles, 11008 -> 4096 17.6 us (21.5), 4096 -> 4096 11.9 (12.7), 4096 -> 32000 47.9 (50.1), SwiGLU
 // 4096 -> 11008 30.0 (32.2); at 16 rows 23.1 (25.8), 11.7 (12.7), 50.2 (52.2), 33.8 (34.2).  4096 -> 12288 (three feature
 // tiles): see streaming_row_tiles.
-template <bool SWIGLU, bool XT, int WAVES, int U, int FT, int RT>
+// LORA: none, or a LoraTerm: the rows' low-rank term is added to the accumulators, its adapters shared among the wavefronts.
+template <bool SWIGLU, bool XT, int WAVES, int U, int FT, int RT, typename... LORA>
 __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __restrict__ x,
                                                             const u32x4* __restrict__ w,
                                                             const u32x4* __restrict__ w2, const uint16_t* residual,
                                                             LinearOut dst, uint32_t rows, uint32_t K,
-                                                            uint32_t out_tiled) {
+                                                            uint32_t out_tiled, LORA... lora) {
   constexpr int NW2 = SWIGLU ? 2 : 1;   // weight matrices
   constexpr int NS = FT * NW2;          // weight streams of a wavefront: stream s = feature tile s / NW2 of matrix s % NW2
   constexpr int NTHR = 64 * WAVES;
@@ -135,6 +137,16 @@ __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __re
           acc[s][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[u][j]),
                                                               __builtin_bit_cast(bf16x8, b[u][s]), acc[s][j], 0, 0, 0);
     }
+  }
+  if constexpr (sizeof...(LORA) > 0) {
+    auto tile = [&](int s) -> uint32_t { return nt0 + s / NW2; };
+    auto segment = [&](int s) -> uint32_t {
+      if (SWIGLU) return s % NW2;
+      const uint32_t n = 16 * tile(s);
+      return n >= dst.start[2] ? 2 : n >= dst.start[1] ? 1 : 0;
+    };
+    lora_add<RT, NS, NW2>(lora..., r0, rows, dst.start[3], wave, WAVES, segment, tile,
+                          [&](int i, int s) -> f32x4& { return acc[s][i]; });
   }
   // accumulator element v of a lane: token row 4 * kg + v of the row tile, feature jl.  Per feature tile
   // the partials of all wavefronts go through LDS (one matrix at a time through the same buffer) and
@@ -358,16 +370,17 @@ using namespace bct;
 
 template <int WV, int UN, int FT, int RT>
 static void launch_linear_rt(const void* x, const void* w, const void* residual, const LinearOut& dst, uint32_t rows,
-                             uint32_t K, uint32_t N, uint32_t flags, void* hip_stream) {
+                             uint32_t K, uint32_t N, uint32_t flags, const LoraTerm* lora, void* hip_stream) {
   const dim3 grid(N / (16 * FT), (rows + 16 * RT - 1) / (16 * RT)), block(64 * WV);
-  if (flags & BCTM_X_TILED)
-    hipLaunchKernelGGL((linear_kernel<false, true, WV, UN, FT, RT>), grid, block, 0, (hipStream_t)hip_stream,
-                       (const uint16_t*)x, (const u32x4*)w, (const u32x4*)nullptr, (const uint16_t*)residual, dst, rows,
-                       K, 0u);
-  else
-    hipLaunchKernelGGL((linear_kernel<false, false, WV, UN, FT, RT>), grid, block, 0, (hipStream_t)hip_stream,
-                       (const uint16_t*)x, (const u32x4*)w, (const u32x4*)nullptr, (const uint16_t*)residual, dst, rows,
-                       K, 0u);
+  auto launch = [&](auto kernel, auto... more) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, (hipStream_t)hip_stream, (const uint16_t*)x, (const u32x4*)w,
+                       (const u32x4*)nullptr, (const uint16_t*)residual, dst, rows, K, 0u, more...);
+  };
+  if (lora) {
+    if (flags & BCTM_X_TILED) launch(linear_kernel<false, true, WV, UN, FT, RT, LoraTerm>, *lora);
+    else launch(linear_kernel<false, false, WV, UN, FT, RT, LoraTerm>, *lora);
+  } else if (flags & BCTM_X_TILED) launch(linear_kernel<false, true, WV, UN, FT, RT>);
+  else launch(linear_kernel<false, false, WV, UN, FT, RT>);
 }
 // Row tiles of a streaming launch with FT feature tiles a workgroup.
 static uint32_t streaming_row_tiles(uint32_t FT, uint32_t rows, uint32_t N, uint32_t flags) {
@@ -381,10 +394,10 @@ static uint32_t streaming_row_tiles(uint32_t FT, uint32_t rows, uint32_t N, uint
 }
 template <int WV, int UN, int FT>
 static void launch_linear_w(const void* x, const void* w, const void* residual, const LinearOut& dst, uint32_t rows,
-                            uint32_t K, uint32_t N, uint32_t flags, void* hip_stream) {
+                            uint32_t K, uint32_t N, uint32_t flags, const LoraTerm* lora, void* hip_stream) {
   if (streaming_row_tiles(FT, rows, N, flags) == 1)
-    launch_linear_rt<WV, UN, FT, 1>(x, w, residual, dst, rows, K, N, flags, hip_stream);
-  else launch_linear_rt<WV, UN, FT, 2>(x, w, residual, dst, rows, K, N, flags, hip_stream);
+    launch_linear_rt<WV, UN, FT, 1>(x, w, residual, dst, rows, K, N, flags, lora, hip_stream);
+  else launch_linear_rt<WV, UN, FT, 2>(x, w, residual, dst, rows, K, N, flags, lora, hip_stream);
 }
 
 // The kernel of a projection shape.  Many rows (from 128 on): the matrix-core kernel (bct_linear_rows.hip); its two values
@@ -420,15 +433,18 @@ static LinearTile streaming_tile(uint32_t kernel, uint32_t rows, uint32_t N, boo
 
 template <int WV, int UN, int FT, int RT>
 static void launch_swiglu_w(const void* x, const void* wg, const void* wu, const LinearOut& dst, uint32_t rows,
-                            uint32_t K, uint32_t N, uint32_t flags, void* hip_stream) {
+                            uint32_t K, uint32_t N, uint32_t flags, const LoraTerm* lora, void* hip_stream) {
   const dim3 grid(N / (16 * FT), (rows + 16 * RT - 1) / (16 * RT)), block(64 * WV);
   const uint32_t ot = flags & BCTM_OUT_TILED ? 1u : 0u;
-  if (flags & BCTM_X_TILED)
-    hipLaunchKernelGGL((linear_kernel<true, true, WV, UN, FT, RT>), grid, block, 0, (hipStream_t)hip_stream,
-                       (const uint16_t*)x, (const u32x4*)wg, (const u32x4*)wu, (const uint16_t*)nullptr, dst, rows, K, ot);
-  else
-    hipLaunchKernelGGL((linear_kernel<true, false, WV, UN, FT, RT>), grid, block, 0, (hipStream_t)hip_stream,
-                       (const uint16_t*)x, (const u32x4*)wg, (const u32x4*)wu, (const uint16_t*)nullptr, dst, rows, K, ot);
+  auto launch = [&](auto kernel, auto... more) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, (hipStream_t)hip_stream, (const uint16_t*)x, (const u32x4*)wg, (const u32x4*)wu,
+                       (const uint16_t*)nullptr, dst, rows, K, ot, more...);
+  };
+  if (lora) {
+    if (flags & BCTM_X_TILED) launch(linear_kernel<true, true, WV, UN, FT, RT, LoraTerm>, *lora);
+    else launch(linear_kernel<true, false, WV, UN, FT, RT, LoraTerm>, *lora);
+  } else if (flags & BCTM_X_TILED) launch(linear_kernel<true, true, WV, UN, FT, RT>);
+  else launch(linear_kernel<true, false, WV, UN, FT, RT>);
 }
 
 extern "C" {
@@ -492,30 +508,47 @@ bct_status bctm_pack_weight(const void* w, void* packed, uint32_t N, uint32_t K,
 }
 
 static bct_status launch_linear(const void* x, const void* w, const void* residual, const LinearOut& dst,
-                                uint32_t rows, uint32_t K, uint32_t N, uint32_t flags, void* hip_stream) {
+                                uint32_t rows, uint32_t K, uint32_t N, uint32_t flags, const LoraTerm* lora, void* hip_stream) {
   const uint32_t kernel = linear_kernel_of(rows, K, N, false);
   if (kernel == BCTM_KERNEL_TILE128 || kernel == BCTM_KERNEL_TILE256)
     return launched("linear", launch_linear_rows(x, w, nullptr, residual, dst, rows, K, N, flags & BCTM_X_TILED, false,
-                                                 (hipStream_t)hip_stream));
-  if (kernel == BCTM_KERNEL_STREAMING_WIDE) launch_linear_w<8, 4, 2>(x, w, residual, dst, rows, K, N, flags, hip_stream);
-  else if (kernel == BCTM_KERNEL_STREAMING_TRIPLE) launch_linear_w<8, 4, 3>(x, w, residual, dst, rows, K, N, flags, hip_stream);
-  else launch_linear_w<16, 8, 1>(x, w, residual, dst, rows, K, N, flags, hip_stream);
+                                                 (hipStream_t)hip_stream, lora));
+  if (kernel == BCTM_KERNEL_STREAMING_WIDE) launch_linear_w<8, 4, 2>(x, w, residual, dst, rows, K, N, flags, lora, hip_stream);
+  else if (kernel == BCTM_KERNEL_STREAMING_TRIPLE) launch_linear_w<8, 4, 3>(x, w, residual, dst, rows, K, N, flags, lora, hip_stream);
+  else launch_linear_w<16, 8, 1>(x, w, residual, dst, rows, K, N, flags, lora, hip_stream);
   return launched("linear");
 }
 
-bct_status bctm_linear(const void* x, const void* w, const void* residual, void* out, uint32_t rows, uint32_t K,
-                       uint32_t N, uint32_t flags, void* hip_stream) {
+static bct_status linear_call(const void* x, const void* w, const void* residual, void* out, uint32_t rows, uint32_t K,
+                              uint32_t N, uint32_t flags, const bctm_lora* lora, void* hip_stream) {
   const bct_status st = check_linear(x, w, out, rows, K, N);
   if (st != BCT_OK) return st;
   if (flags & ~BCTM_X_TILED) return mfail(BCT_ERR_INVALID_ARG, "linear takes only BCTM_X_TILED");
   if (x == out) return mfail(BCT_ERR_INVALID_ARG, "out must not be x");
   if (!al16(residual)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
   const LinearOut dst = {{(uint16_t*)out, nullptr, nullptr}, {0u, N, N, N}};
-  return launch_linear(x, w, residual, dst, rows, K, N, flags, hip_stream);
+  LoraTerm term;
+  if (lora) {
+    bct_status ls = check_lora(lora, rows, K, N, 1, false);
+    if (ls == BCT_OK) ls = launch_lora_inputs(*lora, x, rows, K, flags & BCTM_X_TILED, 1, (hipStream_t)hip_stream, &term);
+    if (ls != BCT_OK) return ls;
+  }
+  return launch_linear(x, w, residual, dst, rows, K, N, flags, lora ? &term : nullptr, hip_stream);
 }
 
-bct_status bctm_linear_split(const void* x, const void* w, void* out0, uint32_t N0, void* out1, uint32_t N1,
-                             void* out2, uint32_t N2, uint32_t rows, uint32_t K, uint32_t flags, void* hip_stream) {
+bct_status bctm_linear(const void* x, const void* w, const void* residual, void* out, uint32_t rows, uint32_t K,
+                       uint32_t N, uint32_t flags, void* hip_stream) {
+  return linear_call(x, w, residual, out, rows, K, N, flags, nullptr, hip_stream);
+}
+bct_status bctm_linear_lora(const void* x, const void* w, const void* residual, void* out, uint32_t rows, uint32_t K,
+                            uint32_t N, uint32_t flags, const bctm_lora* lora, void* hip_stream) {
+  if (!lora) return mfail(BCT_ERR_INVALID_ARG, "NULL adapters");
+  return linear_call(x, w, residual, out, rows, K, N, flags, lora, hip_stream);
+}
+
+static bct_status linear_split_call(const void* x, const void* w, void* out0, uint32_t N0, void* out1, uint32_t N1, void* out2,
+                                    uint32_t N2, uint32_t rows, uint32_t K, uint32_t flags, const bctm_lora* lora,
+                                    void* hip_stream) {
   if (N0 == 0 || N1 == 0) return mfail(BCT_ERR_INVALID_ARG, "the first two outputs must not be empty");
   if ((uint64_t)N0 + N1 + N2 > 0xFFFFFFF0ull) return mfail(BCT_ERR_UNSUPPORTED, "too many features");
   const uint32_t N = N0 + N1 + N2;
@@ -528,11 +561,29 @@ bct_status bctm_linear_split(const void* x, const void* w, void* out0, uint32_t 
   if (x == out0 || x == out1 || x == out2) return mfail(BCT_ERR_INVALID_ARG, "out must not be x");
   if (!al16(out1) || !al16(out2)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
   const LinearOut dst = {{(uint16_t*)out0, (uint16_t*)out1, (uint16_t*)out2}, {0u, N0, N0 + N1, N}};
-  return launch_linear(x, w, nullptr, dst, rows, K, N, flags, hip_stream);
+  LoraTerm term;
+  if (lora) {
+    const uint32_t segments = N2 ? 3 : 2;
+    bct_status ls = check_lora(lora, rows, K, N, segments, false);
+    if (ls == BCT_OK) ls = launch_lora_inputs(*lora, x, rows, K, flags & BCTM_X_TILED, segments, (hipStream_t)hip_stream, &term);
+    if (ls != BCT_OK) return ls;
+  }
+  return launch_linear(x, w, nullptr, dst, rows, K, N, flags, lora ? &term : nullptr, hip_stream);
 }
 
-bct_status bctm_swiglu(const void* x, const void* w_gate, const void* w_up, void* out, uint32_t rows, uint32_t K,
-                       uint32_t N, uint32_t flags, void* hip_stream) {
+bct_status bctm_linear_split(const void* x, const void* w, void* out0, uint32_t N0, void* out1, uint32_t N1,
+                             void* out2, uint32_t N2, uint32_t rows, uint32_t K, uint32_t flags, void* hip_stream) {
+  return linear_split_call(x, w, out0, N0, out1, N1, out2, N2, rows, K, flags, nullptr, hip_stream);
+}
+bct_status bctm_linear_split_lora(const void* x, const void* w, void* out0, uint32_t N0, void* out1, uint32_t N1, void* out2,
+                                  uint32_t N2, uint32_t rows, uint32_t K, uint32_t flags, const bctm_lora* lora,
+                                  void* hip_stream) {
+  if (!lora) return mfail(BCT_ERR_INVALID_ARG, "NULL adapters");
+  return linear_split_call(x, w, out0, N0, out1, N1, out2, N2, rows, K, flags, lora, hip_stream);
+}
+
+static bct_status swiglu_call(const void* x, const void* w_gate, const void* w_up, void* out, uint32_t rows, uint32_t K,
+                              uint32_t N, uint32_t flags, const bctm_lora* lora, void* hip_stream) {
   const bct_status st = check_linear(x, w_gate, out, rows, K, N);
   if (st != BCT_OK) return st;
   if (flags & ~(BCTM_X_TILED | BCTM_OUT_TILED)) return mfail(BCT_ERR_INVALID_ARG, "unknown flag");
@@ -542,14 +593,32 @@ bct_status bctm_swiglu(const void* x, const void* w_gate, const void* w_up, void
     return mfail(BCT_ERR_UNSUPPORTED, "tiled activations need a multiple of 32 columns");
   if (!al16(w_up)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
   const LinearOut dst = {{(uint16_t*)out, nullptr, nullptr}, {0u, N, N, N}};
+  LoraTerm term;
+  if (lora) {
+    bct_status ls = check_lora(lora, rows, K, N, 2, true);
+    if (ls == BCT_OK) ls = launch_lora_inputs(*lora, x, rows, K, flags & BCTM_X_TILED, 2, (hipStream_t)hip_stream, &term);
+    if (ls != BCT_OK) return ls;
+  }
+  const LoraTerm* more = lora ? &term : nullptr;
   const uint32_t kernel = linear_kernel_of(rows, K, N, true);
   if (kernel == BCTM_KERNEL_TILE128 || kernel == BCTM_KERNEL_TILE256)
     return launched("swiglu", launch_linear_rows(x, w_gate, w_up, nullptr, dst, rows, K, N, flags & BCTM_X_TILED,
-                                                 flags & BCTM_OUT_TILED, (hipStream_t)hip_stream));
+                                                 flags & BCTM_OUT_TILED, (hipStream_t)hip_stream, more));
   // 36 us at 32 rows, 4096 -> 11008 (8 wavefronts: 38)
-  if (streaming_row_tiles(1, rows, N, flags) == 1) launch_swiglu_w<4, 8, 1, 1>(x, w_gate, w_up, dst, rows, K, N, flags, hip_stream);
-  else launch_swiglu_w<4, 8, 1, 2>(x, w_gate, w_up, dst, rows, K, N, flags, hip_stream);
+  if (streaming_row_tiles(1, rows, N, flags) == 1)
+    launch_swiglu_w<4, 8, 1, 1>(x, w_gate, w_up, dst, rows, K, N, flags, more, hip_stream);
+  else launch_swiglu_w<4, 8, 1, 2>(x, w_gate, w_up, dst, rows, K, N, flags, more, hip_stream);
   return launched("swiglu");
+}
+
+bct_status bctm_swiglu(const void* x, const void* w_gate, const void* w_up, void* out, uint32_t rows, uint32_t K,
+                       uint32_t N, uint32_t flags, void* hip_stream) {
+  return swiglu_call(x, w_gate, w_up, out, rows, K, N, flags, nullptr, hip_stream);
+}
+bct_status bctm_swiglu_lora(const void* x, const void* w_gate, const void* w_up, void* out, uint32_t rows, uint32_t K,
+                            uint32_t N, uint32_t flags, const bctm_lora* lora, void* hip_stream) {
+  if (!lora) return mfail(BCT_ERR_INVALID_ARG, "NULL adapters");
+  return swiglu_call(x, w_gate, w_up, out, rows, K, N, flags, lora, hip_stream);
 }
 
 bct_status bctm_linear_plan(uint32_t rows, uint32_t K, uint32_t N, uint32_t swiglu, uint32_t* kernel) {

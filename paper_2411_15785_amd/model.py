@@ -16,6 +16,7 @@ from .binding import BCT_OK, BctCache, BctError, _dptr, _launch, _torch
 
 MODEL_EXPORTS = ["bctm_embed", "bctm_rmsnorm", "bctm_pack_weight", "bctm_pack_rows", "bctm_linear", "bctm_linear_split",
                  "bctm_swiglu", "bctm_linear_plan", "bctm_linear_tile", "bctm_qk_norm_rope",
+                 "bctm_lora_workspace", "bctm_lora_pack", "bctm_linear_lora", "bctm_linear_split_lora", "bctm_swiglu_lora",
                  "bctm_argmax", "bctm_sample", "bctm_last_error"]
 
 BCTM_KERNEL_STREAMING, BCTM_KERNEL_STREAMING_WIDE, BCTM_KERNEL_TILE128, BCTM_KERNEL_TILE256 = 0, 1, 2, 3
@@ -25,6 +26,14 @@ BCTM_X_TILED = 1
 BCTM_OUT_TILED = 2
 BCTM_HEAD_NORM = 4
 BCTM_ROPE_INTERLEAVED = 8
+
+
+
+class _bctm_lora(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("a", "b", "b_up", "scale", "adapter")] + \
+        [("n_adapters", ctypes.c_uint32), ("rank", ctypes.c_uint32), ("workspace", ctypes.c_void_p),
+         ("workspace_bytes", ctypes.c_size_t)]
+
 
 _ready = False
 
@@ -48,6 +57,12 @@ def mlib() -> ctypes.CDLL:
     L.bctm_qk_norm_rope.argtypes = [vp, vp, vp, u32, u32, u32] * 2 + [vp, vp, u32, u32, u32, ctypes.c_float, ctypes.c_int32, u32,
                                                                       vp]
     L.bctm_argmax.argtypes = [vp, vp, u32, u32, vp]
+    lora = ctypes.POINTER(_bctm_lora)
+    L.bctm_lora_workspace.argtypes = [u32, u32, u32, u32, ctypes.POINTER(ctypes.c_size_t)]
+    L.bctm_lora_pack.argtypes = [vp, vp, u32, u32, vp]
+    L.bctm_linear_lora.argtypes = L.bctm_linear.argtypes[:-1] + [lora, vp]
+    L.bctm_linear_split_lora.argtypes = L.bctm_linear_split.argtypes[:-1] + [lora, vp]
+    L.bctm_swiglu_lora.argtypes = L.bctm_swiglu.argtypes[:-1] + [lora, vp]
     L.bctm_sample.argtypes = [vp, ctypes.c_size_t] + [vp] * 7 + [u32, u32, ctypes.c_int32, vp]
     for n in MODEL_EXPORTS[:-1]:
         getattr(L, n).restype = ctypes.c_int
@@ -253,8 +268,7 @@ def _x_arg(x):
     return x, x.shape[0], x.shape[1], 0
 
 
-def bctm_linear(x, w, residual=None, out=None):
-    """x: a [rows][K] tensor or a TiledRows; out / residual row-major [rows][N]."""
+def _linear_args(x, w, residual, out):
     torch = _torch()
     xd, rows, K, xf = _x_arg(x)
     _packed(w, "w", K)
@@ -266,13 +280,17 @@ def bctm_linear(x, w, residual=None, out=None):
         _bf16_2d(residual, "residual", N)
     if out.shape[0] != rows or (residual is not None and residual.shape[0] != rows):
         raise ValueError("out / residual: one row per row of x")
-    _ck(_launch(mlib().bctm_linear, xd.device, _dptr(xd), _dptr(w.data), _dptr(residual), _dptr(out), rows, K,
-                N, xf), "bctm_linear")
+    return out, (xd.device, _dptr(xd), _dptr(w.data), _dptr(residual), _dptr(out), rows, K, N, xf)
+
+
+def bctm_linear(x, w, residual=None, out=None):
+    """x: a [rows][K] tensor or a TiledRows; out / residual row-major [rows][N]."""
+    out, args = _linear_args(x, w, residual, out)
+    _ck(_launch(mlib().bctm_linear, *args), "bctm_linear")
     return out
 
 
-def bctm_linear_split(x, w, outs):
-    """One projection into two or three row-major outputs whose widths add up to w.N."""
+def _split_args(x, w, outs):
     xd, rows, K, xf = _x_arg(x)
     _packed(w, "w", K)
     if len(outs) not in (2, 3) or sum(o.shape[1] for o in outs) != w.N:
@@ -282,13 +300,17 @@ def bctm_linear_split(x, w, outs):
         if o.shape[0] != rows:
             raise ValueError("outs: one row per row of x")
     o2, n2 = (outs[2], outs[2].shape[1]) if len(outs) == 3 else (None, 0)
-    _ck(_launch(mlib().bctm_linear_split, xd.device, _dptr(xd), _dptr(w.data), _dptr(outs[0]), outs[0].shape[1],
-                _dptr(outs[1]), outs[1].shape[1], _dptr(o2), n2, rows, K, xf), "bctm_linear_split")
+    return (xd.device, _dptr(xd), _dptr(w.data), _dptr(outs[0]), outs[0].shape[1], _dptr(outs[1]), outs[1].shape[1], _dptr(o2), n2,
+            rows, K, xf)
+
+
+def bctm_linear_split(x, w, outs):
+    """One projection into two or three row-major outputs whose widths add up to w.N."""
+    _ck(_launch(mlib().bctm_linear_split, *_split_args(x, w, outs)), "bctm_linear_split")
     return outs
 
 
-def bctm_swiglu(x, w_gate, w_up, out=None, tiled=False):
-    """x: a [rows][K] tensor or a TiledRows; out: a [rows][N] tensor, or (tiled=True) a TiledRows."""
+def _swiglu_args(x, w_gate, w_up, out, tiled):
     torch = _torch()
     xd, rows, K, xf = _x_arg(x)
     _packed(w_gate, "w_gate", K)
@@ -309,8 +331,102 @@ def bctm_swiglu(x, w_gate, w_up, out=None, tiled=False):
         if out.shape[0] != rows:
             raise ValueError("out: one row per row of x")
         dst = out
-    _ck(_launch(mlib().bctm_swiglu, xd.device, _dptr(xd), _dptr(w_gate.data), _dptr(w_up.data), _dptr(dst), rows,
-                K, N, xf | (BCTM_OUT_TILED if tiled else 0)), "bctm_swiglu")
+    return out, (xd.device, _dptr(xd), _dptr(w_gate.data), _dptr(w_up.data), _dptr(dst), rows, K, N,
+                 xf | (BCTM_OUT_TILED if tiled else 0))
+
+
+def bctm_swiglu(x, w_gate, w_up, out=None, tiled=False):
+    """x: a [rows][K] tensor or a TiledRows; out: a [rows][N] tensor, or (tiled=True) a TiledRows."""
+    out, args = _swiglu_args(x, w_gate, w_up, out, tiled)
+    _ck(_launch(mlib().bctm_swiglu, *args), "bctm_swiglu")
+    return out
+
+
+class LoraWeights:
+    """The low-rank adapters of one projection, packed (bctm_lora_pack): n of them, each rank x K per segment and N x rank."""
+
+    def __init__(self, a, b, b_up, scale, n, segments, rank, K, N):
+        self.a, self.b, self.b_up, self.scale = a, b, b_up, scale
+        self.n, self.segments, self.rank, self.K, self.N = n, segments, rank, K, N
+
+    def workspace_bytes(self, rows):
+        v = ctypes.c_size_t(0)
+        _ck(mlib().bctm_lora_workspace(rows, self.K, self.rank, self.segments, ctypes.byref(v)), "bctm_lora_workspace")
+        return v.value
+
+
+def bctm_lora_pack(a, b, scale=None):
+    """n adapters of one projection -> LoraWeights.  a [n][rank][K], or [n][segments][rank][K] where every output of a split (or
+    the gate and the up matrix of a SwiGLU) has its own; b [n][N][rank], or for a SwiGLU the pair (gate's, up's), bf16; a list
+    of one tensor is that tensor.  scale float32 [n] or None = 1.  Any rank to 256: filled up with zeros to a multiple of 16."""
+    torch = _torch()
+    bs = list(b) if isinstance(b, (list, tuple)) else [b]
+    if a.dim() == 3:
+        a = a[:, None]
+    if a.dim() != 4 or a.dtype != torch.bfloat16 or not a.is_cuda or len(bs) not in (1, 2):
+        raise ValueError("a: expected bf16 [n][rank][K] or [n][segments][rank][K] on the GPU; b: one tensor or two")
+    n, segments, rank, K = a.shape
+    for t in bs:
+        if t.dtype != torch.bfloat16 or t.dim() != 3 or t.device != a.device or t.shape != (n, bs[0].shape[1], rank):
+            raise ValueError(f"b: expected bf16 [{n}][N][{rank}] on {a.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if len(bs) == 2 and segments != 2:
+        raise ValueError("a: two segments for a SwiGLU, the gate's and the up matrix's")
+    if scale is not None and (scale.dtype != torch.float32 or scale.shape != (n,) or not scale.is_contiguous() or
+                              scale.device != a.device):
+        raise ValueError(f"scale: expected a contiguous float32 vector of {n} on {a.device}")
+    N, r = bs[0].shape[1], (rank + 15) // 16 * 16
+    if r != rank:
+        a = torch.nn.functional.pad(a, (0, 0, 0, r - rank))
+        bs = [torch.nn.functional.pad(t, (0, r - rank)) for t in bs]
+    pa = bctm_pack_weight(a.reshape(n * segments * r, K).contiguous()).data
+    packed = []
+    for t in bs:
+        t = t.contiguous()
+        p = torch.empty(n * N * r, dtype=torch.bfloat16, device=a.device)
+        _ck(_launch(mlib().bctm_lora_pack, a.device, _dptr(t), _dptr(p), n * N, r), "bctm_lora_pack")
+        packed.append(p)
+    return LoraWeights(pa, packed[0], packed[1] if len(packed) == 2 else None, scale, n, segments, r, K, N)
+
+
+def _lora_arg(lora, ids, workspace, device, rows, K, N, segments, swiglu):
+    torch = _torch()
+    if not isinstance(lora, LoraWeights):
+        raise ValueError("lora: expected LoraWeights (bctm_lora_pack)")
+    if (lora.K, lora.N, lora.segments) != (K, N, segments) or (lora.b_up is not None) != swiglu or lora.a.device != device:
+        raise ValueError(f"lora: packed for {lora.K} -> {lora.N} in {lora.segments} segments on {lora.a.device}, the projection is "
+                         f"{K} -> {N} in {segments} on {device}")
+    if ids.dtype != torch.int32 or ids.shape != (rows,) or not ids.is_contiguous() or ids.device != device:
+        raise ValueError(f"ids: expected a contiguous int32 vector of {rows} on {device}")
+    if workspace is None:
+        workspace = torch.empty(lora.workspace_bytes(rows), dtype=torch.uint8, device=device)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != device:
+        raise ValueError(f"workspace: expected contiguous torch.uint8 on {device}")
+    return _bctm_lora(_dptr(lora.a), _dptr(lora.b), _dptr(lora.b_up), _dptr(lora.scale), _dptr(ids), lora.n, lora.rank,
+                      _dptr(workspace), workspace.numel()), workspace
+
+
+def bctm_linear_lora(x, w, lora, ids, residual=None, out=None, workspace=None):
+    """bctm_linear with the adapter ids[r] (int32, none where outside lora's) added to row r.  workspace: torch.uint8 of
+    lora.workspace_bytes(rows), or None to take one from torch for this call."""
+    out, args = _linear_args(x, w, residual, out)
+    l, keep = _lora_arg(lora, ids, workspace, args[0], args[5], args[6], args[7], 1, False)
+    _ck(_launch(mlib().bctm_linear_lora, *args, ctypes.byref(l)), "bctm_linear_lora")
+    return out
+
+
+def bctm_linear_split_lora(x, w, lora, ids, outs, workspace=None):
+    """bctm_linear_split with adapters: lora has a segment for each output."""
+    args = _split_args(x, w, outs)
+    l, keep = _lora_arg(lora, ids, workspace, args[0], args[9], args[10], w.N, len(outs), False)
+    _ck(_launch(mlib().bctm_linear_split_lora, *args, ctypes.byref(l)), "bctm_linear_split_lora")
+    return outs
+
+
+def bctm_swiglu_lora(x, w_gate, w_up, lora, ids, out=None, tiled=False, workspace=None):
+    """bctm_swiglu with adapters of both matrices."""
+    out, args = _swiglu_args(x, w_gate, w_up, out, tiled)
+    l, keep = _lora_arg(lora, ids, workspace, args[0], args[5], args[6], args[7], 2, True)
+    _ck(_launch(mlib().bctm_swiglu_lora, *args, ctypes.byref(l)), "bctm_swiglu_lora")
     return out
 
 

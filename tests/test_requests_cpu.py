@@ -67,3 +67,50 @@ def sample(ML, **kw):
 def test_sample_refusals(ML, kw, status):
     assert sample(ML, **kw) == status
     assert ML.bctm_last_error() != b""
+
+
+def lora_args(**kw):
+    l = model._bctm_lora(0x6000000, 0x7000000, None, None, 0x8000000, 4, 16, 0x9000000, 1 << 20)
+    for k, v in kw.items():
+        assert k in dict(l._fields_)
+        setattr(l, k, v)
+    return ctypes.byref(l)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(a=None), P.BCT_ERR_INVALID_ARG), (dict(b=None), P.BCT_ERR_INVALID_ARG), (dict(adapter=None), P.BCT_ERR_INVALID_ARG),
+    (dict(n_adapters=0), P.BCT_ERR_INVALID_ARG), (dict(rank=0), P.BCT_ERR_INVALID_ARG), (dict(rank=24), P.BCT_ERR_UNSUPPORTED),
+    (dict(rank=272), P.BCT_ERR_UNSUPPORTED), (dict(n_adapters=1 << 31), P.BCT_ERR_UNSUPPORTED),
+    (dict(a=0x6000008), P.BCT_ERR_MISALIGNED), (dict(b=0x7000008), P.BCT_ERR_MISALIGNED), (dict(workspace=0x9000004), P.BCT_ERR_MISALIGNED),
+    (dict(workspace=None), P.BCT_ERR_BUFFER_TOO_SMALL), (dict(workspace_bytes=255), P.BCT_ERR_BUFFER_TOO_SMALL),
+])
+def test_adapter_refusals(ML, kw, status):
+    assert ML.bctm_linear_lora(A, B, None, C, 4, 64, 32, 0, lora_args(**kw), None) == status
+    assert ML.bctm_linear_split_lora(A, B, C, 16, D, 16, None, 0, 4, 64, 0, lora_args(**kw), None) == status
+    up = dict(b_up=0xA000000)
+    assert ML.bctm_swiglu_lora(A, B, C, D, 4, 64, 32, 0, lora_args(**{**up, **kw}), None) == status
+    assert ML.bctm_last_error() != b""
+
+
+def test_adapter_calls_refuse_what_the_projections_refuse(ML):
+    l = lora_args()
+    assert ML.bctm_linear_lora(A, B, None, C, 4, 72, 32, 0, l, None) == P.BCT_ERR_UNSUPPORTED
+    assert ML.bctm_linear_lora(A, B, None, A, 4, 64, 32, 0, l, None) == P.BCT_ERR_INVALID_ARG
+    assert ML.bctm_linear_lora(A, B, None, C, 4, 64, 32, 2, l, None) == P.BCT_ERR_INVALID_ARG
+    assert ML.bctm_linear_lora(A, B, None, C, 4, 64, 32, 0, None, None) == P.BCT_ERR_INVALID_ARG
+    assert ML.bctm_linear_split_lora(A, B, C, 16, D, 16, None, 0, 4, 64, 0, None, None) == P.BCT_ERR_INVALID_ARG
+    assert ML.bctm_linear_split_lora(A, B, C, 16, None, 16, None, 0, 4, 64, 0, l, None) == P.BCT_ERR_INVALID_ARG
+    assert ML.bctm_swiglu_lora(A, B, C, D, 4, 64, 32, 0, None, None) == P.BCT_ERR_INVALID_ARG
+    assert ML.bctm_swiglu_lora(A, B, C, D, 4, 64, 32, 0, l, None) == P.BCT_ERR_INVALID_ARG                       # no b_up
+    assert ML.bctm_linear_lora(A, B, None, C, 4, 64, 32, 0, lora_args(b_up=0xA000000), None) == P.BCT_ERR_INVALID_ARG
+    size = ctypes.c_size_t(0)
+    assert ML.bctm_lora_workspace(4, 64, 16, 1, ctypes.byref(size)) == 0 and size.value >= 4 * 16 * 4
+    assert ML.bctm_lora_workspace(4, 64, 16, 4, ctypes.byref(size)) == P.BCT_ERR_UNSUPPORTED
+    assert ML.bctm_lora_workspace(4, 65, 16, 1, ctypes.byref(size)) == P.BCT_ERR_UNSUPPORTED
+    assert ML.bctm_lora_workspace(0, 64, 16, 1, ctypes.byref(size)) == P.BCT_ERR_INVALID_ARG
+    assert ML.bctm_lora_workspace(4, 64, 16, 1, None) == P.BCT_ERR_INVALID_ARG
+    assert ML.bctm_lora_pack(A, B, 24, 16, None) == P.BCT_ERR_UNSUPPORTED
+    assert ML.bctm_lora_pack(A, B, 32, 24, None) == P.BCT_ERR_UNSUPPORTED
+    assert ML.bctm_lora_pack(A, A, 32, 16, None) == P.BCT_ERR_INVALID_ARG
+    assert ML.bctm_lora_pack(A, None, 32, 16, None) == P.BCT_ERR_INVALID_ARG
+    assert ML.bctm_lora_pack(A, ctypes.c_void_p(0x2000008), 32, 16, None) == P.BCT_ERR_MISALIGNED
