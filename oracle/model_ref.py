@@ -79,6 +79,33 @@ def argmax(logits):
     return np.argmax(bf16_to_f64(logits), axis=1).astype(np.int32)
 
 
+def head_norm_rope(x, gain, eps, positions, inv_freq, interleaved):
+    """x [rows][heads][d]: each head over its root mean square times gain (eps None: not), then pairs of elements turned by
+    position * inv_freq (positions None: not)."""
+    y = bf16_to_f64(x)
+    if eps is not None:
+        y = y / np.sqrt(np.mean(y * y, axis=-1, keepdims=True) + float(np.float32(eps)))
+        if gain is not None:
+            y = y * bf16_to_f64(gain)
+    if positions is not None:
+        n = len(inv_freq)
+        first, second = (np.arange(0, 2 * n, 2), np.arange(1, 2 * n, 2)) if interleaved else (np.arange(n), np.arange(n, 2 * n))
+        t = np.asarray(positions, np.float64)[:, None, None] * np.asarray(inv_freq, np.float64)
+        a, b = y[..., first].copy(), y[..., second].copy()
+        y[..., first], y[..., second] = a * np.cos(t) - b * np.sin(t), a * np.sin(t) + b * np.cos(t)
+    return f64_to_bf16(y)
+
+
+def low_rank(x, ids, a, b, scale):
+    """scale[i] (x[r] a[i]^T) b[i]^T of each row's adapter i = ids[r], in float64; zero without one."""
+    xf = bf16_to_f64(x)
+    out = np.zeros((len(xf), b.shape[1]))
+    for i in range(len(a)):
+        at = np.flatnonzero(np.asarray(ids) == i)
+        out[at] = float(scale[i]) * (xf[at] @ bf16_to_f64(a[i]).T) @ bf16_to_f64(b[i]).T
+    return out
+
+
 class RefStack:
     """The decoder stack on the CPU.  shape: an object with n_layers, dim, n_q_heads, n_kv_heads, head_dim,
     ffn, vocab, capacity_M, batch, eps; weights: the same dictionary layout as the GPU driver, as uint16 arrays."""
@@ -94,13 +121,31 @@ class RefStack:
             c.set_values(None)
             self.caches.append(c)
 
-    def forward(self, ids, T=1, trace=None):
-        """ids [B*T] -> (next ids, logits bits).  trace, if a list, receives the residual stream after each layer."""
+    def forward(self, ids, T=1, trace=None, positions=None, adapters=None, lora=None):
+        """ids [B*T] -> (next ids, logits bits).  trace, if a list, receives the residual stream after each layer.
+        lora: per layer {projection: (a, b, scale)} of any projection by its weight's name; adapters: each row's."""
         s = self.s
         x = embed(ids, self.w["embed"])
+        rope = getattr(s, "rope_base", 0.0)
+        rot = (getattr(s, "rotary_dim", 0) or s.head_dim) if rope else 0
+        inv_freq = [rope ** (-2.0 * j / rot) for j in range(rot // 2)]
+
+        def project(l, name, y):
+            out = linear_f64(y, self.w["layers"][l][name])
+            if lora is not None and name in lora[l]:
+                out = out + low_rank(y, adapters, *lora[l][name])
+            return out
+
         for l, lw in enumerate(self.w["layers"]):
             h = rmsnorm(x, lw["attn_norm"], s.eps)
-            q, wq, wv = linear(h, lw["w_q"]), linear(h, lw["w_wq"]), linear(h, lw["w_wv"])
+            q, wq, wv = (f64_to_bf16(project(l, n, h)) for n in ("w_q", "w_wq", "w_wv"))
+            if rope or getattr(s, "head_norm", False):
+                turned = []
+                for t, heads, gain in ((q, s.n_q_heads, lw.get("q_norm")), (wq, s.n_kv_heads, lw.get("wq_norm"))):
+                    t = head_norm_rope(t.reshape(-1, heads, s.head_dim), gain, s.eps if s.head_norm else None, positions, inv_freq,
+                                       s.rope_interleaved)
+                    turned.append(t.reshape(-1, heads * s.head_dim))
+                q, wq = turned
             c = self.caches[l]
             if T == 1:
                 a = c.decode_step(q.reshape(s.batch, s.n_q_heads, s.head_dim),
@@ -110,9 +155,12 @@ class RefStack:
                 a = c.prefill(q.reshape(s.batch, T, s.n_q_heads, s.head_dim),
                               wq.reshape(s.batch, T, s.n_kv_heads, s.head_dim),
                               wv.reshape(s.batch, T, s.n_kv_heads, s.head_dim), T)
-            x = linear(a.reshape(s.batch * T, -1), lw["w_o"], x)
+            x = f64_to_bf16(project(l, "w_o", a.reshape(s.batch * T, -1)) + bf16_to_f64(x))
             h = rmsnorm(x, lw["mlp_norm"], s.eps)
-            x = linear(swiglu(h, lw["w_gate"], lw["w_up"]), lw["w_down"], x)
+            g, u = project(l, "w_gate", h), project(l, "w_up", h)
+            with np.errstate(over="ignore"):
+                f = f64_to_bf16(g / (1.0 + np.exp(-g)) * u)
+            x = f64_to_bf16(project(l, "w_down", f) + bf16_to_f64(x))
             if trace is not None:
                 trace.append(x.copy())
         h = rmsnorm(x, self.w["final_norm"], s.eps)

@@ -483,8 +483,15 @@ class StackShape:
     capacity_M: int
     batch: int
     eps: float = 1e-5
+    head_norm: bool = False       # queries and write queries normalised head by head (weights q_norm and wq_norm)
+    rope_base: float = 0.0        # > 0: turned by their token's position, inv_freq[j] = rope_base ** (-2 j / rotary_dim)
+    rotary_dim: int = 0           # how much of each head is turned (0: all of it)
+    rope_interleaved: bool = False
 
     def __post_init__(self):
+        if (self.head_norm or self.rope_base) and (self.head_dim % 16 or self.rotary_dim % 16 or
+                                                   not 0 <= self.rotary_dim <= self.head_dim or self.rope_base < 0):
+            raise ValueError("head_dim and rotary_dim must be multiples of 16, rotary_dim at most head_dim, rope_base not negative")
         if self.dim % 32 or (self.n_q_heads * self.head_dim) % 32 or self.ffn % 32 or self.vocab % 16 or \
                 (self.n_kv_heads * self.head_dim) % 16:
             raise ValueError("dim, n_q_heads * head_dim and ffn must be multiples of 32; vocab and "
@@ -502,20 +509,34 @@ class StackShape:
         """name -> shape of every per-layer weight, in the order load_layer expects."""
         return {"attn_norm": (self.dim,), "w_q": (self.q_width, self.dim), "w_wq": (self.kv_width, self.dim),
                 "w_wv": (self.kv_width, self.dim), "w_o": (self.dim, self.q_width), "mlp_norm": (self.dim,),
-                "w_gate": (self.ffn, self.dim), "w_up": (self.ffn, self.dim), "w_down": (self.dim, self.ffn)}
+                "w_gate": (self.ffn, self.dim), "w_up": (self.ffn, self.dim), "w_down": (self.dim, self.ffn),
+                **({"q_norm": (self.head_dim,), "wq_norm": (self.head_dim,)} if self.head_norm else {})}
 
     def weight_bytes(self):
         per_layer = sum(math.prod(s) for s in self.weight_shapes().values())
         return 2 * (self.n_layers * per_layer + 2 * self.vocab * self.dim + self.dim)
 
 
+@dataclass
+class Sampling:
+    """How each row of logits gets its next token (bctm_sample): device vectors of one entry a row, None = off.  They are read
+    when the step runs, so a captured step takes what they hold at each replay."""
+    uniform: object
+    temperature: object = None
+    top_k: object = None
+    top_p: object = None
+    min_p: object = None
+    prob: object = None       # receives the drawn tokens' probabilities
+
+
 class BctStack:
-    """Token ids in, greedy next ids out: embedding, n_layers x (RMSNorm, W_q / W_wq / W_wv,
+    """Token ids in, next ids out (greedy, or drawn): embedding, n_layers x (RMSNorm, W_q / W_wq / W_wv,
     bounded-cache attention, W_o + residual, RMSNorm, SwiGLU MLP + residual), RMSNorm, output head, arg-max.
 
     weights: {"embed": [vocab][dim], "final_norm": [dim], "head": [vocab][dim],
               "layers": [ {name: tensor} per layer, names of StackShape.weight_shapes() ],
               "keys": [ MK per layer, [Hkv][M][d] ]}  -- all bf16 device tensors.
+    With shape.head_norm and / or shape.rope_base, q and wq pass bctm_qk_norm_rope before the cache.
     """
 
     def __init__(self, shape: StackShape, weights, max_prefill_T=0, device="cuda:0"):
@@ -548,7 +569,39 @@ class BctStack:
             self.layers.append(pl)
         self.embed, self.final_norm = weights["embed"], weights["final_norm"]
         self.head = bctm_pack_weight(weights["head"])
+        self.adapters = None
+        self.inv_freq = None
+        if s.rope_base:
+            rot = s.rotary_dim or s.head_dim
+            self.inv_freq = torch.tensor([s.rope_base ** (-2.0 * j / rot) for j in range(rot // 2)], dtype=torch.float64,
+                                         device=self.device)
         self._bufs = {}
+
+    def set_adapters(self, layers):
+        """layers: per layer a dictionary of LoraWeights for any of "qkv" (three segments: q, wq, wv), "o", "gate_up" and "down";
+        forward(adapters=) then says which adapter a row has.  None: no adapters."""
+        if layers is not None:
+            if len(layers) != self.shape.n_layers:
+                raise ValueError(f"adapters: expected {self.shape.n_layers} layers")
+            s = self.shape
+            want = {"qkv": (s.dim, s.q_width + 2 * s.kv_width, 3, False), "o": (s.q_width, s.dim, 1, False),
+                    "gate_up": (s.dim, s.ffn, 2, True), "down": (s.ffn, s.dim, 1, False)}
+            for l, d in enumerate(layers):
+                for n, a in d.items():
+                    if n not in want or not isinstance(a, LoraWeights) or (a.K, a.N, a.segments, a.b_up is not None) != want[n] \
+                            or a.a.device != self.embed.device:
+                        raise ValueError(f"layer {l} {n}: expected LoraWeights of (K, N, segments) {want.get(n, tuple(want))[:3]} "
+                                         f"on {self.embed.device}")
+        self.adapters = layers
+        self._bufs = {k: v for k, v in self._bufs.items() if k[0] != "lora"}
+
+    def _lora_workspace(self, rows):
+        torch = _torch()
+        k = ("lora", rows)
+        if k not in self._bufs:
+            n = max([a.workspace_bytes(rows) for d in self.adapters for a in d.values()], default=16)
+            self._bufs[k] = torch.empty(n, dtype=torch.uint8, device=self.device)
+        return self._bufs[k]
 
     def _buf(self, name, rows, cols):
         torch = _torch()
@@ -563,12 +616,15 @@ class BctStack:
             self._bufs[k] = TiledRows(rows, cols, self.device)
         return self._bufs[k]
 
-    def forward(self, ids, T=1, next_ids=None, head="all"):
+    def forward(self, ids, T=1, next_ids=None, head="all", positions=None, adapters=None, sampling=None):
         """ids int32 [B*T] (sequence-major: row b*T + t) -> (next ids, logits).
         T = 1 is a decode step; T > 1 pushes a chunk of T tokens per sequence through bct_prefill.
-        head = "all": logits [B*T][vocab] and greedy ids [B*T] for every row; head = "last": only for the last
+        head = "all": logits [B*T][vocab] and next ids [B*T] for every row; head = "last": only for the last
         token of every sequence ([B][vocab], [B]) - what a prompt needs, without a [B*T][vocab] product.
-        next_ids: where to write the greedy tokens (may be ids itself: it is read first, written last).
+        next_ids: where to write the next tokens (may be ids itself: it is read first, written last).
+        positions: int32 [B*T], where each token stands; needed with shape.rope_base, else None.
+        adapters: int32 [B*T], each row's adapter of those set_adapters has been given (outside them: none); None: no row has one.
+        sampling: a Sampling with one entry per row of logits, or None: the most likely token.
         After the first call of a given (B, T, head) no memory is allocated, so a call can be captured in a
         HIP graph."""
         s = self.shape
@@ -577,6 +633,11 @@ class BctStack:
             raise ValueError(f"ids: expected {rows} entries")
         if head not in ("all", "last"):
             raise ValueError('head: "all" or "last"')
+        if (positions is not None) != bool(s.rope_base):
+            raise ValueError("positions go with a shape that has a rope_base")
+        if adapters is not None and self.adapters is None:
+            raise ValueError("adapters: none have been set (set_adapters)")
+        lora_ws = self._lora_workspace(rows) if adapters is not None else None
         x = bctm_embed(ids, self.embed, self._buf("x", rows, s.dim))
         # every input of a projection is kept tiled, so that the projections read it in whole kilobytes
         h, f = self._tiled("h", rows, s.dim), self._tiled("f", rows, s.ffn)
@@ -587,7 +648,15 @@ class BctStack:
         at = self._tiled("a", rows, s.q_width) if rows >= 128 else None
         for l, lw in enumerate(self.layers):
             bctm_rmsnorm(x, lw["attn_norm"], s.eps, h, tiled=True)
-            bctm_linear_split(h, lw["w_qkv"], (q, wq, wv))
+            lora = self.adapters[l] if adapters is not None else {}
+            if "qkv" in lora:
+                bctm_linear_split_lora(h, lw["w_qkv"], lora["qkv"], adapters, (q, wq, wv), lora_ws)
+            else:
+                bctm_linear_split(h, lw["w_qkv"], (q, wq, wv))
+            if s.head_norm or s.rope_base:
+                qh, kh = q.view(rows, s.n_q_heads, s.head_dim), wq.view(rows, s.n_kv_heads, s.head_dim)
+                bctm_qk_norm_rope(qh, kh, lw.get("q_norm"), lw.get("wq_norm"), s.eps if s.head_norm else None, positions,
+                                  self.inv_freq, s.rope_interleaved, qh, kh)
             c = self.caches[l]
             if T == 1:
                 c.decode_step(q.view(s.batch, s.n_q_heads, s.head_dim), wq.view(s.batch, s.n_kv_heads, s.head_dim),
@@ -597,10 +666,20 @@ class BctStack:
                 c.prefill(q.view(s.batch, T, s.n_q_heads, s.head_dim), wq.view(s.batch, T, s.n_kv_heads, s.head_dim),
                           wv.view(s.batch, T, s.n_kv_heads, s.head_dim), T,
                           a.view(s.batch, T, s.n_q_heads, s.head_dim))
-            bctm_linear(bctm_pack_rows(a, at) if at is not None else a, lw["w_o"], x, x)
+            ax = bctm_pack_rows(a, at) if at is not None else a
+            if "o" in lora:
+                bctm_linear_lora(ax, lw["w_o"], lora["o"], adapters, x, x, lora_ws)
+            else:
+                bctm_linear(ax, lw["w_o"], x, x)
             bctm_rmsnorm(x, lw["mlp_norm"], s.eps, h, tiled=True)
-            bctm_swiglu(h, lw["w_gate"], lw["w_up"], f, tiled=True)
-            bctm_linear(f, lw["w_down"], x, x)
+            if "gate_up" in lora:
+                bctm_swiglu_lora(h, lw["w_gate"], lw["w_up"], lora["gate_up"], adapters, f, True, lora_ws)
+            else:
+                bctm_swiglu(h, lw["w_gate"], lw["w_up"], f, tiled=True)
+            if "down" in lora:
+                bctm_linear_lora(f, lw["w_down"], lora["down"], adapters, x, x, lora_ws)
+            else:
+                bctm_linear(f, lw["w_down"], x, x)
         if head == "last" and T > 1:
             # rows b*T + T-1, gathered with the embedding kernel (a row lookup) from x as the table
             torch = _torch()
@@ -612,5 +691,8 @@ class BctStack:
             h = self._tiled("h_last", rows, s.dim)
         bctm_rmsnorm(x, self.final_norm, s.eps, h, tiled=True)
         logits = bctm_linear(h, self.head, None, self._buf("logits", rows, s.vocab))
-        nxt = bctm_argmax(logits, next_ids)
+        if sampling is None:
+            return bctm_argmax(logits, next_ids), logits
+        nxt, _ = bctm_sample(logits, sampling.uniform, sampling.temperature, sampling.top_k, sampling.top_p, sampling.min_p, next_ids,
+                             sampling.prob)
         return nxt, logits
