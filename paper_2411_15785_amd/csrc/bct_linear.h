@@ -22,97 +22,143 @@ __device__ __forceinline__ size_t tiled_chunk(uint32_t r, uint32_t k, uint32_t K
   return ((((size_t)(r / 32) * (K / 32) + k / 32) * 2 + (r % 32) / 16) * 64) + 16 * ((k % 32) / 8) + r % 16;
 }
 
-// The low-rank term of a projection's rows (bct_lora.hip): out[r] += t[r] B_a^T, a = adapter[r].  t is fp32 [parts][rows][width],
-// the parts to be added up, column segment * rank + j: the rank-j input of output `segment` (of the gate and up matrices in a
-// SwiGLU).  b: per adapter 16-byte chunks of 8 ranks of one feature, chunk (feature / 16 * rank / 8 + j / 8) * 16 + feature % 16.
+// The low-rank term of a projection's rows (bct_lora.hip): out[r] += t[r] B_a^T, a = adapter[r].
+// t, for the streaming kernel: fp32 [parts][rows][width], the parts to be added up, column segment * rank + j: the rank-j input
+// of output `segment` (of the gate and up matrices in a SwiGLU).
+// op, for the matrix-core kernel: A operands of v_mfma_f32_16x16x32_bf16, 16 rows x 16 ranks each as two bf16 addends side by
+// side in the contraction (entries 0-15 the rounding of t, 16-31 the rounding of what that left: 16 bits of t count), number
+// (row / 16 * segments + segment) * (rank / 16) + j / 16.
+// b: per adapter 16-byte chunks of 8 ranks of one feature, chunk (feature / 16 * rank / 8 + j / 8) * 16 + feature % 16.
 struct LoraTerm {
   const float* t;
-  const u32x4 *b, *b2;
+  const u32x4 *op, *b, *b2;
   const int32_t* adapter;
   uint32_t n, rank, width, parts, segments;
 };
 
-// The rows of an adapter a row tile has, one adapter after the other in ascending order: ids of the tiles' rows, one a lane of
-// 16 (n from a row without one); the least id from `from` on, n if there is none.
-template <int RT>
-__device__ __forceinline__ uint32_t next_adapter(const uint32_t* id, uint32_t from, uint32_t n) {
-  uint32_t m = n;
-#pragma unroll
-  for (int i = 0; i < RT; ++i) m = min(m, id[i] >= from ? id[i] : n);
-#pragma unroll
-  for (int o = 1; o < 16; o *= 2) m = min(m, (uint32_t)__shfl_xor(m, o, 64));
-  return __builtin_amdgcn_readfirstlane(m);
-}
+// The adapter of a row: n for none, which is also that of rows past the end.
 __device__ __forceinline__ uint32_t adapter_of(const int32_t* adapter, uint32_t row, uint32_t rows, uint32_t n) {
   const uint32_t id = (uint32_t)adapter[min(row, rows - 1)];   // a negative one is beyond n
   return row < rows ? min(id, n) : n;
 }
-
-// Adds the term to RT row tiles (of 16, from row0) x CT tiles of 16 features whose accumulators are acc(i, j), lane layout of
-// v_mfma_f32_16x16x32_bf16.  MATS = 2: the tiles of two matrices in turn (j % 2), each a column segment of t; else segment(j).
-// tile(j): the feature tile.  A product takes 16 ranks: t goes in as two bf16 addends side by side in the contraction, its
-// rounding in entries 0-15 and what that left in 16-31, both against the same B, so 16 bits of t count.  The wavefronts share
-// the work by adapter and rank.  The products of a row tile are selected by row, not multiplied by zero, for rows of other
-// adapters or of none: an infinity or a NaN in one adapter's weights stays in its rows.
-template <int RT, int CT, int MATS, typename SEG, typename TILE, typename ACC>
-__device__ __forceinline__ void lora_add(const LoraTerm& L, uint32_t row0, uint32_t rows, uint32_t N, uint32_t share, uint32_t shares,
-                                         SEG segment, TILE tile, ACC acc) {
-  const uint32_t lane = threadIdx.x % 64, jl = lane % 16, kg = lane / 16, half = kg % 2;
+// The adapters that RT tiles of 16 rows have, one after the other: id is that of row 16 i + lane % 16, todo[i] the lanes whose
+// adapter has not come yet.  next: the adapter of the first of them and all rows that have it.
+template <int RT>
+struct AdapterWalk {
   uint32_t id[RT];
+  uint64_t todo[RT], match[RT];
+  uint32_t cur;
+  __device__ __forceinline__ AdapterWalk(const int32_t* adapter, uint32_t row0, uint32_t rows, uint32_t n) {
 #pragma unroll
-  for (int i = 0; i < RT; ++i) id[i] = adapter_of(L.adapter, row0 + 16 * i + jl, rows, L.n);
-  uint32_t turn = 0;
-  for (uint32_t cur = next_adapter<RT>(id, 0, L.n); cur < L.n; cur = next_adapter<RT>(id, cur + 1, L.n)) {
-    const size_t mat0 = (size_t)cur * (N / 16) * (L.rank / 8) * 16;
-    for (uint32_t ks = 0; ks < L.rank / 16; ++ks) {
-      if (turn++ % shares != share) continue;
-      u32x4 b[CT];
+    for (int i = 0; i < RT; ++i) id[i] = adapter_of(adapter, row0 + 16 * i + threadIdx.x % 16, rows, n);
 #pragma unroll
-      for (int j = 0; j < CT; ++j)
-        b[j] = (MATS == 2 && j % 2 ? L.b2 : L.b)[mat0 + ((size_t)tile(j) * (L.rank / 8) + 2 * ks + half) * 16 + jl];
+    for (int i = 0; i < RT; ++i) todo[i] = __ballot(id[i] < n);
+  }
+  __device__ __forceinline__ bool next() {
+    bool any = false;
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        __builtin_amdgcn_sched_barrier(0);   // one row tile after the other: their operands need not be there at once
-        const uint64_t match = __ballot(id[i] == cur);
-        if (match == 0) continue;
-        const uint32_t mine = (uint32_t)(match >> (4 * kg));   // bit v: row 4 kg + v of the tile
-        const float* row = L.t + (size_t)min(row0 + 16 * i + jl, rows - 1) * L.width + 16 * ks + 8 * half;
-        auto operand = [&](uint32_t seg) -> bf16x8 {
-          const float* t = row + seg * L.rank;
-          f32x4 lo = *(const f32x4*)t, hi = *(const f32x4*)(t + 4);
-          for (uint32_t p = 1; p < L.parts; ++p) {
-            t += (size_t)rows * L.width;
-            lo += *(const f32x4*)t;
-            hi += *(const f32x4*)(t + 4);
-          }
-          u32x4 a;
+    for (int i = RT - 1; i >= 0; --i)
+      if (todo[i]) {
+        cur = __builtin_amdgcn_readlane(id[i], (int)__builtin_ctzll(todo[i]));
+        any = true;
+      }
+    if (!any) return false;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = e < 2 ? lo[2 * e] : hi[2 * e - 4], y = e < 2 ? lo[2 * e + 1] : hi[2 * e - 3];
-            const uint32_t r = pack_bf16x2(x, y);
-            a[e] = kg < 2 ? r : pack_bf16x2(x - __uint_as_float(r << 16), y - __uint_as_float(r & 0xFFFF0000u));
-          }
-          return __builtin_bit_cast(bf16x8, a);
-        };
-        auto product = [&](bf16x8 a, int j, uint32_t take) {
-          const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, b[j]), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+    for (int i = 0; i < RT; ++i) {
+      match[i] = __ballot(id[i] == cur);
+      todo[i] &= ~match[i];
+    }
+    return true;
+  }
+};
+
+// The adapter that all rows of 16 have (L.n: they have not), row0 the first of them.
+__device__ __forceinline__ uint32_t tile_adapter(const LoraTerm& L, uint32_t row0, uint32_t rows) {
+  const uint32_t id = adapter_of(L.adapter, row0 + threadIdx.x % 16, rows, L.n), first = __builtin_amdgcn_readfirstlane(id);
+  return __ballot(id == first) == ~0ull ? first : L.n;
+}
+
+// The wavefront's part of a term, operands and accumulators in the lane layout of v_mfma_f32_16x16x32_bf16: CT tiles of 16
+// features; MATS = 2: those of two matrices in turn (j % 2), each a column segment of t, else segment(j); tile(j): the feature
+// tile; N: all features.
+template <int CT, int MATS, typename SEG, typename TILE>
+struct LoraTiles {
+  const LoraTerm& L;
+  uint32_t N;
+  SEG segment;
+  TILE tile;
+  static constexpr int kSets = MATS;   // operands of t for a row tile and 16 ranks
+  // a product takes 16 ranks: both halves of the contraction meet the same weights
+  __device__ __forceinline__ void weights(uint32_t adapter, uint32_t ks, bf16x8 (&b)[CT]) const {
+    const size_t at = ((size_t)adapter * (N / 16) * (L.rank / 8) + 2 * ks) * 16 + threadIdx.x / 16 % 2 * 16 + threadIdx.x % 16;
 #pragma unroll
-          for (int v = 0; v < 4; ++v) acc(i, j)[v] = (take >> v & 1) ? acc(i, j)[v] + d[v] : acc(i, j)[v];
-        };
-        if constexpr (MATS == 2) {
+    for (int j = 0; j < CT; ++j)
+      b[j] = __builtin_bit_cast(bf16x8, (MATS == 2 && j % 2 ? L.b2 : L.b)[at + (size_t)tile(j) * (L.rank / 8) * 16]);
+  }
+  __device__ __forceinline__ bf16x8 operand(uint32_t row_tile, uint32_t seg, uint32_t ks) const {
+    return __builtin_bit_cast(bf16x8, L.op[(((size_t)row_tile * L.segments + seg) * (L.rank / 16) + ks) * 64 + threadIdx.x % 64]);
+  }
+};
+
+// Adds the term of the row tiles (RT of 16 rows, from row0) whose rows all have one adapter to the accumulators acc(i, j).
+// share, of shares: the 16 ranks that are this wavefront's.
+template <int RT, int CT, int MATS, typename SEG, typename TILE, typename ACC>
+__device__ __forceinline__ void lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T, uint32_t row0, uint32_t rows, uint32_t share,
+                                         uint32_t shares, ACC acc) {
+  const uint32_t last = (rows - 1) / 16, n = T.L.n;
+  uint32_t cur[RT];
 #pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            const bf16x8 a = operand(m);
+  for (int i = 0; i < RT; ++i) cur[i] = tile_adapter(T.L, row0 + 16 * i, rows);
+  for (uint32_t ks = share; ks < T.L.rank / 16; ks += shares) {
+    constexpr int G = RT * MATS > 8 ? 8 / MATS : RT;   // row tiles whose operands are requested at once
+    bf16x8 a[G][MATS], b[CT];
 #pragma unroll
-            for (int j = m; j < CT; j += 2) product(a, j, mine);
-          }
-        } else {
-          // one segment for all tiles, but where the border between two outputs lies within them
-          for (uint32_t seg = segment(0); seg <= segment(CT - 1); ++seg) {
-            const bf16x8 a = operand(seg);
+    for (int i0 = 0; i0 < RT; i0 += G) {
+      // a row tile past the end or without an adapter takes an operand that is there, and no product
 #pragma unroll
-            for (int j = 0; j < CT; ++j) product(a, j, segment(j) == seg ? mine : 0u);
-          }
+      for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) a[g][m] = T.operand(min(row0 / 16 + i0 + g, last), MATS == 2 ? m : T.segment(0), ks);
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int i = i0 + g;
+        if (cur[i] >= n) continue;
+        if (i == 0 || cur[i] != cur[i - (i > 0)]) T.weights(cur[i], ks, b);
+#pragma unroll
+        for (int j = 0; j < CT; ++j) {
+          // where the border between two outputs lies within the tiles
+          if (MATS == 1 && j > 0 && T.segment(j) != T.segment(j - 1)) a[g][0] = T.operand(row0 / 16 + i, T.segment(j), ks);
+          acc(i, j) = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[g][j % MATS], b[j], acc(i, j), 0, 0, 0);
+        }
+      }
+    }
+  }
+}
+
+// The term of a row tile (16 rows from row0) that has several adapters, or rows without one; zero for any other.  A product has all
+// 16 rows in it and each row takes that of its own adapter: selected, not multiplied by zero, so an infinity or a NaN in one
+// adapter's weights stays in its rows.
+template <int CT, int MATS, typename SEG, typename TILE>
+__device__ __forceinline__ void lora_mixed(const LoraTiles<CT, MATS, SEG, TILE>& T, uint32_t row0, uint32_t rows, f32x4 (&sum)[CT]) {
+  const uint32_t kg = threadIdx.x % 64 / 16;
+#pragma unroll
+  for (int j = 0; j < CT; ++j) sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  AdapterWalk<1> walk(T.L.adapter, row0, rows, T.L.n);
+  if (tile_adapter(T.L, row0, rows) < T.L.n) return;
+  const uint32_t seg0 = MATS == 2 ? 0 : T.segment(0), seg1 = MATS == 2 ? 1 : T.segment(CT - 1);
+  while (walk.next()) {
+    const uint32_t mine = (uint32_t)(walk.match[0] >> (4 * kg));   // bit v: row 4 kg + v
+    for (uint32_t ks = 0; ks < T.L.rank / 16; ++ks) {
+      bf16x8 b[CT];
+      T.weights(walk.cur, ks, b);
+      for (uint32_t seg = seg0; seg <= seg1; ++seg) {
+        const bf16x8 a = T.operand(row0 / 16, seg, ks);
+#pragma unroll
+        for (int j = 0; j < CT; ++j) {
+          const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[j], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          const uint32_t take = (MATS == 2 ? (uint32_t)(j % 2) : T.segment(j)) == seg ? mine : 0u;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sum[j][v] = (take >> v & 1) ? sum[j][v] + d[v] : sum[j][v];
         }
       }
     }

@@ -116,6 +116,20 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  auto lora_tiles = [&](const auto& term) {
+    // B tile j of the wavefront: features past the end take the last tile's, as their weights do
+    auto tile = [&](int j) -> uint32_t {
+      const uint32_t bt = NJ * wc + j, most = dst.start[3] / 16 - 1;
+      return SWIGLU ? min(nt * (TB / 2) + bt / 2, most) : min(nt * TB + bt, most);
+    };
+    auto segment = [=](int j) -> uint32_t {
+      if (SWIGLU) return j % 2;   // a wavefront's tiles begin with a gate tile
+      const uint32_t n = 16 * tile(j);
+      return n >= dst.start[2] ? 2 : n >= dst.start[1] ? 1 : 0;
+    };
+    return LoraTiles<NJ, SWIGLU ? 2 : 1, decltype(segment), decltype(tile)>{term, dst.start[3], segment, tile};
+  };
+
   auto stage = [&](auto c) -> u32x4* {
     if constexpr (decltype(c)::v % S == 0) return st0;
     else if constexpr (decltype(c)::v % S == 1) return st1;
@@ -191,6 +205,9 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   __builtin_amdgcn_sched_barrier(0);
   request(Int<2>{}, 2, Int<PAIR ? NA : 0>{}, Int<ND>{});
   __builtin_amdgcn_sched_barrier(0);
+  // The low-rank term first, while the stages fill: what it loads is waited for together with them.
+  if constexpr (sizeof...(LORA) > 0)
+    lora_add<MI>(lora_tiles(lora...), r0 + wr * (16 * MI), rows, grp, KS, [&](int i, int j) -> f32x4& { return acc[i][j]; });
   __builtin_amdgcn_s_waitcnt(wait_vm((S - 2) * (PAIR ? NB : ND)));
   bare_barrier();
   const bool second = PING && wv >= 4;   // the wavefront of a SIMD that is half a step behind
@@ -209,22 +226,6 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   if (PING && !second) bare_barrier();   // every wavefront passes the same number of barriers
   __builtin_amdgcn_s_waitcnt(wait_vm(0));   // the stages are free once the last requests have arrived
   __syncthreads();
-
-  if constexpr (sizeof...(LORA) > 0) {
-    // B tile j of the wavefront: features past the end take the last tile's, as their weights do
-    const uint32_t most = dst.start[3] / 16 - 1;
-    auto tile = [&](int j) -> uint32_t {
-      const uint32_t bt = NJ * wc + j;
-      return SWIGLU ? min(nt * (TB / 2) + bt / 2, most) : min(nt * TB + bt, most);
-    };
-    auto segment = [&](int j) -> uint32_t {
-      if (SWIGLU) return j % 2;   // a wavefront's tiles begin with a gate tile
-      const uint32_t n = 16 * tile(j);
-      return n >= dst.start[2] ? 2 : n >= dst.start[1] ? 1 : 0;
-    };
-    lora_add<MI, NJ, SWIGLU ? 2 : 1>(lora..., r0 + wr * (16 * MI), rows, dst.start[3], grp, KS, segment, tile,
-                                     [&](int i, int j) -> f32x4& { return acc[i][j]; });
-  }
 
   // the row tiles this wavefront writes out: with two groups, the first half is summed and written by group 0,
   // the second by group 1
@@ -272,10 +273,13 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   float(*e)[ES] = (float(*)[ES])((wv % 2 ? (char*)st1 : (char*)st0) + (wv / 2) * (16 * ES * 4));
 #pragma unroll
   for (int i = 0; i < MO; ++i) {
+    f32x4 mixed[NJ];
+    if constexpr (sizeof...(LORA) > 0) lora_mixed(lora_tiles(lora...), r0 + wr * (16 * MI) + (grp * MO + i) * 16, rows, mixed);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
+      if constexpr (sizeof...(LORA) > 0) res[i][j] += mixed[j];
       const int col = SWIGLU ? (int)(CW / 2) * (j % 2) + 16 * (j / 2) + jl : 16 * j + jl;
 #pragma unroll
       for (int v = 0; v < 4; ++v) e[4 * kg + v][col] = res[i][j][v];

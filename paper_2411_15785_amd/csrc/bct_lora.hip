@@ -4,13 +4,13 @@
 //   out[r] = x[r] W^T + scale_a (x[r] A_a^T) B_a^T
 //
 // The first half, t = scale_a x A_a^T, is this file's kernel; the second is added to the accumulators of the projection
-// itself (lora_add), so the rows' outputs are rounded once and not read again.
+// itself (lora_add) or to the outputs before their rounding (lora_outputs), so they are rounded once and not read again.
 //
 // The first half reads every adapter in use once, A_a [rank][K], and is bound by that in a decode batch, where every row
 // may have another one, and by reading x for many rows.  A workgroup takes 16 rows and the adapters they have, one after the
 // other, on v_mfma_f32_16x16x32_bf16 (rows = token rows, columns = ranks); rows of other adapters go through the product as
 // well and are not stored.  What fills the chip when rows are few: the adapters of a row tile are dealt out to several
-// workgroups, and so is K, in parts that the second half adds up.
+// workgroups, and so is K, in parts that the second half (a decode batch) or a small kernel (many rows) adds up.
 #include "bct_lora.h"
 
 #include "bct_device.h"
@@ -23,84 +23,142 @@ namespace {
 constexpr uint32_t kMaxRank = 256;
 
 struct LoraPlan {
+  uint32_t row_tiles;     // of 16 rows, of a workgroup
   uint32_t parts;         // of K
   uint32_t chunks, each;  // the columns of t: so many workgroups, each so many tiles of 16
 };
+
+uint32_t tiles_of(uint32_t rows, uint32_t each) { return rows / each + (rows % each != 0); }
 
 LoraPlan lora_plan(uint32_t rows, uint32_t K, uint32_t width) {
   LoraPlan p;
   const uint32_t tiles = width / 16;
   p.chunks = (tiles + 3) / 4;
   p.each = (tiles + p.chunks - 1) / p.chunks;
+  p.row_tiles = rows >= 512 ? 2 : 1;
   // as many parts as give the chip two workgroups a compute unit, each wavefront at least two steps of 32 inputs
-  const uint64_t groups = (uint64_t)((rows / 16 + (rows % 16 != 0))) * p.chunks;
+  const uint64_t groups = (uint64_t)tiles_of(rows, 16 * p.row_tiles) * p.chunks;
   p.parts = 1;
   while (p.parts < 8 && groups * p.parts * 2 <= 512 && K / 32 >= 16 * p.parts) p.parts *= 2;
   return p;
 }
 
-template <bool XT, int CT>
+// Where the operands of 16 rows x 16 ranks are written: 8 ranks of a row, as their rounding and the rounding of what it left.
+__device__ __forceinline__ void store_operand(u32x4* op, size_t number, uint32_t row, uint32_t half, const float* t) {
+  u32x4 hi, lo;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t r = pack_bf16x2(t[2 * e], t[2 * e + 1]);
+    hi[e] = r;
+    lo[e] = pack_bf16x2(t[2 * e] - __uint_as_float(r << 16), t[2 * e + 1] - __uint_as_float(r & 0xFFFF0000u));
+  }
+  op[number * 64 + 16 * half + row] = hi;
+  op[number * 64 + 16 * (2 + half) + row] = lo;
+}
+
+// OP: t goes out as operands (one part of K), else as fp32.
+template <bool XT, int CT, int RT, bool OP>
 __global__ __launch_bounds__(256) void lora_inputs_kernel(const uint16_t* __restrict__ x, const u32x4* __restrict__ a,
                                                           const float* __restrict__ scale,
                                                           const int32_t* __restrict__ adapter, float* __restrict__ t,
                                                           uint32_t rows, uint32_t K, uint32_t width, uint32_t n, uint32_t chunks) {
   constexpr int WAVES = 4, U = 4;
-  __shared__ float sC[WAVES][CT][16][17];
+  __shared__ __attribute__((aligned(16))) float sC[WAVES][CT][RT][16][20];
   const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, jl = lane % 16, kg = lane / 16;
-  const uint32_t r0 = blockIdx.x / chunks * 16, ct0 = blockIdx.x % chunks * CT, tiles = width / 16, KT = K / 32;
+  const uint32_t r0 = blockIdx.x / chunks * (16 * RT), ct0 = blockIdx.x % chunks * CT, tiles = width / 16, KT = K / 32;
   const uint32_t part = blockIdx.z, parts = gridDim.z;
   const uint32_t p0 = (uint32_t)((uint64_t)part * KT / parts), p1 = (uint32_t)((uint64_t)(part + 1) * KT / parts);
   const uint32_t kt0 = p0 + wave * (p1 - p0) / WAVES, n_t = p0 + (wave + 1) * (p1 - p0) / WAVES - kt0;
-  const uint16_t* xr = XT ? x + (((size_t)(r0 / 32) * KT + kt0) * 128 + r0 % 32 / 16 * 64 + lane) * 8
-                          : x + (size_t)min(r0 + jl, rows - 1) * K + (size_t)kt0 * 32 + kg * 8;
+  const uint16_t* xr[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)   // RT = 2: both halves of a group of 32 rows
+    xr[i] = XT ? x + (((size_t)(r0 / 32) * KT + kt0) * 128 + (r0 % 32 / 16 + i) * 64 + lane) * 8
+               : x + (size_t)min(r0 + 16 * i + jl, rows - 1) * K + (size_t)kt0 * 32 + kg * 8;
   constexpr size_t xstep = XT ? 128 * 8 : 32;
-  const uint32_t id[1] = {adapter_of(adapter, r0 + jl, rows, n)};
+  AdapterWalk<RT> walk(adapter, r0, rows, n);
   uint32_t turn = 0;
-  for (uint32_t cur = next_adapter<1>(id, 0, n); cur < n; cur = next_adapter<1>(id, cur + 1, n)) {
+  while (walk.next()) {
     if (turn++ % gridDim.y != blockIdx.y) continue;
     const u32x4* at[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c)   // tiles past the end: the last one again, not stored
-      at[c] = a + (((size_t)cur * tiles + min(ct0 + c, tiles - 1)) * KT + kt0) * 64 + lane;
-    f32x4 acc[CT];
+      at[c] = a + (((size_t)walk.cur * tiles + min(ct0 + c, tiles - 1)) * KT + kt0) * 64 + lane;
+    f32x4 acc[CT][RT];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int i = 0; i < RT; ++i) acc[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (uint32_t s = 0; s < n_t; s += U) {
-      u32x4 av[U][CT], xv[U];
+      u32x4 av[U][CT], xv[U][RT];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint32_t i = min(s + u, n_t - 1);
 #pragma unroll
         for (int c = 0; c < CT; ++c) av[u][c] = at[c][(size_t)i * 64];
-        xv[u] = *(const u32x4*)(xr + i * xstep);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) xv[u][r] = *(const u32x4*)(xr[r] + i * xstep);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (s + u < n_t) {
 #pragma unroll
           for (int c = 0; c < CT; ++c)
-            acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[u]),
-                                                             __builtin_bit_cast(bf16x8, av[u][c]), acc[c], 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+              acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[u][r]),
+                                                                  __builtin_bit_cast(bf16x8, av[u][c]), acc[c][r], 0, 0, 0);
         }
     }
     __syncthreads();   // the sums of the adapter before have been read
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) sC[wave][c][4 * kg + v][jl] = acc[c][v];
-    __syncthreads();
-    const uint32_t row = r0 + threadIdx.x / 16, col = threadIdx.x % 16;
-    if (adapter_of(adapter, row, rows, n) == cur) {
-      const float f = scale ? scale[cur] : 1.0f;
+      for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
-        if (ct0 + c < tiles) {
-          const uint32_t i = threadIdx.x / 16;
-          t[((size_t)part * rows + row) * width + (ct0 + c) * 16 + col] =
-              f * ((sC[0][c][i][col] + sC[1][c][i][col]) + (sC[2][c][i][col] + sC[3][c][i][col]));
-        }
+        for (int v = 0; v < 4; ++v) sC[wave][c][r][4 * kg + v][jl] = acc[c][r][v];
+    __syncthreads();
+    // eight ranks of a row at a time
+    const float f = scale ? scale[walk.cur] : 1.0f;
+    for (uint32_t e = threadIdx.x; e < CT * RT * 32; e += 256) {
+      const uint32_t half = e % 2, i = e / 2 % 16, r = e / 32 % RT, c = e / 32 / RT, row = r0 + 16 * r + i;
+      if (ct0 + c >= tiles || adapter_of(adapter, row, rows, n) != walk.cur) continue;
+      float sum[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t j = 8 * half + k;
+        sum[k] = f * ((sC[0][c][r][i][j] + sC[1][c][r][i][j]) + (sC[2][c][r][i][j] + sC[3][c][r][i][j]));
+      }
+      if (OP) {
+        store_operand((u32x4*)t, (size_t)(row / 16) * tiles + ct0 + c, i, half, sum);
+      } else {
+        float* o = t + ((size_t)part * rows + row) * width + (ct0 + c) * 16 + 8 * half;
+        *(f32x4*)o = f32x4{sum[0], sum[1], sum[2], sum[3]};
+        *(f32x4*)(o + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+      }
     }
   }
+}
+
+// The parts of t, fp32, added up into operands: a thread takes eight ranks of a row.
+__global__ __launch_bounds__(256) void lora_operands_kernel(const float* __restrict__ t, u32x4* __restrict__ op,
+                                                            uint32_t rows, uint32_t width, uint32_t parts) {
+  const uint32_t eights = width / 8;
+  const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= (size_t)rows * eights) return;
+  const uint32_t row = (uint32_t)(e / eights), c = (uint32_t)(e % eights);
+  float sum[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum[k] = 0.f;
+  for (uint32_t p = 0; p < parts; ++p) {
+    const f32x4* v = (const f32x4*)(t + ((size_t)p * rows + row) * width + 8 * c);
+    const f32x4 lo = v[0], hi = v[1];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      sum[k] += lo[k];
+      sum[4 + k] += hi[k];
+    }
+  }
+  store_operand(op, (size_t)(row / 16) * (width / 16) + c / 2, row % 16, c % 2, sum);
 }
 
 // Row-major b [N][rank] -> 16-byte chunks of 8 ranks of one feature, (n / 16 * rank / 8 + k / 8) * 16 + n % 16.
@@ -112,8 +170,10 @@ __global__ __launch_bounds__(256) void lora_pack_kernel(const uint16_t* __restri
   packed[c] = *(const u32x4*)(b + n * rank + c / 16 % (rank / 8) * 8);
 }
 
+// Room for the parts in fp32 and for the operands, which are whole tiles of 16 rows.
 size_t lora_bytes(uint32_t rows, uint32_t K, uint32_t width) {
-  return (size_t)lora_plan(rows, K, width).parts * rows * width * sizeof(float);
+  const size_t one = (size_t)tiles_of(rows, 16) * 16 * width * sizeof(float);
+  return one * (lora_plan(rows, K, width).parts + 1);
 }
 
 }  // namespace
@@ -123,7 +183,7 @@ bct_status check_lora(const bctm_lora* l, uint32_t rows, uint32_t K, uint32_t N,
   if (swiglu != (l->b_up != nullptr)) return mfail(BCT_ERR_INVALID_ARG, "adapters: b_up goes with a SwiGLU");
   if (l->rank % 16 != 0 || l->rank > kMaxRank) return mfail(BCT_ERR_UNSUPPORTED, "adapters: rank must be a multiple of 16, at most 256");
   if (l->n_adapters > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many adapters");
-  if ((uint64_t)((rows / 16 + (rows % 16 != 0))) * lora_plan(rows, K, segments * l->rank).chunks > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many rows");
+  if ((uint64_t)tiles_of(rows, 16) * lora_plan(rows, K, segments * l->rank).chunks > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many rows");
   if ((uint64_t)l->n_adapters * l->rank > (1ull << 56) / ((uint64_t)N + (uint64_t)segments * K)) return mfail(BCT_ERR_UNSUPPORTED, "too many adapters");
   if (!al16(l->a) || !al16(l->b) || !al16(l->b_up) || !al16(l->workspace)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
   if (!l->workspace || l->workspace_bytes < lora_bytes(rows, K, segments * l->rank))
@@ -131,32 +191,52 @@ bct_status check_lora(const bctm_lora* l, uint32_t rows, uint32_t K, uint32_t N,
   return BCT_OK;
 }
 
-template <bool XT>
-static void launch_inputs(const bctm_lora& l, const void* x, uint32_t rows, uint32_t K, uint32_t width, const LoraPlan& p,
+template <bool XT, int RT, bool OP>
+static void launch_inputs(const bctm_lora& l, const void* x, void* t, uint32_t rows, uint32_t K, uint32_t width, const LoraPlan& p,
                           hipStream_t s) {
-  const uint32_t tiles = (rows / 16 + (rows % 16 != 0)), most = l.n_adapters < 16 ? l.n_adapters : 16;
+  const uint32_t tiles = tiles_of(rows, 16 * RT), most = l.n_adapters < 16 * RT ? l.n_adapters : 16 * RT;
   uint32_t slots = 1;
   while (slots < most && rows > 1 && (uint64_t)tiles * p.chunks * p.parts * slots * 2 <= 1024) slots *= 2;
   const dim3 grid(tiles * p.chunks, slots, p.parts), block(256);
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, block, 0, s, (const uint16_t*)x, (const u32x4*)l.a, l.scale, l.adapter, (float*)l.workspace,
-                       rows, K, width, l.n_adapters, p.chunks);
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, (const uint16_t*)x, (const u32x4*)l.a, l.scale, l.adapter, (float*)t, rows, K,
+                       width, l.n_adapters, p.chunks);
   };
   switch (p.each) {
-    case 1: return launch(lora_inputs_kernel<XT, 1>);
-    case 2: return launch(lora_inputs_kernel<XT, 2>);
-    case 3: return launch(lora_inputs_kernel<XT, 3>);
-    default: return launch(lora_inputs_kernel<XT, 4>);
+    case 1: return launch(lora_inputs_kernel<XT, 1, RT, OP>);
+    case 2: return launch(lora_inputs_kernel<XT, 2, RT, OP>);
+    case 3: return launch(lora_inputs_kernel<XT, 3, RT, OP>);
+    default: return launch(lora_inputs_kernel<XT, 4, RT, OP>);
+  }
+}
+template <bool XT>
+static void launch_inputs_of(const bctm_lora& l, const void* x, void* t, uint32_t rows, uint32_t K, uint32_t width,
+                             const LoraPlan& p, bool operands, hipStream_t s) {
+  if (p.row_tiles == 2) {
+    if (operands) launch_inputs<XT, 2, true>(l, x, t, rows, K, width, p, s);
+    else launch_inputs<XT, 2, false>(l, x, t, rows, K, width, p, s);
+  } else {
+    if (operands) launch_inputs<XT, 1, true>(l, x, t, rows, K, width, p, s);
+    else launch_inputs<XT, 1, false>(l, x, t, rows, K, width, p, s);
   }
 }
 
 bct_status launch_lora_inputs(const bctm_lora& l, const void* x, uint32_t rows, uint32_t K, bool x_tiled, uint32_t segments,
-                              hipStream_t s, LoraTerm* term) {
+                              bool operands, hipStream_t s, LoraTerm* term) {
   const uint32_t width = segments * l.rank;
   const LoraPlan p = lora_plan(rows, K, width);
-  if (x_tiled) launch_inputs<true>(l, x, rows, K, width, p, s);
-  else launch_inputs<false>(l, x, rows, K, width, p, s);
-  *term = {(const float*)l.workspace, (const u32x4*)l.b, (const u32x4*)l.b_up, l.adapter, l.n_adapters, l.rank, width, p.parts, segments};
+  // the operands first, then the parts
+  u32x4* op = (u32x4*)l.workspace;
+  float* t = (float*)l.workspace + (size_t)tiles_of(rows, 16) * 16 * width;
+  const bool at_once = operands && p.parts == 1;
+  if (x_tiled) launch_inputs_of<true>(l, x, at_once ? (void*)op : t, rows, K, width, p, at_once, s);
+  else launch_inputs_of<false>(l, x, at_once ? (void*)op : t, rows, K, width, p, at_once, s);
+  if (operands && !at_once) {
+    const size_t blocks = ((size_t)rows * (width / 8) + 255) / 256;
+    if (blocks > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many rows");
+    hipLaunchKernelGGL(lora_operands_kernel, dim3((unsigned)blocks), dim3(256), 0, s, t, op, rows, width, p.parts);
+  }
+  *term = {t, op, (const u32x4*)l.b, (const u32x4*)l.b_up, l.adapter, l.n_adapters, l.rank, width, p.parts, segments};
   return launched("lora");
 }
 

@@ -58,6 +58,75 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const uint16_t* __restri
   packed[c] = *(const u32x4*)(x + (size_t)r * K + k);
 }
 
+// The low-rank term of the outputs that a thread of the streaming kernel writes: output o = threadIdx + q * NTHR of feature tile
+// f, row o / 16 and feature o % 16.  A decode batch has an adapter for nearly every row, so a matrix product would compute 16
+// rows for one; a thread takes the dot product of its own row's t with its own feature's row of B instead, rank fp32 products.
+// t comes through LDS, 32 ranks at a time, where its parts are added up once for the workgroup.
+template <bool SWIGLU, int FT, int ROWS, int NTHR, int OPT>
+__device__ __forceinline__ void lora_outputs(const LoraTerm& L, const LinearOut& dst, uint32_t r0, uint32_t nt0, uint32_t rows,
+                                             float (&delta)[FT][SWIGLU ? 2 : 1][OPT]) {
+  constexpr int NW2 = SWIGLU ? 2 : 1, RC = 32;
+  __shared__ __attribute__((aligned(16))) float sT[ROWS][RC + 4];
+  const uint32_t N = dst.start[3];
+  auto segment_of = [&](int f) -> uint32_t {
+    const uint32_t n = 16 * (nt0 + f);
+    return n >= dst.start[2] ? 2 : n >= dst.start[1] ? 1 : 0;
+  };
+  uint32_t id[OPT];
+#pragma unroll
+  for (int q = 0; q < OPT; ++q) id[q] = adapter_of(L.adapter, r0 + (threadIdx.x + q * NTHR) % (ROWS * 16) / 16, rows, L.n);
+#pragma unroll
+  for (int f = 0; f < FT; ++f)
+#pragma unroll
+    for (int m = 0; m < NW2; ++m)
+#pragma unroll
+      for (int q = 0; q < OPT; ++q) delta[f][m][q] = 0.f;
+  const uint32_t seg0 = SWIGLU ? 0 : segment_of(0), seg1 = SWIGLU ? 1 : segment_of(FT - 1);
+  for (uint32_t seg = seg0; seg <= seg1; ++seg)
+    for (uint32_t c0 = 0; c0 < L.rank; c0 += RC) {
+      const uint32_t cn = min(L.rank - c0, (uint32_t)RC);   // 16 or 32
+      __syncthreads();                                      // what the last round read
+      for (uint32_t e = threadIdx.x; e < ROWS * cn; e += NTHR) {
+        const uint32_t i = e / cn, k = e % cn;
+        if (adapter_of(L.adapter, r0 + i, rows, L.n) < L.n) {
+          const float* t = L.t + (size_t)(r0 + i) * L.width + seg * L.rank + c0 + k;
+          const size_t part = (size_t)rows * L.width;
+          float sum = 0.f;
+          for (uint32_t p = 0; p < L.parts; p += 4) {   // 1, 2, 4 or 8 parts; four requests at once
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = t[min(p + u, L.parts - 1) * part];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) sum += p + u < L.parts ? v[u] : 0.f;
+          }
+          sT[i][k] = sum;
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int f = 0; f < FT; ++f) {
+        if (!SWIGLU && segment_of(f) != seg) continue;
+#pragma unroll
+        for (int q = 0; q < OPT; ++q) {
+          if (id[q] >= L.n) continue;
+          const uint32_t o = (threadIdx.x + q * NTHR) % (ROWS * 16), i = o / 16, j = o % 16;
+          const u32x4* b = (SWIGLU && seg ? L.b2 : L.b) + (((size_t)id[q] * (N / 16) + nt0 + f) * (L.rank / 8) + c0 / 8) * 16 + j;
+          float sum = 0.f;
+          for (uint32_t k = 0; k < cn; k += 16) {
+            float v[16];
+            unpack16<BF16>(b[k * 2], v);
+            unpack16<BF16>(b[k * 2 + 16], v + 8);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum = __builtin_fmaf(v[e], sT[i][k + e], sum);
+          }
+#pragma unroll
+          for (int m = 0; m < NW2; ++m)
+            if (!SWIGLU || m == (int)seg) delta[f][m][q] += sum;
+        }
+      }
+    }
+}
+
 // FT: feature tiles (of 16) per workgroup.  Every wavefront streams FT (x 2 for SwiGLU) weight tiles against
 // each activation fragment it loads: the activations come from L2, where all workgroups ask for the same
 // lines at the same time, and with one weight tile per fragment that traffic (2 KB per KB of weights)
@@ -66,7 +135,7 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const uint16_t* __restri
 // two row tiles, 11008 -> 4096 17.6 us (21.5), 4096 -> 4096 11.9 (12.7), 4096 -> 32000 47.9 (50.1), SwiGLU
 // 4096 -> 11008 30.0 (32.2); at 16 rows 23.1 (25.8), 11.7 (12.7), 50.2 (52.2), 33.8 (34.2).  4096 -> 12288 (three feature
 // tiles): see streaming_row_tiles.
-// LORA: none, or a LoraTerm: the rows' low-rank term is added to the accumulators, its adapters shared among the wavefronts.
+// LORA: none, or a LoraTerm: the rows' low-rank term is added to the outputs (lora_outputs).
 template <bool SWIGLU, bool XT, int WAVES, int U, int FT, int RT, typename... LORA>
 __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __restrict__ x,
                                                             const u32x4* __restrict__ w,
@@ -96,6 +165,9 @@ __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __re
     xr[j] = XT ? x + (((size_t)(r0 / 32) * KT + kt0) * 128 + j * 64 + lane) * 8
                : x + (size_t)min(r0 + 16 * j + jl, rows - 1) * K + (size_t)kt0 * 32 + kg * 8;
   constexpr size_t xstep = XT ? 128 * 8 : 32;
+  constexpr int OPT = (ROWS * 16 + NTHR - 1) / NTHR;   // outputs per thread and tile
+  float delta[FT][NW2][OPT];                           // the low-rank term of a thread's outputs
+  if constexpr (sizeof...(LORA) > 0) lora_outputs<SWIGLU, FT, ROWS, NTHR, OPT>(lora..., dst, r0, nt0, rows, delta);
   f32x4 acc[NS][RT];
 #pragma unroll
   for (int s = 0; s < NS; ++s)
@@ -138,20 +210,9 @@ __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __re
                                                               __builtin_bit_cast(bf16x8, b[u][s]), acc[s][j], 0, 0, 0);
     }
   }
-  if constexpr (sizeof...(LORA) > 0) {
-    auto tile = [&](int s) -> uint32_t { return nt0 + s / NW2; };
-    auto segment = [&](int s) -> uint32_t {
-      if (SWIGLU) return s % NW2;
-      const uint32_t n = 16 * tile(s);
-      return n >= dst.start[2] ? 2 : n >= dst.start[1] ? 1 : 0;
-    };
-    lora_add<RT, NS, NW2>(lora..., r0, rows, dst.start[3], wave, WAVES, segment, tile,
-                          [&](int i, int s) -> f32x4& { return acc[s][i]; });
-  }
   // accumulator element v of a lane: token row 4 * kg + v of the row tile, feature jl.  Per feature tile
   // the partials of all wavefronts go through LDS (one matrix at a time through the same buffer) and
   // every thread adds them in wave order for the outputs it owns (ROWS x 16 per tile).
-  constexpr int OPT = (ROWS * 16 + NTHR - 1) / NTHR;   // outputs per thread and tile
 #pragma unroll
   for (int f = 0; f < FT; ++f) {
     float sum[NW2][OPT];
@@ -170,6 +231,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __re
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) a += sC[k][oi][oj];
         sum[pass][q] = a;
+        if constexpr (sizeof...(LORA) > 0) sum[pass][q] += delta[f][pass][q];
       }
     }
 #pragma unroll
@@ -519,6 +581,11 @@ static bct_status launch_linear(const void* x, const void* w, const void* residu
   return launched("linear");
 }
 
+static bool many_rows(uint32_t rows, uint32_t K, uint32_t N, bool swiglu) {   // the matrix-core kernel?
+  const uint32_t kernel = linear_kernel_of(rows, K, N, swiglu);
+  return kernel == BCTM_KERNEL_TILE128 || kernel == BCTM_KERNEL_TILE256;
+}
+
 static bct_status linear_call(const void* x, const void* w, const void* residual, void* out, uint32_t rows, uint32_t K,
                               uint32_t N, uint32_t flags, const bctm_lora* lora, void* hip_stream) {
   const bct_status st = check_linear(x, w, out, rows, K, N);
@@ -530,7 +597,7 @@ static bct_status linear_call(const void* x, const void* w, const void* residual
   LoraTerm term;
   if (lora) {
     bct_status ls = check_lora(lora, rows, K, N, 1, false);
-    if (ls == BCT_OK) ls = launch_lora_inputs(*lora, x, rows, K, flags & BCTM_X_TILED, 1, (hipStream_t)hip_stream, &term);
+    if (ls == BCT_OK) ls = launch_lora_inputs(*lora, x, rows, K, flags & BCTM_X_TILED, 1, many_rows(rows, K, N, false), (hipStream_t)hip_stream, &term);
     if (ls != BCT_OK) return ls;
   }
   return launch_linear(x, w, residual, dst, rows, K, N, flags, lora ? &term : nullptr, hip_stream);
@@ -565,7 +632,7 @@ static bct_status linear_split_call(const void* x, const void* w, void* out0, ui
   if (lora) {
     const uint32_t segments = N2 ? 3 : 2;
     bct_status ls = check_lora(lora, rows, K, N, segments, false);
-    if (ls == BCT_OK) ls = launch_lora_inputs(*lora, x, rows, K, flags & BCTM_X_TILED, segments, (hipStream_t)hip_stream, &term);
+    if (ls == BCT_OK) ls = launch_lora_inputs(*lora, x, rows, K, flags & BCTM_X_TILED, segments, many_rows(rows, K, N, false), (hipStream_t)hip_stream, &term);
     if (ls != BCT_OK) return ls;
   }
   return launch_linear(x, w, nullptr, dst, rows, K, N, flags, lora ? &term : nullptr, hip_stream);
@@ -596,7 +663,7 @@ static bct_status swiglu_call(const void* x, const void* w_gate, const void* w_u
   LoraTerm term;
   if (lora) {
     bct_status ls = check_lora(lora, rows, K, N, 2, true);
-    if (ls == BCT_OK) ls = launch_lora_inputs(*lora, x, rows, K, flags & BCTM_X_TILED, 2, (hipStream_t)hip_stream, &term);
+    if (ls == BCT_OK) ls = launch_lora_inputs(*lora, x, rows, K, flags & BCTM_X_TILED, 2, many_rows(rows, K, N, true), (hipStream_t)hip_stream, &term);
     if (ls != BCT_OK) return ls;
   }
   const LoraTerm* more = lora ? &term : nullptr;
