@@ -38,7 +38,8 @@ struct LoraTerm {
 
 // The adapter of a row: n for none, which is also that of rows past the end.
 __device__ __forceinline__ uint32_t adapter_of(const int32_t* adapter, uint32_t row, uint32_t rows, uint32_t n) {
-  const uint32_t id = (uint32_t)adapter[min(row, rows - 1)];   // a negative one is beyond n
+  uint32_t id = (uint32_t)adapter[min(row, rows - 1)];   // a negative one is beyond n
+  asm("" : "+v"(id));   // requested in any case: behind a branch, several of them would be waited for one by one
   return row < rows ? min(id, n) : n;
 }
 // The adapters that RT tiles of 16 rows have, one after the other: id is that of row 16 i + lane % 16, todo[i] the lanes whose

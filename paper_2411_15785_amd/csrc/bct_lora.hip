@@ -35,7 +35,7 @@ LoraPlan lora_plan(uint32_t rows, uint32_t K, uint32_t width) {
   const uint32_t tiles = width / 16;
   p.chunks = (tiles + 3) / 4;
   p.each = (tiles + p.chunks - 1) / p.chunks;
-  p.row_tiles = rows >= 512 ? 2 : 1;
+  p.row_tiles = rows >= 1024 ? 4 : rows >= 256 ? 2 : 1;
   // as many parts as give the chip two workgroups a compute unit, each wavefront at least two steps of 32 inputs
   const uint64_t groups = (uint64_t)tiles_of(rows, 16 * p.row_tiles) * p.chunks;
   p.parts = 1;
@@ -56,29 +56,42 @@ __device__ __forceinline__ void store_operand(u32x4* op, size_t number, uint32_t
   op[number * 64 + 16 * (2 + half) + row] = lo;
 }
 
-// OP: t goes out as operands (one part of K), else as fp32.
+// OP: t goes out as operands (one part of K), else as fp32.  Workgroup ids go round the eight XCDs: the parts of K are dealt to
+// them, so that an XCD's L2 sees one part of every adapter.
 template <bool XT, int CT, int RT, bool OP>
 __global__ __launch_bounds__(256) void lora_inputs_kernel(const uint16_t* __restrict__ x, const u32x4* __restrict__ a,
                                                           const float* __restrict__ scale,
                                                           const int32_t* __restrict__ adapter, float* __restrict__ t,
-                                                          uint32_t rows, uint32_t K, uint32_t width, uint32_t n, uint32_t chunks) {
+                                                          uint32_t rows, uint32_t K, uint32_t width, uint32_t n, uint32_t chunks,
+                                                          uint32_t slots, uint32_t parts) {
   constexpr int WAVES = 4, U = 4;
-  __shared__ __attribute__((aligned(16))) float sC[WAVES][CT][RT][16][20];
+  __shared__ __attribute__((aligned(16))) float sC[WAVES][RT][16][20];
   const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, jl = lane % 16, kg = lane / 16;
-  const uint32_t r0 = blockIdx.x / chunks * (16 * RT), ct0 = blockIdx.x % chunks * CT, tiles = width / 16, KT = K / 32;
-  const uint32_t part = blockIdx.z, parts = gridDim.z;
+  const uint32_t part = blockIdx.x % 8 % parts, work = blockIdx.x / 8 * (8 / parts) + blockIdx.x % 8 / parts;
+  const uint32_t groups = rows / (16 * RT) + (rows % (16 * RT) != 0), slot = work / (groups * chunks);
+  if (slot >= slots) return;   // the last round of ids
+  const uint32_t r0 = work / chunks % groups * (16 * RT), ct0 = work % chunks * CT, tiles = width / 16, KT = K / 32;
   const uint32_t p0 = (uint32_t)((uint64_t)part * KT / parts), p1 = (uint32_t)((uint64_t)(part + 1) * KT / parts);
   const uint32_t kt0 = p0 + wave * (p1 - p0) / WAVES, n_t = p0 + (wave + 1) * (p1 - p0) / WAVES - kt0;
   const uint16_t* xr[RT];
 #pragma unroll
-  for (int i = 0; i < RT; ++i)   // RT = 2: both halves of a group of 32 rows
-    xr[i] = XT ? x + (((size_t)(r0 / 32) * KT + kt0) * 128 + (r0 % 32 / 16 + i) * 64 + lane) * 8
-               : x + (size_t)min(r0 + 16 * i + jl, rows - 1) * K + (size_t)kt0 * 32 + kg * 8;
+  for (int i = 0; i < RT; ++i) {   // row tiles past the end: the last one again, not stored
+    const uint32_t row = min(r0 + 16 * i, (rows - 1) / 16 * 16);
+    xr[i] = XT ? x + (((size_t)(row / 32) * KT + kt0) * 128 + row % 32 / 16 * 64 + lane) * 8
+               : x + (size_t)min(row + jl, rows - 1) * K + (size_t)kt0 * 32 + kg * 8;
+  }
   constexpr size_t xstep = XT ? 128 * 8 : 32;
   AdapterWalk<RT> walk(adapter, r0, rows, n);
   uint32_t turn = 0;
   while (walk.next()) {
-    if (turn++ % gridDim.y != blockIdx.y) continue;
+    if (turn++ % slots != slot) continue;
+    // a row tile without this adapter is read as one that has it, from cache
+    const uint16_t* xs[RT];
+#pragma unroll
+    for (int i = RT - 1; i >= 0; --i)
+      if (walk.match[i]) xs[0] = xr[i];
+#pragma unroll
+    for (int i = RT - 1; i >= 0; --i) xs[i] = walk.match[i] ? xr[i] : xs[0];
     const u32x4* at[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c)   // tiles past the end: the last one again, not stored
@@ -88,75 +101,86 @@ __global__ __launch_bounds__(256) void lora_inputs_kernel(const uint16_t* __rest
     for (int c = 0; c < CT; ++c)
 #pragma unroll
       for (int i = 0; i < RT; ++i) acc[c][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // U steps' loads are issued before the first product; those past the end are the last step's again, against zeros
     for (uint32_t s = 0; s < n_t; s += U) {
+      const bool whole = s + U <= n_t;
       u32x4 av[U][CT], xv[U][RT];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const uint32_t i = min(s + u, n_t - 1);
+        const size_t i = whole ? s + u : min(s + u, n_t - 1);
 #pragma unroll
-        for (int c = 0; c < CT; ++c) av[u][c] = at[c][(size_t)i * 64];
+        for (int c = 0; c < CT; ++c) av[u][c] = at[c][i * 64];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) xv[u][r] = *(const u32x4*)(xr[r] + i * xstep);
+        for (int r = 0; r < RT; ++r) xv[u][r] = *(const u32x4*)(xs[r] + i * xstep);
+      }
+      if (!whole) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (s + u >= n_t) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) av[u][c] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int r = 0; r < RT; ++r) xv[u][r] = u32x4{0u, 0u, 0u, 0u};
+          }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (s + u < n_t) {
 #pragma unroll
-          for (int c = 0; c < CT; ++c)
+        for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-              acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[u][r]),
-                                                                  __builtin_bit_cast(bf16x8, av[u][c]), acc[c][r], 0, 0, 0);
-        }
+          for (int r = 0; r < RT; ++r)
+            acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[u][r]),
+                                                                __builtin_bit_cast(bf16x8, av[u][c]), acc[c][r], 0, 0, 0);
     }
-    __syncthreads();   // the sums of the adapter before have been read
+    // the wavefronts' sums, one tile of ranks after the other; eight ranks of a row at a time go out
+    const float f = scale ? scale[walk.cur] : 1.0f;
 #pragma unroll
-    for (int c = 0; c < CT; ++c)
+    for (int c = 0; c < CT; ++c) {
+      __syncthreads();   // what was there has been read
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) sC[wave][c][r][4 * kg + v][jl] = acc[c][r][v];
-    __syncthreads();
-    // eight ranks of a row at a time
-    const float f = scale ? scale[walk.cur] : 1.0f;
-    for (uint32_t e = threadIdx.x; e < CT * RT * 32; e += 256) {
-      const uint32_t half = e % 2, i = e / 2 % 16, r = e / 32 % RT, c = e / 32 / RT, row = r0 + 16 * r + i;
-      if (ct0 + c >= tiles || adapter_of(adapter, row, rows, n) != walk.cur) continue;
-      float sum[8];
+        for (int v = 0; v < 4; ++v) sC[wave][r][4 * kg + v][jl] = acc[c][r][v];
+      __syncthreads();
+      const uint32_t e = threadIdx.x, half = e % 2, i = e / 2 % 16, r = e / 32, row = r0 + 16 * r + i;
+      if (e < RT * 32 && ct0 + c < tiles && adapter_of(adapter, row, rows, n) == walk.cur) {
+        float sum[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint32_t j = 8 * half + k;
-        sum[k] = f * ((sC[0][c][r][i][j] + sC[1][c][r][i][j]) + (sC[2][c][r][i][j] + sC[3][c][r][i][j]));
-      }
-      if (OP) {
-        store_operand((u32x4*)t, (size_t)(row / 16) * tiles + ct0 + c, i, half, sum);
-      } else {
-        float* o = t + ((size_t)part * rows + row) * width + (ct0 + c) * 16 + 8 * half;
-        *(f32x4*)o = f32x4{sum[0], sum[1], sum[2], sum[3]};
-        *(f32x4*)(o + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t j = 8 * half + k;
+          sum[k] = f * ((sC[0][r][i][j] + sC[1][r][i][j]) + (sC[2][r][i][j] + sC[3][r][i][j]));
+        }
+        if (OP) {
+          store_operand((u32x4*)t, (size_t)(row / 16) * tiles + ct0 + c, i, half, sum);
+        } else {
+          float* o = t + ((size_t)part * rows + row) * width + (ct0 + c) * 16 + 8 * half;
+          *(f32x4*)o = f32x4{sum[0], sum[1], sum[2], sum[3]};
+          *(f32x4*)(o + 4) = f32x4{sum[4], sum[5], sum[6], sum[7]};
+        }
       }
     }
   }
 }
 
 // The parts of t, fp32, added up into operands: a thread takes eight ranks of a row.
+template <int PARTS>
 __global__ __launch_bounds__(256) void lora_operands_kernel(const float* __restrict__ t, u32x4* __restrict__ op,
-                                                            uint32_t rows, uint32_t width, uint32_t parts) {
+                                                            uint32_t rows, uint32_t width) {
   const uint32_t eights = width / 8;
   const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
   if (e >= (size_t)rows * eights) return;
   const uint32_t row = (uint32_t)(e / eights), c = (uint32_t)(e % eights);
+  f32x4 v[PARTS][2];
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) v[p][h] = ((const f32x4*)(t + ((size_t)p * rows + row) * width + 8 * c))[h];
   float sum[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) sum[k] = 0.f;
-  for (uint32_t p = 0; p < parts; ++p) {
-    const f32x4* v = (const f32x4*)(t + ((size_t)p * rows + row) * width + 8 * c);
-    const f32x4 lo = v[0], hi = v[1];
+  for (int k = 0; k < 8; ++k) {
+    sum[k] = v[0][k / 4][k % 4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      sum[k] += lo[k];
-      sum[4 + k] += hi[k];
-    }
+    for (int p = 1; p < PARTS; ++p) sum[k] += v[p][k / 4][k % 4];
   }
   store_operand(op, (size_t)(row / 16) * (width / 16) + c / 2, row % 16, c % 2, sum);
 }
@@ -183,7 +207,7 @@ bct_status check_lora(const bctm_lora* l, uint32_t rows, uint32_t K, uint32_t N,
   if (swiglu != (l->b_up != nullptr)) return mfail(BCT_ERR_INVALID_ARG, "adapters: b_up goes with a SwiGLU");
   if (l->rank % 16 != 0 || l->rank > kMaxRank) return mfail(BCT_ERR_UNSUPPORTED, "adapters: rank must be a multiple of 16, at most 256");
   if (l->n_adapters > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many adapters");
-  if ((uint64_t)tiles_of(rows, 16) * lora_plan(rows, K, segments * l->rank).chunks > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many rows");
+  if ((uint64_t)tiles_of(rows, 16) * lora_plan(rows, K, segments * l->rank).chunks > 0x0FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many rows");
   if ((uint64_t)l->n_adapters * l->rank > (1ull << 56) / ((uint64_t)N + (uint64_t)segments * K)) return mfail(BCT_ERR_UNSUPPORTED, "too many adapters");
   if (!al16(l->a) || !al16(l->b) || !al16(l->b_up) || !al16(l->workspace)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
   if (!l->workspace || l->workspace_bytes < lora_bytes(rows, K, segments * l->rank))
@@ -194,13 +218,14 @@ bct_status check_lora(const bctm_lora* l, uint32_t rows, uint32_t K, uint32_t N,
 template <bool XT, int RT, bool OP>
 static void launch_inputs(const bctm_lora& l, const void* x, void* t, uint32_t rows, uint32_t K, uint32_t width, const LoraPlan& p,
                           hipStream_t s) {
-  const uint32_t tiles = tiles_of(rows, 16 * RT), most = l.n_adapters < 16 * RT ? l.n_adapters : 16 * RT;
+  const uint32_t groups = tiles_of(rows, 16 * RT), most = l.n_adapters < 16 * RT ? l.n_adapters : 16 * RT;
   uint32_t slots = 1;
-  while (slots < most && rows > 1 && (uint64_t)tiles * p.chunks * p.parts * slots * 2 <= 1024) slots *= 2;
-  const dim3 grid(tiles * p.chunks, slots, p.parts), block(256);
+  while (slots < most && rows > 1 && (uint64_t)groups * p.chunks * p.parts * slots * 2 <= 1024) slots *= 2;
+  const uint64_t work = (uint64_t)groups * p.chunks * slots, per = 8 / p.parts;   // of one part
+  const dim3 grid((unsigned)(8 * ((work + per - 1) / per))), block(256);
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, s, (const uint16_t*)x, (const u32x4*)l.a, l.scale, l.adapter, (float*)t, rows, K,
-                       width, l.n_adapters, p.chunks);
+                       width, l.n_adapters, p.chunks, slots, p.parts);
   };
   switch (p.each) {
     case 1: return launch(lora_inputs_kernel<XT, 1, RT, OP>);
@@ -212,7 +237,10 @@ static void launch_inputs(const bctm_lora& l, const void* x, void* t, uint32_t r
 template <bool XT>
 static void launch_inputs_of(const bctm_lora& l, const void* x, void* t, uint32_t rows, uint32_t K, uint32_t width,
                              const LoraPlan& p, bool operands, hipStream_t s) {
-  if (p.row_tiles == 2) {
+  if (p.row_tiles == 4) {
+    if (operands) launch_inputs<XT, 4, true>(l, x, t, rows, K, width, p, s);
+    else launch_inputs<XT, 4, false>(l, x, t, rows, K, width, p, s);
+  } else if (p.row_tiles == 2) {
     if (operands) launch_inputs<XT, 2, true>(l, x, t, rows, K, width, p, s);
     else launch_inputs<XT, 2, false>(l, x, t, rows, K, width, p, s);
   } else {
@@ -234,7 +262,8 @@ bct_status launch_lora_inputs(const bctm_lora& l, const void* x, uint32_t rows, 
   if (operands && !at_once) {
     const size_t blocks = ((size_t)rows * (width / 8) + 255) / 256;
     if (blocks > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many rows");
-    hipLaunchKernelGGL(lora_operands_kernel, dim3((unsigned)blocks), dim3(256), 0, s, t, op, rows, width, p.parts);
+    const auto kernel = p.parts == 2 ? lora_operands_kernel<2> : p.parts == 4 ? lora_operands_kernel<4> : lora_operands_kernel<8>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, t, op, rows, width);
   }
   *term = {t, op, (const u32x4*)l.b, (const u32x4*)l.b_up, l.adapter, l.n_adapters, l.rank, width, p.parts, segments};
   return launched("lora");
