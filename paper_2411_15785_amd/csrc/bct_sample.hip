@@ -6,11 +6,16 @@
 //   n = the least of  top_k,  the fewest with cum(n) >= top_p * cum(top_k),  how many have w >= min_p;  at least 1
 //   drawn: the first j with cum(j) > u * cum(n)
 //
-// No sort: what is asked of the order is only where cumulated weights or counts pass a threshold.  A histogram of the row
-// over 1/64 octaves of w, with the count and the weight of each bin, says in which bin that is; a histogram of the keys of
-// that bin alone, once more where they are many, at which logit; and equal logits have equal weights, so the rest is a
-// division.  A token is a whole number, so the sums must not depend on an order of additions, nor on fp32 roundings: weights
-// are whole multiples of 2^-S, S at least 40 (a bit over half the digits of an fp64), added as 64-bit integers.
+// No sort: what is asked of the order is only where cumulated weights or counts pass a threshold, and histograms tell that.
+// A token is a whole number, so the sums must not depend on an order of additions, nor on fp32 roundings: weights are whole
+// multiples of 2^-S, S at least 40, added as 64-bit integers.
+//   bf16   a value is one of 65536, so the row is counted by value, exactly, in 128 KB of LDS (16 bits a value), and a weight
+//          is worked out for each value that occurs instead of for each token.  Sums over groups of 128 values say in which
+//          group the threshold is passed, the counts of that group at which value.
+//   fp32   a histogram of weights over 1/64 octaves of w; the bin where the threshold is passed is gathered and divided
+//          further by value.
+// Equal values have equal weights, so the rest is a division, and the token the nth with its value in the order of the indexes.
+// One workgroup a row, which it keeps in registers (bf16 up to 131072 tokens, fp32 65536; beyond, it is read again).
 #include <math.h>
 
 #include "bct_device.h"
@@ -21,8 +26,9 @@ namespace bct {
 namespace {
 
 constexpr uint32_t kThreads = 1024;
-constexpr uint32_t kPerOctave = 64, kOctaves = 47, kBins = kPerOctave * kOctaves, kBinsEach = (kBins + kThreads - 1) / kThreads;
-constexpr uint32_t kSub = 1024;    // bins of keys, and blocks of indexes: one a thread
+constexpr uint32_t kSub = 1024;      // bins of keys, and blocks of indexes: one a thread
+constexpr uint32_t kGroup = 128, kGroups = 65536 / kGroup;   // bf16 values of a group
+constexpr uint32_t kList = 4096;
 constexpr uint32_t kMaxVocab = 1u << 22;
 
 typedef unsigned long long u64;
@@ -37,80 +43,66 @@ struct SampleArgs {
   uint32_t N, S;   // S: weights are multiples of 2^-S
 };
 
-// Keys order like the logits, as integers: 32 bits of an fp32, 16 of a bf16.
+// Keys order like the logits, as integers: 32 bits of an fp32, 16 of a bf16; 2^31 or 2^15 is zero of either sign.  A NaN lies
+// beyond the infinities.
 template <typename DT>
 struct Key;
 template <>
 struct Key<F32> {
-  static constexpr uint32_t kMinusInf = 0x007FFFFFu, kInf = 0xFF800000u;
-  static __device__ __forceinline__ uint32_t of(float l) {
-    const uint32_t b = __float_as_uint(l + 0.0f);   // -0 is 0
-    return b ^ ((b >> 31) ? 0xFFFFFFFFu : 0x80000000u);
+  static constexpr uint32_t kMinusInf = 0x00800000u, kInf = 0xFF800000u;
+  static __device__ __forceinline__ uint32_t of(uint32_t bits) {
+    const uint32_t sign = (uint32_t)((int32_t)bits >> 31);
+    return (((bits & 0x7FFFFFFFu) ^ sign) - sign) ^ 0x80000000u;
   }
-  static __device__ __forceinline__ float value(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
+  static __device__ __forceinline__ float value(uint32_t k) {
+    const int32_t v = (int32_t)(k ^ 0x80000000u);
+    return __uint_as_float(v < 0 ? 0x80000000u | (uint32_t)-v : (uint32_t)v);
+  }
 };
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
 template <>
 struct Key<BF16> {
-  static constexpr uint32_t kMinusInf = 0x007Fu, kInf = 0xFF80u;
-  static __device__ __forceinline__ uint32_t of(float l) { return Key<F32>::of(l) >> 16; }
+  static constexpr uint32_t kMinusInf = 0x0080u, kInf = 0xFF80u;
+  static __device__ __forceinline__ uint32_t of(uint32_t bits) {   // two values of a word
+    const i16x2 sign = __builtin_bit_cast(i16x2, bits) >> (int16_t)15;
+    const i16x2 v = __builtin_bit_cast(i16x2, (bits & 0x7FFF7FFFu) ^ __builtin_bit_cast(uint32_t, sign)) - sign;
+    return __builtin_bit_cast(uint32_t, v) ^ 0x80008000u;
+  }
   static __device__ __forceinline__ float value(uint32_t k) {
-    const uint32_t b = k ^ ((k >> 15) ? 0x8000u : 0xFFFFu);
-    return __uint_as_float(b << 16);
+    const int32_t v = (int32_t)k - 0x8000;
+    return __uint_as_float((v < 0 ? 0x8000u | (uint32_t)-v : (uint32_t)v) << 16);
   }
 };
-template <typename DT>
-__device__ __forceinline__ bool allowed(uint32_t key) { return key > Key<DT>::kMinusInf && key <= Key<DT>::kInf; }
 
-// A row's weights: 2^y with y = (l - max) * log2(e) / T.
+// A row's weights: 2^(t / 64) with t = 64 (l - max) log2(e) / T.
+constexpr uint32_t kPerOctave = 64;
 struct Weigher {
   float top;   // the largest logit
-  double c;    // log2(e) / T
+  double c;    // 64 log2(e) / T
   uint32_t S;
-  // at least -1000, which is as good as no weight; the largest logit (an infinity too) has 0
-  __device__ __forceinline__ double octaves(float l) const { return l == top ? 0.0 : fmax(((double)l - (double)top) * c, -1000.0); }
-  static __device__ __forceinline__ uint32_t bin(double y) { return min((uint32_t)(-y * kPerOctave), kBins); }   // kBins: none
-  // 2^(y + S): the fraction of y by its Taylor series up to degree 10, within 2e-13
-  __device__ __forceinline__ double scaled(double y) const {
-    const double n = rint(y), f = y - n;
-    double p = 7.054911620801121e-09;
-    p = __builtin_fma(p, f, 1.0178086009239696e-07);
-    p = __builtin_fma(p, f, 1.3215486790144305e-06);
-    p = __builtin_fma(p, f, 1.5252733804059838e-05);
-    p = __builtin_fma(p, f, 0.00015403530393381606);
-    p = __builtin_fma(p, f, 0.0013333558146428441);
-    p = __builtin_fma(p, f, 0.009618129107628477);
-    p = __builtin_fma(p, f, 0.055504108664821576);
-    p = __builtin_fma(p, f, 0.2402265069591007);
-    p = __builtin_fma(p, f, 0.6931471805599453);
+  const double* table;   // 2^(i / 64), i < 64
+  // at least -64000, which is as good as no weight; the largest logit (an infinity too) has 0
+  __device__ __forceinline__ double sixtyfourths(float l) const { return l == top ? 0.0 : fmax(((double)l - (double)top) * c, -64000.0); }
+  // 2^(t / 64 + S): the whole part of t from the table, the rest by its Taylor series up to degree 4, within 2e-12
+  __device__ __forceinline__ double scaled(double t) const {
+    const double n = floor(t), f = t - n;
+    const int i = (int)n;
+    double p = 5.732851688640402e-10;
+    p = __builtin_fma(p, f, 2.1173137155464774e-07);
+    p = __builtin_fma(p, f, 5.864904955056169e-05);
+    p = __builtin_fma(p, f, 0.010830424696249145);
     p = __builtin_fma(p, f, 1.0);
-    return ldexp(p, (int)n + (int)S);
+    return ldexp(p * table[i & 63], (i >> 6) + (int)S);
   }
   // rounded to a whole number by adding 2^52, whose last place is 1 (S is at most 46)
-  __device__ __forceinline__ u64 weight(double y) const {
-    return (u64)__double_as_longlong(scaled(y) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+  __device__ __forceinline__ u64 weight(double t) const {
+    return (u64)__double_as_longlong(scaled(t) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
   }
+  __device__ __forceinline__ u64 weight_of(float l) const { return weight(sixtyfourths(l)); }
 };
-
-// f(index, logit) for every logit of the row, 16 bytes a lane where the row is aligned.
-template <typename DT, bool VEC, typename F>
-__device__ __forceinline__ void each_logit(const typename DT::elem* row, uint32_t N, F f) {
-  constexpr uint32_t E = DT::kElemsPerVec;
-  const uint32_t nvec = VEC ? N / E : 0u;
-  for (uint32_t v0 = threadIdx.x; v0 < nvec; v0 += 4 * kThreads) {
-    u32x4 raw[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (v0 + i * kThreads < nvec) raw[i] = *(const u32x4*)(row + (size_t)(v0 + i * kThreads) * E);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (v0 + i * kThreads < nvec) {
-        float l[E];
-        unpack16<DT>(raw[i], l);
-#pragma unroll
-        for (uint32_t e = 0; e < E; ++e) f((v0 + i * kThreads) * E + e, l[e]);
-      }
-  }
-  for (uint32_t j = nvec * E + threadIdx.x; j < N; j += kThreads) f(j, load_elem(row, j));
+__device__ __forceinline__ void fill_table(double* table) {   // a barrier follows
+  if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x / kPerOctave);
 }
 
 struct Sums {
@@ -118,23 +110,17 @@ struct Sums {
   u64 mass;
 };
 
-struct SampleShared {
-  u64 mass[kBins + 1];        // of the bins before each; the last entry: of all
-  uint32_t count[kBins + 1];
-  u64 sub_mass[kSub];
-  uint32_t sub_count[kSub];
-  u64 wave_mass[kThreads / 64];
-  uint32_t wave_count[kThreads / 64];
-  uint32_t found[2];
-  uint32_t range[2];
+struct WaveSums {
+  u64 mass[kThreads / 64];
+  uint32_t count[kThreads / 64];
 };
 
-// What the threads before this one hold, and what all hold.
-__device__ __forceinline__ Sums before_thread(SampleShared& s, Sums mine, Sums* all) {
-  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  Sums run = mine;
+// What the first lanes hold, up to this one's; LANES 16: of a row of 16.
+template <int LANES = 64>
+__device__ __forceinline__ Sums up_to_lane(Sums run) {
+  const uint32_t lane = threadIdx.x % LANES;
 #pragma unroll
-  for (uint32_t o = 1; o < 64; o *= 2) {
+  for (uint32_t o = 1; o < LANES; o *= 2) {
     const uint32_t c = __shfl_up(run.count, o, 64);
     const u64 m = __shfl_up(run.mass, o, 64);
     if (lane >= o) {
@@ -142,23 +128,38 @@ __device__ __forceinline__ Sums before_thread(SampleShared& s, Sums mine, Sums* 
       run.mass += m;
     }
   }
+  return run;
+}
+__device__ __forceinline__ uint32_t up_to_lane(uint32_t run) {
+  const uint32_t lane = threadIdx.x % 64;
+#pragma unroll
+  for (uint32_t o = 1; o < 64; o *= 2) {
+    const uint32_t c = __shfl_up(run, o, 64);
+    run += lane >= o ? c : 0u;
+  }
+  return run;
+}
+__device__ __forceinline__ u64 lane_of(u64 v, int lane) {
+  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+// What the threads before this one hold, and what all hold.
+__device__ __forceinline__ Sums before_thread(WaveSums& s, Sums mine, Sums* all) {
+  constexpr int W = kThreads / 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const Sums run = up_to_lane(mine);
   __syncthreads();   // the last call's sums have been read
-  if (lane == 63) {
-    s.wave_count[wave] = run.count;
-    s.wave_mass[wave] = run.mass;
+  if (threadIdx.x % 64 == 63) {
+    s.count[wave] = run.count;
+    s.mass[wave] = run.mass;
   }
   __syncthreads();
-  Sums before = {run.count - mine.count, run.mass - mine.mass}, total = {0u, 0ull};
-#pragma unroll
-  for (uint32_t w = 0; w < kThreads / 64; ++w) {
-    if (w < wave) {
-      before.count += s.wave_count[w];
-      before.mass += s.wave_mass[w];
-    }
-    total.count += s.wave_count[w];
-    total.mass += s.wave_mass[w];
+  const Sums waves = up_to_lane<W>({s.count[threadIdx.x % W], s.mass[threadIdx.x % W]});
+  Sums before = {run.count - mine.count, run.mass - mine.mass};
+  if (wave > 0) {
+    before.count += (uint32_t)__builtin_amdgcn_readlane((int)waves.count, wave - 1);
+    before.mass += lane_of(waves.mass, wave - 1);
   }
-  *all = total;
+  *all = {(uint32_t)__builtin_amdgcn_readlane((int)waves.count, W - 1), lane_of(waves.mass, W - 1)};
   return before;
 }
 
@@ -179,246 +180,706 @@ __device__ __forceinline__ uint32_t least_key(uint32_t none, uint32_t top, P is)
   return hi;
 }
 
-struct Place {   // a logit in the order of the row
-  uint32_t key;
-  Sums before;   // of the larger ones
-  uint32_t equal;   // how many have this key
+// What is asked of the order, one after the other: where top-k ends, where min-p, where top-p, and which token u draws.
+enum Stage { kTopK, kMinP, kTopP, kDraw, kStages };
+
+// The row's keys, NV 16-byte vectors a thread (two bf16 keys to a word); a token that is never drawn has one of at most
+// kMinusInf.  ONE: that is the whole row, it is loaded once and stays; else it is loaded piece by piece for each pass.  Vector v
+// has the tokens v * E and on; behind the last whole one, the first threads have one token each.
+template <typename DT, int NV, bool ONE>
+struct RowKeys {
+  static constexpr uint32_t E = DT::kElemsPerVec, kLoad = kThreads * NV;   // vectors of a load
+  static constexpr uint32_t kNone = E == 8 ? 0x00010001u : 1u;             // keys of no token
+  typedef typename DT::elem elem;
+  const elem* row;
+  uint32_t N, loads, at;
+  u32x4 k[NV];
+  uint32_t last;
+
+  __device__ __forceinline__ RowKeys(const elem* row_, uint32_t N_) : row(row_), N(N_) {
+    loads = ONE ? 1 : (N / E + kLoad - 1) / kLoad;
+    if (ONE) fetch(0);
+  }
+  __device__ __forceinline__ void load(uint32_t n) {   // the nth piece of the row
+    if (!ONE) fetch(n);
+  }
+  static __device__ __forceinline__ uint32_t without_nan(uint32_t keys) {
+    if constexpr (E == 8) return ((keys & 0xFFFFu) > Key<DT>::kInf ? 0u : keys & 0xFFFFu) | (keys >> 16 > Key<DT>::kInf ? 0u : keys & 0xFFFF0000u);
+    else return keys > Key<DT>::kInf ? 0u : keys;
+  }
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    if constexpr (E == 8) return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    else return max(a, b);
+  }
+  static __device__ __forceinline__ uint32_t largest_of(uint32_t keys) { return E == 8 ? max(keys & 0xFFFFu, keys >> 16) : keys; }
+  uint32_t most;   // the largest keys of what is loaded
+  __device__ __forceinline__ void fetch(uint32_t n) {
+    at = n;
+    const uint32_t nvec = N / E, v0 = n * kLoad + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const uint32_t v = v0 + i * kThreads;
+      k[i] = u32x4{~0u, ~0u, ~0u, ~0u};   // NaNs of the sign whose keys are the least
+      if (v < nvec) {   // element by element as the row may begin anywhere; the compiler makes one load of 16 bytes of it
+        const elem* p = row + (size_t)v * E;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (E == 8) k[i][e] = (uint32_t)p[2 * e] | (uint32_t)p[2 * e + 1] << 16;
+          else k[i][e] = __float_as_uint(p[e]);
+        }
+      }
+    }
+    const uint32_t j = nvec * E + threadIdx.x;
+    last = kNone;
+    if (n == loads - 1 && threadIdx.x < E && j < N) {
+      if constexpr (E == 8) last = Key<DT>::of(row[j] | 0xFFFF0000u);
+      else last = Key<DT>::of(__float_as_uint(row[j]));
+    }
+    most = last;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        k[i][e] = Key<DT>::of(k[i][e]);
+        most = larger(most, k[i][e]);
+      }
+    if (largest_of(most) > Key<DT>::kInf) {   // a NaN is among them
+      last = without_nan(last);
+      most = last;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          k[i][e] = without_nan(k[i][e]);
+          most = larger(most, k[i][e]);
+        }
+    }
+  }
+  // f(vector, index of its first token) for the vectors of a thread, and for the token left over, in a vector of its own
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) f(k[i], (at * kLoad + i * kThreads + threadIdx.x) * E);
+    f(u32x4{last, kNone, kNone, kNone}, N / E * E + threadIdx.x);
+  }
+  // The same for a long f: it stands there for four vectors, and they are moved past it.  after(): when four are done.
+  static constexpr int kFours = (NV + 3) / 4;
+  template <typename F, typename A>
+  __device__ __forceinline__ void each_four(F f, A after) {
+#pragma unroll 1
+    for (int n = 0; n < kFours; ++n) {
+#pragma unroll
+      for (int i = 0; i < 4 && i < NV; ++i) f(k[i]);
+      if (n == 0) f(u32x4{last, kNone, kNone, kNone});
+      if constexpr (kFours > 1) {
+        u32x4 first[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) first[i] = k[i];
+#pragma unroll
+        for (int i = 0; i + 4 < NV; ++i) k[i] = k[i + 4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[NV - 4 + i] = first[i];
+      }
+      after();
+    }
+  }
+  // g(key) for every token of a vector
+  template <typename G>
+  static __device__ __forceinline__ void tokens(u32x4 v, G g) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (E == 8) {
+        g(v[e] & 0xFFFFu);
+        g(v[e] >> 16);
+      } else {
+        g(v[e]);
+      }
+    }
+  }
+  // The key of one token, read from the row; at most kMinusInf for none.
+  __device__ __forceinline__ uint32_t key_at(uint32_t j) const {
+    uint32_t key;
+    if constexpr (E == 8) key = Key<DT>::of(row[j]) & 0xFFFFu;
+    else key = Key<DT>::of(__float_as_uint(row[j]));
+    return key > Key<DT>::kInf ? 0u : key;
+  }
+  // How many tokens of a vector have this key.
+  static __device__ __forceinline__ uint32_t how_many(u32x4 v, uint32_t key) {
+    uint32_t others = 0;
+    if constexpr (E == 8) {
+      const uint32_t both = key | key << 16;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        others += __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, v[e] ^ both), (u16x2){1, 1}));
+      return 8 - (others & 0xFFFFu) - (others >> 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) others += v[e] == key ? 1u : 0u;
+      return others;
+    }
+  }
+  __device__ __forceinline__ uint32_t largest(uint32_t* waves) {   // over the row, for all threads
+    uint32_t top = 0;
+    for (uint32_t n = 0; n < loads; ++n) {
+      load(n);
+      top = max(top, largest_of(most));
+    }
+#pragma unroll
+    for (uint32_t o = 1; o < 64; o *= 2) top = max(top, (uint32_t)__shfl_xor(top, o, 64));
+    if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = top;
+    __syncthreads();
+    top = waves[threadIdx.x % (kThreads / 64)];
+#pragma unroll
+    for (uint32_t o = 1; o < kThreads / 64; o *= 2) top = max(top, (uint32_t)__shfl_xor(top, o, 64));
+    return __builtin_amdgcn_readfirstlane(top);
+  }
 };
 
-// The logit at which the counts (by_count) or weights cumulated in the row's order reach `threshold`, at least 1 and at
-// most what all of them have.
-template <typename DT, bool VEC>
-__device__ Place place_of(SampleShared& s, const typename DT::elem* row, uint32_t N, const Weigher& w, uint32_t top_key,
-                          bool by_count, u64 threshold) {
-  __syncthreads();
-  for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) {
-    const u64 from = by_count ? s.count[b] : s.mass[b], to = by_count ? s.count[b + 1] : s.mass[b + 1];
-    if (from < threshold && threshold <= to) s.found[0] = b;
-  }
-  __syncthreads();
-  const uint32_t bin = s.found[0];
-  Place at;
-  at.before = {s.count[bin], s.mass[bin]};
-  // the bin's keys, smallest and largest
-  if (threadIdx.x < 64) {
-    const uint32_t k = least_key(Key<DT>::kMinusInf, top_key, [&](uint32_t key) { return w.bin(w.octaves(Key<DT>::value(key))) <= bin; });
-    if (threadIdx.x == 0) s.range[0] = k;
-  } else if (threadIdx.x < 128) {
-    uint32_t k = top_key + 1;
-    if (bin > 0) k = least_key(Key<DT>::kMinusInf, top_key, [&](uint32_t key) { return w.bin(w.octaves(Key<DT>::value(key))) < bin; });
-    if (threadIdx.x == 64) s.range[1] = k - 1;
-  }
-  __syncthreads();
-  uint32_t lo = s.range[0], hi = s.range[1];
-  for (;;) {
-    uint32_t shift = 0;
-    while (((hi - lo) >> shift) >= kSub) ++shift;
-    s.sub_count[threadIdx.x] = 0;
-    s.sub_mass[threadIdx.x] = 0;
-    __syncthreads();
-    each_logit<DT, VEC>(row, N, [&](uint32_t, float l) {
-      const uint32_t key = Key<DT>::of(l);
-      if (key >= lo && key <= hi) {
-        atomicAdd(&s.sub_count[(hi - key) >> shift], 1u);
-        atomicAdd(&s.sub_mass[(hi - key) >> shift], w.weight(w.octaves(l)));
-      }
-    });
-    __syncthreads();
-    Sums mine = {s.sub_count[threadIdx.x], s.sub_mass[threadIdx.x]}, all;
-    const Sums ahead = before_thread(s, mine, &all);
-    const u64 from = by_count ? at.before.count + ahead.count : at.before.mass + ahead.mass, to = from + (by_count ? mine.count : mine.mass);
-    if (from < threshold && threshold <= to) {
-      s.found[1] = threadIdx.x;
-      s.sub_count[0] = ahead.count;   // both have been read by their threads before the barriers in before_thread
-      s.sub_mass[0] = ahead.mass;
-      s.sub_count[1] = mine.count;
-    }
-    __syncthreads();
-    at.before.count += s.sub_count[0];
-    at.before.mass += s.sub_mass[0];
-    at.equal = s.sub_count[1];
-    const uint32_t f = s.found[1], top = hi - (f << shift), span = (1u << shift) - 1;
-    __syncthreads();
-    hi = top;
-    lo = top - lo > span ? top - span : lo;
-    if (shift == 0) break;
-  }
-  at.key = hi;
-  return at;
+// The settings of a row, as the integers that sums are compared with.
+struct Settings {
+  float T;
+  int32_t k;
+  float p, min_p;
+  u64 p64, u64ths;   // top_p and u as multiples of 2^-64
+};
+__device__ __forceinline__ u64 of_two_to_64(float x) { return (u64)((double)x * 18446744073709551616.0); }   // 0 < x < 1
+__device__ __forceinline__ Settings settings_of(const SampleArgs& a, uint32_t r) {
+  Settings s;
+  s.T = a.temperature ? a.temperature[r] : 1.0f;
+  s.k = a.top_k ? a.top_k[r] : 0;
+  s.p = a.top_p ? a.top_p[r] : 1.0f;
+  s.min_p = a.min_p ? a.min_p[r] : 0.0f;
+  const float u = a.u[r];
+  s.p64 = s.p > 0.f && s.p < 1.f ? of_two_to_64(s.p) : 0ull;
+  s.u64ths = u > 0.f ? u < 1.f ? of_two_to_64(u) : ~0ull : 0ull;
+  return s;
 }
+// The least cumulated weight that is top_p of `mass`: the product's whole part and one more if there is a rest; at least 1.
+__device__ __forceinline__ u64 top_p_threshold(const Settings& s, u64 mass) {
+  const u64 need = __umul64hi(mass, s.p64) + (mass * s.p64 != 0 ? 1 : 0);
+  return need > 0 ? need : 1;
+}
+// How many tokens of weight m reach `threshold` above `before`, rounded up.
+__device__ __forceinline__ u64 tokens_to(u64 threshold, u64 before, u64 m) { return (threshold - before + m - 1) / m; }
 
-template <typename DT, bool VEC>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
-  typedef typename DT::elem elem;
-  __shared__ SampleShared s;
-  const uint32_t r = blockIdx.x, N = a.N;
-  const elem* row = (const elem*)a.logits + (size_t)r * a.ld;
-
-  // the largest logit
-  uint32_t top_key = 0;
-  each_logit<DT, VEC>(row, N, [&](uint32_t, float l) {
-    const uint32_t key = Key<DT>::of(l);
-    if (allowed<DT>(key)) top_key = max(top_key, key);
-  });
-#pragma unroll
-  for (uint32_t o = 1; o < 64; o *= 2) top_key = max(top_key, (uint32_t)__shfl_xor(top_key, o, 64));
-  if (threadIdx.x % 64 == 0) s.wave_count[threadIdx.x / 64] = top_key;
-  __syncthreads();
-#pragma unroll
-  for (uint32_t i = 0; i < kThreads / 64; ++i) top_key = max(top_key, s.wave_count[i]);
-  if (top_key == 0) {   // no token is left
-    if (threadIdx.x == 0) {
-      a.ids[r] = -1;
-      if (a.prob) a.prob[r] = 0.f;
-    }
-    return;
-  }
-
-  const float T = a.temperature ? a.temperature[r] : 1.0f;
-  uint32_t key = top_key, nth = 1;   // the token drawn: the nth with this key
-  float prob = 1.0f;
-  if (T > 0.f) {
-    const Weigher w = {Key<DT>::value(top_key), 1.4426950408889634074 / (double)T, a.S};
-    for (uint32_t b = threadIdx.x; b <= kBins; b += kThreads) {
-      s.count[b] = 0;
-      s.mass[b] = 0;
-    }
-    __syncthreads();
-    each_logit<DT, VEC>(row, N, [&](uint32_t, float l) {
-      const uint32_t k = Key<DT>::of(l);
-      if (!allowed<DT>(k)) return;
-      const double y = w.octaves(l);
-      const uint32_t b = w.bin(y);
-      if (b >= kBins) return;   // below 2^-47: no weight
-      const u64 m = w.weight(y);
-      // where a wavefront's logits are all equal, one lane adds them
-      const uint32_t first = __builtin_amdgcn_readfirstlane(k);
-      const u64 here = __ballot(1), same = __ballot(k == first);
-      if (here == same) {
-        const uint32_t n = __popcll(here);
-        if (threadIdx.x % 64 == __builtin_ctzll(here)) {
-          atomicAdd(&s.count[b], n);
-          atomicAdd(&s.mass[b], m * n);
-        }
-      } else {
-        atomicAdd(&s.count[b], 1u);
-        atomicAdd(&s.mass[b], m);
-      }
-    });
-    __syncthreads();
-    // sums of the bins before each
-    Sums bins[kBinsEach], mine = {0u, 0ull}, all;
-#pragma unroll
-    for (uint32_t i = 0; i < kBinsEach; ++i) {
-      const uint32_t b = threadIdx.x * kBinsEach + i;
-      bins[i] = {b < kBins ? s.count[b] : 0u, b < kBins ? s.mass[b] : 0ull};
-      mine.count += bins[i].count;
-      mine.mass += bins[i].mass;
-    }
-    Sums before = before_thread(s, mine, &all);
-#pragma unroll
-    for (uint32_t i = 0; i < kBinsEach; ++i) {
-      const uint32_t b = threadIdx.x * kBinsEach + i;
-      if (b <= kBins) {
-        s.count[b] = before.count;
-        s.mass[b] = before.mass;
-      }
-      before.count += bins[i].count;
-      before.mass += bins[i].mass;
-    }
-    if (threadIdx.x == 0) {
-      s.count[kBins] = all.count;
-      s.mass[kBins] = all.mass;
-    }
-    __syncthreads();
-
-    // the weight that is kept, of the first so many
-    u64 kept = all.mass;
-    const int32_t k = a.top_k ? a.top_k[r] : 0;
-    if (k > 0 && (uint32_t)k < all.count) {
-      const Place at = place_of<DT, VEC>(s, row, N, w, top_key, true, (u64)k);
-      kept = at.before.mass + (k - at.before.count) * w.weight(w.octaves(Key<DT>::value(at.key)));
-    }
-    const float p = a.top_p ? a.top_p[r] : 1.0f;
-    const u64 of_k = kept;
-    if (p < 1.f) {
-      // cum >= p * cum(k): p as a multiple of 2^-64, the product's whole part and whether there is more
-      const u64 p64 = p > 0.f ? (u64)((double)p * 18446744073709551616.0) : 0ull;
-      const u64 need = __umul64hi(of_k, p64) + (of_k * p64 != 0 ? 1 : 0);
-      const u64 threshold = need > 0 ? need : 1;
-      const Place at = place_of<DT, VEC>(s, row, N, w, top_key, false, threshold);
-      const u64 m = w.weight(w.octaves(Key<DT>::value(at.key)));
-      kept = at.before.mass + (threshold - at.before.mass + m - 1) / m * m;
-    }
-    const float mp = a.min_p ? a.min_p[r] : 0.0f;
-    if (mp > 0.f) {
-      const u64 one = 1ull << a.S;
-      u64 of_m = one;   // beyond 1 nothing has as much: the first
-      if (mp <= 1.f) {
-        const u64 least = (u64)ceil((double)mp * (double)one);
-        __syncthreads();
-        if (threadIdx.x < 64) {
-          const uint32_t from = least_key(Key<DT>::kMinusInf, top_key, [&](uint32_t key) { return w.weight(w.octaves(Key<DT>::value(key))) >= least; });
-          if (threadIdx.x == 0) s.range[0] = from;
-        }
-        __syncthreads();
-        const uint32_t from = s.range[0], b = min(w.bin(w.octaves(Key<DT>::value(from))), kBins - 1);
-        Sums inside = {0u, 0ull}, sum;
-        each_logit<DT, VEC>(row, N, [&](uint32_t, float l) {
-          const uint32_t key = Key<DT>::of(l);
-          if (key < from || key > top_key) return;
-          const double y = w.octaves(l);
-          if (w.bin(y) == b) inside.mass += w.weight(y);
-        });
-        before_thread(s, inside, &sum);
-        of_m = s.mass[b] + sum.mass;
-      }
-      kept = min(kept, of_m);
-    }
-
-    const float u = a.u[r];
-    const u64 u64ths = u > 0.f ? u < 1.f ? (u64)((double)u * 18446744073709551616.0) : ~0ull : 0ull;
-    const u64 threshold = __umul64hi(kept, u64ths) + 1;
-    const Place at = place_of<DT, VEC>(s, row, N, w, top_key, false, threshold);
-    const double y = w.octaves(Key<DT>::value(at.key));
-    const u64 m = w.weight(y);
-    key = at.key;
-    nth = (uint32_t)((threshold - at.before.mass + m - 1) / m);
-    prob = (float)(w.scaled(y) / (double)kept);
-  }
-
-  // the nth logit with this key in the order of the indexes: how many each block of indexes has, then inside one block
+// The nth token with this key in the order of the indexes: how many each block of indexes has, then inside one block.
+template <typename DT, int NV, bool ONE>
+__device__ __forceinline__ void write_token(RowKeys<DT, NV, ONE>& keys, WaveSums& waves, uint32_t* blocks, uint32_t* found,
+                                            uint32_t key, uint32_t nth, int32_t* id) {
   uint32_t bits = 6;
-  while ((N - 1) >> bits >= kSub) ++bits;
-  s.sub_count[threadIdx.x] = 0;
+  while ((keys.N - 1) >> bits >= kSub) ++bits;
+  blocks[threadIdx.x] = 0;
   __syncthreads();
-  each_logit<DT, VEC>(row, N, [&](uint32_t j, float l) {
-    if (Key<DT>::of(l) == key) atomicAdd(&s.sub_count[j >> bits], 1u);
-  });
+  for (uint32_t n = 0; n < keys.loads; ++n) {
+    keys.load(n);
+    keys.each([&](u32x4 v, uint32_t index) {   // a vector's tokens lie in one block
+      const uint32_t here = keys.how_many(v, key);
+      if (here) atomicAdd(&blocks[index >> bits], here);
+    });
+  }
   __syncthreads();
-  Sums mine = {s.sub_count[threadIdx.x], 0ull}, all;
-  const Sums before = before_thread(s, mine, &all);
-  if (before.count < nth && nth <= before.count + mine.count) {
-    s.found[0] = threadIdx.x;
-    s.found[1] = nth - before.count;
+  const uint32_t mine = blocks[threadIdx.x], run = up_to_lane(mine), wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  if (lane == 63) waves.count[wave] = run;
+  __syncthreads();
+  uint32_t before = run - mine;
+  for (uint32_t w = 0; w < wave; ++w) before += waves.count[w];
+  if (before < nth && nth <= before + mine) {
+    found[0] = threadIdx.x;
+    found[1] = nth - before;
   }
   __syncthreads();
   if (threadIdx.x < 64) {
-    uint32_t left = s.found[1];
-    const uint32_t from = s.found[0] << bits;
+    uint32_t left = found[1];
+    const uint32_t from = found[0] << bits;
     for (uint32_t at = from; at < from + (1u << bits); at += 64) {
-      const uint32_t j = at + threadIdx.x;
-      const u64 yes = __ballot(j < N && Key<DT>::of(load_elem(row, j < N ? j : N - 1)) == key);
+      const uint32_t j = at + lane;
+      const u64 yes = __ballot(j < keys.N && keys.key_at(min(j, keys.N - 1)) == key);
       const uint32_t n = __popcll(yes);
       if (left <= n) {
         // the lane that is the left-th of them
-        if ((yes >> threadIdx.x & 1) && __popcll(yes & ((2ull << threadIdx.x) - 1)) == left) a.ids[r] = (int32_t)j;
+        if ((yes >> lane & 1) && __popcll(yes & ((2ull << lane) - 1)) == left) *id = (int32_t)j;
         break;
       }
       left -= n;
     }
-    if (threadIdx.x == 0 && a.prob) a.prob[r] = prob;
   }
+}
+
+__device__ __forceinline__ void write_none(const SampleArgs& a, uint32_t r) {
+  if (threadIdx.x == 0) {
+    a.ids[r] = -1;
+    if (a.prob) a.prob[r] = 0.f;
+  }
+}
+
+// ---------------------------------------------------------------- bf16: counted by value
+
+struct CountShared {
+  uint32_t count[32768];        // 16 bits a value
+  u64 mass[kGroups];            // of each group of values; then of the groups above each
+  uint32_t tokens[kGroups];
+  uint32_t one[kSub];           // counts of one group's values; blocks of indexes
+  double table[kPerOctave];
+  WaveSums waves;
+  uint32_t found[2], range[2], nth, key;
+  Sums above;                   // the groups above the one that is looked at
+  u64 kept, of_k;
+  float prob;
+};
+
+// The values of a vector counted, those from `cut` on; one of a wavefront's lanes adds for all where they have the same words.
+__device__ __forceinline__ void count_values(uint32_t* count, u32x4 v, uint32_t cut) {
+  auto add = [&](uint32_t k, uint32_t n) {
+    if (k >= cut) atomicAdd(&count[k >> 1], (k & 1) * (n * 0xFFFFu) + n);
+  };
+  const uint32_t first = __builtin_amdgcn_readfirstlane(v[0]);
+  if (__ballot(v[0] == first) == ~0ull) {
+#pragma unroll 1
+    for (int e = 0; e < 4; ++e) {
+      const bool same = __ballot(v[0] == __builtin_amdgcn_readfirstlane(v[0])) == ~0ull;
+      if (!same || threadIdx.x % 64 == 0) {
+        add(v[0] & 0xFFFFu, same ? 64 : 1);
+        add(v[0] >> 16, same ? 64 : 1);
+      }
+#pragma unroll
+      for (int i = 0; i < 3; ++i) v[i] = v[i + 1];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      add(v[e] & 0xFFFFu, 1);
+      add(v[e] >> 16, 1);
+    }
+  }
+}
+
+template <int NV, bool ONE>
+__global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
+  __shared__ CountShared s;
+  const uint32_t r = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  RowKeys<BF16, NV, ONE> keys((const uint16_t*)a.logits + (size_t)r * a.ld, a.N);
+  for (uint32_t i = threadIdx.x; i < 32768 / 4; i += kThreads) ((u32x4*)s.count)[i] = u32x4{0u, 0u, 0u, 0u};
+  if (threadIdx.x < kGroups) {
+    s.mass[threadIdx.x] = 0;
+    s.tokens[threadIdx.x] = 0;
+  }
+  fill_table(s.table);
+  const Settings set = settings_of(a, r);
+  const uint32_t top_key = keys.largest(s.waves.count);
+  if (top_key <= Key<BF16>::kMinusInf) return write_none(a, r);
+
+  if (!(set.T > 0.f)) {
+    if (threadIdx.x == 0) {
+      s.key = top_key;
+      s.nth = 1;
+      s.prob = 1.0f;
+    }
+  } else {
+    const Weigher w = {Key<BF16>::value(top_key), 92.332482616893656877 / (double)set.T, a.S, s.table};
+    auto weight_of = [&](uint32_t k) -> u64 { return w.weight_of(Key<BF16>::value(k)); };
+    // the least value that has a weight, and the least that has min_p (none where it is beyond 1)
+    const u64 one = 1ull << a.S;
+    if (threadIdx.x < 128) {
+      const u64 need = wave && set.min_p > 0.f && set.min_p <= 1.f ? (u64)ceil((double)set.min_p * (double)one) : 1;
+      const uint32_t k = least_key(Key<BF16>::kMinusInf, top_key, [&](uint32_t k) { return weight_of(k) >= need; });
+      if (lane == 0) s.range[wave] = k;
+    }
+    __syncthreads();
+    const uint32_t cut = s.range[0], from_p = s.range[1];
+
+    // The counts into the groups' sums: a wavefront takes 128 values at a time, the next one the next.
+    auto add_up = [&](bool clear) {
+      __syncthreads();
+      const uint32_t g1 = top_key / kGroup;
+#pragma unroll 1
+      for (uint32_t g0 = cut / kGroup + wave; g0 <= g1; g0 += 4 * (kThreads / 64)) {
+        uint32_t c[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+          const uint32_t g = g0 + i * (kThreads / 64);
+          c[i] = g <= g1 ? s.count[g * 64 + lane] : 0u;
+        }
+#pragma unroll 1
+        for (uint32_t g = g0; g < g0 + 4 * (kThreads / 64); g += kThreads / 64) {
+          const uint32_t now = c[0];
+#pragma unroll
+          for (int i = 0; i < 3; ++i) c[i] = c[i + 1];
+          c[3] = 0;
+          if (__ballot(now != 0) == 0) continue;
+          const uint32_t i = g * 64 + lane;
+          Sums t = {(now & 0xFFFFu) + (now >> 16), 0ull};
+          if (now) {
+            if (clear) s.count[i] = 0;
+            t.mass = (now & 0xFFFFu) * weight_of(2 * i) + (now >> 16) * weight_of(2 * i + 1);
+          }
+          t = up_to_lane(t);
+          if (lane == 63) {
+            s.tokens[g] += t.count;
+            s.mass[g] += t.mass;
+          }
+        }
+      }
+      __syncthreads();
+    };
+    // 16 bits a value: should one of more than 65535 tokens occur that often, the counts' sum is too small (a carry out of the
+    // lower half counts for 65536 fewer, one of the upper half is lost), and all is done again in portions of 32768
+    bool portions = false;
+    Sums mine, above, all;
+    for (;;) {
+      uint32_t counted = 0;
+      for (uint32_t n = 0; n < keys.loads; ++n) {
+        keys.load(n);
+        keys.each_four(
+            [&](u32x4 v) {
+              count_values(s.count, v, cut);
+              if (NV > 4 || !ONE) keys.tokens(v, [&](uint32_t k) { counted += k >= cut ? 1u : 0u; });
+            },
+            [&] { if ((NV > 4 || !ONE) && portions) add_up(true); });
+      }
+      if (!portions) add_up(false);
+      // sums of the groups above each; thread t has group kGroups - 1 - t
+      mine = {0u, 0ull};
+      if (threadIdx.x < kGroups) mine = {s.tokens[kGroups - 1 - threadIdx.x], s.mass[kGroups - 1 - threadIdx.x]};
+      above = before_thread(s.waves, mine, &all);
+      if constexpr (NV <= 4 && ONE) break;
+      Sums sum;
+      before_thread(s.waves, {counted, 0ull}, &sum);
+      if (portions || sum.count == all.count) break;
+      portions = true;
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < 32768; i += kThreads) s.count[i] = 0;
+      if (threadIdx.x < kGroups) {
+        s.mass[threadIdx.x] = 0;
+        s.tokens[threadIdx.x] = 0;
+      }
+      __syncthreads();
+    }
+    if (threadIdx.x < kGroups) s.mass[kGroups - 1 - threadIdx.x] = above.mass;
+    if (threadIdx.x == 0) s.kept = s.of_k = all.mass;   // the weight that is kept, of the first so many; what top-k leaves
+
+#pragma unroll 1
+    for (int stage = kTopK; stage < kStages; ++stage) {
+      // the value where the counts (top-k) or weights cumulated in the row's order reach `threshold`, or the key of min-p
+      u64 threshold = 0;
+      const bool by_count = stage == kTopK;
+      __syncthreads();
+      const u64 kept = s.kept;
+      if (stage == kTopK) {
+        if (set.k <= 0 || (uint32_t)set.k >= all.count) continue;
+        threshold = (u64)set.k;
+      } else if (stage == kMinP) {
+        if (!(set.min_p > 0.f)) continue;
+        const u64 least = set.min_p > 1.f ? one : s.mass[from_p / kGroup];   // beyond 1 nothing has as much: the first
+        if (least >= kept) continue;                                           // it cuts nothing off
+        if (set.min_p > 1.f) {
+          __syncthreads();
+          if (threadIdx.x == 0) s.kept = one;
+          continue;
+        }
+      } else if (stage == kTopP) {
+        threshold = top_p_threshold(set, s.of_k);
+        if (!(set.p < 1.f) || threshold > kept) continue;
+      } else {
+        threshold = __umul64hi(kept, set.u64ths) + 1;
+      }
+      if (stage == kMinP) {
+        if (threadIdx.x == 0) {
+          s.found[0] = from_p / kGroup;
+          s.above = {0u, s.mass[from_p / kGroup]};
+        }
+      } else {
+        const u64 from = by_count ? above.count : above.mass, to = from + (by_count ? mine.count : mine.mass);
+        if (from < threshold && threshold <= to) {
+          s.found[0] = kGroups - 1 - threadIdx.x;
+          s.above = above;
+        }
+      }
+      if (portions && threadIdx.x < kGroup) s.one[threadIdx.x] = 0;
+      __syncthreads();
+      const uint32_t g = s.found[0];
+      if (portions) {   // the group's counts once more
+        for (uint32_t j0 = 0; j0 < keys.N; j0 += kThreads) {
+          const uint32_t j = j0 + threadIdx.x, k = j < keys.N ? keys.key_at(j) : 0u;
+          if (k / kGroup != g || k < cut) continue;
+          const u64 here = __ballot(1);
+          const bool same = __ballot(k == __builtin_amdgcn_readfirstlane(k)) == here;
+          if (!same || lane == __builtin_ctzll(here)) atomicAdd(&s.one[k % kGroup], same ? (uint32_t)__popcll(here) : 1u);
+        }
+        __syncthreads();
+      }
+      if (threadIdx.x < 64) {   // from the largest value down, two a lane
+        const uint32_t i = kGroup - 1 - 2 * lane, k = g * kGroup + i, c = s.count[k >> 1];
+        const uint32_t n1 = portions ? s.one[i] : c >> 16, n0 = portions ? s.one[i - 1] : c & 0xFFFFu;
+        const u64 m1 = n1 ? weight_of(k) : 0ull, m0 = n0 ? weight_of(k - 1) : 0ull;
+        const Sums hi = {n1, n1 * m1}, both = {n1 + n0, n1 * m1 + n0 * m0}, run = up_to_lane(both);
+        Sums b = {s.above.count + run.count - both.count, s.above.mass + run.mass - both.mass};
+        const u64 f = by_count ? b.count : b.mass, h = f + (by_count ? hi.count : hi.mass), t = f + (by_count ? both.count : both.mass);
+        const bool here = stage == kMinP ? k == from_p || k - 1 == from_p : f < threshold && threshold <= t;
+        if (here) {
+          const bool second = stage == kMinP ? k != from_p : threshold > h;
+          if (second) b = {b.count + hi.count, b.mass + hi.mass};
+          const u64 m = second ? m0 : m1;
+          if (stage == kTopK) {
+            s.of_k = s.kept = b.mass + ((uint32_t)set.k - b.count) * m;
+          } else if (stage == kMinP) {
+            s.kept = min(kept, b.mass + (second ? n0 : n1) * m);
+          } else if (stage == kTopP) {
+            s.kept = min(kept, b.mass + tokens_to(threshold, b.mass, m) * m);
+          } else {
+            s.key = second ? k - 1 : k;
+            s.nth = (uint32_t)tokens_to(threshold, b.mass, m);
+            s.prob = (float)(w.scaled(w.sixtyfourths(Key<BF16>::value(s.key))) / (double)kept);
+          }
+        }
+      }
+    }
+  }
+  __syncthreads();
+  write_token(keys, s.waves, s.one, s.found, s.key, s.nth, a.ids + r);
+  if (threadIdx.x == 0 && a.prob) a.prob[r] = s.prob;
+}
+
+// ---------------------------------------------------------------- fp32: weights over octaves
+
+constexpr uint32_t kBins = kPerOctave * 47, kBinsEach = (kBins + kThreads - 1) / kThreads;   // below 2^-47 there is no weight
+struct OctaveShared {
+  u64 mass[kBins + 1];        // of the bins before each; the last entry: of all
+  uint32_t count[kBins + 1];
+  u64 sub_mass[kSub];
+  uint32_t sub_count[kSub];
+  uint32_t list[kList];       // the keys of one bin
+  double table[kPerOctave];
+  WaveSums waves;
+  uint32_t found[2], range[2], listed, nth, key;
+  u64 kept;
+  float prob;
+};
+
+template <int NV, bool ONE>
+__global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
+  __shared__ OctaveShared s;
+  const uint32_t r = blockIdx.x, lane = threadIdx.x % 64;
+  RowKeys<F32, NV, ONE> keys((const float*)a.logits + (size_t)r * a.ld, a.N);
+  fill_table(s.table);
+  const Settings set = settings_of(a, r);
+  const uint32_t top_key = keys.largest(s.waves.count);
+  if (top_key <= Key<F32>::kMinusInf) return write_none(a, r);
+
+  if (!(set.T > 0.f)) {
+    if (threadIdx.x == 0) {
+      s.key = top_key;
+      s.nth = 1;
+      s.prob = 1.0f;
+    }
+  } else {
+    const Weigher w = {Key<F32>::value(top_key), 92.332482616893656877 / (double)set.T, a.S, s.table};
+    auto weight_of = [&](uint32_t k) -> u64 { return w.weight_of(Key<F32>::value(k)); };
+    auto bin_at = [](double t) -> uint32_t { return min((uint32_t)-t, kBins); };
+    auto bin_of = [&](uint32_t k) -> uint32_t { return bin_at(w.sixtyfourths(Key<F32>::value(k))); };
+    const u64 one = 1ull << a.S;
+    if (threadIdx.x < 64) {   // the least key that has min_p
+      const u64 need = set.min_p > 0.f && set.min_p <= 1.f ? (u64)ceil((double)set.min_p * (double)one) : 1;
+      const uint32_t k = least_key(Key<F32>::kMinusInf, top_key, [&](uint32_t k) { return weight_of(k) >= need; });
+      if (lane == 0) s.range[0] = k;
+    }
+    __syncthreads();
+    const uint32_t from_p = s.range[0];
+
+    // f(key) for the keys of a gathered bin: from the list, or from the row where that is too short
+    auto members = [&](auto f) {
+      const bool listed = s.listed <= kList;
+      const uint32_t n = listed ? s.listed : keys.N, lo = s.range[0], hi = s.range[1];
+#pragma unroll 1
+      for (uint32_t j = threadIdx.x; j < n; j += kThreads) {
+        const uint32_t k = listed ? s.list[j] : keys.key_at(j);
+        if (k >= lo && k <= hi) f(k);
+      }
+    };
+
+    u64 kept = 0, of_k = 0;   // the weight that is kept, of the first so many; what top-k leaves
+    uint32_t least = Key<F32>::kMinusInf + 1;   // the keys that are weighed: top-k's and all that equal its last
+    u64 too_many = 0;                           // of those, how many it leaves out
+#pragma unroll 1
+    for (int stage = kTopK; stage < kStages; ++stage) {
+      const bool by_count = stage == kTopK;
+      __syncthreads();
+      if (by_count && (set.k <= 0 || (uint32_t)set.k >= keys.N)) continue;
+      if (stage == kTopP && !(set.p < 1.f)) continue;
+      Sums all = {0u, 0ull};
+      if (stage <= kMinP) {
+        // the histogram over octaves of the tokens from key `least` on, by count or by weight; each bin's sum, then that of
+        // the bins before it
+        for (uint32_t b = threadIdx.x; b <= kBins; b += kThreads) {
+          s.count[b] = 0;
+          s.mass[b] = 0;
+        }
+        __syncthreads();
+        auto token = [&](uint32_t k) {
+          if (k < least) return;
+          const double t = w.sixtyfourths(Key<F32>::value(k));
+          const uint32_t b = bin_at(t);
+          if (b >= kBins) return;
+          if (by_count) atomicAdd(&s.count[b], 1u);
+          else atomicAdd(&s.mass[b], w.weight(t));
+        };
+        for (uint32_t n = 0; n < keys.loads; ++n) {
+          keys.load(n);
+          keys.each_four(
+              [&](u32x4 v) {
+                // where a wavefront's logits are all equal, one lane adds them
+                bool same = true;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) same = same && __ballot(v[e] == __builtin_amdgcn_readfirstlane(v[0])) == ~0ull;
+                if (same) {
+                  const double t = w.sixtyfourths(Key<F32>::value(v[0]));
+                  const uint32_t b = bin_at(t);
+                  if (v[0] >= least && b < kBins && lane == 0) {
+                    if (by_count) atomicAdd(&s.count[b], 256u);
+                    else atomicAdd(&s.mass[b], w.weight(t) * 256);
+                  }
+                } else {
+                  keys.tokens(v, token);
+                }
+              },
+              [] {});
+        }
+        __syncthreads();
+        Sums bins[kBinsEach], mine = {0u, 0ull};
+#pragma unroll
+        for (uint32_t i = 0; i < kBinsEach; ++i) {
+          const uint32_t b = threadIdx.x * kBinsEach + i;
+          bins[i] = {b < kBins ? s.count[b] : 0u, b < kBins ? s.mass[b] : 0ull};
+          mine.count += bins[i].count;
+          mine.mass += bins[i].mass;
+        }
+        Sums before = before_thread(s.waves, mine, &all);
+#pragma unroll
+        for (uint32_t i = 0; i < kBinsEach; ++i) {
+          const uint32_t b = threadIdx.x * kBinsEach + i;
+          if (b <= kBins) {
+            s.count[b] = before.count;
+            s.mass[b] = before.mass;
+          }
+          before.count += bins[i].count;
+          before.mass += bins[i].mass;
+        }
+        if (threadIdx.x == 0) {
+          s.count[kBins] = all.count;
+          s.mass[kBins] = all.mass;
+        }
+        __syncthreads();
+      }
+      if (stage == kMinP) of_k = kept = all.mass - too_many * weight_of(least);
+      // the value where the counts (top-k) or weights cumulated in the row's order reach `threshold`, or the key of min-p
+      u64 threshold = 0;
+      uint32_t bin = 0;
+      if (by_count) {
+        if ((uint32_t)set.k >= all.count) continue;
+        threshold = (u64)set.k;
+      } else if (stage == kMinP) {
+        if (!(set.min_p > 0.f)) continue;
+        if (set.min_p > 1.f) kept = min(kept, one);   // nothing has as much: the first
+        bin = min(bin_of(max(from_p, least)), kBins - 1);
+        if (set.min_p > 1.f || s.mass[bin] >= kept) continue;   // or it cuts nothing off
+      } else if (stage == kTopP) {
+        threshold = top_p_threshold(set, of_k);
+        if (threshold > kept) continue;
+      } else {
+        threshold = __umul64hi(kept, set.u64ths) + 1;
+      }
+      if (stage != kMinP) {
+        for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) {
+          const u64 from = by_count ? s.count[b] : s.mass[b], to = by_count ? s.count[b + 1] : s.mass[b + 1];
+          if (from < threshold && threshold <= to) s.found[0] = b;
+        }
+        __syncthreads();
+        bin = s.found[0];
+      }
+      // the bin's keys, smallest and largest, and their list
+      if (threadIdx.x < 64) {
+        const uint32_t k = least_key(Key<F32>::kMinusInf, top_key, [&](uint32_t k) { return bin_of(k) <= bin; });
+        if (threadIdx.x == 0) s.range[0] = max(k, least);
+      } else if (threadIdx.x < 128) {
+        uint32_t k = top_key + 1;
+        if (bin > 0) k = least_key(Key<F32>::kMinusInf, top_key, [&](uint32_t k) { return bin_of(k) < bin; });
+        if (threadIdx.x == 64) s.range[1] = k - 1;
+      } else if (threadIdx.x == 128) {
+        s.listed = 0;
+      }
+      __syncthreads();
+      uint32_t lo = s.range[0], hi = s.range[1];
+      for (uint32_t n = 0; n < keys.loads; ++n) {
+        keys.load(n);
+        keys.each([&](u32x4 v, uint32_t) {
+          keys.tokens(v, [&](uint32_t k) {
+            if (k >= lo && k <= hi) {
+              const uint32_t i = atomicAdd(&s.listed, 1u);
+              if (i < kList) s.list[i] = k;
+            }
+          });
+        });
+      }
+      __syncthreads();
+      if (stage == kMinP) {
+        Sums inside = {0u, 0ull}, sum;
+        members([&](uint32_t k) { inside.mass += k >= from_p ? weight_of(k) : 0ull; });
+        before_thread(s.waves, inside, &sum);
+        kept = min(kept, s.mass[bin] + sum.mass);
+        continue;
+      }
+      Sums before = {s.count[bin], s.mass[bin]};
+      uint32_t equal;
+      for (;;) {
+        uint32_t shift = 0;
+        while (((hi - lo) >> shift) >= kSub) ++shift;
+        s.sub_count[threadIdx.x] = 0;
+        s.sub_mass[threadIdx.x] = 0;
+        __syncthreads();
+        members([&](uint32_t k) {
+          if (k < lo || k > hi) return;
+          atomicAdd(&s.sub_count[(hi - k) >> shift], 1u);
+          if (!by_count) atomicAdd(&s.sub_mass[(hi - k) >> shift], weight_of(k));
+        });
+        __syncthreads();
+        Sums mine = {s.sub_count[threadIdx.x], s.sub_mass[threadIdx.x]}, sum;
+        const Sums ahead = before_thread(s.waves, mine, &sum);
+        const u64 from = by_count ? before.count + ahead.count : before.mass + ahead.mass, to = from + (by_count ? mine.count : mine.mass);
+        if (from < threshold && threshold <= to) {
+          s.found[1] = threadIdx.x;
+          s.sub_count[0] = ahead.count;   // all have been read by their threads before the barriers in before_thread
+          s.sub_mass[0] = ahead.mass;
+          s.sub_count[1] = mine.count;
+        }
+        __syncthreads();
+        before.count += s.sub_count[0];
+        before.mass += s.sub_mass[0];
+        equal = s.sub_count[1];
+        const uint32_t f = s.found[1], top = hi - (f << shift), span = (1u << shift) - 1;
+        __syncthreads();
+        hi = top;
+        lo = top - lo > span ? top - span : lo;
+        if (shift == 0) break;
+      }
+      if (stage == kTopK) {
+        least = hi;
+        too_many = before.count + equal - (uint32_t)set.k;
+      } else {
+        if (threadIdx.x == 0) {
+          const double t = w.sixtyfourths(Key<F32>::value(hi));
+          const u64 m = w.weight(t), n = tokens_to(threshold, before.mass, m);
+          s.kept = min(kept, before.mass + n * m);
+          s.key = hi;
+          s.nth = (uint32_t)n;
+          s.prob = (float)(w.scaled(t) / (double)kept);
+        }
+        __syncthreads();
+        if (stage == kTopP) kept = s.kept;
+      }
+    }
+  }
+  __syncthreads();
+  write_token(keys, s.waves, s.sub_count, s.found, s.key, s.nth, a.ids + r);
+  if (threadIdx.x == 0 && a.prob) a.prob[r] = s.prob;
 }
 
 }  // namespace
@@ -439,9 +900,19 @@ extern "C" bct_status bctm_sample(const void* logits, size_t ld, const float* te
   uint32_t log2n = 0;
   while ((1u << log2n) < N) ++log2n;
   const SampleArgs a = {logits, ld, temperature, top_p, min_p, u, top_k, ids, prob, N, log2n <= 16 ? 46u : 62u - log2n};
-  const bool vec = al16(logits) && ld * size % 16 == 0;
-  const auto kernel = dtype == BCT_F32 ? (vec ? sample_kernel<F32, true> : sample_kernel<F32, false>)
-                                       : (vec ? sample_kernel<BF16, true> : sample_kernel<BF16, false>);
-  hipLaunchKernelGGL(kernel, dim3(rows), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+  const uint32_t vectors = N / (uint32_t)(16 / size);   // of a row
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(rows), dim3(kThreads), 0, (hipStream_t)hip_stream, a); };
+  // one, four or sixteen vectors a thread hold the row; a longer one is read four vectors a thread at a time
+  if (dtype == BCT_F32) {
+    if (vectors <= kThreads) launch(sample_f32_kernel<1, true>);
+    else if (vectors <= 4 * kThreads) launch(sample_f32_kernel<4, true>);
+    else if (vectors <= 16 * kThreads) launch(sample_f32_kernel<16, true>);
+    else launch(sample_f32_kernel<4, false>);
+  } else {
+    if (vectors <= kThreads) launch(sample_bf16_kernel<1, true>);
+    else if (vectors <= 4 * kThreads) launch(sample_bf16_kernel<4, true>);
+    else if (vectors <= 16 * kThreads) launch(sample_bf16_kernel<16, true>);
+    else launch(sample_bf16_kernel<4, false>);
+  }
   return launched("sample");
 }

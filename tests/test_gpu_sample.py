@@ -223,3 +223,23 @@ def test_another_stream_and_a_captured_graph(M):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want), step
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [65535, 65536, 65537, 131071, 131080, 200003])
+def test_one_value_of_many_tokens(M, N, dtype):
+    """A value that occurs in nearly all of a long row, beside others: counts around 65536, of the even and the odd of two
+    values next to each other, and both."""
+    rows = 6
+    x = torch.full((rows, N), 1.0, dtype=DT[dtype], device="cuda")
+    nxt = 1.0 + torch.finfo(DT[dtype]).eps
+    x[1] = nxt
+    x[2, : N // 2] = nxt
+    x[3, ::7] = 4.0
+    x[4] = -2.0
+    x[4, N - 1] = 3.0
+    x[5] = logits(1, N, dtype, N)[0]
+    x[5, ::2] = 0.0
+    u = np.array([0.9999, 0.5, 0.7, 0.99, 0.999, 0.6])
+    check(M, x, u, what="plain")
+    check(M, x, u, k=N // 3, p=0.9, m=1e-3, what="all settings")
