@@ -28,7 +28,7 @@ namespace {
 constexpr uint32_t kThreads = 1024;
 constexpr uint32_t kSub = 1024;      // bins of keys, and blocks of indexes: one a thread
 constexpr uint32_t kGroup = 128, kGroups = 65536 / kGroup;   // bf16 values of a group
-constexpr uint32_t kList = 4096;
+constexpr uint32_t kList = 4096, kFew = 128;
 constexpr uint32_t kMaxVocab = 1u << 22;
 
 typedef unsigned long long u64;
@@ -82,12 +82,19 @@ struct Weigher {
   double c;    // 64 log2(e) / T
   uint32_t S;
   const double* table;   // 2^(i / 64), i < 64
-  // at least -64000, which is as good as no weight; the largest logit (an infinity too) has 0
-  __device__ __forceinline__ double sixtyfourths(float l) const { return l == top ? 0.0 : fmax(((double)l - (double)top) * c, -64000.0); }
-  // 2^(t / 64 + S): the whole part of t from the table, the rest by its Taylor series up to degree 4, within 2e-12
-  __device__ __forceinline__ double scaled(double t) const {
-    const double n = floor(t), f = t - n;
-    const int i = (int)n;
+  // t's whole part, at least -64000, which is as good as no weight, and its rest; the largest logit (an infinity too) has 0
+  struct Parts {
+    int i;
+    double f;
+  };
+  __device__ __forceinline__ Parts sixtyfourths(float l) const {
+    const double t = l == top ? 0.0 : fmax(((double)l - (double)top) * c, -64000.0), n = floor(t);
+    return {(int)n, t - n};
+  }
+  // 2^(t / 64 + S): the whole part from the table, the rest by its Taylor series up to degree 4, within 2e-12
+  __device__ __forceinline__ double scaled(Parts t) const {
+    const int i = t.i;
+    const double f = t.f;
     double p = 5.732851688640402e-10;
     p = __builtin_fma(p, f, 2.1173137155464774e-07);
     p = __builtin_fma(p, f, 5.864904955056169e-05);
@@ -96,7 +103,7 @@ struct Weigher {
     return ldexp(p * table[i & 63], (i >> 6) + (int)S);
   }
   // rounded to a whole number by adding 2^52, whose last place is 1 (S is at most 46)
-  __device__ __forceinline__ u64 weight(double t) const {
+  __device__ __forceinline__ u64 weight(Parts t) const {
     return (u64)__double_as_longlong(scaled(t) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
   }
   __device__ __forceinline__ u64 weight_of(float l) const { return weight(sixtyfourths(l)); }
@@ -115,29 +122,33 @@ struct WaveSums {
   uint32_t count[kThreads / 64];
 };
 
-// What the first lanes hold, up to this one's; LANES 16: of a row of 16.
-template <int LANES = 64>
-__device__ __forceinline__ Sums up_to_lane(Sums run) {
-  const uint32_t lane = threadIdx.x % LANES;
-#pragma unroll
-  for (uint32_t o = 1; o < LANES; o *= 2) {
-    const uint32_t c = __shfl_up(run.count, o, 64);
-    const u64 m = __shfl_up(run.mass, o, 64);
-    if (lane >= o) {
-      run.count += c;
-      run.mass += m;
-    }
+// The value of the lane that the data-parallel-primitive control names, 0 where there is none or the row is not in ROWS: no
+// trip through the LDS crossbar.
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ uint32_t other_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ u64 other_lane(u64 v) {
+  return (u64)other_lane<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | other_lane<CTRL, ROWS>((uint32_t)v);
+}
+// What the lanes up to this one hold, of its row of 16 or of all: lanes 1, 2, 4 and 8 before (row_shr), then the last lane of the
+// row before (row_bcast15 into rows 1 and 3) and of the second row (row_bcast31 into rows 2 and 3).
+template <int LANES = 64, typename V>
+__device__ __forceinline__ V up_to_lane(V run) {
+  run += other_lane<0x111>(run);
+  run += other_lane<0x112>(run);
+  run += other_lane<0x114>(run);
+  run += other_lane<0x118>(run);
+  if (LANES == 64) {
+    run += other_lane<0x142, 0xA>(run);
+    run += other_lane<0x143, 0xC>(run);
   }
   return run;
 }
-__device__ __forceinline__ uint32_t up_to_lane(uint32_t run) {
-  const uint32_t lane = threadIdx.x % 64;
-#pragma unroll
-  for (uint32_t o = 1; o < 64; o *= 2) {
-    const uint32_t c = __shfl_up(run, o, 64);
-    run += lane >= o ? c : 0u;
-  }
-  return run;
+template <int LANES = 64>
+__device__ __forceinline__ Sums up_to_lane(Sums run) {
+  return {up_to_lane<LANES>(run.count), up_to_lane<LANES>(run.mass)};
 }
 __device__ __forceinline__ u64 lane_of(u64 v, int lane) {
   return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
@@ -378,11 +389,12 @@ __device__ __forceinline__ void write_token(RowKeys<DT, NV, ONE>& keys, WaveSums
     });
   }
   __syncthreads();
-  const uint32_t mine = blocks[threadIdx.x], run = up_to_lane(mine), wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const uint32_t mine = blocks[threadIdx.x], run = up_to_lane(mine), lane = threadIdx.x % 64;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   if (lane == 63) waves.count[wave] = run;
   __syncthreads();
-  uint32_t before = run - mine;
-  for (uint32_t w = 0; w < wave; ++w) before += waves.count[w];
+  const uint32_t sums = up_to_lane<kThreads / 64>(waves.count[threadIdx.x % (kThreads / 64)]);
+  const uint32_t before = run - mine + (wave > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)sums, wave - 1) : 0u);
   if (before < nth && nth <= before + mine) {
     found[0] = threadIdx.x;
     found[1] = nth - before;
@@ -651,7 +663,7 @@ struct OctaveShared {
   double table[kPerOctave];
   WaveSums waves;
   uint32_t found[2], range[2], listed, nth, key;
-  u64 kept;
+  u64 kept, above;
   float prob;
 };
 
@@ -674,8 +686,16 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
   } else {
     const Weigher w = {Key<F32>::value(top_key), 92.332482616893656877 / (double)set.T, a.S, s.table};
     auto weight_of = [&](uint32_t k) -> u64 { return w.weight_of(Key<F32>::value(k)); };
-    auto bin_at = [](double t) -> uint32_t { return min((uint32_t)-t, kBins); };
+    auto bin_at = [](Weigher::Parts t) -> uint32_t { return min((uint32_t)-t.i, kBins); };
     auto bin_of = [&](uint32_t k) -> uint32_t { return bin_at(w.sixtyfourths(Key<F32>::value(k))); };
+    // The least key of the bins up to `bin`.  It lies next to the value where the bin ends, but for roundings: looked for there,
+    // and among all keys where it is not.
+    auto least_of_bin = [&](uint32_t bin) -> uint32_t {
+      const uint32_t near = Key<F32>::of(__float_as_uint((float)((double)w.top - (double)bin / w.c)));
+      const uint32_t none = Key<F32>::kMinusInf, lo = near > none + 1000 ? near - 1000 : none, hi = near < top_key - 1000 ? near + 1000 : top_key;
+      const bool there = lo < hi && hi <= top_key && (lo == none || bin_of(lo) > bin) && bin_of(hi) <= bin;
+      return least_key(there ? lo : none, there ? hi : top_key, [&](uint32_t k) { return bin_of(k) <= bin; });
+    };
     const u64 one = 1ull << a.S;
     if (threadIdx.x < 64) {   // the least key that has min_p
       const u64 need = set.min_p > 0.f && set.min_p <= 1.f ? (u64)ceil((double)set.min_p * (double)one) : 1;
@@ -716,7 +736,7 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
         __syncthreads();
         auto token = [&](uint32_t k) {
           if (k < least) return;
-          const double t = w.sixtyfourths(Key<F32>::value(k));
+          const Weigher::Parts t = w.sixtyfourths(Key<F32>::value(k));
           const uint32_t b = bin_at(t);
           if (b >= kBins) return;
           if (by_count) atomicAdd(&s.count[b], 1u);
@@ -731,7 +751,7 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) same = same && __ballot(v[e] == __builtin_amdgcn_readfirstlane(v[0])) == ~0ull;
                 if (same) {
-                  const double t = w.sixtyfourths(Key<F32>::value(v[0]));
+                  const Weigher::Parts t = w.sixtyfourths(Key<F32>::value(v[0]));
                   const uint32_t b = bin_at(t);
                   if (v[0] >= least && b < kBins && lane == 0) {
                     if (by_count) atomicAdd(&s.count[b], 256u);
@@ -797,11 +817,10 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
       }
       // the bin's keys, smallest and largest, and their list
       if (threadIdx.x < 64) {
-        const uint32_t k = least_key(Key<F32>::kMinusInf, top_key, [&](uint32_t k) { return bin_of(k) <= bin; });
+        const uint32_t k = least_of_bin(bin);
         if (threadIdx.x == 0) s.range[0] = max(k, least);
       } else if (threadIdx.x < 128) {
-        uint32_t k = top_key + 1;
-        if (bin > 0) k = least_key(Key<F32>::kMinusInf, top_key, [&](uint32_t k) { return bin_of(k) < bin; });
+        const uint32_t k = bin > 0 ? least_of_bin(bin - 1) : top_key + 1;
         if (threadIdx.x == 64) s.range[1] = k - 1;
       } else if (threadIdx.x == 128) {
         s.listed = 0;
@@ -829,7 +848,35 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
       }
       Sums before = {s.count[bin], s.mass[bin]};
       uint32_t equal;
-      for (;;) {
+      const uint32_t few = s.listed;
+      if (few <= kFew) {   // each key against every other
+        const uint32_t k = threadIdx.x < few ? s.list[threadIdx.x] : 0u;
+        if (threadIdx.x < few) s.sub_mass[threadIdx.x] = by_count ? 1 : k >= least ? weight_of(k) : 0;
+        __syncthreads();
+        if (threadIdx.x < few) {
+          u64 above = 0;
+          uint32_t count = 0, same = 0;
+          for (uint32_t j = 0; j < few; ++j) {
+            const uint32_t other = s.list[j];
+            const u64 m = s.sub_mass[j];
+            above += other > k ? m : 0;
+            count += other > k ? 1u : 0u;
+            same += other == k ? 1u : 0u;
+          }
+          const u64 from = (by_count ? (u64)before.count : before.mass) + above;
+          if (from < threshold && threshold <= from + same * s.sub_mass[threadIdx.x]) {   // those with one key write the same
+            s.range[0] = k;
+            s.sub_count[0] = count;
+            s.sub_count[1] = same;
+            s.above = above;
+          }
+        }
+        __syncthreads();
+        hi = s.range[0];
+        before.count += s.sub_count[0];
+        before.mass += by_count ? 0 : s.above;
+        equal = s.sub_count[1];
+      } else for (;;) {
         uint32_t shift = 0;
         while (((hi - lo) >> shift) >= kSub) ++shift;
         s.sub_count[threadIdx.x] = 0;
@@ -865,7 +912,7 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
         too_many = before.count + equal - (uint32_t)set.k;
       } else {
         if (threadIdx.x == 0) {
-          const double t = w.sixtyfourths(Key<F32>::value(hi));
+          const Weigher::Parts t = w.sixtyfourths(Key<F32>::value(hi));
           const u64 m = w.weight(t), n = tokens_to(threshold, before.mass, m);
           s.kept = min(kept, before.mass + n * m);
           s.key = hi;
