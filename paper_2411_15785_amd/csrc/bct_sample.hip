@@ -660,9 +660,10 @@ struct OctaveShared {
   u64 sub_mass[kSub];
   uint32_t sub_count[kSub];
   uint32_t list[kList];       // the keys of one bin
+  uint32_t row[kList];        // all keys that are weighed, where they are so few
   double table[kPerOctave];
   WaveSums waves;
-  uint32_t found[2], range[2], listed, nth, key;
+  uint32_t found[2], range[2], listed, in_row, nth, key;
   u64 kept, above;
   float prob;
 };
@@ -688,18 +689,21 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
     auto weight_of = [&](uint32_t k) -> u64 { return w.weight_of(Key<F32>::value(k)); };
     auto bin_at = [](Weigher::Parts t) -> uint32_t { return min((uint32_t)-t.i, kBins); };
     auto bin_of = [&](uint32_t k) -> uint32_t { return bin_at(w.sixtyfourths(Key<F32>::value(k))); };
-    // The least key of the bins up to `bin`.  It lies next to the value where the bin ends, but for roundings: looked for there,
-    // and among all keys where it is not.
-    auto least_of_bin = [&](uint32_t bin) -> uint32_t {
-      const uint32_t near = Key<F32>::of(__float_as_uint((float)((double)w.top - (double)bin / w.c)));
-      const uint32_t none = Key<F32>::kMinusInf, lo = near > none + 1000 ? near - 1000 : none, hi = near < top_key - 1000 ? near + 1000 : top_key;
-      const bool there = lo < hi && hi <= top_key && (lo == none || bin_of(lo) > bin) && bin_of(hi) <= bin;
-      return least_key(there ? lo : none, there ? hi : top_key, [&](uint32_t k) { return bin_of(k) <= bin; });
+    // The least key for which `is` holds, from some key on.  It lies next to the logit `near`, but for roundings: looked for
+    // there, and among all keys where it is not.
+    auto least_near = [&](double near, auto is) -> uint32_t {
+      const uint32_t at = Key<F32>::of(__float_as_uint((float)near));
+      const uint32_t none = Key<F32>::kMinusInf, lo = at > none + 1000 ? at - 1000 : none, hi = at < top_key - 1000 ? at + 1000 : top_key;
+      const bool there = lo < hi && hi <= top_key && (lo == none || !is(lo)) && is(hi);
+      return least_key(there ? lo : none, there ? hi : top_key, is);
+    };
+    auto least_of_bin = [&](uint32_t bin) -> uint32_t {   // of the bins up to this one
+      return least_near((double)w.top - (double)bin / w.c, [&](uint32_t k) { return bin_of(k) <= bin; });
     };
     const u64 one = 1ull << a.S;
-    if (threadIdx.x < 64) {   // the least key that has min_p
-      const u64 need = set.min_p > 0.f && set.min_p <= 1.f ? (u64)ceil((double)set.min_p * (double)one) : 1;
-      const uint32_t k = least_key(Key<F32>::kMinusInf, top_key, [&](uint32_t k) { return weight_of(k) >= need; });
+    if (threadIdx.x < 64 && set.min_p > 0.f && set.min_p <= 1.f) {   // the least key that has min_p
+      const u64 need = (u64)ceil((double)set.min_p * (double)one);
+      const uint32_t k = least_near((double)w.top + log2((double)set.min_p) * kPerOctave / w.c, [&](uint32_t k) { return weight_of(k) >= need; });
       if (lane == 0) s.range[0] = k;
     }
     __syncthreads();
@@ -719,10 +723,38 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
     u64 kept = 0, of_k = 0;   // the weight that is kept, of the first so many; what top-k leaves
     uint32_t least = Key<F32>::kMinusInf + 1;   // the keys that are weighed: top-k's and all that equal its last
     u64 too_many = 0;                           // of those, how many it leaves out
+    // Where few tokens are left, by a mask that comes with the logits or by top-k, they are listed and the row is not looked
+    // at again.
+    uint32_t drawable = 0;
+    for (uint32_t n = 0; n < keys.loads; ++n) {
+      keys.load(n);
+      keys.each([&](u32x4 v, uint32_t) { keys.tokens(v, [&](uint32_t k) { drawable += k >= least ? 1u : 0u; }); });
+    }
+    Sums drawables;
+    before_thread(s.waves, {drawable, 0ull}, &drawables);
+    bool to_list = drawables.count <= kList, row_listed = false;
 #pragma unroll 1
     for (int stage = kTopK; stage < kStages; ++stage) {
       const bool by_count = stage == kTopK;
       __syncthreads();
+      if (to_list) {
+        if (threadIdx.x == 0) s.in_row = 0;
+        __syncthreads();
+        for (uint32_t n = 0; n < keys.loads; ++n) {
+          keys.load(n);
+          keys.each([&](u32x4 v, uint32_t) {
+            keys.tokens(v, [&](uint32_t k) {
+              if (k >= least) {
+                const uint32_t i = atomicAdd(&s.in_row, 1u);
+                if (i < kList) s.row[i] = k;
+              }
+            });
+          });
+        }
+        __syncthreads();
+        row_listed = s.in_row <= kList;
+        to_list = false;
+      }
       if (by_count && (set.k <= 0 || (uint32_t)set.k >= keys.N)) continue;
       if (stage == kTopP && !(set.p < 1.f)) continue;
       Sums all = {0u, 0ull};
@@ -742,7 +774,8 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
           if (by_count) atomicAdd(&s.count[b], 1u);
           else atomicAdd(&s.mass[b], w.weight(t));
         };
-        for (uint32_t n = 0; n < keys.loads; ++n) {
+        for (uint32_t j = threadIdx.x; row_listed && j < s.in_row; j += kThreads) token(s.row[j]);
+        for (uint32_t n = 0; !row_listed && n < keys.loads; ++n) {
           keys.load(n);
           keys.each_four(
               [&](u32x4 v) {
@@ -827,16 +860,16 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
       }
       __syncthreads();
       uint32_t lo = s.range[0], hi = s.range[1];
-      for (uint32_t n = 0; n < keys.loads; ++n) {
+      auto take = [&](uint32_t k) {
+        if (k >= lo && k <= hi) {
+          const uint32_t i = atomicAdd(&s.listed, 1u);
+          if (i < kList) s.list[i] = k;
+        }
+      };
+      for (uint32_t j = threadIdx.x; row_listed && j < s.in_row; j += kThreads) take(s.row[j]);
+      for (uint32_t n = 0; !row_listed && n < keys.loads; ++n) {
         keys.load(n);
-        keys.each([&](u32x4 v, uint32_t) {
-          keys.tokens(v, [&](uint32_t k) {
-            if (k >= lo && k <= hi) {
-              const uint32_t i = atomicAdd(&s.listed, 1u);
-              if (i < kList) s.list[i] = k;
-            }
-          });
-        });
+        keys.each([&](u32x4 v, uint32_t) { keys.tokens(v, take); });
       }
       __syncthreads();
       if (stage == kMinP) {
@@ -910,6 +943,7 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
       if (stage == kTopK) {
         least = hi;
         too_many = before.count + equal - (uint32_t)set.k;
+        to_list = !row_listed && before.count + equal <= kList;
       } else {
         if (threadIdx.x == 0) {
           const Weigher::Parts t = w.sixtyfourths(Key<F32>::value(hi));
