@@ -51,8 +51,8 @@ __device__ __forceinline__ void turn_of(int32_t position, double inv_freq, float
 }
 
 // G lanes to a head (the power of two from d / 2E on), HPG heads to a group of them: slot s of the `slots` groups of a row
-// has the heads s, s + slots, ...  q's heads come first, then k's.
-template <typename DT, bool NORM, RopePairs PAIRS, int G, int HPG>
+// has the heads s, s + slots, ...  q's heads come first, then k's.  PAST: loads and stores leave the caches as they are.
+template <typename DT, bool NORM, RopePairs PAIRS, int G, int HPG, bool PAST>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(HeadBlock q, HeadBlock k, const int32_t* __restrict__ positions,
                                                            const double* __restrict__ inv_freq, uint32_t rot, uint32_t rows,
                                                            uint32_t d, uint32_t slots, float eps) {
@@ -72,8 +72,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(HeadBlock q, HeadBloc
     const uint32_t h = slot + i * slots;
     if (mine && h < q.n + k.n) {
       const elem* p = h < q.n ? (const elem*)q.in + (size_t)row * q.ld + (size_t)h * d : (const elem*)k.in + (size_t)row * k.ld + (size_t)(h - q.n) * d;
-      v[i][0] = *(const u32x4*)(p + e0);
-      v[i][1] = *(const u32x4*)(p + e1);
+      v[i][0] = PAST ? __builtin_nontemporal_load((const u32x4*)(p + e0)) : *(const u32x4*)(p + e0);
+      v[i][1] = PAST ? __builtin_nontemporal_load((const u32x4*)(p + e1)) : *(const u32x4*)(p + e1);
     } else {
       v[i][0] = v[i][1] = u32x4{0u, 0u, 0u, 0u};
     }
@@ -129,8 +129,14 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(HeadBlock q, HeadBloc
     }
     if (mine && h < q.n + k.n) {
       elem* o = h < q.n ? (elem*)q.out + (size_t)row * q.out_ld + (size_t)h * d : (elem*)k.out + (size_t)row * k.out_ld + (size_t)(h - q.n) * d;
-      *(u32x4*)(o + e0) = pack16_round<DT>(f);
-      *(u32x4*)(o + e1) = pack16_round<DT>(f + E);
+      const u32x4 o0 = pack16_round<DT>(f), o1 = pack16_round<DT>(f + E);
+      if (PAST) {
+        __builtin_nontemporal_store(o0, (u32x4*)(o + e0));
+        __builtin_nontemporal_store(o1, (u32x4*)(o + e1));
+      } else {
+        *(u32x4*)(o + e0) = o0;
+        *(u32x4*)(o + e1) = o1;
+      }
     }
   }
 }
@@ -144,19 +150,29 @@ struct RopeCall {
   hipStream_t s;
 };
 
-template <typename DT, bool NORM, RopePairs PAIRS, int G, int HPG>
+template <typename DT, bool NORM, RopePairs PAIRS, int G, int HPG, bool PAST>
 bct_status launch_rope(const RopeCall& c) {
   const uint32_t heads = c.q.n + c.k.n, slots = (heads + HPG - 1) / HPG;
   const uint64_t blocks = ((uint64_t)c.rows * slots * G + 255) / 256;
   if (blocks > 0x7FFFFFFFull) return mfail(BCT_ERR_UNSUPPORTED, "too many rows and heads for one launch");
-  hipLaunchKernelGGL((qk_norm_rope_kernel<DT, NORM, PAIRS, G, HPG>), dim3((unsigned)blocks), dim3(256), 0, c.s, c.q, c.k,
+  hipLaunchKernelGGL((qk_norm_rope_kernel<DT, NORM, PAIRS, G, HPG, PAST>), dim3((unsigned)blocks), dim3(256), 0, c.s, c.q, c.k,
                      c.positions, c.inv_freq, c.rot, c.rows, c.d, slots, c.eps);
   return launched("qk_norm_rope");
 }
 
+// Two heads a group, once one leaves eight wavefronts for each of 256 compute units: its loads are in flight at once and
+// the angles are worked out for two.  us, 1 | 2 | 4 | 8 heads, bf16: 1 row of 64 heads of 128 3.27 | 3.58 | 4.69 | 6.74; 256 rows x 64
+// x 64 (2048 wavefronts) 3.69 | 4.09 | 5.11 | 7.36; x 128 (4096) 4.83 | 4.40 | 5.46 | 7.66; 2048 x 64 x 128 16.2 | 15.0 | 14.5 | 15.7; 16384 x
+// 64 x 128 122 | 97.5 | 97.3 | 102; fp32 256 x 64 x 64 4.22 | 3.89 | 5.38 | 6.29, 16384 x 64 x 128 371 | 378 | 375 | 402 for heads of 256, 187
+// | 186 | 192 | 198.
+// Past the caches where what is read and written is more than the last-level cache's 256 MB, so that nothing of it would be found
+// there: 16384 x 64 x 128 bf16 (537 MB) 104 | 94.4 us (5.7 TB/s).  Smaller outputs are in that cache for the step that follows.
 template <typename DT, bool NORM, RopePairs PAIRS, int G>
 bct_status rope_heads(const RopeCall& c) {
-  return launch_rope<DT, NORM, PAIRS, G, 1>(c);
+  const bool two = (uint64_t)c.rows * (c.q.n + c.k.n) * G >= 8ull * 64 * 256;
+  const uint64_t elements = (uint64_t)c.rows * (c.q.n + c.k.n) * c.d;
+  if (2 * elements * (16 / DT::kElemsPerVec) > 256ull << 20) return launch_rope<DT, NORM, PAIRS, G, 2, true>(c);
+  return two ? launch_rope<DT, NORM, PAIRS, G, 2, false>(c) : launch_rope<DT, NORM, PAIRS, G, 1, false>(c);
 }
 template <typename DT, bool NORM, RopePairs PAIRS>
 bct_status rope_group(const RopeCall& c) {

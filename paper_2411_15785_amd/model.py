@@ -174,60 +174,67 @@ def bctm_rmsnorm(x, gain, eps, out=None, tiled=False):
     return out
 
 
-def _heads(t, name, like=None):
-    """t [rows][heads][d] with contiguous heads, its rows at any distance (a part of a wider row)."""
-    torch = _torch()
-    want = (torch.float32, torch.bfloat16) if like is None else (like.dtype,)
-    if t.dtype not in want or t.dim() != 3 or not t.is_cuda or t.stride(2) != 1 or \
-            (t.shape[1] > 1 and t.stride(1) != t.shape[2]) or (like is not None and t.device != like.device):
-        raise ValueError(f"{name}: expected [rows][heads][d] heads side by side"
-                         + (", float32 or bf16, on the GPU" if like is None else f", {like.dtype} on {like.device}")
-                         + f", got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+def _heads(t, name, dtype, device):
+    """t [rows][heads][d] with contiguous heads, its rows at any distance (a part of a wider row) -> shape, that distance."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not dtype or len(shape) != 3 or t.get_device() != device or stride[2] != 1 or \
+            (stride[1] != shape[2] and shape[1] > 1):
+        raise ValueError(f"{name}: expected {dtype} [rows][heads][d] on cuda:{device}, heads side by side, got {t.dtype} "
+                         f"{tuple(shape)} strides {stride} on {t.device}")
     # the distance of a single row is not looked at
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
+    return shape, stride[0] if shape[0] > 1 else max(stride[0], shape[1] * shape[2])
 
 
 def bctm_qk_norm_rope(q, k=None, q_gain=None, k_gain=None, eps=None, positions=None, inv_freq=None, interleaved=False,
                       q_out=None, k_out=None):
-    """Queries [rows][Hq][d] and write queries [rows][Hkv][d] (or None): each head normalised (eps given) and turned by its
-    row's position (positions int32 [rows] with inv_freq float64 [rotary_dim / 2], radians per position) -> (q_out, k_out).
-    q and k may be parts of wider rows; q_out=q and k_out=k work in place."""
+    """Queries [rows][Hq][d] and write queries [rows][Hkv][d] (or None), float32 or bf16: each head normalised (eps given) and
+    turned by its row's position (positions int32 [rows] with inv_freq float64 [rotary_dim / 2], radians per position)
+    -> (q_out, k_out).  q and k may be parts of wider rows; q_out=q and k_out=k work in place."""
     torch = _torch()
-    ldq = _heads(q, "q")
-    rows, hq, d = q.shape
+    dtype, device = q.dtype, q.get_device()
+    if device < 0 or (dtype is not torch.bfloat16 and dtype is not torch.float32):
+        raise ValueError(f"q: expected float32 or bf16 on the GPU, got {dtype} on {q.device}")
+    qs, ldq = _heads(q, "q", dtype, device)
+    rows, hq, d = qs
     if q_out is None:
-        q_out = torch.empty((rows, hq, d), dtype=q.dtype, device=q.device)
-    ldqo = _heads(q_out, "q_out", q)
+        q_out = torch.empty(qs, dtype=dtype, device=q.device)
+    qos, ldqo = (qs, ldq) if q_out is q else _heads(q_out, "q_out", dtype, device)
     hk = ldk = ldko = 0
     if k is not None:
-        ldk = _heads(k, "k", q)
-        if k.shape[0] != rows or k.shape[2] != d:
+        ks, ldk = _heads(k, "k", dtype, device)
+        if ks[0] != rows or ks[2] != d:
             raise ValueError("k: one row per row of q, heads of the same size")
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=q.dtype, device=q.device)
-        ldko = _heads(k_out, "k_out", q)
-        hk = k.shape[1]
-    if q_out.shape != q.shape or (k is None) != (k_out is None) or (k is not None and k_out.shape != k.shape):
-        raise ValueError("q_out / k_out: the shapes of q / k")
+            k_out = torch.empty(ks, dtype=dtype, device=q.device)
+        kos, ldko = (ks, ldk) if k_out is k else _heads(k_out, "k_out", dtype, device)
+        hk = ks[1]
+        if kos != ks:
+            raise ValueError("k_out: the shape of k")
+    elif k_out is not None:
+        raise ValueError("k_out goes with k")
+    if qos != qs:
+        raise ValueError("q_out: the shape of q")
     for g, n in ((q_gain, "q_gain"), (k_gain, "k_gain")):
-        if g is not None and (g.dtype != q.dtype or g.shape != (d,) or not g.is_contiguous() or g.device != q.device):
-            raise ValueError(f"{n}: expected a contiguous {q.dtype} vector of {d} on {q.device}")
-    if (positions is None) != (inv_freq is None):
-        raise ValueError("positions and inv_freq: both or neither")
+        if g is not None and (g.dtype is not dtype or g.shape != (d,) or not g.is_contiguous() or g.get_device() != device):
+            raise ValueError(f"{n}: expected a contiguous {dtype} vector of {d} on cuda:{device}")
     rot = 0
-    if positions is not None:
-        if positions.dtype != torch.int32 or positions.shape != (rows,) or not positions.is_contiguous() or \
-                positions.device != q.device:
-            raise ValueError(f"positions: expected a contiguous int32 vector of {rows} on {q.device}")
-        if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.device != q.device:
-            raise ValueError(f"inv_freq: expected a contiguous float64 vector on {q.device}")
+    if positions is not None and inv_freq is not None:
+        if positions.dtype is not torch.int32 or positions.shape != (rows,) or not positions.is_contiguous() or \
+                positions.get_device() != device:
+            raise ValueError(f"positions: expected a contiguous int32 vector of {rows} on cuda:{device}")
+        if inv_freq.dtype is not torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or \
+                inv_freq.get_device() != device:
+            raise ValueError(f"inv_freq: expected a contiguous float64 vector on cuda:{device}")
         rot = 2 * inv_freq.numel()
+    elif positions is not inv_freq:
+        raise ValueError("positions and inv_freq: both or neither")
     if eps is not None and not eps >= 0:
         raise ValueError("eps must not be negative")
     flags = (BCTM_HEAD_NORM if eps is not None else 0) | (BCTM_ROPE_INTERLEAVED if interleaved else 0)
-    _ck(_launch(mlib().bctm_qk_norm_rope, q.device, _dptr(q), _dptr(q_out), _dptr(q_gain), hq, ldq, ldqo, _dptr(k), _dptr(k_out),
-                _dptr(k_gain), hk, ldk, ldko, _dptr(positions), _dptr(inv_freq), rot, rows, d, eps or 0.0,
-                binding.BCT_F32 if q.dtype == torch.float32 else binding.BCT_BF16, flags), "bctm_qk_norm_rope")
+    st = _launch(mlib().bctm_qk_norm_rope, q.device, q.data_ptr(), q_out.data_ptr(), _dptr(q_gain), hq, ldq, ldqo, _dptr(k),
+                 _dptr(k_out), _dptr(k_gain), hk, ldk, ldko, _dptr(positions), _dptr(inv_freq), rot, rows, d, eps or 0.0,
+                 binding.BCT_F32 if dtype is torch.float32 else binding.BCT_BF16, flags)
+    _ck(st, "bctm_qk_norm_rope")
     return q_out, k_out
 
 
@@ -348,11 +355,16 @@ class LoraWeights:
     def __init__(self, a, b, b_up, scale, n, segments, rank, K, N):
         self.a, self.b, self.b_up, self.scale = a, b, b_up, scale
         self.n, self.segments, self.rank, self.K, self.N = n, segments, rank, K, N
+        self._sizes = {}   # rows -> bytes of workspace
 
     def workspace_bytes(self, rows):
-        v = ctypes.c_size_t(0)
-        _ck(mlib().bctm_lora_workspace(rows, self.K, self.rank, self.segments, ctypes.byref(v)), "bctm_lora_workspace")
-        return v.value
+        if rows not in self._sizes:
+            v = ctypes.c_size_t(0)
+            _ck(mlib().bctm_lora_workspace(rows, self.K, self.rank, self.segments, ctypes.byref(v)), "bctm_lora_workspace")
+            if len(self._sizes) >= 64:   # of row counts that come and go
+                self._sizes.clear()
+            self._sizes[rows] = v.value
+        return self._sizes[rows]
 
 
 def bctm_lora_pack(a, b, scale=None):
@@ -392,17 +404,18 @@ def _lora_arg(lora, ids, workspace, device, rows, K, N, segments, swiglu):
     torch = _torch()
     if not isinstance(lora, LoraWeights):
         raise ValueError("lora: expected LoraWeights (bctm_lora_pack)")
-    if (lora.K, lora.N, lora.segments) != (K, N, segments) or (lora.b_up is not None) != swiglu or lora.a.device != device:
+    if lora.K != K or lora.N != N or lora.segments != segments or (lora.b_up is not None) != swiglu or lora.a.device != device:
         raise ValueError(f"lora: packed for {lora.K} -> {lora.N} in {lora.segments} segments on {lora.a.device}, the projection is "
                          f"{K} -> {N} in {segments} on {device}")
-    if ids.dtype != torch.int32 or ids.shape != (rows,) or not ids.is_contiguous() or ids.device != device:
+    if ids.dtype is not torch.int32 or ids.shape != (rows,) or not ids.is_contiguous() or ids.device != device:
         raise ValueError(f"ids: expected a contiguous int32 vector of {rows} on {device}")
     if workspace is None:
         workspace = torch.empty(lora.workspace_bytes(rows), dtype=torch.uint8, device=device)
-    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != device:
+    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.device != device:
         raise ValueError(f"workspace: expected contiguous torch.uint8 on {device}")
-    return _bctm_lora(_dptr(lora.a), _dptr(lora.b), _dptr(lora.b_up), _dptr(lora.scale), _dptr(ids), lora.n, lora.rank,
-                      _dptr(workspace), workspace.numel()), workspace
+    # read by the call, which the second value outlives
+    return _bctm_lora(lora.a.data_ptr(), lora.b.data_ptr(), _dptr(lora.b_up), _dptr(lora.scale), ids.data_ptr(), lora.n, lora.rank,
+                      workspace.data_ptr(), workspace.numel()), workspace
 
 
 def bctm_linear_lora(x, w, lora, ids, residual=None, out=None, workspace=None):
