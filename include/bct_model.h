@@ -7,10 +7,13 @@
  * of such a stack, so that a token can go through whole layers on the GPU:
  * embedding lookup, RMS normalisation, the projections (W_q, W_wq, W_wv, W_o,
  * the SwiGLU MLP, the output head) and the greedy arg-max.  The attention
- * itself stays bct_decode_step / bct_prefill (include/bct.h).
+ * itself stays bct_decode_step / bct_prefill (include/bct.h).  For what each
+ * request of a batch brings of its own: head norms with the rotation by its
+ * position (bctm_qk_norm_rope), low-rank adapters beside the projections
+ * (bctm_lora) and sampled instead of greedy tokens (bctm_sample).
  *
  * All data pointers are DEVICE memory owned by the caller, bf16, row-major,
- * 16-byte aligned; token ids are int32.  Calls enqueue on the given stream and
+ * 16-byte aligned, unless a call says otherwise; token ids are int32.  Calls enqueue on the given stream and
  * return.  Status codes are those of include/bct.h.
  */
 #ifndef BCT_MODEL_H
