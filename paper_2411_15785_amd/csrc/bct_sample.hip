@@ -433,7 +433,7 @@ struct CountShared {
   uint32_t one[kSub];           // counts of one group's values; blocks of indexes
   double table[kPerOctave];
   WaveSums waves;
-  uint32_t found[2], range[2], nth, key;
+  uint32_t found[2], from_p, nth, key;
   Sums above;                   // the groups above the one that is looked at
   u64 kept, of_k;
   float prob;
@@ -489,15 +489,17 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
   } else {
     const Weigher w = {Key<BF16>::value(top_key), 92.332482616893656877 / (double)set.T, a.S, s.table};
     auto weight_of = [&](uint32_t k) -> u64 { return w.weight_of(Key<BF16>::value(k)); };
-    // the least value that has a weight, and the least that has min_p (none where it is beyond 1)
     const u64 one = 1ull << a.S;
-    if (threadIdx.x < 128) {
-      const u64 need = wave && set.min_p > 0.f && set.min_p <= 1.f ? (u64)ceil((double)set.min_p * (double)one) : 1;
+    // values that are counted: those 47 octaves below the largest and less have no weight (the value there may be a step off)
+    uint32_t cut = Key<BF16>::kMinusInf + 1;
+    const double end = (double)w.top - 47 * kPerOctave / w.c;
+    if (end > -3e38) cut = max(cut, (Key<BF16>::of(__float_as_uint((float)end) >> 16) & 0xFFFFu) - 2);
+
+    if (threadIdx.x < 64 && set.min_p > 0.f && set.min_p <= 1.f) {   // the least value that has min_p
+      const u64 need = (u64)ceil((double)set.min_p * (double)one);
       const uint32_t k = least_key(Key<BF16>::kMinusInf, top_key, [&](uint32_t k) { return weight_of(k) >= need; });
-      if (lane == 0) s.range[wave] = k;
+      if (lane == 0) s.from_p = k;
     }
-    __syncthreads();
-    const uint32_t cut = s.range[0], from_p = s.range[1];
 
     // The counts into the groups' sums: a wavefront takes 128 values at a time, the next one the next.
     auto add_up = [&](bool clear) {
@@ -569,6 +571,7 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
     if (threadIdx.x < kGroups) s.mass[kGroups - 1 - threadIdx.x] = above.mass;
     if (threadIdx.x == 0) s.kept = s.of_k = all.mass;   // the weight that is kept, of the first so many; what top-k leaves
 
+    uint32_t from_p = 0;
 #pragma unroll 1
     for (int stage = kTopK; stage < kStages; ++stage) {
       // the value where the counts (top-k) or weights cumulated in the row's order reach `threshold`, or the key of min-p
@@ -581,13 +584,12 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
         threshold = (u64)set.k;
       } else if (stage == kMinP) {
         if (!(set.min_p > 0.f)) continue;
-        const u64 least = set.min_p > 1.f ? one : s.mass[from_p / kGroup];   // beyond 1 nothing has as much: the first
-        if (least >= kept) continue;                                           // it cuts nothing off
-        if (set.min_p > 1.f) {
-          __syncthreads();
-          if (threadIdx.x == 0) s.kept = one;
+        if (set.min_p > 1.f) {   // nothing has as much: the first
+          if (threadIdx.x == 0) s.kept = min(kept, one);
           continue;
         }
+        from_p = s.from_p;
+        if (s.mass[from_p / kGroup] >= kept) continue;   // it cuts nothing off
       } else if (stage == kTopP) {
         threshold = top_p_threshold(set, s.of_k);
         if (!(set.p < 1.f) || threshold > kept) continue;
