@@ -9,9 +9,10 @@
 // No sort: what is asked of the order is only where cumulated weights or counts pass a threshold, and histograms tell that.
 // A token is a whole number, so the sums must not depend on an order of additions, nor on fp32 roundings: weights are whole
 // multiples of 2^-S, S at least 40, added as 64-bit integers.
-//   bf16   a value is one of 65536, so the row is counted by value, exactly, in 128 KB of LDS (16 bits a value), and a weight
-//          is worked out for each value that occurs instead of for each token.  Sums over groups of 128 values say in which
-//          group the threshold is passed, the counts of that group at which value.
+//   bf16   a value is one of 65536, and those with a weight seldom span more than 36864 of them (not where logits are beyond
+//          2^17), so the row is counted by value, exactly, in 144 KB of LDS, and a weight is worked out for each value that
+//          occurs instead of for each token.  Sums over groups of 128 values say in which group the threshold is passed, the
+//          counts of that group at which value.
 //   fp32   a histogram of weights over 1/64 octaves of w; the bin where the threshold is passed is gathered and divided
 //          further by value.
 // Equal values have equal weights, so the rest is a division, and the token the nth with its value in the order of the indexes.
@@ -27,7 +28,7 @@ namespace {
 
 constexpr uint32_t kThreads = 1024;
 constexpr uint32_t kSub = 1024;      // bins of keys, and blocks of indexes: one a thread
-constexpr uint32_t kGroup = 128, kGroups = 65536 / kGroup;   // bf16 values of a group
+constexpr uint32_t kGroup = 128, kGroups = 65536 / kGroup, kWindow = 288;   // bf16 values of a group; groups counted at a time
 constexpr uint32_t kList = 4096, kFew = 128;
 constexpr uint32_t kMaxVocab = 1u << 22;
 
@@ -271,18 +272,16 @@ struct RowKeys {
   __device__ __forceinline__ void each(F f) const {
 #pragma unroll
     for (int i = 0; i < NV; ++i) f(k[i], (at * kLoad + i * kThreads + threadIdx.x) * E);
-    f(u32x4{last, kNone, kNone, kNone}, N / E * E + threadIdx.x);
+    if (N % E != 0 && threadIdx.x < 64) f(u32x4{last, kNone, kNone, kNone}, N / E * E + threadIdx.x);
   }
-  // The same for a long f: it stands there for four vectors, and they are moved past it.  after(): when four are done.
-  static constexpr int kFours = (NV + 3) / 4;
-  template <typename F, typename A>
-  __device__ __forceinline__ void each_four(F f, A after) {
+  // The same for a long f: it stands there for four vectors, and they are moved past it.
+  template <typename F>
+  __device__ __forceinline__ void each_four(F f) {
 #pragma unroll 1
-    for (int n = 0; n < kFours; ++n) {
+    for (int n = 0; n < (NV + 3) / 4; ++n) {
 #pragma unroll
       for (int i = 0; i < 4 && i < NV; ++i) f(k[i]);
-      if (n == 0) f(u32x4{last, kNone, kNone, kNone});
-      if constexpr (kFours > 1) {
+      if constexpr (NV > 4) {
         u32x4 first[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) first[i] = k[i];
@@ -291,8 +290,8 @@ struct RowKeys {
 #pragma unroll
         for (int i = 0; i < 4; ++i) k[NV - 4 + i] = first[i];
       }
-      after();
     }
+    if (N % E != 0 && threadIdx.x < 64) f(u32x4{last, kNone, kNone, kNone});
   }
   // g(key) for every token of a vector
   template <typename G>
@@ -427,40 +426,39 @@ __device__ __forceinline__ void write_none(const SampleArgs& a, uint32_t r) {
 // ---------------------------------------------------------------- bf16: counted by value
 
 struct CountShared {
-  uint32_t count[32768];        // 16 bits a value
-  u64 mass[kGroups];            // of each group of values; then of the groups above each
+  uint32_t count[kWindow * kGroup];   // of each value
+  u64 mass[kGroups];                  // of each group of values; then of the groups above each
   uint32_t tokens[kGroups];
-  uint32_t one[kSub];           // counts of one group's values; blocks of indexes
+  uint32_t one[kSub];                 // counts of one group's values; blocks of indexes
   double table[kPerOctave];
   WaveSums waves;
   uint32_t found[2], from_p, nth, key;
-  Sums above;                   // the groups above the one that is looked at
+  Sums above;                         // the groups above the one that is looked at
   u64 kept, of_k;
   float prob;
 };
 
-// The values of a vector counted, those from `cut` on; one of a wavefront's lanes adds for all where they have the same words.
-__device__ __forceinline__ void count_values(uint32_t* count, u32x4 v, uint32_t cut) {
-  auto add = [&](uint32_t k, uint32_t n) {
-    if (k >= cut) atomicAdd(&count[k >> 1], (k & 1) * (n * 0xFFFFu) + n);
-  };
+// The values of a vector counted, those from `base` on, `span` of them; one of a wavefront's lanes adds for all where they
+// have the same words.
+__device__ __forceinline__ void count_values(uint32_t* count, u32x4 v, uint32_t base, uint32_t span) {
   const uint32_t first = __builtin_amdgcn_readfirstlane(v[0]);
   if (__ballot(v[0] == first) == ~0ull) {
 #pragma unroll 1
-    for (int e = 0; e < 4; ++e) {
-      const bool same = __ballot(v[0] == __builtin_amdgcn_readfirstlane(v[0])) == ~0ull;
-      if (!same || threadIdx.x % 64 == 0) {
-        add(v[0] & 0xFFFFu, same ? 64 : 1);
-        add(v[0] >> 16, same ? 64 : 1);
-      }
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t k = v[0] & 0xFFFFu;
+      const bool same = __ballot(k == __builtin_amdgcn_readfirstlane(k)) == ~0ull;
+      if (k - base < span && (!same || threadIdx.x % 64 == 0)) atomicAdd(&count[k - base], same ? 64u : 1u);
 #pragma unroll
-      for (int i = 0; i < 3; ++i) v[i] = v[i + 1];
+      for (int i = 0; i < 4; ++i) v[i] = v[i] >> 16 | (i < 3 ? v[(i + 1) % 4] << 16 : 0u);
     }
   } else {
+    auto add = [&](uint32_t at) {   // in bytes
+      if (at < 4 * span) atomicAdd((uint32_t*)((char*)count + at), 1u);
+    };
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      add(v[e] & 0xFFFFu, 1);
-      add(v[e] >> 16, 1);
+      add((v[e] << 2 & 0x3FFFCu) - 4 * base);
+      add((v[e] >> 14 & 0x3FFFCu) - 4 * base);
     }
   }
 }
@@ -470,7 +468,10 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
   __shared__ CountShared s;
   const uint32_t r = blockIdx.x, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
   RowKeys<BF16, NV, ONE> keys((const uint16_t*)a.logits + (size_t)r * a.ld, a.N);
-  for (uint32_t i = threadIdx.x; i < 32768 / 4; i += kThreads) ((u32x4*)s.count)[i] = u32x4{0u, 0u, 0u, 0u};
+  auto clear = [&] {
+    for (uint32_t i = threadIdx.x; i < kWindow * kGroup / 4; i += kThreads) ((u32x4*)s.count)[i] = u32x4{0u, 0u, 0u, 0u};
+  };
+  clear();
   if (threadIdx.x < kGroups) {
     s.mass[threadIdx.x] = 0;
     s.tokens[threadIdx.x] = 0;
@@ -501,73 +502,52 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
       if (lane == 0) s.from_p = k;
     }
 
-    // The counts into the groups' sums: a wavefront takes 128 values at a time, the next one the next.
-    auto add_up = [&](bool clear) {
-      __syncthreads();
-      const uint32_t g1 = top_key / kGroup;
-#pragma unroll 1
-      for (uint32_t g0 = cut / kGroup + wave; g0 <= g1; g0 += 4 * (kThreads / 64)) {
-        uint32_t c[4];
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-          const uint32_t g = g0 + i * (kThreads / 64);
-          c[i] = g <= g1 ? s.count[g * 64 + lane] : 0u;
-        }
-#pragma unroll 1
-        for (uint32_t g = g0; g < g0 + 4 * (kThreads / 64); g += kThreads / 64) {
-          const uint32_t now = c[0];
-#pragma unroll
-          for (int i = 0; i < 3; ++i) c[i] = c[i + 1];
-          c[3] = 0;
-          if (__ballot(now != 0) == 0) continue;
-          const uint32_t i = g * 64 + lane;
-          Sums t = {(now & 0xFFFFu) + (now >> 16), 0ull};
-          if (now) {
-            if (clear) s.count[i] = 0;
-            t.mass = (now & 0xFFFFu) * weight_of(2 * i) + (now >> 16) * weight_of(2 * i + 1);
-          }
-          t = up_to_lane(t);
-          if (lane == 63) {
-            s.tokens[g] += t.count;
-            s.mass[g] += t.mass;
-          }
-        }
-      }
-      __syncthreads();
-    };
-    // 16 bits a value: should one of more than 65535 tokens occur that often, the counts' sum is too small (a carry out of the
-    // lower half counts for 65536 fewer, one of the upper half is lost), and all is done again in portions of 32768
-    bool portions = false;
-    Sums mine, above, all;
+    // Counted, and the counts added up into the groups' sums, a window of groups at a time from the largest value down
+    const uint32_t g_cut = cut / kGroup;
+    uint32_t g1 = top_key / kGroup, g0;
+    bool one_window = true;
     for (;;) {
-      uint32_t counted = 0;
+      g0 = g1 >= g_cut + kWindow ? g1 - kWindow + 1 : g_cut;
       for (uint32_t n = 0; n < keys.loads; ++n) {
         keys.load(n);
-        keys.each_four(
-            [&](u32x4 v) {
-              count_values(s.count, v, cut);
-              if (NV > 4 || !ONE) keys.tokens(v, [&](uint32_t k) { counted += k >= cut ? 1u : 0u; });
-            },
-            [&] { if ((NV > 4 || !ONE) && portions) add_up(true); });
+        keys.each_four([&](u32x4 v) { count_values(s.count, v, g0 * kGroup, (g1 - g0 + 1) * kGroup); });
       }
-      if (!portions) add_up(false);
-      // sums of the groups above each; thread t has group kGroups - 1 - t
-      mine = {0u, 0ull};
-      if (threadIdx.x < kGroups) mine = {s.tokens[kGroups - 1 - threadIdx.x], s.mass[kGroups - 1 - threadIdx.x]};
-      above = before_thread(s.waves, mine, &all);
-      if constexpr (NV <= 4 && ONE) break;
-      Sums sum;
-      before_thread(s.waves, {counted, 0ull}, &sum);
-      if (portions || sum.count == all.count) break;
-      portions = true;
       __syncthreads();
-      for (uint32_t i = threadIdx.x; i < 32768; i += kThreads) s.count[i] = 0;
-      if (threadIdx.x < kGroups) {
-        s.mass[threadIdx.x] = 0;
-        s.tokens[threadIdx.x] = 0;
+      // a wavefront takes 128 values at a time, the next one the next
+#pragma unroll 1
+      for (uint32_t g = g0 + wave; g <= g1; g += 4 * (kThreads / 64)) {
+        uint2 c[4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+          c[i] = g + i * (kThreads / 64) <= g1 ? ((const uint2*)s.count)[(g + i * (kThreads / 64) - g0) * 64 + lane] : uint2{0u, 0u};
+#pragma unroll 1
+        for (uint32_t i = 0; i < 4; ++i) {
+          const uint2 now = c[0];
+          c[0] = c[1];
+          c[1] = c[2];
+          c[2] = c[3];
+          if (__ballot((now.x | now.y) != 0) == 0) continue;
+          const uint32_t of = g + i * (kThreads / 64), k = of * kGroup + 2 * lane;
+          Sums t = {now.x + now.y, 0ull};
+          if (t.count) t.mass = now.x * weight_of(k) + now.y * weight_of(k + 1);
+          t = up_to_lane(t);
+          if (lane == 63) {
+            s.tokens[of] = t.count;
+            s.mass[of] = t.mass;
+          }
+        }
       }
+      __syncthreads();
+      if (g0 == g_cut) break;
+      one_window = false;
+      g1 = g0 - 1;
+      clear();
       __syncthreads();
     }
+    // sums of the groups above each; thread t has group kGroups - 1 - t
+    Sums mine = {0u, 0ull}, all;
+    if (threadIdx.x < kGroups) mine = {s.tokens[kGroups - 1 - threadIdx.x], s.mass[kGroups - 1 - threadIdx.x]};
+    const Sums above = before_thread(s.waves, mine, &all);
     if (threadIdx.x < kGroups) s.mass[kGroups - 1 - threadIdx.x] = above.mass;
     if (threadIdx.x == 0) s.kept = s.of_k = all.mass;   // the weight that is kept, of the first so many; what top-k leaves
 
@@ -608,13 +588,13 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
           s.above = above;
         }
       }
-      if (portions && threadIdx.x < kGroup) s.one[threadIdx.x] = 0;
+      if (!one_window && threadIdx.x < kGroup) s.one[threadIdx.x] = 0;
       __syncthreads();
       const uint32_t g = s.found[0];
-      if (portions) {   // the group's counts once more
+      if (!one_window) {   // the group's counts once more
         for (uint32_t j0 = 0; j0 < keys.N; j0 += kThreads) {
           const uint32_t j = j0 + threadIdx.x, k = j < keys.N ? keys.key_at(j) : 0u;
-          if (k / kGroup != g || k < cut) continue;
+          if (k / kGroup != g) continue;
           const u64 here = __ballot(1);
           const bool same = __ballot(k == __builtin_amdgcn_readfirstlane(k)) == here;
           if (!same || lane == __builtin_ctzll(here)) atomicAdd(&s.one[k % kGroup], same ? (uint32_t)__popcll(here) : 1u);
@@ -622,8 +602,9 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
         __syncthreads();
       }
       if (threadIdx.x < 64) {   // from the largest value down, two a lane
-        const uint32_t i = kGroup - 1 - 2 * lane, k = g * kGroup + i, c = s.count[k >> 1];
-        const uint32_t n1 = portions ? s.one[i] : c >> 16, n0 = portions ? s.one[i - 1] : c & 0xFFFFu;
+        const uint32_t i = kGroup - 1 - 2 * lane, k = g * kGroup + i;
+        const uint32_t* counts = one_window ? s.count + (g - g0) * kGroup : s.one;
+        const uint32_t n1 = counts[i], n0 = counts[i - 1];
         const u64 m1 = n1 ? weight_of(k) : 0ull, m0 = n0 ? weight_of(k - 1) : 0ull;
         const Sums hi = {n1, n1 * m1}, both = {n1 + n0, n1 * m1 + n0 * m0}, run = up_to_lane(both);
         Sums b = {s.above.count + run.count - both.count, s.above.mass + run.mass - both.mass};
@@ -779,24 +760,22 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
         for (uint32_t j = threadIdx.x; row_listed && j < s.in_row; j += kThreads) token(s.row[j]);
         for (uint32_t n = 0; !row_listed && n < keys.loads; ++n) {
           keys.load(n);
-          keys.each_four(
-              [&](u32x4 v) {
-                // where a wavefront's logits are all equal, one lane adds them
-                bool same = true;
+          keys.each_four([&](u32x4 v) {
+            // where a wavefront's logits are all equal, one lane adds them
+            bool same = true;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) same = same && __ballot(v[e] == __builtin_amdgcn_readfirstlane(v[0])) == ~0ull;
-                if (same) {
-                  const Weigher::Parts t = w.sixtyfourths(Key<F32>::value(v[0]));
-                  const uint32_t b = bin_at(t);
-                  if (v[0] >= least && b < kBins && lane == 0) {
-                    if (by_count) atomicAdd(&s.count[b], 256u);
-                    else atomicAdd(&s.mass[b], w.weight(t) * 256);
-                  }
-                } else {
-                  keys.tokens(v, token);
-                }
-              },
-              [] {});
+            for (int e = 0; e < 4; ++e) same = same && __ballot(v[e] == __builtin_amdgcn_readfirstlane(v[0])) == ~0ull;
+            if (same) {
+              const Weigher::Parts t = w.sixtyfourths(Key<F32>::value(v[0]));
+              const uint32_t b = bin_at(t);
+              if (v[0] >= least && b < kBins && lane == 0) {
+                if (by_count) atomicAdd(&s.count[b], 256u);
+                else atomicAdd(&s.mass[b], w.weight(t) * 256);
+              }
+            } else {
+              keys.tokens(v, token);
+            }
+          });
         }
         __syncthreads();
         Sums bins[kBinsEach], mine = {0u, 0ull};
