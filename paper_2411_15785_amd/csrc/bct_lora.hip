@@ -35,11 +35,18 @@ LoraPlan lora_plan(uint32_t rows, uint32_t K, uint32_t width) {
   const uint32_t tiles = width / 16;
   p.chunks = (tiles + 3) / 4;
   p.each = (tiles + p.chunks - 1) / p.chunks;
-  p.row_tiles = rows >= 1024 ? 4 : rows >= 256 ? 2 : 1;
-  // as many parts as give the chip two workgroups a compute unit, each wavefront at least two steps of 32 inputs
-  const uint64_t groups = (uint64_t)tiles_of(rows, 16 * p.row_tiles) * p.chunks;
+  // Row tiles of a workgroup: more of them read A fewer times where rows share an adapter, and multiply each adapter with more rows
+  // of others where they do not, which the host cannot see.  us of the whole first half, 1 | 2 | 4 row tiles, rows in runs of 512: 1024
+  // rows, K = 4096, rank 16 5.0 | 5.4 | 5.8, rank 64 9.0 | 9.8 | 10.6; 4096 rows 9.2 | 8.2 | 10.0, 18.0 | 16.4 | 19.6, K = 11008, rank 64
+  // 29.6 | 26.1 | 27.8; 16384 28 | 27 | 29, 56 | 50 | 48, 143 | 106 | 93; a whole call, 3587 rows of 6 adapters from memory 302 | - | 289.
+  // An adapter for each row: 1024 rows 15.9 | 20.6 | 44.4, 4096 45.9 | 53.5 | 105.
+  p.row_tiles = rows < 2048 ? 1 : p.each < 3 ? 2 : 4;
+  // As many parts as give the chip one or two workgroups a compute unit, each wavefront at least two steps of 32 inputs.  us, one
+  // | two: 1024 rows, 1 row tile, runs of 512 5.0 | 5.4, rank 64 9.0 | 10.0, an adapter for each row 14.5 | 15.9, 37 | 50; the call
+  // of 3587 rows, 4 row tiles, 298 | 290.
+  const uint64_t groups = (uint64_t)tiles_of(rows, 16 * p.row_tiles) * p.chunks, most = p.row_tiles == 1 ? 256 : 512;
   p.parts = 1;
-  while (p.parts < 8 && groups * p.parts * 2 <= 512 && K / 32 >= 16 * p.parts) p.parts *= 2;
+  while (p.parts < 8 && groups * p.parts * 2 <= most && K / 32 >= 16 * p.parts) p.parts *= 2;
   return p;
 }
 
@@ -219,6 +226,9 @@ template <bool XT, int RT, bool OP>
 static void launch_inputs(const bctm_lora& l, const void* x, void* t, uint32_t rows, uint32_t K, uint32_t width, const LoraPlan& p,
                           hipStream_t s) {
   const uint32_t groups = tiles_of(rows, 16 * RT), most = l.n_adapters < 16 * RT ? l.n_adapters : 16 * RT;
+  // how many workgroups share the adapters of a row tile: us, all in one | up to 256 | 1024 | 4096 workgroups in all: 32 rows of 32
+  // adapters, K = 4096, rank 16 13.1 | 5.0 | 5.0 | 5.0, rank 64 43.6 | 13.0 | 13.0 | 13.0; 100 rows 13.9 | 7.0 | 7.1 | 7.0, 44 | 20 | 18.6 | 18.7; one
+  // adapter a tile, 4096 rows 10.0 | 10.0 | 9.9 | 14.9
   uint32_t slots = 1;
   while (slots < most && rows > 1 && (uint64_t)groups * p.chunks * p.parts * slots * 2 <= 1024) slots *= 2;
   const uint64_t work = (uint64_t)groups * p.chunks * slots, per = 8 / p.parts;   // of one part
