@@ -118,7 +118,7 @@ bct_status bctm_swiglu(const void* x, const void* w_gate_packed, const void* w_u
  *   rank    a multiple of 16, at most 256; adapters of fewer ranks are filled up with zeros
  * workspace: 16-byte aligned, at least bctm_lora_workspace bytes, holds nothing between calls; it must not be in use by a call
  * on another stream.  All but the struct is device memory.  x A^T is summed in fp32 and enters the second product with 16 bits.
- * A NaN or an infinity in one adapter reaches the rows of that adapter alone. */
+ * A NaN or an infinity in one adapter reaches the rows of that adapter alone; an infinite weight of b may come out as a NaN. */
 typedef struct {
   const void* a;
   const void* b;
@@ -130,7 +130,7 @@ typedef struct {
   size_t workspace_bytes;
 } bctm_lora;
 
-/* Bytes of workspace a call of these sizes needs (host call, no GPU needed). */
+/* Bytes of workspace a call of these sizes, or of fewer rows, needs (host call, no GPU needed). */
 bct_status bctm_lora_workspace(uint32_t rows, uint32_t K, uint32_t rank, uint32_t segments, size_t* bytes);
 
 /* Repacks row-major b [N][rank] into 16-byte chunks of 8 ranks of one feature, chunk (n / 16 * rank / 8 + k / 8) * 16 + n % 16.

@@ -13,6 +13,8 @@
 // workgroups, and so is K, in parts that the second half (a decode batch) or a small kernel (many rows) adds up.
 #include "bct_lora.h"
 
+#include <algorithm>
+
 #include "bct_device.h"
 #include "bct_model_internal.h"
 
@@ -27,6 +29,7 @@ struct LoraPlan {
   uint32_t parts;         // of K
   uint32_t chunks, each;  // the columns of t: so many workgroups, each so many tiles of 16
 };
+constexpr uint32_t kGroupsFew = 256, kGroupsMany = 512, kMostParts = 8, kMostRowTiles = 4;
 
 uint32_t tiles_of(uint32_t rows, uint32_t each) { return rows / each + (rows % each != 0); }
 
@@ -44,9 +47,9 @@ LoraPlan lora_plan(uint32_t rows, uint32_t K, uint32_t width) {
   // As many parts as give the chip one or two workgroups a compute unit, each wavefront at least two steps of 32 inputs.  us, one
   // | two: 1024 rows, 1 row tile, runs of 512 5.0 | 5.4, rank 64 9.0 | 10.0, an adapter for each row 14.5 | 15.9, 37 | 50; the call
   // of 3587 rows, 4 row tiles, 298 | 290.
-  const uint64_t groups = (uint64_t)tiles_of(rows, 16 * p.row_tiles) * p.chunks, most = p.row_tiles == 1 ? 256 : 512;
+  const uint64_t groups = (uint64_t)tiles_of(rows, 16 * p.row_tiles) * p.chunks, most = p.row_tiles == 1 ? kGroupsFew : kGroupsMany;
   p.parts = 1;
-  while (p.parts < 8 && groups * p.parts * 2 <= most && K / 32 >= 16 * p.parts) p.parts *= 2;
+  while (p.parts < kMostParts && groups * p.parts * 2 <= most && K / 32 >= 16 * p.parts) p.parts *= 2;
   return p;
 }
 
@@ -57,7 +60,8 @@ __device__ __forceinline__ void store_operand(u32x4* op, size_t number, uint32_t
   for (int e = 0; e < 4; ++e) {
     const uint32_t r = pack_bf16x2(t[2 * e], t[2 * e + 1]);
     hi[e] = r;
-    lo[e] = pack_bf16x2(t[2 * e] - __uint_as_float(r << 16), t[2 * e + 1] - __uint_as_float(r & 0xFFFF0000u));
+    const float h0 = __uint_as_float(r << 16), h1 = __uint_as_float(r & 0xFFFF0000u);
+    lo[e] = pack_bf16x2(fabsf(h0) < INFINITY ? t[2 * e] - h0 : 0.f, fabsf(h1) < INFINITY ? t[2 * e + 1] - h1 : 0.f);   // inf - inf
   }
   op[number * 64 + 16 * half + row] = hi;
   op[number * 64 + 16 * (2 + half) + row] = lo;
@@ -201,10 +205,12 @@ __global__ __launch_bounds__(256) void lora_pack_kernel(const uint16_t* __restri
   packed[c] = *(const u32x4*)(b + n * rank + c / 16 % (rank / 8) * 8);
 }
 
-// Room for the parts in fp32 and for the operands, which are whole tiles of 16 rows.
-size_t lora_bytes(uint32_t rows, uint32_t K, uint32_t width) {
-  const size_t one = (size_t)tiles_of(rows, 16) * 16 * width * sizeof(float);
-  return one * (lora_plan(rows, K, width).parts + 1);
+// Room for the parts in fp32 and for the operands, which are whole tiles of 16 rows: for any number of rows up to this one.  Where
+// K is in several parts, they and the workgroups are at most kGroupsMany.
+size_t lora_bytes(uint32_t rows, uint32_t width) {
+  const uint32_t tiles = tiles_of(rows, 16), split = kMostRowTiles * (kGroupsMany / ((width / 16 + 3) / 4));
+  const size_t parts = std::max<size_t>(tiles, std::min<size_t>((size_t)kMostParts * tiles, split));
+  return (tiles + parts) * 16 * width * sizeof(float);
 }
 
 }  // namespace
@@ -217,7 +223,7 @@ bct_status check_lora(const bctm_lora* l, uint32_t rows, uint32_t K, uint32_t N,
   if ((uint64_t)tiles_of(rows, 16) * lora_plan(rows, K, segments * l->rank).chunks > 0x0FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many rows");
   if ((uint64_t)l->n_adapters * l->rank > (1ull << 56) / ((uint64_t)N + (uint64_t)segments * K)) return mfail(BCT_ERR_UNSUPPORTED, "too many adapters");
   if (!al16(l->a) || !al16(l->b) || !al16(l->b_up) || !al16(l->workspace)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
-  if (!l->workspace || l->workspace_bytes < lora_bytes(rows, K, segments * l->rank))
+  if (!l->workspace || l->workspace_bytes < lora_bytes(rows, segments * l->rank))
     return mfail(BCT_ERR_BUFFER_TOO_SMALL, "adapters: the workspace is smaller than bctm_lora_workspace says");
   return BCT_OK;
 }
@@ -289,7 +295,7 @@ bct_status bctm_lora_workspace(uint32_t rows, uint32_t K, uint32_t rank, uint32_
   if (!bytes || rows == 0 || K == 0 || rank == 0 || segments == 0) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
   if (K % 32 != 0 || rank % 16 != 0 || rank > kMaxRank || segments > 3)
     return mfail(BCT_ERR_UNSUPPORTED, "K must be a multiple of 32, rank of 16 and at most 256, segments at most 3");
-  *bytes = lora_bytes(rows, K, segments * rank);
+  *bytes = lora_bytes(rows, segments * rank);
   return BCT_OK;
 }
 

@@ -592,7 +592,8 @@ class BctStack:
 
     def set_adapters(self, layers):
         """layers: per layer a dictionary of LoraWeights for any of "qkv" (three segments: q, wq, wv), "o", "gate_up" and "down";
-        forward(adapters=) then says which adapter a row has.  None: no adapters."""
+        forward(adapters=) then says which adapter a row has.  None: no adapters.  A graph that was captured before holds the
+        adapters of then: capture again."""
         if layers is not None:
             if len(layers) != self.shape.n_layers:
                 raise ValueError(f"adapters: expected {self.shape.n_layers} layers")
@@ -638,8 +639,8 @@ class BctStack:
         positions: int32 [B*T], where each token stands; needed with shape.rope_base, else None.
         adapters: int32 [B*T], each row's adapter of those set_adapters has been given (outside them: none); None: no row has one.
         sampling: a Sampling with one entry per row of logits, or None: the most likely token.
-        After the first call of a given (B, T, head) no memory is allocated, so a call can be captured in a
-        HIP graph."""
+        After the first call of a given (B, T, head), and the first one with adapters, no memory is allocated, so a call can be
+        captured in a HIP graph."""
         s = self.shape
         rows = s.batch * T
         if ids.numel() != rows:

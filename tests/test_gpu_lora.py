@@ -86,6 +86,8 @@ SHAPES = [
     # the matrix-core kernel's tiles: 64 x 64, 128 x 64 and 128 x 128 with K in two, 128 x 128, 128 x 256, 256 x 256, 128 x 512
     (128, 32, 128, 16, 2, 1), (130, 320, 256, 48, 60, 1), (257, 160, 400, 16, 9, 30), (320, 512, 4096, 32, 12, 11), (640, 160, 4096, 64, 3, 200),
     (1030, 96, 4224, 16, 300, 1), (1030, 160, 4096, 128, 5, 129), (1000, 64, 32768, 16, 4, 100), (557, 160, 23552, 32, 17, 7), (2050, 96, 512, 8, 3, 1000),
+    # four row tiles a workgroup in the first half, K whole and in parts
+    (2075, 4096, 64, 48, 9, 60), (2300, 64, 256, 64, 5, 1), (2049, 1088, 128, 100, 20, 7),
 ]
 
 
@@ -189,6 +191,34 @@ def test_an_adapter_reaches_its_own_rows_alone(M, rows, K, N):
         got = M.bctm_linear_lora(x, w, lora, ids, workspace=ws)
         keep = torch.arange(rows, device="cuda") != rows // 2
         assert same(got[keep], want[keep])
+
+
+@pytest.mark.parametrize("rows", [4, 160])
+def test_an_infinity_stays_one(M, rows):
+    """Positive throughout, and one entry of A infinite: so are its outputs, with one addend of t (few rows) or two."""
+    K, N, rank = 64, 128, 16
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    r = lambda *s: (torch.rand(s, generator=g, device="cuda") + 0.5).bfloat16()
+    x, w, a, b = r(rows, K), M.bctm_pack_weight(r(N, K)), r(2, rank, K), r(2, N, rank)
+    a[1, 3, 5] = float("inf")
+    ids = (torch.arange(rows, device="cuda") // 16 % 2).to(torch.int32)
+    ids[::7] = 1
+    out = M.bctm_linear_lora(x, w, M.bctm_lora_pack(a, b), ids).float()
+    assert bool((out[ids == 1] == float("inf")).all()) and bool(torch.isfinite(out[ids == 0]).all())
+
+
+@pytest.mark.parametrize("rows,K,rank", [(1, 4096, 16), (40, 4096, 16), (300, 2048, 64), (2047, 4096, 16), (2048, 4096, 64), (2100, 512, 240),
+                                         (4100, 2048, 33)])
+def test_the_workspace_is_not_left(M, rows, K, rank):
+    """What lies behind the workspace stays as it was, and one of more rows serves as well."""
+    c = Case(rows, K, 32, rank, 3)
+    (w,), lora = c.pack(M)
+    ids = adapters(rows, 3, rows, 5)
+    n = lora.workspace_bytes(rows)
+    ws = torch.full((n + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    out = M.bctm_linear_lora(c.x, w, lora, ids, workspace=ws[:n])
+    assert bool((ws[n:] == 0x5A).all())
+    assert same(out, M.bctm_linear_lora(c.x, w, lora, ids, workspace=torch.empty(lora.workspace_bytes(5000), dtype=torch.uint8, device="cuda")))
 
 
 def test_one_weight_at_a_time_selects_the_right_operands(M):

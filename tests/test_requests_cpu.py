@@ -114,3 +114,12 @@ def test_adapter_calls_refuse_what_the_projections_refuse(ML):
     assert ML.bctm_lora_pack(A, A, 32, 16, None) == P.BCT_ERR_INVALID_ARG
     assert ML.bctm_lora_pack(A, None, 32, 16, None) == P.BCT_ERR_INVALID_ARG
     assert ML.bctm_lora_pack(A, ctypes.c_void_p(0x2000008), 32, 16, None) == P.BCT_ERR_MISALIGNED
+
+
+@pytest.mark.parametrize("K,rank,segments", [(4096, 16, 1), (11008, 64, 3), (64, 256, 2), (2048, 48, 2)])
+def test_workspace_serves_fewer_rows(ML, K, rank, segments):
+    size, before = ctypes.c_size_t(0), 0
+    for rows in sorted({r + d for e in range(18) for r in (1 << e, 3 << e) for d in (-1, 0, 1) if r + d > 0}):
+        assert ML.bctm_lora_workspace(rows, K, rank, segments, ctypes.byref(size)) == 0
+        assert size.value >= before, rows
+        before = size.value
