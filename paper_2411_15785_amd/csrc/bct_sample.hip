@@ -29,7 +29,7 @@ namespace {
 constexpr uint32_t kThreads = 1024;
 constexpr uint32_t kSub = 1024;      // bins of keys, and blocks of indexes: one a thread
 constexpr uint32_t kGroup = 128, kGroups = 65536 / kGroup, kWindow = 288;   // bf16 values of a group; groups counted at a time
-constexpr uint32_t kList = 4096, kFew = 128;
+constexpr uint32_t kList = 4096, kFew = kThreads / 8;
 constexpr uint32_t kMaxVocab = 1u << 22;
 
 typedef unsigned long long u64;
@@ -150,6 +150,14 @@ __device__ __forceinline__ V up_to_lane(V run) {
 template <int LANES = 64>
 __device__ __forceinline__ Sums up_to_lane(Sums run) {
   return {up_to_lane<LANES>(run.count), up_to_lane<LANES>(run.mass)};
+}
+// The sum over eight lanes side by side: with lane ^ 1 and lane ^ 2 of its quad, then with the lane mirrored in the eight.
+template <typename V>
+__device__ __forceinline__ V of_eight(V v) {
+  v += other_lane<0xB1>(v);
+  v += other_lane<0x4E>(v);
+  v += other_lane<0x141>(v);
+  return v;
 }
 __device__ __forceinline__ u64 lane_of(u64 v, int lane) {
   return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
@@ -850,7 +858,12 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
       for (uint32_t j = threadIdx.x; row_listed && j < s.in_row; j += kThreads) take(s.row[j]);
       for (uint32_t n = 0; !row_listed && n < keys.loads; ++n) {
         keys.load(n);
-        keys.each([&](u32x4 v, uint32_t) { keys.tokens(v, take); });
+        keys.each([&](u32x4 v, uint32_t) {
+          bool any = false;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) any |= v[e] - lo <= hi - lo;
+          if (any) keys.tokens(v, take);
+        });
       }
       __syncthreads();
       if (stage == kMinP) {
@@ -863,27 +876,31 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
       Sums before = {s.count[bin], s.mass[bin]};
       uint32_t equal;
       const uint32_t few = s.listed;
-      if (few <= kFew) {   // each key against every other
-        const uint32_t k = threadIdx.x < few ? s.list[threadIdx.x] : 0u;
-        if (threadIdx.x < few) s.sub_mass[threadIdx.x] = by_count ? 1 : k >= least ? weight_of(k) : 0;
-        __syncthreads();
+      if (few <= kFew) {   // each key against every other, eight threads to a key
         if (threadIdx.x < few) {
-          u64 above = 0;
-          uint32_t count = 0, same = 0;
-          for (uint32_t j = 0; j < few; ++j) {
-            const uint32_t other = s.list[j];
-            const u64 m = s.sub_mass[j];
-            above += other > k ? m : 0;
-            count += other > k ? 1u : 0u;
-            same += other == k ? 1u : 0u;
-          }
-          const u64 from = (by_count ? (u64)before.count : before.mass) + above;
-          if (from < threshold && threshold <= from + same * s.sub_mass[threadIdx.x]) {   // those with one key write the same
-            s.range[0] = k;
-            s.sub_count[0] = count;
-            s.sub_count[1] = same;
-            s.above = above;
-          }
+          const uint32_t k = s.list[threadIdx.x];
+          s.sub_mass[threadIdx.x] = by_count ? 1 : k >= least ? weight_of(k) : 0;
+        }
+        __syncthreads();
+        const uint32_t i = min(threadIdx.x / 8, few - 1), k = s.list[i];
+        u64 above = 0;
+        uint32_t count = 0, same = 0;
+        for (uint32_t j = threadIdx.x % 8; j < few; j += 8) {
+          const uint32_t other = s.list[j];
+          const u64 m = s.sub_mass[j];
+          above += other > k ? m : 0;
+          count += other > k ? 1u : 0u;
+          same += other == k ? 1u : 0u;
+        }
+        above = of_eight(above);
+        count = of_eight(count);
+        same = of_eight(same);
+        const u64 from = (by_count ? (u64)before.count : before.mass) + above;
+        if (from < threshold && threshold <= from + same * s.sub_mass[i]) {   // those with one key write the same
+          s.range[0] = k;
+          s.sub_count[0] = count;
+          s.sub_count[1] = same;
+          s.above = above;
         }
         __syncthreads();
         hi = s.range[0];
