@@ -275,11 +275,14 @@ struct RowKeys {
         }
     }
   }
+  // whether any thread has an ith vector
+  __device__ __forceinline__ bool there(uint32_t i) const { return at * kLoad + i * kThreads < N / E; }
   // f(vector, index of its first token) for the vectors of a thread, and for the token left over, in a vector of its own
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) f(k[i], (at * kLoad + i * kThreads + threadIdx.x) * E);
+    for (int i = 0; i < NV; ++i)
+      if (E == 4 || i == 0 || there(i)) f(k[i], (at * kLoad + i * kThreads + threadIdx.x) * E);
     if (N % E != 0 && threadIdx.x < 64) f(u32x4{last, kNone, kNone, kNone}, N / E * E + threadIdx.x);
   }
   // The same for a long f: it stands there for four vectors, and they are moved past it.
@@ -287,8 +290,10 @@ struct RowKeys {
   __device__ __forceinline__ void each_four(F f) {
 #pragma unroll 1
     for (int n = 0; n < (NV + 3) / 4; ++n) {
+      if (n == 0 || there(4 * n)) {
 #pragma unroll
-      for (int i = 0; i < 4 && i < NV; ++i) f(k[i]);
+        for (int i = 0; i < 4 && i < NV; ++i) f(k[i]);
+      }
       if constexpr (NV > 4) {
         u32x4 first[4];
 #pragma unroll
