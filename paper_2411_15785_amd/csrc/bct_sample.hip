@@ -986,15 +986,17 @@ extern "C" bct_status bctm_sample(const void* logits, size_t ld, const float* te
   const SampleArgs a = {logits, ld, temperature, top_p, min_p, u, top_k, ids, prob, N, log2n <= 16 ? 46u : 62u - log2n};
   const uint32_t vectors = N / (uint32_t)(16 / size);   // of a row
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(rows), dim3(kThreads), 0, (hipStream_t)hip_stream, a); };
-  // one, four or sixteen vectors a thread hold the row; a longer one is read four vectors a thread at a time
+  // one, four, eight or sixteen vectors a thread hold the row; a longer one is read four vectors a thread at a time
   if (dtype == BCT_F32) {
     if (vectors <= kThreads) launch(sample_f32_kernel<1, true>);
     else if (vectors <= 4 * kThreads) launch(sample_f32_kernel<4, true>);
+    else if (vectors <= 8 * kThreads) launch(sample_f32_kernel<8, true>);
     else if (vectors <= 16 * kThreads) launch(sample_f32_kernel<16, true>);
     else launch(sample_f32_kernel<4, false>);
   } else {
     if (vectors <= kThreads) launch(sample_bf16_kernel<1, true>);
     else if (vectors <= 4 * kThreads) launch(sample_bf16_kernel<4, true>);
+    else if (vectors <= 8 * kThreads) launch(sample_bf16_kernel<8, true>);
     else if (vectors <= 16 * kThreads) launch(sample_bf16_kernel<16, true>);
     else launch(sample_bf16_kernel<4, false>);
   }
