@@ -292,7 +292,15 @@ struct RowKeys {
     for (int n = 0; n < (NV + 3) / 4; ++n) {
       if (n == 0 || there(4 * n)) {
 #pragma unroll
-        for (int i = 0; i < 4 && i < NV; ++i) f(k[i]);
+        for (int i = 0; i < 4 && i < NV; ++i) {
+          uint32_t now[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            now[e] = k[i][e];
+            asm volatile("" : "+v"(now[e]));   // what f makes of a key is not kept from one stage for the next: the registers are full
+          }
+          f(u32x4{now[0], now[1], now[2], now[3]});
+        }
       }
       if constexpr (NV > 4) {
         u32x4 first[4];
