@@ -285,32 +285,24 @@ struct RowKeys {
       if (E == 4 || i == 0 || there(i)) f(k[i], (at * kLoad + i * kThreads + threadIdx.x) * E);
     if (N % E != 0 && threadIdx.x < 64) f(u32x4{last, kNone, kNone, kNone}, N / E * E + threadIdx.x);
   }
-  // The same for a long f: it stands there for four vectors, and they are moved past it.
+  // The same for a long f: it stands there for four vectors, which are copied one four after the other.  What f makes of a key is
+  // not kept from one stage for the next, the registers are full without.
   template <typename F>
-  __device__ __forceinline__ void each_four(F f) {
+  __device__ __forceinline__ void each_four(F f) const {
 #pragma unroll 1
-    for (int n = 0; n < (NV + 3) / 4; ++n) {
-      if (n == 0 || there(4 * n)) {
+    for (uint32_t n = 0; n < NV && (n == 0 || there(n)); n += 4) {
+      uint32_t now[4][4];
 #pragma unroll
-        for (int i = 0; i < 4 && i < NV; ++i) {
-          uint32_t now[4];
+      for (int m = 0; m < NV; m += 4)
+        if (NV <= 4 || n == m) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            now[e] = k[i][e];
-            asm volatile("" : "+v"(now[e]));   // what f makes of a key is not kept from one stage for the next: the registers are full
+          for (int i = 0; i < 16 && i < 4 * NV; ++i) {
+            now[i / 4][i % 4] = k[m + i / 4][i % 4];
+            asm volatile("" : "+v"(now[i / 4][i % 4]));
           }
-          f(u32x4{now[0], now[1], now[2], now[3]});
         }
-      }
-      if constexpr (NV > 4) {
-        u32x4 first[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) first[i] = k[i];
-#pragma unroll
-        for (int i = 0; i + 4 < NV; ++i) k[i] = k[i + 4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) k[NV - 4 + i] = first[i];
-      }
+      for (int i = 0; i < 4 && i < NV; ++i) f(u32x4{now[i][0], now[i][1], now[i][2], now[i][3]});
     }
     if (N % E != 0 && threadIdx.x < 64) f(u32x4{last, kNone, kNone, kNone});
   }
