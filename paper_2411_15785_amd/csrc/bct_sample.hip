@@ -76,41 +76,44 @@ struct Key<BF16> {
   }
 };
 
-// A row's weights: 2^(t / 64) with t = 64 (l - max) log2(e) / T.
-constexpr uint32_t kPerOctave = 64;
+// A row's weights: 2^(-s / 64) with s = 64 log2(e) (max - l) / T.
+constexpr uint32_t kPerOctave = 64, kBins = kPerOctave * 47;   // 2^-47 and less is no weight
+// ALL: the table has 2^S times the weight of every whole s, else 2^(-i / 64) for i < 64.
+template <bool ALL>
 struct Weigher {
-  float top;   // the largest logit
+  double top;  // the largest logit; where that is infinite, far above every other
   double c;    // 64 log2(e) / T
   uint32_t S;
-  const double* table;   // 2^(i / 64), i < 64
-  // t's whole part, at least -64000, which is as good as no weight, and its rest; the largest logit (an infinity too) has 0
+  const double* table;
+  __device__ __forceinline__ Weigher(float largest, float T, uint32_t S_, const double* table_)
+      : top(largest < INFINITY ? (double)largest : 1e300), c(fmax(92.332482616893656877 / (double)T, 1e-290)), S(S_), table(table_) {}
+  // the whole number next to s, and what it is beyond s; an infinite logit, which is the largest, has 0
   struct Parts {
-    int i;
+    uint32_t b;
     double f;
   };
-  __device__ __forceinline__ Parts sixtyfourths(float l) const {
-    const double t = l == top ? 0.0 : fmax(((double)l - (double)top) * c, -64000.0), n = floor(t);
-    return {(int)n, t - n};
+  __device__ __forceinline__ Parts parts(float l) const {
+    const double s = fmin(fmax((top - (double)l) * c, 0.0), (double)kBins), n = rint(s);
+    return {(uint32_t)n, n - s};
   }
-  // 2^(t / 64 + S): the whole part from the table, the rest by its Taylor series up to degree 4, within 2e-12
+  // 2^(S - s / 64): the whole part from the table, the rest by its Taylor series up to degree 4, within 4e-14
   __device__ __forceinline__ double scaled(Parts t) const {
-    const int i = t.i;
     const double f = t.f;
     double p = 5.732851688640402e-10;
     p = __builtin_fma(p, f, 2.1173137155464774e-07);
     p = __builtin_fma(p, f, 5.864904955056169e-05);
     p = __builtin_fma(p, f, 0.010830424696249145);
     p = __builtin_fma(p, f, 1.0);
-    return ldexp(p * table[i & 63], (i >> 6) + (int)S);
+    return ALL ? p * table[t.b] : ldexp(p * table[t.b % kPerOctave], (int)S - (int)(t.b / kPerOctave));
   }
   // rounded to a whole number by adding 2^52, whose last place is 1 (S is at most 46)
   __device__ __forceinline__ u64 weight(Parts t) const {
     return (u64)__double_as_longlong(scaled(t) + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
   }
-  __device__ __forceinline__ u64 weight_of(float l) const { return weight(sixtyfourths(l)); }
+  __device__ __forceinline__ u64 weight_of(float l) const { return weight(parts(l)); }
 };
-__device__ __forceinline__ void fill_table(double* table) {   // a barrier follows
-  if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x / kPerOctave);
+__device__ __forceinline__ void fill_octave(double* table) {   // a barrier follows
+  if (threadIdx.x < kPerOctave) table[threadIdx.x] = exp2(-(double)threadIdx.x / kPerOctave);
 }
 
 struct Sums {
@@ -443,7 +446,7 @@ struct CountShared {
   u64 mass[kGroups];                  // of each group of values; then of the groups above each
   uint32_t tokens[kGroups];
   uint32_t one[kSub];                 // counts of one group's values; blocks of indexes
-  double table[kPerOctave];
+  double octave[kPerOctave];
   WaveSums waves;
   uint32_t found[2], from_p, nth, key;
   Sums above;                         // the groups above the one that is looked at
@@ -489,7 +492,7 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
     s.mass[threadIdx.x] = 0;
     s.tokens[threadIdx.x] = 0;
   }
-  fill_table(s.table);
+  fill_octave(s.octave);
   const Settings set = settings_of(a, r);
   const uint32_t top_key = keys.largest(s.waves.count);
   if (top_key <= Key<BF16>::kMinusInf) return write_none(a, r);
@@ -501,12 +504,12 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
       s.prob = 1.0f;
     }
   } else {
-    const Weigher w = {Key<BF16>::value(top_key), 92.332482616893656877 / (double)set.T, a.S, s.table};
+    const Weigher<false> w(Key<BF16>::value(top_key), set.T, a.S, s.octave);
     auto weight_of = [&](uint32_t k) -> u64 { return w.weight_of(Key<BF16>::value(k)); };
     const u64 one = 1ull << a.S;
     // values that are counted: those 47 octaves below the largest and less have no weight (the value there may be a step off)
     uint32_t cut = Key<BF16>::kMinusInf + 1;
-    const double end = (double)w.top - 47 * kPerOctave / w.c;
+    const double end = w.top - kBins / w.c;
     if (end > -3e38) cut = max(cut, (Key<BF16>::of(__float_as_uint((float)end) >> 16) & 0xFFFFu) - 2);
 
     if (threadIdx.x < 64 && set.min_p > 0.f && set.min_p <= 1.f) {   // the least value that has min_p
@@ -636,7 +639,7 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
           } else {
             s.key = second ? k - 1 : k;
             s.nth = (uint32_t)tokens_to(threshold, b.mass, m);
-            s.prob = (float)(w.scaled(w.sixtyfourths(Key<BF16>::value(s.key))) / (double)kept);
+            s.prob = (float)(w.scaled(w.parts(Key<BF16>::value(s.key))) / (double)kept);
           }
         }
       }
@@ -649,7 +652,7 @@ __global__ __launch_bounds__(kThreads) void sample_bf16_kernel(SampleArgs a) {
 
 // ---------------------------------------------------------------- fp32: weights over octaves
 
-constexpr uint32_t kBins = kPerOctave * 47, kBinsEach = (kBins + kThreads - 1) / kThreads;   // below 2^-47 there is no weight
+constexpr uint32_t kBinsEach = (kBins + kThreads - 1) / kThreads;
 struct OctaveShared {
   u64 mass[kBins + 1];        // of the bins before each; the last entry: of all
   uint32_t count[kBins + 1];
@@ -657,7 +660,7 @@ struct OctaveShared {
   uint32_t sub_count[kSub];
   uint32_t list[kList];       // the keys of one bin
   uint32_t row[kList];        // all keys that are weighed, where they are so few
-  double table[kPerOctave];
+  double octave[kPerOctave], table[kBins + 1];
   WaveSums waves;
   uint32_t found[2], range[2], listed, in_row, nth, key;
   u64 kept, above;
@@ -669,7 +672,7 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
   __shared__ OctaveShared s;
   const uint32_t r = blockIdx.x, lane = threadIdx.x % 64;
   RowKeys<F32, NV, ONE> keys((const float*)a.logits + (size_t)r * a.ld, a.N);
-  fill_table(s.table);
+  fill_octave(s.octave);
   const Settings set = settings_of(a, r);
   const uint32_t top_key = keys.largest(s.waves.count);
   if (top_key <= Key<F32>::kMinusInf) return write_none(a, r);
@@ -681,10 +684,9 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
       s.prob = 1.0f;
     }
   } else {
-    const Weigher w = {Key<F32>::value(top_key), 92.332482616893656877 / (double)set.T, a.S, s.table};
+    const Weigher<true> w(Key<F32>::value(top_key), set.T, a.S, s.table);
     auto weight_of = [&](uint32_t k) -> u64 { return w.weight_of(Key<F32>::value(k)); };
-    auto bin_at = [](Weigher::Parts t) -> uint32_t { return min((uint32_t)-t.i, kBins); };
-    auto bin_of = [&](uint32_t k) -> uint32_t { return bin_at(w.sixtyfourths(Key<F32>::value(k))); };
+    auto bin_of = [&](uint32_t k) -> uint32_t { return w.parts(Key<F32>::value(k)).b; };
     // The least key for which `is` holds, from some key on.  It lies next to the logit `near`, but for roundings: looked for
     // there, and among all keys where it is not.
     auto least_near = [&](double near, auto is) -> uint32_t {
@@ -694,12 +696,15 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
       return least_key(there ? lo : none, there ? hi : top_key, is);
     };
     auto least_of_bin = [&](uint32_t bin) -> uint32_t {   // of the bins up to this one
-      return least_near((double)w.top - (double)bin / w.c, [&](uint32_t k) { return bin_of(k) <= bin; });
+      return least_near(w.top - (bin + 0.5) / w.c, [&](uint32_t k) { return bin_of(k) <= bin; });
     };
+    for (uint32_t b = threadIdx.x; b <= kBins; b += kThreads)
+      s.table[b] = b < kBins ? ldexp(s.octave[b % kPerOctave], (int)a.S - (int)(b / kPerOctave)) : 0.0;
+    __syncthreads();
     const u64 one = 1ull << a.S;
     if (threadIdx.x < 64 && set.min_p > 0.f && set.min_p <= 1.f) {   // the least key that has min_p
       const u64 need = (u64)ceil((double)set.min_p * (double)one);
-      const uint32_t k = least_near((double)w.top + log2((double)set.min_p) * kPerOctave / w.c, [&](uint32_t k) { return weight_of(k) >= need; });
+      const uint32_t k = least_near(w.top + log2((double)set.min_p) * kPerOctave / w.c, [&](uint32_t k) { return weight_of(k) >= need; });
       if (lane == 0) s.range[0] = k;
     }
     __syncthreads();
@@ -763,12 +768,10 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
         }
         __syncthreads();
         auto token = [&](uint32_t k) {
-          if (k < least) return;
-          const Weigher::Parts t = w.sixtyfourths(Key<F32>::value(k));
-          const uint32_t b = bin_at(t);
-          if (b >= kBins) return;
-          if (by_count) atomicAdd(&s.count[b], 1u);
-          else atomicAdd(&s.mass[b], w.weight(t));
+          const auto t = w.parts(Key<F32>::value(k));
+          if (k < least || t.b >= kBins) return;
+          if (by_count) atomicAdd(&s.count[t.b], 1u);
+          else atomicAdd(&s.mass[t.b], w.weight(t));
         };
         for (uint32_t j = threadIdx.x; row_listed && j < s.in_row; j += kThreads) token(s.row[j]);
         for (uint32_t n = 0; !row_listed && n < keys.loads; ++n) {
@@ -779,11 +782,10 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) same = same && __ballot(v[e] == __builtin_amdgcn_readfirstlane(v[0])) == ~0ull;
             if (same) {
-              const Weigher::Parts t = w.sixtyfourths(Key<F32>::value(v[0]));
-              const uint32_t b = bin_at(t);
-              if (v[0] >= least && b < kBins && lane == 0) {
-                if (by_count) atomicAdd(&s.count[b], 256u);
-                else atomicAdd(&s.mass[b], w.weight(t) * 256);
+              const auto t = w.parts(Key<F32>::value(v[0]));
+              if (v[0] >= least && t.b < kBins && lane == 0) {
+                if (by_count) atomicAdd(&s.count[t.b], 256u);
+                else atomicAdd(&s.mass[t.b], w.weight(t) * 256);
               }
             } else {
               keys.tokens(v, token);
@@ -949,7 +951,7 @@ __global__ __launch_bounds__(kThreads) void sample_f32_kernel(SampleArgs a) {
         to_list = !row_listed && before.count + equal <= kList;
       } else {
         if (threadIdx.x == 0) {
-          const Weigher::Parts t = w.sixtyfourths(Key<F32>::value(hi));
+          const auto t = w.parts(Key<F32>::value(hi));
           const u64 m = w.weight(t), n = tokens_to(threshold, before.mass, m);
           s.kept = min(kept, before.mass + n * m);
           s.key = hi;
