@@ -73,12 +73,6 @@ struct AdapterWalk {
   }
 };
 
-// The adapter that all rows of 16 have (L.n: they have not), row0 the first of them.
-__device__ __forceinline__ uint32_t tile_adapter(const LoraTerm& L, uint32_t row0, uint32_t rows) {
-  const uint32_t id = adapter_of(L.adapter, row0 + threadIdx.x % 16, rows, L.n), first = __builtin_amdgcn_readfirstlane(id);
-  return __ballot(id == first) == ~0ull ? first : L.n;
-}
-
 // The wavefront's part of a term, operands and accumulators in the lane layout of v_mfma_f32_16x16x32_bf16: CT tiles of 16
 // features; MATS = 2: those of two matrices in turn (j % 2), each a column segment of t, else segment(j); tile(j): the feature
 // tile; N: all features.
@@ -102,14 +96,22 @@ struct LoraTiles {
 };
 
 // Adds the term of the row tiles (RT of 16 rows, from row0) whose rows all have one adapter to the accumulators acc(i, j).
-// share, of shares: the 16 ranks that are this wavefront's.
+// share, of shares: the 16 ranks that are this wavefront's.  -> bit i: row tile i is not one of those, nor one without adapters.
 template <int RT, int CT, int MATS, typename SEG, typename TILE, typename ACC>
-__device__ __forceinline__ void lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T, uint32_t row0, uint32_t rows, uint32_t share,
-                                         uint32_t shares, ACC acc) {
+__device__ __forceinline__ uint32_t lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T, uint32_t row0, uint32_t rows, uint32_t share,
+                                             uint32_t shares, ACC acc) {
   const uint32_t last = (rows - 1) / 16, n = T.L.n;
-  uint32_t cur[RT];
+  uint32_t id[RT], cur[RT], mixed = 0;
 #pragma unroll
-  for (int i = 0; i < RT; ++i) cur[i] = tile_adapter(T.L, row0 + 16 * i, rows);
+  for (int i = 0; i < RT; ++i) id[i] = adapter_of(T.L.adapter, row0 + 16 * i + threadIdx.x % 16, rows, n);
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    cur[i] = __builtin_amdgcn_readfirstlane(id[i]);
+    if (__ballot(id[i] == cur[i]) != ~0ull) {
+      cur[i] = n;
+      mixed |= 1u << i;
+    }
+  }
   for (uint32_t ks = share; ks < T.L.rank / 16; ks += shares) {
     constexpr int G = RT * MATS > 8 ? 8 / MATS : RT;   // row tiles whose operands are requested at once
     bf16x8 a[G][MATS], b[CT];
@@ -134,35 +136,48 @@ __device__ __forceinline__ void lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T
       }
     }
   }
+  return mixed;
 }
 
-// The term of a row tile (16 rows from row0) that has several adapters, or rows without one; zero for any other.  A product has all
+// The term of a row tile (16 rows from row0) that has several adapters, or rows without one, added to sum.  A product has all
 // 16 rows in it and each row takes that of its own adapter: selected, not multiplied by zero, so an infinity or a NaN in one
-// adapter's weights stays in its rows.
+// adapter's weights stays in its rows.  The next product's operands are requested before this one is made.
 template <int CT, int MATS, typename SEG, typename TILE>
 __device__ __forceinline__ void lora_mixed(const LoraTiles<CT, MATS, SEG, TILE>& T, uint32_t row0, uint32_t rows, f32x4 (&sum)[CT]) {
-  const uint32_t kg = threadIdx.x % 64 / 16;
-#pragma unroll
-  for (int j = 0; j < CT; ++j) sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t kg = threadIdx.x % 64 / 16, seg0 = MATS == 2 ? 0 : T.segment(0), seg1 = MATS == 2 ? 1 : T.segment(CT - 1);
   AdapterWalk<1> walk(T.L.adapter, row0, rows, T.L.n);
-  if (tile_adapter(T.L, row0, rows) < T.L.n) return;
-  const uint32_t seg0 = MATS == 2 ? 0 : T.segment(0), seg1 = MATS == 2 ? 1 : T.segment(CT - 1);
-  while (walk.next()) {
-    const uint32_t mine = (uint32_t)(walk.match[0] >> (4 * kg));   // bit v: row 4 kg + v
-    for (uint32_t ks = 0; ks < T.L.rank / 16; ++ks) {
-      bf16x8 b[CT];
-      T.weights(walk.cur, ks, b);
-      for (uint32_t seg = seg0; seg <= seg1; ++seg) {
-        const bf16x8 a = T.operand(row0 / 16, seg, ks);
+  bool more = walk.next();
+  if (!more) return;
+  uint32_t ks = 0;
+  bf16x8 a[MATS], b[CT];
+  T.weights(walk.cur, ks, b);
 #pragma unroll
-        for (int j = 0; j < CT; ++j) {
-          const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[j], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-          const uint32_t take = (MATS == 2 ? (uint32_t)(j % 2) : T.segment(j)) == seg ? mine : 0u;
+  for (int m = 0; m < MATS; ++m) a[m] = T.operand(row0 / 16, seg0 + m, ks);
+  while (more) {
+    const uint32_t mine = (uint32_t)(walk.match[0] >> (4 * kg)), now = ks;   // bit v: row 4 kg + v
+    if (++ks == T.L.rank / 16) {
+      ks = 0;
+      more = walk.next();   // no more: the last one's first operands once again
+    }
+    bf16x8 next_a[MATS], next_b[CT];
+    T.weights(walk.cur, ks, next_b);
 #pragma unroll
-          for (int v = 0; v < 4; ++v) sum[j][v] = (take >> v & 1) ? sum[j][v] + d[v] : sum[j][v];
-        }
+    for (int m = 0; m < MATS; ++m) next_a[m] = T.operand(row0 / 16, seg0 + m, ks);
+    for (uint32_t seg = seg0; seg <= seg1; ++seg) {
+      // where the border between two outputs lies within the tiles
+      const bf16x8 at = MATS == 1 && seg > seg0 ? T.operand(row0 / 16, seg, now) : MATS == 2 && seg > seg0 ? a[MATS - 1] : a[0];
+#pragma unroll
+      for (int j = 0; j < CT; ++j) {
+        const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(at, b[j], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+        const uint32_t take = (MATS == 2 ? (uint32_t)(j % 2) : T.segment(j)) == seg ? mine : 0u;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) sum[j][v] = (take >> v & 1) ? sum[j][v] + d[v] : sum[j][v];
       }
     }
+#pragma unroll
+    for (int m = 0; m < MATS; ++m) a[m] = next_a[m];
+#pragma unroll
+    for (int j = 0; j < CT; ++j) b[j] = next_b[j];
   }
 }
 

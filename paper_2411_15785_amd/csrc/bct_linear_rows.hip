@@ -206,8 +206,9 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   request(Int<2>{}, 2, Int<PAIR ? NA : 0>{}, Int<ND>{});
   __builtin_amdgcn_sched_barrier(0);
   // The low-rank term first, while the stages fill: what it loads is waited for together with them.
+  [[maybe_unused]] uint32_t mixed_tiles = 0;
   if constexpr (sizeof...(LORA) > 0)
-    lora_add<MI>(lora_tiles(lora...), r0 + wr * (16 * MI), rows, grp, KS, [&](int i, int j) -> f32x4& { return acc[i][j]; });
+    mixed_tiles = lora_add<MI>(lora_tiles(lora...), r0 + wr * (16 * MI), rows, grp, KS, [&](int i, int j) -> f32x4& { return acc[i][j]; });
   __builtin_amdgcn_s_waitcnt(wait_vm((S - 2) * (PAIR ? NB : ND)));
   bare_barrier();
   const bool second = PING && wv >= 4;   // the wavefront of a SIMD that is half a step behind
@@ -274,7 +275,11 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
 #pragma unroll
   for (int i = 0; i < MO; ++i) {
     f32x4 mixed[NJ];
-    if constexpr (sizeof...(LORA) > 0) lora_mixed(lora_tiles(lora...), r0 + wr * (16 * MI) + (grp * MO + i) * 16, rows, mixed);
+    if constexpr (sizeof...(LORA) > 0) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) mixed[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (mixed_tiles >> (grp * MO + i) & 1) lora_mixed(lora_tiles(lora...), r0 + wr * (16 * MI) + (grp * MO + i) * 16, rows, mixed);
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll

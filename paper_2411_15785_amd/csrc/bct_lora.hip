@@ -50,6 +50,9 @@ LoraPlan lora_plan(uint32_t rows, uint32_t K, uint32_t width) {
   const uint64_t groups = (uint64_t)tiles_of(rows, 16 * p.row_tiles) * p.chunks, most = p.row_tiles == 1 ? kGroupsFew : kGroupsMany;
   p.parts = 1;
   while (p.parts < kMostParts && groups * p.parts * 2 <= most && K / 32 >= 16 * p.parts) p.parts *= 2;
+  // Two parts of a short K do not make up for the kernel that adds them (many rows only): us of a call with two | one, K = 512 19.2 |
+  // 17.1, 736 12.3 | 10.9, 960 61.4 | 59.0, 1184 19.6 | 18.5, 2016 116 | 116, 5184 41.6 | 43.3.
+  if (p.parts == 2 && K < 2048 && rows >= 128) p.parts = 1;
   return p;
 }
 
