@@ -61,11 +61,16 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const uint16_t* __restri
 // The low-rank term of the outputs that a thread of the streaming kernel writes: output o = threadIdx + q * NTHR of feature tile
 // f, row o / 16 and feature o % 16.  A decode batch has an adapter for nearly every row, so a matrix product would compute 16
 // rows for one; a thread takes the dot product of its own row's t with its own feature's row of B instead, rank fp32 products.
-// t comes through LDS, 32 ranks at a time, where its parts are added up once for the workgroup.
+// t comes through LDS, 32 ranks at a time, where its parts are added up once for the workgroup.  What a round of 32 ranks needs from
+// memory is requested at once, B too with one feature tile; with two or three that takes registers of the main loop.  us, requested in
+// turn | at once | B tile by tile: SwiGLU of 74 rows, K = 704, N = 2112, rank 64 28.2 | 19.7 | -, 32 x 4096 x 12288 in three outputs, rank 16
+// 28.3 | 29.1 | 27.5.
 template <bool SWIGLU, int FT, int ROWS, int NTHR, int OPT>
 __device__ __forceinline__ void lora_outputs(const LoraTerm& L, const LinearOut& dst, uint32_t r0, uint32_t nt0, uint32_t rows,
                                              float (&delta)[FT][SWIGLU ? 2 : 1][OPT]) {
   constexpr int NW2 = SWIGLU ? 2 : 1, RC = 32;
+  constexpr bool EARLY = FT == 1;
+  static_assert(ROWS * RC / 4 <= NTHR, "a thread stages four ranks of a row");
   __shared__ __attribute__((aligned(16))) float sT[ROWS][RC + 4];
   const uint32_t N = dst.start[3];
   auto segment_of = [&](int f) -> uint32_t {
@@ -84,44 +89,73 @@ __device__ __forceinline__ void lora_outputs(const LoraTerm& L, const LinearOut&
   const uint32_t seg0 = SWIGLU ? 0 : segment_of(0), seg1 = SWIGLU ? 1 : segment_of(FT - 1);
   for (uint32_t seg = seg0; seg <= seg1; ++seg)
     for (uint32_t c0 = 0; c0 < L.rank; c0 += RC) {
-      const uint32_t cn = min(L.rank - c0, (uint32_t)RC);   // 16 or 32
-      __syncthreads();                                      // what the last round read
-      for (uint32_t e = threadIdx.x; e < ROWS * cn; e += NTHR) {
-        const uint32_t i = e / cn, k = e % cn;
-        if (adapter_of(L.adapter, r0 + i, rows, L.n) < L.n) {
-          const float* t = L.t + (size_t)(r0 + i) * L.width + seg * L.rank + c0 + k;
-          const size_t part = (size_t)rows * L.width;
-          float sum = 0.f;
-          for (uint32_t p = 0; p < L.parts; p += 4) {   // 1, 2, 4 or 8 parts; four requests at once
-            float v[4];
+      const bool both = L.rank - c0 > 16;   // 32 ranks, or the last 16
+      const uint32_t per = both ? 8 : 4, i = threadIdx.x / per, k = threadIdx.x % per * 4;
+      f32x4 v[8];
+      if (i < ROWS) {   // 1, 2, 4 or 8 parts; those of a row without an adapter hold anything, and are not used
+        const f32x4* t = (const f32x4*)(L.t + (size_t)min(r0 + i, rows - 1) * L.width + seg * L.rank + c0 + k);
+        const size_t part = (size_t)rows * L.width / 4;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = t[min(p + u, L.parts - 1) * part];
+        for (uint32_t u = 0; u < 4; ++u) v[u] = t[min(u, L.parts - 1) * part];
+        if (L.parts > 4) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) sum += p + u < L.parts ? v[u] : 0.f;
-          }
-          sT[i][k] = sum;
+          for (uint32_t u = 4; u < 8; ++u) v[u] = t[u * part];
         }
+      }
+      // 16 bytes are eight ranks of the thread's feature; an output without an adapter reads those of one that is there
+      u32x4 w[EARLY ? FT : 1][OPT][4];
+      auto request = [&](int f) {
+#pragma unroll
+        for (int q = 0; q < OPT; ++q) {
+          const uint32_t j = (threadIdx.x + q * NTHR) % 16;
+          const u32x4* b = (SWIGLU && seg ? L.b2 : L.b) +
+                           (((size_t)(id[q] < L.n ? id[q] : 0) * (N / 16) + nt0 + f) * (L.rank / 8) + c0 / 8) * 16 + j;
+          u32x4(&to)[4] = w[EARLY ? f : 0][q];
+          to[0] = b[0];
+          to[1] = b[16];
+          if (both) {
+            to[2] = b[32];
+            to[3] = b[48];
+          }
+        }
+      };
+      if (EARLY) {
+#pragma unroll
+        for (int f = 0; f < FT; ++f)
+          if (SWIGLU || segment_of(f) == seg) request(f);
+      }
+      __syncthreads();   // what the last round read
+      if (i < ROWS) {
+        f32x4 sum = v[0];
+#pragma unroll
+        for (uint32_t u = 1; u < 4; ++u)
+          if (u < L.parts) sum += v[u];
+        if (L.parts > 4) {
+#pragma unroll
+          for (uint32_t u = 4; u < 8; ++u) sum += v[u];
+        }
+        *(f32x4*)&sT[i][k] = sum;
       }
       __syncthreads();
 #pragma unroll
       for (int f = 0; f < FT; ++f) {
         if (!SWIGLU && segment_of(f) != seg) continue;
+        if (!EARLY) request(f);
 #pragma unroll
         for (int q = 0; q < OPT; ++q) {
-          if (id[q] >= L.n) continue;
-          const uint32_t o = (threadIdx.x + q * NTHR) % (ROWS * 16), i = o / 16, j = o % 16;
-          const u32x4* b = (SWIGLU && seg ? L.b2 : L.b) + (((size_t)id[q] * (N / 16) + nt0 + f) * (L.rank / 8) + c0 / 8) * 16 + j;
+          const float* t = sT[(threadIdx.x + q * NTHR) % (ROWS * 16) / 16];
           float sum = 0.f;
-          for (uint32_t k = 0; k < cn; k += 16) {
-            float v[16];
-            unpack16<BF16>(b[k * 2], v);
-            unpack16<BF16>(b[k * 2 + 16], v + 8);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sum = __builtin_fmaf(v[e], sT[i][k + e], sum);
+          for (int h = 0; h < 4; ++h) {
+            if (h >= 2 && !both) break;
+            float x[8];
+            unpack16<BF16>(w[EARLY ? f : 0][q][h], x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], t[8 * h + e], sum);
           }
 #pragma unroll
           for (int m = 0; m < NW2; ++m)
-            if (!SWIGLU || m == (int)seg) delta[f][m][q] += sum;
+            if ((!SWIGLU || m == (int)seg) && id[q] < L.n) delta[f][m][q] += sum;
         }
       }
     }
