@@ -12,7 +12,7 @@
 // well and are not stored.  What fills the chip when rows are few: the adapters of a row tile are dealt out to several
 // workgroups, and so is K, in parts that the second half (a decode batch) or a small kernel (many rows) adds up.
 // 32 rows of 32 adapters, K = 4096, three segments of rank 16 (12.6 MB of A): 5.5 us; 3587 rows, K = 11008, rank 64 (79 MB of x): 29 us, and
-// 6 for the parts' sums.  Whole calls, without | with: three outputs of 4096 each 19.2 | 28, SwiGLU 2048 x 4096 x 11008 of rank 32 267 |
+// 6 for the parts' sums.  Whole calls, without | with: three outputs of 4096 each 19.2 | 27.5, SwiGLU 2048 x 4096 x 11008 of rank 32 267 |
 // 290, 3587 x 11008 x 4096 244 | 285.
 #include "bct_lora.h"
 
