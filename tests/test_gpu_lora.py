@@ -125,7 +125,9 @@ def test_linear(M, rows, K, N, rank, n, run):
 @pytest.mark.parametrize("rows,K,widths,rank,n,run", [
     (5, 64, (32, 16, 48), 16, 3, 1), (32, 4096, (4096, 4096, 4096), 16, 32, 1), (20, 96, (6144, 6144), 32, 4, 1),
     (300, 96, (112, 80, 64), 24, 6, 25), (640, 288, (4096, 1024, 1024), 16, 20, 31), (1030, 96, (4112, 96, 144), 64, 3, 100),
-    (557, 64, (11792, 256, 11504), 16, 9, 1), (1000, 64, (16400, 16368), 48, 2, 333)])
+    (557, 64, (11792, 256, 11504), 16, 9, 1), (1000, 64, (16400, 16368), 48, 2, 333),
+    # three outputs within 64 features
+    (300, 96, (48, 16, 64), 16, 5, 7), (1030, 64, (16, 32, 4048), 48, 6, 21), (40, 64, (16, 16, 16), 40, 3, 1), (2100, 96, (272, 16, 480), 32, 9, 45)])
 def test_split(M, rows, K, widths, rank, n, run):
     """Each output has an A of its own; borders between outputs inside and between the workgroups' tiles."""
     N = sum(widths)

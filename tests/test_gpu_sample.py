@@ -243,3 +243,15 @@ def test_one_value_of_many_tokens(M, N, dtype):
     u = np.array([0.9999, 0.5, 0.7, 0.99, 0.999, 0.6])
     check(M, x, u, what="plain")
     check(M, x, u, k=N // 3, p=0.9, m=1e-3, what="all settings")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [4095, 4096, 4097, 8192, 8200, 16383, 16384, 16391, 24577, 32767, 32768, 32769, 32776, 40001, 49152, 49153])
+def test_rows_that_fill_their_registers_or_do_not(M, N, dtype):
+    """Rows around the numbers of vectors a thread can hold: the last vector there, missing, or one token of it."""
+    rows = 6
+    x, u = logits(rows, N, dtype, N + 3), uniform(rows, N + 4)
+    x[:, -1] = x[:, 0]                       # a likely token at the end
+    check(M, x, u, t=0.9, what="temperature")
+    check(M, x, u, t=0.9, k=N // 2, p=0.97, m=1e-7, what="all")
+    check(M, x, np.full(rows, 0.99999994), t=3.0, what="the far end")
