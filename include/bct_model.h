@@ -56,16 +56,16 @@ bct_status bctm_rmsnorm(const void* x, const void* gain, void* out, uint32_t row
  *   (y_a, y_b) = (y_a cos t - y_b sin t, y_a sin t + y_b cos t)         t = positions[r] * inv_freq[j], j < rotary_dim / 2
  * a = j and b = j + rotary_dim / 2, or with BCTM_ROPE_INTERLEAVED a = 2 j and b = 2 j + 1; elements from rotary_dim on pass.
  * fp32 arithmetic (the angle in 64 bits, for any position of an int32), one rounding.
- * q: rows of n_q_heads heads side by side, q_ld elements from row to row, so heads are taken out of a wider row (q | wq | wv)
- * where they lie; k likewise, or NULL with n_kv_heads = 0.  An output may be its own input (same row distance); apart from
+ * q: rows of n_q_heads heads side by side, q_ld elements from row to row (any distance of 64 bits), so heads are taken out of a
+ * wider row (q | wq | wv) where they lie; k likewise, or NULL with n_kv_heads = 0.  An output may be its own input (same row distance); apart from
  * that no output shares memory with an input or the other output.  q_gain, k_gain [head_dim], NULL = ones.  positions int32
  * [rows], inv_freq float64 [rotary_dim / 2] in radians per position, both NULL with rotary_dim = 0.  All device memory.
  * head_dim and rotary_dim multiples of 16, at most 256; dtype: BCT_F32 or BCT_BF16, that of q, k, the gains and the outputs. */
 #define BCTM_HEAD_NORM 4u
 #define BCTM_ROPE_INTERLEAVED 8u
-bct_status bctm_qk_norm_rope(const void* q, void* q_out, const void* q_gain, uint32_t n_q_heads, uint32_t q_ld,
-                             uint32_t q_out_ld, const void* k, void* k_out, const void* k_gain, uint32_t n_kv_heads,
-                             uint32_t k_ld, uint32_t k_out_ld, const int32_t* positions, const double* inv_freq,
+bct_status bctm_qk_norm_rope(const void* q, void* q_out, const void* q_gain, uint32_t n_q_heads, size_t q_ld,
+                             size_t q_out_ld, const void* k, void* k_out, const void* k_gain, uint32_t n_kv_heads,
+                             size_t k_ld, size_t k_out_ld, const int32_t* positions, const double* inv_freq,
                              uint32_t rotary_dim, uint32_t rows, uint32_t head_dim, float eps, int32_t dtype,
                              uint32_t flags, void* hip_stream);
 

@@ -22,7 +22,8 @@ struct HeadBlock {   // the heads of one input: rows of n heads side by side, ld
   const void* in;
   void* out;
   const void* gain;   // [d], or NULL for ones
-  uint32_t n, ld, out_ld;
+  size_t ld, out_ld;
+  uint32_t n;
 };
 
 enum RopePairs { kNoRotation, kHalves, kNeighbours };
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(HeadBlock q, HeadBloc
   for (int i = 0; i < HPG; ++i) {
     const uint32_t h = slot + i * slots;
     if (mine && h < q.n + k.n) {
-      const elem* p = h < q.n ? (const elem*)q.in + (size_t)row * q.ld + (size_t)h * d : (const elem*)k.in + (size_t)row * k.ld + (size_t)(h - q.n) * d;
+      const elem* p = h < q.n ? (const elem*)q.in + row * q.ld + (size_t)h * d : (const elem*)k.in + row * k.ld + (size_t)(h - q.n) * d;
       v[i][0] = PAST ? __builtin_nontemporal_load((const u32x4*)(p + e0)) : *(const u32x4*)(p + e0);
       v[i][1] = PAST ? __builtin_nontemporal_load((const u32x4*)(p + e1)) : *(const u32x4*)(p + e1);
     } else {
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(HeadBlock q, HeadBloc
       }
     }
     if (mine && h < q.n + k.n) {
-      elem* o = h < q.n ? (elem*)q.out + (size_t)row * q.out_ld + (size_t)h * d : (elem*)k.out + (size_t)row * k.out_ld + (size_t)(h - q.n) * d;
+      elem* o = h < q.n ? (elem*)q.out + row * q.out_ld + (size_t)h * d : (elem*)k.out + row * k.out_ld + (size_t)(h - q.n) * d;
       const u32x4 o0 = pack16_round<DT>(f), o1 = pack16_round<DT>(f + E);
       if (PAST) {
         __builtin_nontemporal_store(o0, (u32x4*)(o + e0));
@@ -207,9 +208,9 @@ bool rows_overlap(const void* a, uint64_t wide_a, uint64_t lda, const void* b, u
 
 using namespace bct;
 
-extern "C" bct_status bctm_qk_norm_rope(const void* q, void* q_out, const void* q_gain, uint32_t n_q_heads, uint32_t q_ld,
-                                        uint32_t q_out_ld, const void* k, void* k_out, const void* k_gain,
-                                        uint32_t n_kv_heads, uint32_t k_ld, uint32_t k_out_ld, const int32_t* positions,
+extern "C" bct_status bctm_qk_norm_rope(const void* q, void* q_out, const void* q_gain, uint32_t n_q_heads, size_t q_ld,
+                                        size_t q_out_ld, const void* k, void* k_out, const void* k_gain,
+                                        uint32_t n_kv_heads, size_t k_ld, size_t k_out_ld, const int32_t* positions,
                                         const double* inv_freq, uint32_t rotary_dim, uint32_t rows, uint32_t head_dim,
                                         float eps, int32_t dtype, uint32_t flags, void* hip_stream) {
   if (rows == 0 || head_dim == 0 || n_q_heads == 0 || !q || !q_out) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
@@ -228,8 +229,8 @@ extern "C" bct_status bctm_qk_norm_rope(const void* q, void* q_out, const void* 
     return mfail(BCT_ERR_INVALID_ARG, "positions, inv_freq and rotary_dim: all or none");
   const uint64_t size = dtype == BCT_F32 ? 4 : 2, wq = (uint64_t)n_q_heads * head_dim, wk = (uint64_t)n_kv_heads * head_dim;
   if ((uint64_t)n_q_heads + n_kv_heads > 0xFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many heads");
-  const uint32_t widest_q = q_ld > q_out_ld ? q_ld : q_out_ld, widest_k = k_ld > k_out_ld ? k_ld : k_out_ld;
-  if ((uint64_t)rows * (widest_q > widest_k ? widest_q : widest_k) > 1ull << 48) return mfail(BCT_ERR_UNSUPPORTED, "matrix too large");
+  const size_t widest_q = q_ld > q_out_ld ? q_ld : q_out_ld, widest_k = k_ld > k_out_ld ? k_ld : k_out_ld;
+  if ((widest_q > widest_k ? widest_q : widest_k) > (1ull << 48) / rows) return mfail(BCT_ERR_UNSUPPORTED, "matrix too large");
   if (q_ld < wq || q_out_ld < wq || (k && (k_ld < wk || k_out_ld < wk)))
     return mfail(BCT_ERR_INVALID_ARG, "a row distance below the width of the heads");
   if (!al16(q) || !al16(q_out) || !al16(q_gain) || !al16(k) || !al16(k_out) || !al16(k_gain) || !al16(inv_freq) ||
@@ -243,7 +244,7 @@ extern "C" bct_status bctm_qk_norm_rope(const void* q, void* q_out, const void* 
       (k && (clash(k_out, wk, k_out_ld, k, wk, k_ld, true) || clash(q_out, wq, q_out_ld, k, wk, k_ld, false) ||
              clash(k_out, wk, k_out_ld, q, wq, q_ld, false) || clash(q_out, wq, q_out_ld, k_out, wk, k_out_ld, false))))
     return mfail(BCT_ERR_INVALID_ARG, "an output overlaps an input other than its own, or the other output");
-  const RopeCall c = {{q, q_out, q_gain, n_q_heads, q_ld, q_out_ld}, {k, k_out, k_gain, n_kv_heads, k_ld, k_out_ld},
+  const RopeCall c = {{q, q_out, q_gain, q_ld, q_out_ld, n_q_heads}, {k, k_out, k_gain, k_ld, k_out_ld, n_kv_heads},
                       positions, inv_freq, rotary_dim, rows, head_dim, eps, (hipStream_t)hip_stream};
   const RopePairs pairs = rotary_dim == 0 ? kNoRotation : flags & BCTM_ROPE_INTERLEAVED ? kNeighbours : kHalves;
   return dtype == BCT_F32 ? rope_form<F32>(c, norm, pairs) : rope_form<BF16>(c, norm, pairs);

@@ -54,8 +54,8 @@ def mlib() -> ctypes.CDLL:
     L.bctm_swiglu.argtypes = [vp, vp, vp, vp, u32, u32, u32, u32, vp]
     L.bctm_linear_plan.argtypes = [u32, u32, u32, u32, ctypes.POINTER(u32)]
     L.bctm_linear_tile.argtypes = [u32, u32, u32, u32, u32] + [ctypes.POINTER(u32)] * 3
-    L.bctm_qk_norm_rope.argtypes = [vp, vp, vp, u32, u32, u32] * 2 + [vp, vp, u32, u32, u32, ctypes.c_float, ctypes.c_int32, u32,
-                                                                      vp]
+    sz = ctypes.c_size_t   # a number too wide for its argument would be cut without a word
+    L.bctm_qk_norm_rope.argtypes = [vp, vp, vp, u32, sz, sz] * 2 + [vp, vp, u32, u32, u32, ctypes.c_float, ctypes.c_int32, u32, vp]
     L.bctm_argmax.argtypes = [vp, vp, u32, u32, vp]
     lora = ctypes.POINTER(_bctm_lora)
     L.bctm_lora_workspace.argtypes = [u32, u32, u32, u32, ctypes.POINTER(ctypes.c_size_t)]
@@ -181,8 +181,10 @@ def _heads(t, name, dtype, device):
             (stride[1] != shape[2] and shape[1] > 1):
         raise ValueError(f"{name}: expected {dtype} [rows][heads][d] on cuda:{device}, heads side by side, got {t.dtype} "
                          f"{tuple(shape)} strides {stride} on {t.device}")
+    if shape[0] >> 32:
+        raise ValueError(f"{name}: more rows than one call takes")
     # the distance of a single row is not looked at
-    return shape, stride[0] if shape[0] > 1 else max(stride[0], shape[1] * shape[2])
+    return shape, stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
 
 def bctm_qk_norm_rope(q, k=None, q_gain=None, k_gain=None, eps=None, positions=None, inv_freq=None, interleaved=False,
@@ -387,6 +389,8 @@ def bctm_lora_pack(a, b, scale=None):
                               scale.device != a.device):
         raise ValueError(f"scale: expected a contiguous float32 vector of {n} on {a.device}")
     N, r = bs[0].shape[1], (rank + 15) // 16 * 16
+    if max(n * segments * r, n * N, K) >> 32:
+        raise ValueError("more adapters than one call packs")
     if r != rank:
         a = torch.nn.functional.pad(a, (0, 0, 0, r - rank))
         bs = [torch.nn.functional.pad(t, (0, r - rank)) for t in bs]
@@ -465,6 +469,8 @@ def bctm_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p
         raise ValueError(f"logits: expected [rows][N] of float32 or bf16 on the GPU, each row contiguous, got {logits.dtype} "
                          f"{tuple(logits.shape)} strides {logits.stride()} on {logits.device}")
     rows, N = logits.shape
+    if rows >> 32 or N >> 32:
+        raise ValueError("logits: more rows or tokens than one call takes")
     if out is None:
         out = torch.empty(rows, dtype=torch.int32, device=logits.device)
     if prob is True:

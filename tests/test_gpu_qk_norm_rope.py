@@ -184,3 +184,35 @@ def test_another_stream_and_a_captured_graph(M):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(qo, want[0]) and torch.equal(ko, want[1]), step
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_farther_apart_than_32_bits_count(M, dtype):
+    """Two rows at a distance of 2^32 elements and some: read and written where they lie, and nowhere near the distance's lower
+    32 bits."""
+    Hq, Hkv, d, far = 4, 2, 64, (1 << 32) + 4096
+    flat = torch.empty(far + 4096, dtype=DT[dtype], device="cuda")
+    near = flat[:8192]
+    near.zero_()
+    rows = flat.as_strided((2, Hq + Hkv, d), (far, d, 1))
+    rows[0], rows[1] = draw((Hq + Hkv, d), dtype, 1), draw((Hq + Hkv, d), dtype, 2)
+    q, k = rows[:, :Hq], rows[:, Hq:]
+    pos, fr = torch.tensor([3, 1000], dtype=torch.int32).cuda(), freqs(d).cuda()
+    want = M.bctm_qk_norm_rope(q.contiguous(), k.contiguous(), eps=1e-6, positions=pos, inv_freq=fr)
+    got = M.bctm_qk_norm_rope(q, k, eps=1e-6, positions=pos, inv_freq=fr, q_out=torch.empty_like(want[0]), k_out=torch.empty_like(want[1]))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    before = near.clone()
+    M.bctm_qk_norm_rope(q, k, eps=1e-6, positions=pos, inv_freq=fr, q_out=q, k_out=k)     # in place
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+    assert torch.equal(near[(Hq + Hkv) * d:], before[(Hq + Hkv) * d:])
+
+
+def test_one_row_at_any_distance(M):
+    """The distance of a single row is not one: neither its alignment nor its size matters."""
+    flat = draw((33, 67), "bf16", 4).reshape(-1)
+    q = flat.as_strided((1, 4, 64), (1 << 40, 64, 1))
+    odd = flat.as_strided((1, 4, 64), (257, 64, 1))
+    want, _ = M.bctm_qk_norm_rope(q.contiguous(), eps=1e-6)
+    for t in (q, odd):
+        got, _ = M.bctm_qk_norm_rope(t, eps=1e-6, q_out=torch.empty_like(want))
+        assert torch.equal(got, want)

@@ -123,3 +123,11 @@ def test_workspace_serves_fewer_rows(ML, K, rank, segments):
         assert ML.bctm_lora_workspace(rows, K, rank, segments, ctypes.byref(size)) == 0
         assert size.value >= before, rows
         before = size.value
+
+
+@pytest.mark.parametrize("name", ["ldq", "ldqo", "ldk", "ldko"])
+def test_row_distances_beyond_32_bits_arrive_whole(ML, name):
+    """Cut to 32 bits, the first of these distances would be that of a valid call, and the second would be below the width."""
+    for far in ((1 << 49) + 512, (1 << 62) + 8):
+        assert rope(ML, **{name: far}) == P.BCT_ERR_UNSUPPORTED, far
+        assert b"matrix too large" in ML.bctm_last_error()
