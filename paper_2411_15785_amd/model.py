@@ -589,6 +589,7 @@ class BctStack:
         self.embed, self.final_norm = weights["embed"], weights["final_norm"]
         self.head = bctm_pack_weight(weights["head"])
         self.adapters = None
+        self._lora_now = {}   # rows -> the workspace that the present adapters take
         self.inv_freq = None
         if s.rope_base:
             rot = s.rotary_dim or s.head_dim
@@ -598,8 +599,8 @@ class BctStack:
 
     def set_adapters(self, layers):
         """layers: per layer a dictionary of LoraWeights for any of "qkv" (three segments: q, wq, wv), "o", "gate_up" and "down";
-        forward(adapters=) then says which adapter a row has.  None: no adapters.  A graph that was captured before holds the
-        adapters of then: capture again."""
+        forward(adapters=) then says which adapter a row has.  None: no adapters.  A graph that was captured before goes on with
+        the adapters of then, which the caller keeps as long as it is replayed; capture again for the new ones."""
         if layers is not None:
             if len(layers) != self.shape.n_layers:
                 raise ValueError(f"adapters: expected {self.shape.n_layers} layers")
@@ -613,15 +614,19 @@ class BctStack:
                         raise ValueError(f"layer {l} {n}: expected LoraWeights of (K, N, segments) {want.get(n, tuple(want))[:3]} "
                                          f"on {self.embed.device}")
         self.adapters = layers
-        self._bufs = {k: v for k, v in self._bufs.items() if k[0] != "lora"}
+        self._lora_now.clear()
 
     def _lora_workspace(self, rows):
         torch = _torch()
-        k = ("lora", rows)
-        if k not in self._bufs:
+        if rows not in self._lora_now:
             n = max([a.workspace_bytes(rows) for d in self.adapters for a in d.values()], default=16)
-            self._bufs[k] = torch.empty(n, dtype=torch.uint8, device=self.device)
-        return self._bufs[k]
+            # Other adapters' workspace of as many rows serves, if it is large enough.  One that is not stays all the same: a step on
+            # another stream may be using it, and a captured one will.
+            kept = self._bufs.setdefault(("lora", rows), [])
+            if not kept or kept[-1].numel() < n:
+                kept.append(torch.empty(n, dtype=torch.uint8, device=self.device))
+            self._lora_now[rows] = kept[-1]
+        return self._lora_now[rows]
 
     def _buf(self, name, rows, cols):
         torch = _torch()

@@ -177,3 +177,26 @@ def test_refusals(M):
         p.gpu.forward(ids, positions=pos, adapters=ad)
     with pytest.raises(ValueError):
         M.StackShape(**{**SHAPES["gqa"], "rotary_dim": 24})
+
+
+def test_a_captured_step_outlives_its_adapters(M):
+    """A step captured with adapters goes on with them after others have been set, whatever is allocated in between."""
+    p = Pair(M, "gqa")
+    s, packed = p.s, p.gpu.adapters
+    ids, pos, ad = (to(a) for a in p.batch(0))
+    run = lambda stack: stack.forward(ids, positions=pos, adapters=ad)
+    run(p.gpu)
+    run(p.twin)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        _, logits = run(p.gpu)
+    p.gpu.set_adapters(None)
+    size = packed[0]["qkv"].workspace_bytes(s.batch)
+    others = [torch.full((size,), 7, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    for step in range(3):
+        ids.copy_(to(p.batch(step)[0]))
+        g.replay()
+        _, want = run(p.twin)
+        torch.cuda.synchronize()
+        assert torch.equal(logits.view(torch.int16), want.view(torch.int16)), step
+    assert all(bool((o == 7).all()) for o in others)

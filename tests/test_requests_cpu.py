@@ -1,6 +1,7 @@
 """Refusals of the per-request operators (head norms with rotation, adapters, sampling): the C entry points check their
 arguments before the first HIP call, so no GPU is needed."""
 import ctypes
+import weakref
 
 import pytest
 
@@ -131,3 +132,26 @@ def test_row_distances_beyond_32_bits_arrive_whole(ML, name):
     for far in ((1 << 49) + 512, (1 << 62) + 8):
         assert rope(ML, **{name: far}) == P.BCT_ERR_UNSUPPORTED, far
         assert b"matrix too large" in ML.bctm_last_error()
+
+
+def test_new_adapters_leave_the_workspaces_of_old_ones():
+    """What a step on another stream or a captured one uses is not given back; one that is large enough serves on."""
+    torch = pytest.importorskip("torch")
+    s = model.StackShape(n_layers=2, dim=64, n_q_heads=1, n_kv_heads=1, head_dim=32, ffn=64, vocab=16, capacity_M=64, batch=3)
+    stack = object.__new__(model.BctStack)     # no GPU: the bookkeeping alone
+    stack.shape, stack.device, stack.embed = s, torch.device("cpu"), torch.empty(0)
+    stack.adapters, stack._bufs, stack._lora_now = None, {}, {}
+    adapters = lambda rank: [{"o": model.LoraWeights(torch.empty(0), None, None, None, 1, 1, rank, s.q_width, s.dim)} for _ in range(2)]
+    stack.set_adapters(adapters(16))
+    small = stack._lora_workspace(3)
+    assert stack._lora_workspace(3) is small
+    held = weakref.ref(small)
+    where = small.data_ptr()
+    del small
+    stack.set_adapters(adapters(64))
+    large = stack._lora_workspace(3)
+    assert large.numel() >= adapters(64)[0]["o"].workspace_bytes(3) and large.data_ptr() != where
+    stack.set_adapters(None)
+    assert held() is not None
+    stack.set_adapters(adapters(16))
+    assert stack._lora_workspace(3) is large and held() is not None
