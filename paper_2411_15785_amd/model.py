@@ -652,6 +652,7 @@ class BctStack:
         sampling: a Sampling with one entry per row of logits, or None: the most likely token.
         After the first call of a given (B, T, head), and the first one with adapters, no memory is allocated, so a call can be
         captured in a HIP graph."""
+        torch = _torch()
         s = self.shape
         rows = s.batch * T
         if ids.numel() != rows:
@@ -662,6 +663,19 @@ class BctStack:
             raise ValueError("positions go with a shape that has a rope_base")
         if adapters is not None and self.adapters is None:
             raise ValueError("adapters: none have been set (set_adapters)")
+        # here, as the caches take the step's tokens layer by layer: a call that is refused has changed nothing
+        i32, f32, dev = torch.int32, torch.float32, self.embed.device
+        checks = [(positions, "positions", i32, rows), (adapters, "adapters", i32, rows)]
+        if sampling is not None:
+            n = s.batch if head == "last" else rows
+            if sampling.uniform is None or s.vocab > 1 << 22:
+                raise ValueError("sampling needs uniform numbers, and a vocabulary of at most 4194304 tokens")
+            checks += [(sampling.uniform, "uniform", f32, n), (sampling.temperature, "temperature", f32, n), (sampling.top_k, "top_k", i32, n),
+                       (sampling.top_p, "top_p", f32, n), (sampling.min_p, "min_p", f32, n), (next_ids, "next_ids", i32, n),
+                       (None if sampling.prob is True else sampling.prob, "prob", f32, n)]
+        for t, name, dtype, n in checks:
+            if t is not None and (t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous() or t.device != dev):
+                raise ValueError(f"{name}: expected a contiguous {dtype} vector of {n} on {dev}")
         lora_ws = self._lora_workspace(rows) if adapters is not None else None
         x = bctm_embed(ids, self.embed, self._buf("x", rows, s.dim))
         # every input of a projection is kept tiled, so that the projections read it in whole kilobytes
@@ -707,7 +721,6 @@ class BctStack:
                 bctm_linear(f, lw["w_down"], x, x)
         if head == "last" and T > 1:
             # rows b*T + T-1, gathered with the embedding kernel (a row lookup) from x as the table
-            torch = _torch()
             k = ("last_rows", s.batch, T)
             if k not in self._bufs:
                 self._bufs[k] = (torch.arange(s.batch, dtype=torch.int32, device=self.device) * T + (T - 1)).contiguous()

@@ -200,3 +200,24 @@ def test_a_captured_step_outlives_its_adapters(M):
         torch.cuda.synchronize()
         assert torch.equal(logits.view(torch.int16), want.view(torch.int16)), step
     assert all(bool((o == 7).all()) for o in others)
+
+
+def test_a_refused_call_changes_nothing(M):
+    """Wrong vectors of any kind are refused before a layer's cache has taken the tokens: the next call is as if there had been none."""
+    p = Pair(M, "gqa")
+    s, packed = p.s, p.gpu.adapters
+    for stack in (p.gpu, p.twin):      # adapters behind the cache alone
+        stack.set_adapters([{"down": d["down"]} for d in packed])
+    ids, pos, ad = (to(a) for a in p.batch(0))
+    n, f = s.batch, lambda k: torch.zeros(k, device="cuda")
+    u = f(n)
+    for kw in (dict(positions=pos[:-1]), dict(positions=pos.cpu()), dict(adapters=ad[:-1]), dict(adapters=ad.long()), dict(adapters=ad.cpu()),
+               dict(adapters=torch.stack([ad, ad], 1)[:, 0]), dict(sampling=M.Sampling(None)), dict(sampling=M.Sampling(f(n + 1))),
+               dict(sampling=M.Sampling(u, temperature=f(1))), dict(sampling=M.Sampling(u, top_k=f(n))), dict(sampling=M.Sampling(u, top_p=u.double())),
+               dict(sampling=M.Sampling(u, min_p=u.cpu())), dict(sampling=M.Sampling(u, prob=f(n + 1))),
+               dict(sampling=M.Sampling(u), next_ids=torch.empty(n + 1, dtype=torch.int32, device="cuda"))):
+        with pytest.raises(ValueError):
+            p.gpu.forward(ids, **{**dict(positions=pos), **kw})
+    _, a = p.gpu.forward(ids, positions=pos, adapters=ad, sampling=M.Sampling(u, prob=True))
+    _, b = p.twin.forward(ids, positions=pos, adapters=ad)
+    assert torch.equal(a.view(torch.int16), b.view(torch.int16))
