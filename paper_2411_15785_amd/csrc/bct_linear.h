@@ -95,12 +95,14 @@ struct LoraTiles {
   }
 };
 
-// Adds the term of the row tiles (RT of 16 rows, from row0) whose rows all have one adapter to the accumulators acc(i, j).
-// share, of shares: the 16 ranks that are this wavefront's.  -> bit i: row tile i is not one of those, nor one without adapters.
+// Adds the term of RT tiles of 16 rows (from row0) to the accumulators acc(i, j), which are those of the K loop and have nothing else
+// yet.  Each row's sum is one chain over its own adapter's ranks in their
+// order, whether its tile has one adapter or several, so its bits do not depend on its neighbours: a matrix instruction sums
+// every row apart, and where a tile's rows have several adapters, its result is selected for the rows of the one that was
+// multiplied.  Selected, not multiplied by zero, so an infinity or a NaN in one adapter's weights stays in its rows.
 template <int RT, int CT, int MATS, typename SEG, typename TILE, typename ACC>
-__device__ __forceinline__ uint32_t lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T, uint32_t row0, uint32_t rows, uint32_t share,
-                                             uint32_t shares, ACC acc) {
-  const uint32_t last = (rows - 1) / 16, n = T.L.n;
+__device__ __forceinline__ void lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T, uint32_t row0, uint32_t rows, ACC acc) {
+  const uint32_t last = (rows - 1) / 16, n = T.L.n, steps = T.L.rank / 16;
   uint32_t id[RT], cur[RT], mixed = 0;
 #pragma unroll
   for (int i = 0; i < RT; ++i) id[i] = adapter_of(T.L.adapter, row0 + 16 * i + threadIdx.x % 16, rows, n);
@@ -112,8 +114,10 @@ __device__ __forceinline__ uint32_t lora_add(const LoraTiles<CT, MATS, SEG, TILE
       mixed |= 1u << i;
     }
   }
-  for (uint32_t ks = share; ks < T.L.rank / 16; ks += shares) {
-    constexpr int G = RT * MATS > 8 ? 8 / MATS : RT;   // row tiles whose operands are requested at once
+  // the row tiles whose rows all have one adapter
+  for (uint32_t ks = 0; ks < steps; ++ks) {
+    // row tiles whose operands are requested at once: as many as there are registers for beside 32 accumulators
+    constexpr int AT_ONCE = RT * CT > 16 ? 16 / CT : 8, G = RT * MATS > AT_ONCE ? AT_ONCE / MATS : RT;
     bf16x8 a[G][MATS], b[CT];
 #pragma unroll
     for (int i0 = 0; i0 < RT; i0 += G) {
@@ -136,48 +140,52 @@ __device__ __forceinline__ uint32_t lora_add(const LoraTiles<CT, MATS, SEG, TILE
       }
     }
   }
-  return mixed;
-}
-
-// The term of a row tile (16 rows from row0) that has several adapters, or rows without one, added to sum.  A product has all
-// 16 rows in it and each row takes that of its own adapter: selected, not multiplied by zero, so an infinity or a NaN in one
-// adapter's weights stays in its rows.  The next product's operands are requested before this one is made.
-template <int CT, int MATS, typename SEG, typename TILE>
-__device__ __forceinline__ void lora_mixed(const LoraTiles<CT, MATS, SEG, TILE>& T, uint32_t row0, uint32_t rows, f32x4 (&sum)[CT]) {
-  const uint32_t kg = threadIdx.x % 64 / 16, seg0 = MATS == 2 ? 0 : T.segment(0), seg1 = MATS == 2 ? 1 : T.segment(CT - 1);
-  AdapterWalk<1> walk(T.L.adapter, row0, rows, T.L.n);
-  bool more = walk.next();
-  if (!more) return;
-  uint32_t ks = 0;
-  bf16x8 a[MATS], b[CT];
-  T.weights(walk.cur, ks, b);
+  // Those with several, or with rows without one: adapter after adapter, the next product's operands requested before this one
+  // (with eight feature tiles there are no registers for them).
+  constexpr bool AHEAD = CT <= 4;
+  const uint32_t kg = threadIdx.x % 64 / 16;
 #pragma unroll
-  for (int m = 0; m < MATS; ++m) a[m] = T.operand(row0 / 16, seg0 + m, ks);
-  while (more) {
-    const uint32_t mine = (uint32_t)(walk.match[0] >> (4 * kg)), now = ks;   // bit v: row 4 kg + v
-    if (++ks == T.L.rank / 16) {
-      ks = 0;
-      more = walk.next();   // no more: the last one's first operands once again
-    }
-    bf16x8 next_a[MATS], next_b[CT];
-    T.weights(walk.cur, ks, next_b);
+  for (int i = 0; i < RT; ++i) {
+    if (!(mixed >> i & 1)) continue;
+    const uint32_t row_tile = row0 / 16 + i;
+    AdapterWalk<1> walk(T.L.adapter, 16 * row_tile, rows, n);
+    uint32_t ks = 0;
+    bf16x8 a[MATS], b[CT];
+    auto request = [&](bf16x8 (&to_a)[MATS], bf16x8 (&to_b)[CT]) {
+      T.weights(walk.cur, ks, to_b);
 #pragma unroll
-    for (int m = 0; m < MATS; ++m) next_a[m] = T.operand(row0 / 16, seg0 + m, ks);
-    for (uint32_t seg = seg0; seg <= seg1; ++seg) {
-      // where the border between two outputs lies within the tiles
-      const bf16x8 at = MATS == 1 && seg > seg0 ? T.operand(row0 / 16, seg, now) : MATS == 2 && seg > seg0 ? a[MATS - 1] : a[0];
+      for (int m = 0; m < MATS; ++m) to_a[m] = T.operand(row_tile, MATS == 2 ? m : T.segment(0), ks);
+    };
+    bool more = walk.next();   // one at least has an adapter
+    if (AHEAD) request(a, b);
+    while (more) {
+      if (!AHEAD) request(a, b);
+      const uint32_t mine = (uint32_t)(walk.match[0] >> (4 * kg)), now = ks;   // bit v: row 4 kg + v
+      if (++ks == steps) {
+        ks = 0;
+        more = walk.next();   // no more: the last one's first operands once again
+      }
+      bf16x8 next_a[MATS], next_b[CT];
+      if (AHEAD) {
+        request(next_a, next_b);
+        // Before the products, which the compiler sees to by itself in a SwiGLU only.  us, without | with: 256 x 4096 x 12288, 256 adapters of
+        // rank 16 68.5 | 62.2, 512 rows of 64 106 | 93.7, SwiGLU of 256 x 4096 x 11008 of 64 87.2 | 94.3.
+        if (MATS == 1) __builtin_amdgcn_sched_barrier(0);
+      }
 #pragma unroll
       for (int j = 0; j < CT; ++j) {
-        const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(at, b[j], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-        const uint32_t take = (MATS == 2 ? (uint32_t)(j % 2) : T.segment(j)) == seg ? mine : 0u;
+        if (MATS == 1 && j > 0 && T.segment(j) != T.segment(j - 1)) a[0] = T.operand(row_tile, T.segment(j), now);
+        const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[j % MATS], b[j], acc(i, j), 0, 0, 0);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) sum[j][v] = (take >> v & 1) ? sum[j][v] + d[v] : sum[j][v];
+        for (int v = 0; v < 4; ++v) acc(i, j)[v] = (mine >> v & 1) ? d[v] : acc(i, j)[v];
+      }
+      if (AHEAD) {
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) a[m] = next_a[m];
+#pragma unroll
+        for (int j = 0; j < CT; ++j) b[j] = next_b[j];
       }
     }
-#pragma unroll
-    for (int m = 0; m < MATS; ++m) a[m] = next_a[m];
-#pragma unroll
-    for (int j = 0; j < CT; ++j) b[j] = next_b[j];
   }
 }
 

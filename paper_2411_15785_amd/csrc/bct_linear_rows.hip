@@ -205,10 +205,29 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   __builtin_amdgcn_sched_barrier(0);
   request(Int<2>{}, 2, Int<PAIR ? NA : 0>{}, Int<ND>{});
   __builtin_amdgcn_sched_barrier(0);
-  // The low-rank term first, while the stages fill: what it loads is waited for together with them.
-  [[maybe_unused]] uint32_t mixed_tiles = 0;
-  if constexpr (sizeof...(LORA) > 0)
-    mixed_tiles = lora_add<MI>(lora_tiles(lora...), r0 + wr * (16 * MI), rows, grp, KS, [&](int i, int j) -> f32x4& { return acc[i][j]; });
+  // The low-rank term first, while the stages fill: what it loads is waited for together with them.  With two groups, the first
+  // takes that of the first half of the row tiles.
+  if constexpr (sizeof...(LORA) > 0) {
+    if constexpr (KS == 1) {
+      lora_add<MI>(lora_tiles(lora...), r0 + wr * (16 * MI), rows, [&](int i, int j) -> f32x4& { return acc[i][j]; });
+    } else {
+      f32x4 half[MI / KS][NJ];
+#pragma unroll
+      for (int i = 0; i < MI / KS; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) half[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      lora_add<MI / KS>(lora_tiles(lora...), r0 + wr * (16 * MI) + grp * (16 * MI / KS), rows, [&](int i, int j) -> f32x4& { return half[i][j]; });
+#pragma unroll
+      for (int i = 0; i < MI / KS; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            acc[i][j][v] = grp ? 0.f : half[i][j][v];
+            acc[MI / KS + i][j][v] = grp ? half[i][j][v] : 0.f;
+          }
+    }
+  }
   __builtin_amdgcn_s_waitcnt(wait_vm((S - 2) * (PAIR ? NB : ND)));
   bare_barrier();
   const bool second = PING && wv >= 4;   // the wavefront of a SIMD that is half a step behind
@@ -274,17 +293,10 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   float(*e)[ES] = (float(*)[ES])((wv % 2 ? (char*)st1 : (char*)st0) + (wv / 2) * (16 * ES * 4));
 #pragma unroll
   for (int i = 0; i < MO; ++i) {
-    f32x4 mixed[NJ];
-    if constexpr (sizeof...(LORA) > 0) {
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) mixed[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (mixed_tiles >> (grp * MO + i) & 1) lora_mixed(lora_tiles(lora...), r0 + wr * (16 * MI) + (grp * MO + i) * 16, rows, mixed);
-    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      if constexpr (sizeof...(LORA) > 0) res[i][j] += mixed[j];
       const int col = SWIGLU ? (int)(CW / 2) * (j % 2) + 16 * (j / 2) + jl : 16 * j + jl;
 #pragma unroll
       for (int v = 0; v < 4; ++v) e[4 * kg + v][col] = res[i][j][v];

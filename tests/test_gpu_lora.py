@@ -315,3 +315,42 @@ def test_refusals(M):
     with pytest.raises(M.BctModelError):
         M.bctm_lora_pack(torch.zeros((1, 272, 64), dtype=torch.bfloat16, device="cuda"),
                          torch.zeros((1, 32, 272), dtype=torch.bfloat16, device="cuda"))        # rank beyond 256
+
+
+@pytest.mark.parametrize("form,rows,K,N,rank", [
+    ("linear", 130, 320, 256, 48), ("linear", 300, 1024, 512, 16), ("linear", 1030, 160, 4096, 32), ("linear", 557, 160, 23552, 32),
+    ("linear", 640, 160, 4096, 64), ("linear", 1000, 64, 32768, 16), ("linear", 2075, 4096, 64, 48), ("split", 300, 96, 384, 24),
+    ("split", 1030, 96, 4224, 40), ("swiglu", 300, 160, 480, 32), ("swiglu", 2048, 64, 11008, 32), ("swiglu", 557, 160, 11776, 16)])
+def test_a_row_of_many_does_not_depend_on_its_neighbours(M, form, rows, K, N, rank):
+    """From 128 rows on: a row's bits are the same where all rows have its adapter, where its neighbours have others, and where
+    they have none; K whole and in two, several outputs within a tile, the ragged last rows."""
+    n = 7
+    segments, mats = {"linear": (1, 1), "split": (3, 1), "swiglu": (2, 2)}[form]
+    c = Case(rows, K, N, rank, n, segments=segments, mats=mats)
+    ws, lora = c.pack(M)
+
+    def run(ids):
+        if form == "linear":
+            return M.bctm_linear_lora(c.x, ws[0], lora, ids)
+        if form == "swiglu":
+            return M.bctm_swiglu_lora(c.x, *ws, lora, ids)
+        return torch.cat(M.bctm_linear_split_lora(c.x, ws[0], lora, ids, [torch.empty((rows, v), dtype=torch.bfloat16, device="cuda")
+                                                                           for v in (16, 48, N - 64)]), 1)
+
+    full = lambda v: torch.full((rows,), v, dtype=torch.int32, device="cuda")
+    uniform = [run(full(a)) for a in range(n)]
+    plain = run(full(-1))
+    mixed = adapters(rows, n, rows)
+    inside = (mixed >= 0) & (mixed < n)
+    got = run(mixed)
+    for a in range(n):
+        assert same(got[mixed == a], uniform[a][mixed == a]), a
+    assert same(got[~inside], plain[~inside])
+    # one row in 13, and one stretch of rows, among rows without an adapter
+    alone = full(-1)
+    alone[::13] = 3
+    alone[100:140] = 5
+    got = run(alone)
+    for a in (3, 5):
+        assert same(got[alone == a], uniform[a][alone == a]), a
+    assert same(got[alone < 0], plain[alone < 0])
