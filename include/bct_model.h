@@ -117,7 +117,7 @@ bct_status bctm_swiglu(const void* x, const void* w_gate_packed, const void* w_u
  *   scale   float32 [n_adapters], NULL = 1;  adapter: int32 [rows]
  *   rank    a multiple of 16, at most 256; adapters of fewer ranks are filled up with zeros
  * workspace: 16-byte aligned, at least bctm_lora_workspace bytes, holds nothing between calls; it must not be in use by a call
- * on another stream.  All but the struct is device memory.  x A^T is summed in fp32 and enters the second product with 16 bits.
+ * on another stream.  All but the struct is device memory.  x A^T is summed in fp32 and enters the second product as that.
  * A row's bits depend on the sizes of the call and on its own adapter, not on the other rows'.
  * A NaN or an infinity in one adapter reaches the rows of that adapter alone; an infinite weight of b may come out as a NaN. */
 typedef struct {

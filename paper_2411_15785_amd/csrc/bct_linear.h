@@ -25,8 +25,8 @@ __device__ __forceinline__ size_t tiled_chunk(uint32_t r, uint32_t k, uint32_t K
 // The low-rank term of a projection's rows (bct_lora.hip): out[r] += t[r] B_a^T, a = adapter[r].
 // t, for the streaming kernel: fp32 [parts][rows][width], the parts to be added up, column segment * rank + j: the rank-j input
 // of output `segment` (of the gate and up matrices in a SwiGLU).
-// op, for the matrix-core kernel: A operands of v_mfma_f32_16x16x32_bf16, 16 rows x 16 ranks each as two bf16 addends side by
-// side in the contraction (entries 0-15 the rounding of t, 16-31 the rounding of what that left: 16 bits of t count), number
+// op, for the matrix-core kernel: pairs of A operands of v_mfma_f32_16x16x32_bf16, 16 rows x 16 ranks as four bf16 addends side by
+// side in two contractions (entries 0-15 and 16-31 of each), whose sum is t to its last bit; pair number
 // (row / 16 * segments + segment) * (rank / 16) + j / 16.
 // b: per adapter 16-byte chunks of 8 ranks of one feature, chunk (feature / 16 * rank / 8 + j / 8) * 16 + feature % 16.
 struct LoraTerm {
@@ -83,15 +83,21 @@ struct LoraTiles {
   SEG segment;
   TILE tile;
   static constexpr int kSets = MATS;   // operands of t for a row tile and 16 ranks
-  // a product takes 16 ranks: both halves of the contraction meet the same weights
+  // a product takes 16 ranks: all addends of t meet the same weights
   __device__ __forceinline__ void weights(uint32_t adapter, uint32_t ks, bf16x8 (&b)[CT]) const {
     const size_t at = ((size_t)adapter * (N / 16) * (L.rank / 8) + 2 * ks) * 16 + threadIdx.x / 16 % 2 * 16 + threadIdx.x % 16;
 #pragma unroll
     for (int j = 0; j < CT; ++j)
       b[j] = __builtin_bit_cast(bf16x8, (MATS == 2 && j % 2 ? L.b2 : L.b)[at + (size_t)tile(j) * (L.rank / 8) * 16]);
   }
-  __device__ __forceinline__ bf16x8 operand(uint32_t row_tile, uint32_t seg, uint32_t ks) const {
-    return __builtin_bit_cast(bf16x8, L.op[(((size_t)row_tile * L.segments + seg) * (L.rank / 16) + ks) * 64 + threadIdx.x % 64]);
+  __device__ __forceinline__ void operand(uint32_t row_tile, uint32_t seg, uint32_t ks, bf16x8 (&a)[2]) const {
+    const u32x4* op = L.op + (((size_t)row_tile * L.segments + seg) * (L.rank / 16) + ks) * 128 + threadIdx.x % 64;
+    a[0] = __builtin_bit_cast(bf16x8, op[0]);
+    a[1] = __builtin_bit_cast(bf16x8, op[64]);
+  }
+  static __device__ __forceinline__ f32x4 product(const bf16x8 (&a)[2], bf16x8 b, f32x4 sum) {
+    sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0], b, sum, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1], b, sum, 0, 0, 0);
   }
 };
 
@@ -117,15 +123,15 @@ __device__ __forceinline__ void lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T
   // the row tiles whose rows all have one adapter
   for (uint32_t ks = 0; ks < steps; ++ks) {
     // row tiles whose operands are requested at once: as many as there are registers for beside 32 accumulators
-    constexpr int AT_ONCE = RT * CT > 16 ? 16 / CT : 8, G = RT * MATS > AT_ONCE ? AT_ONCE / MATS : RT;
-    bf16x8 a[G][MATS], b[CT];
+    constexpr int AT_ONCE = RT * CT > 16 ? 16 / CT : 8, WANT = AT_ONCE / (2 * MATS), G = WANT < 1 ? 1 : WANT < RT ? WANT : RT;
+    bf16x8 a[G][MATS][2], b[CT];
 #pragma unroll
     for (int i0 = 0; i0 < RT; i0 += G) {
       // a row tile past the end or without an adapter takes an operand that is there, and no product
 #pragma unroll
       for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int m = 0; m < MATS; ++m) a[g][m] = T.operand(min(row0 / 16 + i0 + g, last), MATS == 2 ? m : T.segment(0), ks);
+        for (int m = 0; m < MATS; ++m) T.operand(min(row0 / 16 + i0 + g, last), MATS == 2 ? m : T.segment(0), ks, a[g][m]);
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         const int i = i0 + g;
@@ -134,8 +140,8 @@ __device__ __forceinline__ void lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T
 #pragma unroll
         for (int j = 0; j < CT; ++j) {
           // where the border between two outputs lies within the tiles
-          if (MATS == 1 && j > 0 && T.segment(j) != T.segment(j - 1)) a[g][0] = T.operand(row0 / 16 + i, T.segment(j), ks);
-          acc(i, j) = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[g][j % MATS], b[j], acc(i, j), 0, 0, 0);
+          if (MATS == 1 && j > 0 && T.segment(j) != T.segment(j - 1)) T.operand(row0 / 16 + i, T.segment(j), ks, a[g][0]);
+          acc(i, j) = T.product(a[g][j % MATS], b[j], acc(i, j));
         }
       }
     }
@@ -150,11 +156,11 @@ __device__ __forceinline__ void lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T
     const uint32_t row_tile = row0 / 16 + i;
     AdapterWalk<1> walk(T.L.adapter, 16 * row_tile, rows, n);
     uint32_t ks = 0;
-    bf16x8 a[MATS], b[CT];
-    auto request = [&](bf16x8 (&to_a)[MATS], bf16x8 (&to_b)[CT]) {
+    bf16x8 a[MATS][2], b[CT];
+    auto request = [&](bf16x8 (&to_a)[MATS][2], bf16x8 (&to_b)[CT]) {
       T.weights(walk.cur, ks, to_b);
 #pragma unroll
-      for (int m = 0; m < MATS; ++m) to_a[m] = T.operand(row_tile, MATS == 2 ? m : T.segment(0), ks);
+      for (int m = 0; m < MATS; ++m) T.operand(row_tile, MATS == 2 ? m : T.segment(0), ks, to_a[m]);
     };
     bool more = walk.next();   // one at least has an adapter
     if (AHEAD) request(a, b);
@@ -165,7 +171,7 @@ __device__ __forceinline__ void lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T
         ks = 0;
         more = walk.next();   // no more: the last one's first operands once again
       }
-      bf16x8 next_a[MATS], next_b[CT];
+      bf16x8 next_a[MATS][2], next_b[CT];
       if (AHEAD) {
         request(next_a, next_b);
         // Before the products, which the compiler sees to by itself in a SwiGLU only.  us, without | with: 256 x 4096 x 12288, 256 adapters of
@@ -174,14 +180,14 @@ __device__ __forceinline__ void lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T
       }
 #pragma unroll
       for (int j = 0; j < CT; ++j) {
-        if (MATS == 1 && j > 0 && T.segment(j) != T.segment(j - 1)) a[0] = T.operand(row_tile, T.segment(j), now);
-        const f32x4 d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[j % MATS], b[j], acc(i, j), 0, 0, 0);
+        if (MATS == 1 && j > 0 && T.segment(j) != T.segment(j - 1)) T.operand(row_tile, T.segment(j), now, a[0]);
+        const f32x4 d = T.product(a[j % MATS], b[j], acc(i, j));
 #pragma unroll
         for (int v = 0; v < 4; ++v) acc(i, j)[v] = (mine >> v & 1) ? d[v] : acc(i, j)[v];
       }
       if (AHEAD) {
 #pragma unroll
-        for (int m = 0; m < MATS; ++m) a[m] = next_a[m];
+        for (int m = 0; m < 2 * MATS; ++m) a[m / 2][m % 2] = next_a[m / 2][m % 2];
 #pragma unroll
         for (int j = 0; j < CT; ++j) b[j] = next_b[j];
       }

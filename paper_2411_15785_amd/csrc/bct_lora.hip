@@ -59,18 +59,33 @@ LoraPlan lora_plan(uint32_t rows, uint32_t K, uint32_t width) {
   return p;
 }
 
-// Where the operands of 16 rows x 16 ranks are written: 8 ranks of a row, as their rounding and the rounding of what it left.
+// The addends of a float in bf16: its upper bits, those below and those below these, cut off and not rounded, so that 24 bits of it
+// are in three (an infinity or a NaN is in each).
+__device__ __forceinline__ void addends_of(float t, float (&part)[3]) {
+  const bool finite = fabsf(t) < INFINITY;
+  part[0] = __uint_as_float(__float_as_uint(t) & 0xFFFF0000u);
+  const float rest = t - part[0];
+  part[1] = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u);
+  part[2] = rest - part[1];
+  if (!finite) part[0] = part[1] = part[2] = t;
+}
+// Where the operands of 16 rows x 16 ranks are written: 8 ranks of a row, the third addend in two halves.
 __device__ __forceinline__ void store_operand(u32x4* op, size_t number, uint32_t row, uint32_t half, const float* t) {
-  u32x4 hi, lo;
+  u32x4 w[3];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const uint32_t r = pack_bf16x2(t[2 * e], t[2 * e + 1]);
-    hi[e] = r;
-    const float h0 = __uint_as_float(r << 16), h1 = __uint_as_float(r & 0xFFFF0000u);
-    lo[e] = pack_bf16x2(fabsf(h0) < INFINITY ? t[2 * e] - h0 : 0.f, fabsf(h1) < INFINITY ? t[2 * e + 1] - h1 : 0.f);   // inf - inf
+    float p0[3], p1[3];
+    addends_of(t[2 * e], p0);
+    addends_of(t[2 * e + 1], p1);
+    p0[2] *= 0.5f;
+    p1[2] *= 0.5f;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) w[i][e] = pack_bf16x2(p0[i], p1[i]);
   }
-  op[number * 64 + 16 * half + row] = hi;
-  op[number * 64 + 16 * (2 + half) + row] = lo;
+  op += number * 128 + 16 * half + row;
+  op[0] = w[0];
+  op[32] = w[1];
+  op[64] = op[96] = w[2];
 }
 
 // OP: t goes out as operands (one part of K), else as fp32.  Workgroup ids go round the eight XCDs: the parts of K are dealt to
@@ -211,12 +226,12 @@ __global__ __launch_bounds__(256) void lora_pack_kernel(const uint16_t* __restri
   packed[c] = *(const u32x4*)(b + n * rank + c / 16 % (rank / 8) * 8);
 }
 
-// Room for the parts in fp32 and for the operands, which are whole tiles of 16 rows: for any number of rows up to this one.  Where
+// Room for the parts in fp32 and for the operands, which are whole tiles of 16 rows with four bf16 for each t: for any number of rows up to this one.  Where
 // K is in several parts, they and the workgroups are at most kGroupsMany.
 size_t lora_bytes(uint32_t rows, uint32_t width) {
   const uint32_t tiles = tiles_of(rows, 16), split = kMostRowTiles * (kGroupsMany / ((width / 16 + 3) / 4));
   const size_t parts = std::max<size_t>(tiles, std::min<size_t>((size_t)kMostParts * tiles, split));
-  return (tiles + parts) * 16 * width * sizeof(float);
+  return (2 * tiles + parts) * 16 * width * sizeof(float);
 }
 
 }  // namespace
@@ -277,7 +292,7 @@ bct_status launch_lora_inputs(const bctm_lora& l, const void* x, uint32_t rows, 
   const LoraPlan p = lora_plan(rows, K, width);
   // the operands first, then the parts
   u32x4* op = (u32x4*)l.workspace;
-  float* t = (float*)l.workspace + (size_t)tiles_of(rows, 16) * 16 * width;
+  float* t = (float*)l.workspace + (size_t)tiles_of(rows, 16) * 32 * width;
   const bool at_once = operands && p.parts == 1;
   if (x_tiled) launch_inputs_of<true>(l, x, at_once ? (void*)op : t, rows, K, width, p, at_once, s);
   else launch_inputs_of<false>(l, x, at_once ? (void*)op : t, rows, K, width, p, at_once, s);

@@ -354,3 +354,24 @@ def test_a_row_of_many_does_not_depend_on_its_neighbours(M, form, rows, K, N, ra
     for a in (3, 5):
         assert same(got[alone == a], uniform[a][alone == a]), a
     assert same(got[alone < 0], plain[alone < 0])
+
+
+@pytest.mark.parametrize("rows,N", [(40, 64), (150, 64), (300, 512), (1030, 4096)])
+@pytest.mark.parametrize("run", [1, 1000000])
+def test_the_term_has_24_bits(M, rows, N, run):
+    """The projection cancels the adapters' term but for the sums' roundings: W = -A for every feature, B = 1, all entries positive.  Both
+    sums are fp32, within 2^-20 of the products' absolute values together (see above), 2 t; 16 bits of t would leave 2^-17 of it
+    in places.  In one adapter's rows and in mixed tiles."""
+    K, rank = 64, 16
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    r = lambda *s: (torch.rand(s, generator=g, device="cuda") + 0.5).bfloat16()
+    x, a0 = r(rows, K), r(K)
+    a = torch.zeros((2, rank, K), dtype=torch.bfloat16, device="cuda")
+    a[:, 5] = a0
+    b = torch.zeros((2, N, rank), dtype=torch.bfloat16, device="cuda")
+    b[:, :, 5] = 1.0
+    w = M.bctm_pack_weight((-a0).expand(N, K).contiguous())
+    ids = (torch.arange(rows, device="cuda") // run % 2).to(torch.int32)
+    out = M.bctm_linear_lora(x, w, M.bctm_lora_pack(a, b), ids).double()
+    t = x.double() @ a0.double()
+    assert bool((out.abs() <= 2.0 ** -20 * 2 * t[:, None]).all()), (out.abs() / t[:, None]).max().item()
