@@ -79,7 +79,8 @@ bct_status bctm_pack_weight(const void* w, void* packed, uint32_t N, uint32_t K,
 /* out[r][n] = (residual ? residual[r][n] : 0) + sum_k x[r][k] * w[n][k].
  * x [rows][K] row-major, or tiled with flags = BCTM_X_TILED; w_packed = bctm_pack_weight of w [N][K];
  * out/residual [rows][N] row-major;
- * K a multiple of 32, N a multiple of 16; fp32 accumulation (MFMA), one rounding to bf16 at the end.
+ * K a multiple of 32, N a multiple of 16; fp32 accumulation (MFMA), one rounding to bf16 at the end.  With few rows an infinite
+ * activation may come out as a NaN (K tiles that fill up a round are multiplied by zero weights).
  * out may alias residual; x must not alias out.  Two kernels: up to 127 rows (a decode batch) the weights
  * are streamed once per 32 rows against activations read from cache; from 128 rows on (a prompt chunk), a tiled matrix-core
  * kernel runs instead where N is a multiple of 128 (bctm_swiglu: 64), or N is 128 to 16384 and the streaming kernel would have
@@ -116,10 +117,12 @@ bct_status bctm_swiglu(const void* x, const void* w_gate_packed, const void* w_u
  *           the projection (all outputs together).  b_up: those of the up matrix in bctm_swiglu_lora, else NULL
  *   scale   float32 [n_adapters], NULL = 1;  adapter: int32 [rows]
  *   rank    a multiple of 16, at most 256; adapters of fewer ranks are filled up with zeros
+ *   used    how many of these ranks are the adapters' own, 0 = all: x A^T is 0 for the others, whatever x holds (an infinity times
+ *           a row of zeros would be a NaN)
  * workspace: 16-byte aligned, at least bctm_lora_workspace bytes, holds nothing between calls; it must not be in use by a call
  * on another stream.  All but the struct is device memory.  x A^T is summed in fp32 and enters the second product as that.
  * A row's bits depend on the sizes of the call and on its own adapter, not on the other rows'.
- * A NaN or an infinity in one adapter reaches the rows of that adapter alone; an infinite weight of b may come out as a NaN. */
+ * A NaN or an infinity in one adapter reaches the rows of that adapter alone. */
 typedef struct {
   const void* a;
   const void* b;
@@ -129,6 +132,7 @@ typedef struct {
   uint32_t n_adapters, rank;
   void* workspace;
   size_t workspace_bytes;
+  uint32_t used;
 } bctm_lora;
 
 /* Bytes of workspace a call of these sizes, or of fewer rows, needs (host call, no GPU needed). */

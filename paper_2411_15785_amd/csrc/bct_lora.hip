@@ -60,13 +60,16 @@ LoraPlan lora_plan(uint32_t rows, uint32_t K, uint32_t width) {
 }
 
 // The addends of a float in bf16: its upper bits, those below and those below these, cut off and not rounded, so that 24 bits of it
-// are in three (an infinity or a NaN is in each).
+// are in three and all have its sign.  An addend that would be zero takes a part of the one before it, which is exact, so that an
+// infinite weight times t is one, not as 0 * inf; an infinity or a NaN is in each.
 __device__ __forceinline__ void addends_of(float t, float (&part)[3]) {
   const bool finite = fabsf(t) < INFINITY;
   part[0] = __uint_as_float(__float_as_uint(t) & 0xFFFF0000u);
   const float rest = t - part[0];
   part[1] = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u);
   part[2] = rest - part[1];
+  if (rest == 0.f) part[0] *= 0.5f, part[1] = part[0];
+  if (part[2] == 0.f) part[1] *= 0.5f, part[2] = part[1];
   if (!finite) part[0] = part[1] = part[2] = t;
 }
 // Where the operands of 16 rows x 16 ranks are written: 8 ranks of a row, the third addend in two halves.
@@ -95,7 +98,7 @@ __global__ __launch_bounds__(256) void lora_inputs_kernel(const uint16_t* __rest
                                                           const float* __restrict__ scale,
                                                           const int32_t* __restrict__ adapter, float* __restrict__ t,
                                                           uint32_t rows, uint32_t K, uint32_t width, uint32_t n, uint32_t chunks,
-                                                          uint32_t slots, uint32_t parts) {
+                                                          uint32_t slots, uint32_t parts, uint32_t rank, uint32_t used) {
   constexpr int WAVES = 4, U = 4;
   __shared__ __attribute__((aligned(16))) float sC[WAVES][RT][16][20];
   const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, jl = lane % 16, kg = lane / 16;
@@ -182,6 +185,11 @@ __global__ __launch_bounds__(256) void lora_inputs_kernel(const uint16_t* __rest
           const uint32_t j = 8 * half + k;
           sum[k] = f * ((sC[0][r][i][j] + sC[1][r][i][j]) + (sC[2][r][i][j] + sC[3][r][i][j]));
         }
+        const uint32_t col = (ct0 + c) * 16, rank0 = col - (col >= 2 * rank ? 2 * rank : col >= rank ? rank : 0u);   // of up to three segments
+        if (rank0 + 16 > used) {
+#pragma unroll
+          for (uint32_t k = 0; k < 8; ++k) sum[k] = rank0 + 8 * half + k < used ? sum[k] : 0.f;
+        }
         if (OP) {
           store_operand((u32x4*)t, (size_t)(row / 16) * tiles + ct0 + c, i, half, sum);
         } else {
@@ -240,6 +248,7 @@ bct_status check_lora(const bctm_lora* l, uint32_t rows, uint32_t K, uint32_t N,
   if (!l->a || !l->b || !l->adapter || l->n_adapters == 0 || l->rank == 0) return mfail(BCT_ERR_INVALID_ARG, "adapters: NULL pointer or zero size");
   if (swiglu != (l->b_up != nullptr)) return mfail(BCT_ERR_INVALID_ARG, "adapters: b_up goes with a SwiGLU");
   if (l->rank % 16 != 0 || l->rank > kMaxRank) return mfail(BCT_ERR_UNSUPPORTED, "adapters: rank must be a multiple of 16, at most 256");
+  if (l->used > l->rank) return mfail(BCT_ERR_INVALID_ARG, "adapters: more ranks used than there are");
   if (l->n_adapters > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many adapters");
   if ((uint64_t)tiles_of(rows, 16) * lora_plan(rows, K, segments * l->rank).chunks > 0x0FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many rows");
   if ((uint64_t)l->n_adapters * l->rank > (1ull << 56) / ((uint64_t)N + (uint64_t)segments * K)) return mfail(BCT_ERR_UNSUPPORTED, "too many adapters");
@@ -262,7 +271,7 @@ static void launch_inputs(const bctm_lora& l, const void* x, void* t, uint32_t r
   const dim3 grid((unsigned)(8 * ((work + per - 1) / per))), block(256);
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, s, (const uint16_t*)x, (const u32x4*)l.a, l.scale, l.adapter, (float*)t, rows, K,
-                       width, l.n_adapters, p.chunks, slots, p.parts);
+                       width, l.n_adapters, p.chunks, slots, p.parts, l.rank, l.used ? l.used : l.rank);
   };
   switch (p.each) {
     case 1: return launch(lora_inputs_kernel<XT, 1, RT, OP>);

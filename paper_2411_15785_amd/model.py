@@ -32,7 +32,7 @@ BCTM_ROPE_INTERLEAVED = 8
 class _bctm_lora(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("a", "b", "b_up", "scale", "adapter")] + \
         [("n_adapters", ctypes.c_uint32), ("rank", ctypes.c_uint32), ("workspace", ctypes.c_void_p),
-         ("workspace_bytes", ctypes.c_size_t)]
+         ("workspace_bytes", ctypes.c_size_t), ("used", ctypes.c_uint32)]
 
 
 _ready = False
@@ -354,9 +354,10 @@ def bctm_swiglu(x, w_gate, w_up, out=None, tiled=False):
 class LoraWeights:
     """The low-rank adapters of one projection, packed (bctm_lora_pack): n of them, each rank x K per segment and N x rank."""
 
-    def __init__(self, a, b, b_up, scale, n, segments, rank, K, N):
+    def __init__(self, a, b, b_up, scale, n, segments, rank, K, N, used=0):
         self.a, self.b, self.b_up, self.scale = a, b, b_up, scale
         self.n, self.segments, self.rank, self.K, self.N = n, segments, rank, K, N
+        self.used = used   # of rank: those the adapters had before they were filled up (0: all)
         self._sizes = {}   # rows -> bytes of workspace
 
     def workspace_bytes(self, rows):
@@ -401,7 +402,7 @@ def bctm_lora_pack(a, b, scale=None):
         p = torch.empty(n * N * r, dtype=torch.bfloat16, device=a.device)
         _ck(_launch(mlib().bctm_lora_pack, a.device, _dptr(t), _dptr(p), n * N, r), "bctm_lora_pack")
         packed.append(p)
-    return LoraWeights(pa, packed[0], packed[1] if len(packed) == 2 else None, scale, n, segments, r, K, N)
+    return LoraWeights(pa, packed[0], packed[1] if len(packed) == 2 else None, scale, n, segments, r, K, N, rank)
 
 
 def _lora_arg(lora, ids, workspace, device, rows, K, N, segments, swiglu):
@@ -419,7 +420,7 @@ def _lora_arg(lora, ids, workspace, device, rows, K, N, segments, swiglu):
         raise ValueError(f"workspace: expected contiguous torch.uint8 on {device}")
     # read by the call, which the second value outlives
     return _bctm_lora(lora.a.data_ptr(), lora.b.data_ptr(), _dptr(lora.b_up), _dptr(lora.scale), ids.data_ptr(), lora.n, lora.rank,
-                      workspace.data_ptr(), workspace.numel()), workspace
+                      workspace.data_ptr(), workspace.numel(), lora.used), workspace
 
 
 def bctm_linear_lora(x, w, lora, ids, residual=None, out=None, workspace=None):

@@ -375,3 +375,61 @@ def test_the_term_has_24_bits(M, rows, N, run):
     out = M.bctm_linear_lora(x, w, M.bctm_lora_pack(a, b), ids).double()
     t = x.double() @ a0.double()
     assert bool((out.abs() <= 2.0 ** -20 * 2 * t[:, None]).all()), (out.abs() / t[:, None]).max().item()
+
+
+@pytest.mark.parametrize("form", ["linear", "swiglu"])
+@pytest.mark.parametrize("rows,N,rank,K", [(4, 128, 16, 64), (40, 64, 8, 64), (160, 128, 40, 64), (300, 512, 1, 64), (1030, 4096, 33, 64),
+                                           (4, 128, 8, 4096), (33, 96, 50, 4096), (100, 12288, 1, 4096)])
+def test_infinities_are_those_of_the_formula(M, form, rows, N, rank, K):
+    """Ranks filled up to a multiple of 16 and addends of t multiply nothing by zero that the formula does not.  Positive
+    throughout: an infinite activation, an infinite entry of A and one of B each make infinities, and no NaN.  (An infinite
+    activation that is a NaN in the plain projection of few rows already, which the header allows, is not looked at.)"""
+    n, mats = 3, 2 if form == "swiglu" else 1
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    r = lambda *s: (torch.rand(s, generator=g, device="cuda") + 0.5).bfloat16()
+    x, w = r(rows, K), [M.bctm_pack_weight(r(N, K)) for _ in range(mats)]
+    a, b = r(n, mats, rank, K), [r(n, N, rank) for _ in range(mats)]
+    a[2, :, rank // 2, 5] = float("inf")
+    for t in b:
+        t[1, 7::10, rank - 1] = float("inf")
+    bad = torch.arange(rows, device="cuda") % 5 == 3
+    x[bad, 11] = float("inf")
+    call = M.bctm_swiglu_lora if form == "swiglu" else M.bctm_linear_lora
+    lora = M.bctm_lora_pack(a, b)
+    looked_at = ~torch.isnan((M.bctm_swiglu if form == "swiglu" else M.bctm_linear)(x, *w).float())
+    assert bool(looked_at.all()) or K == 64 and rows < 128
+    for run in (1, 16, 400):      # tiles of several adapters and of one
+        ids = (torch.arange(rows, device="cuda") // run % (n + 1) - 1).to(torch.int32)
+        out = call(x, *w, lora, ids).float()
+        inf = (bad | (ids == 2))[:, None].expand(rows, N).clone()
+        inf[:, 7::10] |= (ids == 1)[:, None]
+        assert torch.equal((out == float("inf"))[looked_at], inf[looked_at]) and not torch.isnan(out[looked_at]).any(), run
+
+
+@pytest.mark.parametrize("rows,N", [(40, 64), (160, 128), (1030, 4096)])
+@pytest.mark.parametrize("what", ["any", "few bits"])
+def test_an_infinite_weight_takes_the_sign_of_its_product(M, rows, N, what):
+    """t of either sign, with bits in all of its addends or in the first alone."""
+    K, rank = 32, 16
+    g = torch.Generator(device="cuda").manual_seed(N)
+    x = torch.randn((rows, K), generator=g, device="cuda").bfloat16()
+    a, b = torch.zeros((1, rank, K), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, N, rank), dtype=torch.bfloat16, device="cuda")
+    if what == "any":
+        a[0, 3] = torch.randn(K, generator=g, device="cuda").bfloat16()
+    else:
+        a[0, 3, 9] = 0.5
+        x[:, 9] = torch.where(x[:, 9] < 0, -1.0, 2.0)
+    b[0, ::3, 3] = float("inf")
+    b[0, 1::3, 3] = -float("inf")
+    b[0, 2::3, 3] = 1.0
+    t = (x.double() @ a[0, 3].double())
+    w = M.bctm_pack_weight(torch.zeros((N, K), dtype=torch.bfloat16, device="cuda"))
+    for ids in (torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.arange(rows, device="cuda").to(torch.int32) % 2):
+        out = M.bctm_linear_lora(x, w, M.bctm_lora_pack(a, b), ids).double()
+        mine = ids == 0
+        inf = torch.full_like(t, float("inf"))[:, None] * t.sign()[:, None]
+        assert bool((out[mine][:, ::3] == inf[mine]).all()) and bool((out[mine][:, 1::3] == -inf[mine]).all())
+        # one term of at most 32 products, rounded to bf16: 2^-8, and the sum's 2^-20 of the products' absolute values
+        slack = 2.0 ** -8 * t.abs() + 2.0 ** -20 * (x.double().abs() @ a[0, 3].double().abs())
+        assert bool(((out[mine][:, 2::3] - t[mine][:, None]).abs() <= slack[mine][:, None]).all())
+        assert bool((out[~mine] == 0).all())

@@ -155,3 +155,8 @@ def test_new_adapters_leave_the_workspaces_of_old_ones():
     assert held() is not None
     stack.set_adapters(adapters(16))
     assert stack._lora_workspace(3) is large and held() is not None
+
+
+def test_no_more_ranks_are_used_than_there_are(ML):
+    assert ML.bctm_linear_lora(A, B, None, C, 4, 64, 32, 0, lora_args(used=17), None) == P.BCT_ERR_INVALID_ARG
+    assert b"ranks" in ML.bctm_last_error()
