@@ -11,6 +11,8 @@
 // 16384 rows x 64 heads of 128 bf16 (537 MB): 94 us, 5.7 TB/s (a copy of 1 GB reaches 6.1); 1 row 3.2 us, the launch.
 #include <math.h>
 
+#include <type_traits>
+
 #include "bct_device.h"
 #include "bct_model_internal.h"
 
@@ -29,25 +31,36 @@ struct HeadBlock {   // the heads of one input: rows of n heads side by side, ld
 enum RopePairs { kNoRotation, kHalves, kNeighbours };
 
 // cos and sin of position * inv_freq.  The angle is a product in 64 bits and loses its whole turns there: in 32 bits a
-// position of 2^20 would leave 0.06 of a radian unknown.  What remains, less its nearest quarter turn, is at most pi / 4, where
-// the Taylor series of degree 9 and 10 are within 2e-9 of sine and cosine.
+// position of 2^20 would leave 0.06 of a radian unknown.  What remains, less its nearest quarter turn, is at most pi / 4; R is
+// the type that it goes on in.  float, for bf16 heads: the Taylor series of degree 9 and 10 are within 2e-9, and roundings leave less than
+// 2^-23, of which the output's rounding leaves nothing.  double, for fp32 heads: degree 11 and 12, within 7e-12, and one rounding to fp32.
+template <typename R>
 __device__ __forceinline__ void turn_of(int32_t position, double inv_freq, float* c, float* s) {
   const double turns = (double)position * inv_freq * 0.15915494309189533577;
   const double quarters = rint(4.0 * turns);
-  const float x = (float)((turns - 0.25 * quarters) * 6.28318530717958647692);
+  const R x = (R)((turns - 0.25 * quarters) * 6.28318530717958647692);
   const float q = (float)(quarters - 4.0 * floor(0.25 * quarters));   // 0 to 3: which quarter turn
-  const float z = x * x;
-  float sn = __builtin_fmaf(z, 2.7557319e-6f, -1.9841270e-4f);
-  sn = __builtin_fmaf(z, sn, 8.3333333e-3f);
-  sn = __builtin_fmaf(z, sn, -1.6666667e-1f);
-  sn = __builtin_fmaf(z * x, sn, x);
-  float cs = __builtin_fmaf(z, -2.7557319e-7f, 2.4801587e-5f);
-  cs = __builtin_fmaf(z, cs, -1.3888889e-3f);
-  cs = __builtin_fmaf(z, cs, 4.1666667e-2f);
-  cs = __builtin_fmaf(z, cs, -0.5f);
-  cs = __builtin_fmaf(z, cs, 1.0f);
+  const R z = x * x;
+  auto fma = [](R a, R b, R c) -> R {
+    if constexpr (sizeof(R) == 4) return __builtin_fmaf(a, b, c);
+    else return __builtin_fma(a, b, c);
+  };
+  R sn = (R)(1.0 / 362880), cs = (R)(-1.0 / 3628800);
+  if constexpr (sizeof(R) == 8) {
+    sn = fma(z, -1.0 / 39916800, sn);
+    cs = fma(z, 1.0 / 479001600, cs);
+  }
+  sn = fma(z, sn, (R)(-1.0 / 5040));
+  sn = fma(z, sn, (R)(1.0 / 120));
+  sn = fma(z, sn, (R)(-1.0 / 6));
+  sn = fma(z * x, sn, x);
+  cs = fma(z, cs, (R)(1.0 / 40320));
+  cs = fma(z, cs, (R)(-1.0 / 720));
+  cs = fma(z, cs, (R)(1.0 / 24));
+  cs = fma(z, cs, (R)-0.5);
+  cs = fma(z, cs, (R)1.0);
   const bool odd = q == 1.f || q == 3.f;
-  const float a = odd ? sn : cs, b = odd ? cs : sn;
+  const float a = (float)(odd ? sn : cs), b = (float)(odd ? cs : sn);
   *c = q == 1.f || q == 2.f ? -a : a;
   *s = q >= 2.f ? -b : b;
 }
@@ -85,7 +98,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(HeadBlock q, HeadBloc
     if (mine && turned) {
       const int32_t at = positions[row];
 #pragma unroll
-      for (uint32_t e = 0; e < E; ++e) turn_of(at, inv_freq[E * l + e], &cs[e], &sn[e]);
+      for (uint32_t e = 0; e < E; ++e) turn_of<std::conditional_t<E == 4, double, float>>(at, inv_freq[E * l + e], &cs[e], &sn[e]);
     } else {
 #pragma unroll
       for (uint32_t e = 0; e < E; ++e) {

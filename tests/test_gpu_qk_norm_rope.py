@@ -216,3 +216,19 @@ def test_one_row_at_any_distance(M):
     for t in (q, odd):
         got, _ = M.bctm_qk_norm_rope(t, eps=1e-6, q_out=torch.empty_like(want))
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_sine_and_cosine_of_fp32_heads_are_rounded_once(M, interleaved):
+    """Pairs (1, 0) become (cos, sin) themselves: within half a step, 2^-24 of the value, 2^-30 of it for the series in 64 bits, and the
+    angle's three roundings of 2^-53 of its size."""
+    rows, d = 5000, 64
+    pos, fr = (torch.arange(rows, dtype=torch.int32) * 7 - 9000).cuda(), freqs(d).cuda()
+    q = torch.zeros((rows, 1, d), device="cuda")
+    a, b = (slice(0, d, 2), slice(1, d, 2)) if interleaved else (slice(0, d // 2), slice(d // 2, d))
+    q[..., a] = 1.0
+    got = M.bctm_qk_norm_rope(q, positions=pos, inv_freq=fr, interleaved=interleaved)[0].double().cpu().numpy()[:, 0]
+    t = pos.cpu().numpy().astype(np.longdouble)[:, None] * fr.cpu().numpy().astype(np.longdouble)
+    for part, want in ((a, np.cos(t)), (b, np.sin(t))):
+        err = np.abs(got[:, part].astype(np.longdouble) - want)
+        assert np.all(err <= np.abs(want) * (2.0 ** -24 + 2.0 ** -30) + 3 * 2.0 ** -53 * np.abs(t))
