@@ -232,3 +232,32 @@ def test_sine_and_cosine_of_fp32_heads_are_rounded_once(M, interleaved):
     for part, want in ((a, np.cos(t)), (b, np.sin(t))):
         err = np.abs(got[:, part].astype(np.longdouble) - want)
         assert np.all(err <= np.abs(want) * (2.0 ** -24 + 2.0 ** -30) + 3 * 2.0 ** -53 * np.abs(t))
+
+
+@pytest.mark.parametrize("rows,Hq,Hkv,d,rot,dtype,interleaved", [
+    (20011, 32, 1, 128, 128, "bf16", False), (20011, 32, 2, 128, 64, "bf16", True), (10007, 32, 1, 128, 128, "f32", False),
+    (2000, 32, 1, 128, 128, "bf16", False), (1003, 4, 1, 256, 256, "f32", True), (17001, 5, 0, 64, 32, "bf16", False), (9001, 3, 2, 112, 112, "f32", False)])
+def test_many_rows_and_odd_numbers_of_heads(M, rows, Hq, Hkv, d, rot, dtype, interleaved):
+    """Two heads a group of lanes with one left over; more than 256 MB, which goes past the caches.  Parts of wider rows, into
+    tensors of their own and in place: each row has the bits of a call with few rows, and those are right."""
+    pos, fr = (torch.arange(rows, dtype=torch.int32) % 5000).cuda(), freqs(rot).cuda()
+    x = torch.randn((rows, Hq + Hkv + 1, d), generator=torch.Generator(device="cuda").manual_seed(rows), device="cuda").to(DT[dtype])
+    q, k = x[:, :Hq], x[:, Hq:Hq + Hkv] if Hkv else None
+    gq, gk = draw((d,), dtype, 3), draw((d,), dtype, 4) if Hkv else None
+    before = x.clone()
+    qo, ko = M.bctm_qk_norm_rope(q, k, gq, gk, 1e-6, pos, fr, interleaved)
+    assert torch.equal(x, before)
+    for at in (0, rows // 2, rows - 40):
+        s = slice(at, at + 40)
+        a, b = M.bctm_qk_norm_rope(q[s], k[s] if Hkv else None, gq, gk, 1e-6, pos[s].contiguous(), fr, interleaved)
+        check(a, q[s], gq, 1e-6, pos[s], fr, interleaved, dtype, f"q from {at}")
+        assert torch.equal(a, qo[s])
+        if Hkv:
+            check(b, k[s], gk, 1e-6, pos[s], fr, interleaved, dtype, f"k from {at}")
+            assert torch.equal(b, ko[s])
+    for at in range(0, rows, 1000):     # all of them
+        s = slice(at, min(rows, at + 1000))
+        a, b = M.bctm_qk_norm_rope(q[s], k[s] if Hkv else None, gq, gk, 1e-6, pos[s].contiguous(), fr, interleaved)
+        assert torch.equal(a, qo[s]) and (not Hkv or torch.equal(b, ko[s])), at
+    M.bctm_qk_norm_rope(q, k, gq, gk, 1e-6, pos, fr, interleaved, q_out=q, k_out=k)
+    assert torch.equal(q, qo) and (not Hkv or torch.equal(k, ko)) and torch.equal(x[:, Hq + Hkv:], before[:, Hq + Hkv:])

@@ -255,3 +255,34 @@ def test_rows_that_fill_their_registers_or_do_not(M, N, dtype):
     check(M, x, u, t=0.9, what="temperature")
     check(M, x, u, t=0.9, k=N // 2, p=0.97, m=1e-7, what="all")
     check(M, x, np.full(rows, 0.99999994), t=3.0, what="the far end")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [1000, 20011, 131072, 131085])
+def test_weights_over_the_whole_range_of_the_type(M, N, dtype):
+    """Temperatures at which logits of both signs and of magnitudes from 1 to 1e38 all have weights: more values than are counted
+    at a time (36864 of bf16), thresholds on either side of that border, ties there, and masked tokens beside them."""
+    rows = 12
+    g = torch.Generator().manual_seed(N)
+    near = torch.tensor([1.0, -1.0, 0.0, 1e5, -1e5, -3e9, -3e10, -1e11, -2e11, -1e20])
+    far = torch.tensor([3e38, 1e38, -1e38, -2e38, 1e30, -1e30, 1e-3, -1e-3, -3e38, 1e38])
+    pick = torch.randint(0, 10, (rows, N), generator=g)
+    x = torch.where(torch.arange(rows)[:, None] % 2 == 0, near[pick] * (0.5 + torch.rand((rows, N), generator=g)),
+                    far[pick] * (0.25 + 0.75 * torch.rand((rows, N), generator=g)))
+    x[2, x[2] > 0] *= 1e-5                     # the largest value next to 1
+    x[4] = near[pick[4]]                       # few values, each of many tokens
+    x[5] = far[pick[5]]
+    x[6:9, ::3] = -float("inf")
+    x[7, 1::5] = float("nan")
+    x = x.to(DT[dtype]).cuda()
+    t = np.array([1e10, 1e37, 3e10, 1e38, 1e11, 3e38, 1e20, 5e37, 1e12, 2e37, 1e21, np.inf], np.float32)
+    k = np.array([N // 2, 1, 7 * N // 10, 9 * N // 10, N // 3, N // 4, N // 2, N // 3, 5, N - 3, 8 * N // 10, N // 2])
+    p = np.array([0.3, 0.7, 0.9, 0.95, 0.6, 0.8, 0.99, 0.4, 0.85, 0.999, 0.2, 0.65])
+    m = np.array([0.9, 0.2, 0.5, 0.01, 1e-6, 0.3, 0.99, 0.05, 1e-9, 0.7, 0.999, 0.1])
+    for s, u in enumerate((uniform(rows, N + 1), uniform(rows, N + 2) * 0.05, 1.0 - 0.05 * uniform(rows, N + 3))):
+        check(M, x, u, t=t, what=f"temperature {s}")
+        check(M, x, u, t=t, k=k, what=f"top-k {s}")
+        check(M, x, u, t=t, p=p, what=f"top-p {s}")
+        check(M, x, u, t=t, m=m, what=f"min-p {s}")
+        check(M, x, u, t=t, k=k, p=p, m=m, what=f"all {s}")
+        check(M, x, u, t=np.roll(t, 2), k=np.roll(k, 1), p=np.roll(p, 3), m=np.roll(m, 4), what=f"all, others {s}")
