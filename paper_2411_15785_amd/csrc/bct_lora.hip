@@ -42,11 +42,20 @@ LoraPlan lora_plan(uint32_t rows, uint32_t K, uint32_t width) {
   p.chunks = (tiles + 3) / 4;
   p.each = (tiles + p.chunks - 1) / p.chunks;
   // Row tiles of a workgroup: more of them read A fewer times where rows share an adapter, and multiply each adapter with more rows
-  // of others where they do not, which the host cannot see.  us of the whole first half, 1 | 2 | 4 row tiles, rows in runs of 512: 1024
-  // rows, K = 4096, rank 16 5.0 | 5.4 | 5.8, rank 64 9.0 | 9.8 | 10.6; 4096 rows 9.2 | 8.2 | 10.0, 18.0 | 16.4 | 19.6, K = 11008, rank 64
-  // 29.6 | 26.1 | 27.8; 16384 28 | 27 | 29, 56 | 50 | 48, 143 | 106 | 93; a whole call, 3587 rows of 6 adapters from memory 302 | - | 289.
-  // An adapter for each row: 1024 rows 15.9 | 20.6 | 44.4, 4096 45.9 | 53.5 | 105.
-  p.row_tiles = rows < 2048 ? 1 : p.each < 3 ? 2 : 4;
+  // of others where they do not, which the host cannot see: two from 12 million activations on, four from 36 million where they
+  // also share what is loaded of x between three column tiles or more.  us of a call with 128 features, 1 | 2 | 4 row tiles, rows of 8 adapters
+  // in runs of 512; of 60; of 64 adapters in turn:
+  //   2048 x 4096 rank 64      29.4 | 30.6 | 30.4     34.0 | 35.8 | 34.9     108 | 148 | 188
+  //   4096 x 1024 rank 64      17.3 | 21.8 | 20.5     20.5 | 26.1 | 25.5     85 | 143 | 184
+  //   1500 x 11008 rank 16     48.6 | 48.7 | 49.3     52.7 | 50.6 | 51.1     104 | 113 | 143
+  //   3000 x 11008 rank 64     64.7 | 60.7 | 61.0     87.3 | 72.6 | 69.5     314 | 357 | 502
+  //   8192 x 4096 rank 32      35.9 | 36.3 | 37.7     39.1 | 39.6 | 40.7     179 | 190 | 261
+  //   8192 x 4096 rank 128     55.5 | 53.3 | 53.8     85.2 | 71.9 | 65.3     518 | 542 | 690
+  //   4096 x 11008 rank 64     73.4 | 67.4 | 66.7     92.4 | 83.8 | 78.4     379 | 434 | 563
+  //   16384 x 4096 rank 16     61.6 | 55.6 | 60.8     62.7 | 60.3 | 64.7     326 | 319 | 361
+  //   16384 x 4096 rank 128    109 | 93.6 | 86.0      145 | 133 | 114        983 | 1040 | 1315
+  const uint64_t x = (uint64_t)rows * K;
+  p.row_tiles = x < 12u << 20 ? 1 : x < 36u << 20 || p.each < 3 ? 2 : 4;
   // As many parts as give the chip one or two workgroups a compute unit, each wavefront at least two steps of 32 inputs.  us, one
   // | two: 1024 rows, 1 row tile, runs of 512 5.0 | 5.4, rank 64 9.0 | 10.0, an adapter for each row 14.5 | 15.9, 37 | 50; the call
   // of 3587 rows, 4 row tiles, 298 | 290.
@@ -273,11 +282,11 @@ static void launch_inputs(const bctm_lora& l, const void* x, void* t, uint32_t r
     hipLaunchKernelGGL(kernel, grid, block, 0, s, (const uint16_t*)x, (const u32x4*)l.a, l.scale, l.adapter, (float*)t, rows, K,
                        width, l.n_adapters, p.chunks, slots, p.parts, l.rank, l.used ? l.used : l.rank);
   };
-  switch (p.each) {
-    case 1: return launch(lora_inputs_kernel<XT, 1, RT, OP>);
-    case 2: return launch(lora_inputs_kernel<XT, 2, RT, OP>);
-    case 3: return launch(lora_inputs_kernel<XT, 3, RT, OP>);
-    default: return launch(lora_inputs_kernel<XT, 4, RT, OP>);
+  if (p.each == 4) return launch(lora_inputs_kernel<XT, 4, RT, OP>);
+  if (p.each == 3) return launch(lora_inputs_kernel<XT, 3, RT, OP>);
+  if constexpr (RT < 4) {   // lora_plan: four row tiles with three column tiles or more
+    if (p.each == 2) return launch(lora_inputs_kernel<XT, 2, RT, OP>);
+    return launch(lora_inputs_kernel<XT, 1, RT, OP>);
   }
 }
 template <bool XT>

@@ -433,3 +433,24 @@ def test_an_infinite_weight_takes_the_sign_of_its_product(M, rows, N, what):
         slack = 2.0 ** -8 * t.abs() + 2.0 ** -20 * (x.double().abs() @ a[0, 3].double().abs())
         assert bool(((out[mine][:, 2::3] - t[mine][:, None]).abs() <= slack[mine][:, None]).all())
         assert bool((out[~mine] == 0).all())
+
+
+@pytest.mark.parametrize("N", [64, 128])          # the streaming kernel, the matrix cores
+@pytest.mark.parametrize("rows,K,rank,n,run", [
+    # two row tiles a workgroup in the first half, one to four column tiles; four row tiles, three and four of them
+    (3101, 4128, 16, 5, 100), (3101, 4128, 25, 30, 1), (3100, 4128, 48, 6, 300), (13000, 992, 64, 9, 37), (3443, 11040, 48, 7, 50),
+    (3443, 11040, 64, 4, 1000), (9002, 4224, 112, 20, 3)])
+def test_row_tiles_of_the_first_half(M, rows, K, rank, n, run, N):
+    c = Case(rows, K, N, rank, n)
+    (w,), lora = c.pack(M)
+    ids = adapters(rows, n, rows + N, run)
+    cols = torch.arange(N, device="cuda")
+    y, slack = c.product(ids, 0, torch.zeros(N, device="cuda"), cols)
+    size = lora.workspace_bytes(rows)
+    ws = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    out = M.bctm_linear_lora(c.x, w, lora, ids, workspace=ws[:size])
+    close(out, y, slack, "linear")
+    assert bool((ws[size:] == 0x5A).all())
+    close(M.bctm_linear_lora(M.bctm_pack_rows(c.x), w, lora, ids), y, slack, "linear, tiled x")
+    none = (ids < 0) | (ids >= n)
+    assert same(out[none], M.bctm_linear(c.x, w)[none])
