@@ -194,8 +194,10 @@ bct_status rope_group(const RopeCall& c) {
   const uint32_t lanes = c.d / (2 * DT::kElemsPerVec);
   if (lanes <= 4) return rope_heads<DT, NORM, PAIRS, 4>(c);
   if (lanes <= 8) return rope_heads<DT, NORM, PAIRS, 8>(c);
-  if (lanes <= 16) return rope_heads<DT, NORM, PAIRS, 16>(c);
-  return rope_heads<DT, NORM, PAIRS, 32>(c);
+  if constexpr (DT::kElemsPerVec == 4) {   // a bf16 head has at most 16 lanes
+    if (lanes > 16) return rope_heads<DT, NORM, PAIRS, 32>(c);
+  }
+  return rope_heads<DT, NORM, PAIRS, 16>(c);
 }
 template <typename DT>
 bct_status rope_form(const RopeCall& c, bool norm, RopePairs pairs) {
