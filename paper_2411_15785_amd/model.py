@@ -614,7 +614,8 @@ class BctStack:
                             or a.a.device != self.embed.device:
                         raise ValueError(f"layer {l} {n}: expected LoraWeights of (K, N, segments) {want.get(n, tuple(want))[:3]} "
                                          f"on {self.embed.device}")
-        self.adapters = layers
+        # a dictionary that changes afterwards would go past the checks
+        self.adapters = None if layers is None else [dict(d) for d in layers]
         self._lora_now.clear()
 
     def _lora_workspace(self, rows):

@@ -160,3 +160,14 @@ def test_new_adapters_leave_the_workspaces_of_old_ones():
 def test_no_more_ranks_are_used_than_there_are(ML):
     assert ML.bctm_linear_lora(A, B, None, C, 4, 64, 32, 0, lora_args(used=17), None) == P.BCT_ERR_INVALID_ARG
     assert b"ranks" in ML.bctm_last_error()
+
+
+def test_set_adapters_are_those_that_were_checked():
+    torch = pytest.importorskip("torch")
+    s = model.StackShape(n_layers=1, dim=64, n_q_heads=1, n_kv_heads=1, head_dim=32, ffn=64, vocab=16, capacity_M=64, batch=3)
+    stack = object.__new__(model.BctStack)     # no GPU: the bookkeeping alone
+    stack.shape, stack.embed, stack._lora_now = s, torch.empty(0), {}
+    own = [{"o": model.LoraWeights(torch.empty(0), None, None, None, 1, 1, 16, s.q_width, s.dim)}]
+    stack.set_adapters(own)
+    own[0]["down"] = None
+    assert set(stack.adapters[0]) == {"o"}
