@@ -55,7 +55,8 @@ bct_status bctm_rmsnorm(const void* x, const void* gain, void* out, uint32_t row
  *   y = x * rsqrt(mean(x^2) + eps) * gain                               with BCTM_HEAD_NORM
  *   (y_a, y_b) = (y_a cos t - y_b sin t, y_a sin t + y_b cos t)         t = positions[r] * inv_freq[j], j < rotary_dim / 2
  * a = j and b = j + rotary_dim / 2, or with BCTM_ROPE_INTERLEAVED a = 2 j and b = 2 j + 1; elements from rotary_dim on pass.
- * fp32 arithmetic (the angle in 64 bits, for any position of an int32), one rounding.
+ * fp32 arithmetic (the angle in 64 bits, for any position of an int32), one rounding.  The memory's keys do not turn, so scores
+ * depend on a token's own position, not on a distance.
  * q: rows of n_q_heads heads side by side, q_ld elements from row to row (any distance of 64 bits), so heads are taken out of a
  * wider row (q | wq | wv) where they lie; k likewise, or NULL with n_kv_heads = 0.  An output may be its own input (same row distance); apart from
  * that no output shares memory with an input or the other output.  q_gain, k_gain [head_dim], NULL = ones.  positions int32
@@ -181,8 +182,8 @@ bct_status bctm_argmax(const void* logits, int32_t* ids, uint32_t rows, uint32_t
  * taken as 0, above as the last number before 1; all device memory.  A temperature of 0 (or below, or NaN) draws the most likely
  * token, bctm_argmax's but for NaN; NaN elsewhere switches that setting off.  Infinite logits share the draw equally.
  * ids int32 [rows]: the tokens, -1 in a row that has none left; prob float32 [rows] or NULL: w / cum(n) of each, 0 with -1.
- * Weights and sums have 40 to 46 bits behind the binary point of the largest weight, added as integers: equal calls draw
- * equal tokens.  N at most 4194304. */
+ * Weights and sums have 46 bits behind the binary point of the largest weight (62 less log2 N beyond 65536 tokens), added as integers:
+ * equal calls draw equal tokens, and a tail of smaller weights is not there.  N at most 4194304. */
 bct_status bctm_sample(const void* logits, size_t ld, const float* temperature, const int32_t* top_k, const float* top_p,
                        const float* min_p, const float* u, int32_t* ids, float* prob, uint32_t rows, uint32_t N,
                        int32_t dtype, void* hip_stream);

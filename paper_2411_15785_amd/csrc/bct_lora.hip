@@ -11,9 +11,9 @@
 // other, on v_mfma_f32_16x16x32_bf16 (rows = token rows, columns = ranks); rows of other adapters go through the product as
 // well and are not stored.  What fills the chip when rows are few: the adapters of a row tile are dealt out to several
 // workgroups, and so is K, in parts that the second half (a decode batch) or a small kernel (many rows) adds up.
-// 32 rows of 32 adapters, K = 4096, three segments of rank 16 (12.6 MB of A): 5.5 us; 3587 rows, K = 11008, rank 64 (79 MB of x): 29 us, and
-// 6 for the parts' sums.  Whole calls, without | with: three outputs of 4096 each 19.2 | 27.5, SwiGLU 2048 x 4096 x 11008 of rank 32 267 |
-// 290, 3587 x 11008 x 4096 244 | 285.
+// 32 rows of 32 adapters, K = 4096, three segments of rank 16 (12.6 MB of A): 5.8 us; 3587 rows, K = 11008, rank 64 (79 MB of x): 27 us, and
+// 5 for the parts' sums.  Whole calls, without | with: three outputs of 4096 each 19.2 | 27.7, SwiGLU 2048 x 4096 x 11008 of rank 32 267 |
+// 296, 3587 x 11008 x 4096 247 | 287.
 #include "bct_lora.h"
 
 #include <algorithm>

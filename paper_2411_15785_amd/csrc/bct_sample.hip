@@ -18,8 +18,9 @@
 // Equal values have equal weights, so the rest is a division, and the token the nth with its value in the order of the indexes.
 // One workgroup a row, which it keeps in registers (bf16 up to 131072 tokens, fp32 65536; beyond, it is read again).
 // Bound by the latency of a workgroup's steps, with long rows by its compute unit: loading a row, counting it in LDS, the 64-bit
-// weights of fp32 tokens.  us in a graph, temperature and top-p: bf16 1 x 32000 15.5, 32 x 32000 17, 24 x 65536 21, 128 x 131072 29.6;
-// fp32 24 x 4096 15.5, 32000 24, 50001 34, 131072 85.
+// weights of fp32 tokens.  us in a graph, temperature and top-p: bf16 1 x 32000 15.5, 32 x 32000 16, 24 x 65536 19, 128 x 131072 29.6,
+// 32 x 131072 26.5, 152064 38, 262144 53; fp32 24 x 4096 15.5, 32000 24, 50001 34 (this size spills 21 registers), 131072 87; with temperature
+// alone fp32 32000 20, 50001 30, 131072 78.
 #include <math.h>
 
 #include "bct_device.h"
