@@ -101,11 +101,11 @@ struct LoraTiles {
   }
 };
 
-// Adds the term of RT tiles of 16 rows (from row0) to the accumulators acc(i, j), which are those of the K loop and have nothing else
-// yet.  Each row's sum is one chain over its own adapter's ranks in their
-// order, whether its tile has one adapter or several, so its bits do not depend on its neighbours: a matrix instruction sums
-// every row apart, and where a tile's rows have several adapters, its result is selected for the rows of the one that was
-// multiplied.  Selected, not multiplied by zero, so an infinity or a NaN in one adapter's weights stays in its rows.
+// Adds the term of RT tiles of 16 rows (from row0) to the accumulators acc(i, j), which are those of the K loop and hold nothing
+// else yet.  Each row's sum is one chain over its own adapter's ranks in their order, whether its tile has one adapter or several,
+// so its bits do not depend on its neighbours: a matrix instruction sums every row apart, and where a tile's rows have
+// several adapters, its result is selected for the rows of the one that was multiplied.  Selected, not multiplied by zero, so
+// an infinity or a NaN in one adapter's weights stays in its rows.
 template <int RT, int CT, int MATS, typename SEG, typename TILE, typename ACC>
 __device__ __forceinline__ void lora_add(const LoraTiles<CT, MATS, SEG, TILE>& T, uint32_t row0, uint32_t rows, ACC acc) {
   const uint32_t last = (rows - 1) / 16, n = T.L.n, steps = T.L.rank / 16;

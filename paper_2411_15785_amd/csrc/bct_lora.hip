@@ -243,7 +243,8 @@ __global__ __launch_bounds__(256) void lora_pack_kernel(const uint16_t* __restri
   packed[c] = *(const u32x4*)(b + n * rank + c / 16 % (rank / 8) * 8);
 }
 
-// Room for the parts in fp32 and for the operands, which are whole tiles of 16 rows with four bf16 for each t: for any number of rows up to this one.  Where
+// Room for the parts in fp32 and for the operands, which are whole tiles of 16 rows with four bf16 for each t: for any number of
+// rows up to this one.  Where
 // K is in several parts, they and the workgroups are at most kGroupsMany.
 size_t lora_bytes(uint32_t rows, uint32_t width) {
   const uint32_t tiles = tiles_of(rows, 16), split = kMostRowTiles * (kGroupsMany / ((width / 16 + 3) / 4));
