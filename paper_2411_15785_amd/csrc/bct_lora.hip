@@ -244,8 +244,7 @@ __global__ __launch_bounds__(256) void lora_pack_kernel(const uint16_t* __restri
 }
 
 // Room for the parts in fp32 and for the operands, which are whole tiles of 16 rows with four bf16 for each t: for any number of
-// rows up to this one.  Where
-// K is in several parts, they and the workgroups are at most kGroupsMany.
+// rows up to this one.  Where K is in several parts, they and the workgroups are at most kGroupsMany.
 size_t lora_bytes(uint32_t rows, uint32_t width) {
   const uint32_t tiles = tiles_of(rows, 16), split = kMostRowTiles * (kGroupsMany / ((width / 16 + 3) / 4));
   const size_t parts = std::max<size_t>(tiles, std::min<size_t>((size_t)kMostParts * tiles, split));
