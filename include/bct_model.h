@@ -152,6 +152,64 @@ bct_status bctm_linear_split_lora(const void* x, const void* w_packed, void* out
 bct_status bctm_swiglu_lora(const void* x, const void* w_gate_packed, const void* w_up_packed, void* out, uint32_t rows,
                             uint32_t K, uint32_t N, uint32_t flags, const bctm_lora* lora, void* hip_stream);
 
+/* out[r][n] = (residual ? residual[r][n] : 0) + act((bias ? bias[n] : 0) + sum_k x[r][k] * w[n][k]), everything after the sum in fp32 and
+ * rounded once.  bias: bf16 [N].  act: one of BCTM_ACT_.  flags: BCTM_X_TILED as in bctm_linear; BCTM_OUT_F32: out is float32
+ * (a router's logits), else bf16; BCTM_OUT_TILED: bf16 as tiled activations (N a multiple of 32).  residual: bf16, row-major; a
+ * row-major bf16 out may be the residual.  Shapes, kernels and sums as in bctm_linear. */
+#define BCTM_OUT_F32 16u
+#define BCTM_ACT_NONE 0u
+#define BCTM_ACT_RELU 1u
+#define BCTM_ACT_SILU 2u      /* y / (1 + exp(-y)) */
+#define BCTM_ACT_GELU 3u      /* y (1 + erf(y / sqrt 2)) / 2 */
+#define BCTM_ACT_GELU_TANH 4u /* y (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))) / 2 */
+#define BCTM_ACT_SIGMOID 5u   /* 1 / (1 + exp(-y)) */
+bct_status bctm_linear_act(const void* x, const void* w_packed, const void* bias, const void* residual, void* out, uint32_t rows,
+                           uint32_t K, uint32_t N, uint32_t act, uint32_t flags, void* hip_stream);
+
+/* Layers with experts: a token goes through k of n_experts MLPs, chosen by a router, and gets the sum of their outputs, weighted.
+ * A pair is a token and one of its slots, number token * k + slot.  n_experts at most 512, k at most 16 and n_experts.
+ *
+ * bctm_route: each token's experts and their weights from its logits [rows], n_experts each, ld >= n_experts elements from row to
+ * row, float32 or bf16 (dtype), aligned to their type.
+ *   p       softmax of the logits, or with BCTM_ROUTE_SIGMOID 1 / (1 + exp(-logit)) of each
+ *   chosen  the k experts with the largest logit, or with a bias (float32 [n_experts]) the largest p + bias, which is compared
+ *           in 64 bits; in descending order, equal ones by number.  A logit of NaN or -inf (or a bias of these) is never chosen.
+ *   weight  scale * p, with BCTM_ROUTE_NORMALISE divided by the sum of the chosen p
+ * experts int32 [rows][k], weights float32 [rows][k]: -1 and 0 in slots for which no expert is left (a padding row: all logits -inf).
+ * plan: the pairs by expert, for the calls below (or NULL).
+ *
+ * bctm_expert_plan: the same plan for experts that the caller chose; outside [0, n_experts): none.
+ *
+ * A plan is 16-byte aligned device memory of at least bctm_expert_plan_bytes bytes and holds for the sizes it was made for; calls only read
+ * it.  As int32 it begins with offsets [n_experts + 1], and at *order (if that is asked for) is order [rows * k]:
+ * the pairs of expert e are order[offsets[e]] .. order[offsets[e + 1] - 1], by number, and those without an expert follow the last.
+ */
+#define BCTM_ROUTE_SIGMOID 1u
+#define BCTM_ROUTE_NORMALISE 2u
+bct_status bctm_expert_plan_bytes(uint32_t rows, uint32_t k, uint32_t n_experts, size_t* bytes, size_t* order);
+bct_status bctm_route(const void* logits, size_t ld, const float* bias, int32_t* experts, float* weights, void* plan,
+                      size_t plan_bytes, uint32_t rows, uint32_t n_experts, uint32_t k, float scale, int32_t dtype, uint32_t flags,
+                      void* hip_stream);
+bct_status bctm_expert_plan(const int32_t* experts, void* plan, size_t plan_bytes, uint32_t rows, uint32_t n_experts, uint32_t k,
+                            void* hip_stream);
+
+/* out[p][n] = silu(g) * u for every pair p with an expert e: g = sum_j x[p / k][j] w_gate[e][n][j], u likewise with w_up; rows of
+ * pairs without one are left as they were.  x [rows][K], out [rows * k][N], row-major; w_gate, w_up: the matrices [N][K] of
+ * all experts one below the other, each packed by one bctm_pack_weight of n_experts * N features (or expert by expert).  K a multiple
+ * of 32, N of 16.  fp32 accumulation, one rounding.  A row's bits depend on the sizes of the call alone, not on the other tokens'
+ * experts. */
+bct_status bctm_expert_swiglu(const void* x, const void* w_gate_packed, const void* w_up_packed, void* out, const void* plan,
+                              uint32_t rows, uint32_t k, uint32_t n_experts, uint32_t K, uint32_t N, void* hip_stream);
+
+/* out[r][n] = (residual ? residual[r][n] : 0) + sum over the slots s of r with an expert e of weights[r][s] * sum_j h[r k + s][j] w[e][n][j].
+ * h [rows * k][K] (rows of pairs without an expert are not read), weights float32 [rows][k], out and residual [rows][N]; out may be the
+ * residual.  Products, weights and sums in fp32, slots in their order, one rounding.  workspace: 16-byte aligned, at least
+ * bctm_expert_workspace bytes, holds nothing between calls; it must not be in use by a call on another stream. */
+bct_status bctm_expert_workspace(uint32_t rows, uint32_t k, uint32_t N, size_t* bytes);
+bct_status bctm_expert_linear(const void* h, const void* w_packed, const void* plan, const float* weights, const void* residual, void* out,
+                              void* workspace, size_t workspace_bytes, uint32_t rows, uint32_t k, uint32_t n_experts, uint32_t K,
+                              uint32_t N, void* hip_stream);
+
 /* Which kernel bctm_linear / bctm_linear_split (swiglu = 0, N their widths together) or bctm_swiglu (swiglu = 1) launches
  * for a shape: host logic only, no GPU call.  *kernel receives one of the values below.  The last two of them
  * name the same matrix-core kernel in two ranges of shapes; which tile it gives a workgroup there is

@@ -1,0 +1,203 @@
+// The products of tokens with their experts (gfx950).  A pair p is token p / k with its slot p % k, e(p) its expert:
+//
+//   h[p]   = silu(x[p / k] Wg_e^T) * (x[p / k] Wu_e^T)                       bctm_expert_swiglu
+//   out[r] = residual[r] + sum over s of weight[r][s] * (h[r k + s] Wd_e^T)  bctm_expert_linear
+//
+// Pairs come by expert (the plan of bct_route.hip), in row tiles that belong to one expert each; rows are gathered where they lie.
+// Few pairs an expert: bound by reading the weights of the experts in use once, so a kernel that streams them against
+// 16 rows.  Many: bound by the matrix cores, the kernel of bct_linear_rows.hip with gathered rows.  The way back leaves each
+// pair's product in fp32, and a second kernel weights and adds up those of a token in the order of its slots.
+#include "bct_linear_rows.h"
+#include "bct_model_internal.h"
+
+namespace bct {
+
+namespace {
+
+// A workgroup has one row tile (up to 16 pairs of an expert) and FT feature tiles of 16; its wavefronts share K.
+template <bool SWIGLU, int WAVES, int U, int FT>
+__global__ __launch_bounds__(64 * WAVES) void expert_few_kernel(const uint16_t* __restrict__ x, const u32x4* __restrict__ w,
+                                                                const u32x4* __restrict__ w2, uint16_t* out, uint32_t K, uint32_t N,
+                                                                ExpertTerm T) {
+  constexpr int NW2 = SWIGLU ? 2 : 1, NS = FT * NW2, NTHR = 64 * WAVES;
+  __shared__ float sC[WAVES][NS][16][17];
+  if (blockIdx.y >= *T.n_tiles) return;
+  const ExpertTile tile = expert_tile(T, blockIdx.y);
+  if (tile.rows == 0) return;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, jl = lane % 16, kg = lane / 16, KT = K / 32, NT = N / 16;
+  const uint32_t kt0 = (uint32_t)((uint64_t)wave * KT / WAVES), kt1 = (uint32_t)((uint64_t)(wave + 1) * KT / WAVES);
+  const int32_t* order = T.order + tile.first;
+  const u32x4* wt[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s)   // a feature tile past the end: the last one again, not stored
+    wt[s] = ((s % NW2) ? w2 : w) + tile.expert * T.stride + ((size_t)min(blockIdx.x * FT + s / NW2, NT - 1) * KT + kt0) * 64 + lane;
+  const bool there = jl < tile.rows;   // lanes of rows that are not there load nothing
+  const uint16_t* xr = x + (size_t)(expert_pair(T, order, there ? jl : 0u) / T.per_row) * K + (size_t)kt0 * 32 + kg * 8;
+  f32x4 acc[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) acc[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t n_t = kt1 - kt0;
+  // Rounds of U tiles, all requested before the first product; the missing tiles of the last round are not loaded and count as 0.
+  for (uint32_t t = 0; t < n_t; t += U) {
+    u32x4 b[U][NS], a[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool is = t + u < n_t;
+      a[u] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int s = 0; s < NS; ++s) b[u][s] = is ? __builtin_nontemporal_load(wt[s] + (size_t)(t + u) * 64) : u32x4{0u, 0u, 0u, 0u};
+      if (is && there) a[u] = *(const u32x4*)(xr + (size_t)(t + u) * 32);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        acc[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[u]), __builtin_bit_cast(bf16x8, b[u][s]), acc[s], 0, 0, 0);
+  }
+  // element v of a lane: row 4 * kg + v, feature jl; the wavefronts' sums are added in their order
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) sC[wave][s][4 * kg + v][jl] = acc[s][v];
+  __syncthreads();
+  for (uint32_t o = threadIdx.x; o < FT * 256; o += NTHR) {
+    const uint32_t f = o / 256, i = o % 256 / 16, j = o % 16, n = (blockIdx.x * FT + f) * 16 + j;
+    if (i >= tile.rows || n >= N) continue;
+    float sum[NW2];
+#pragma unroll
+    for (int m = 0; m < NW2; ++m) {
+      sum[m] = 0.f;
+#pragma unroll
+      for (int k = 0; k < WAVES; ++k) sum[m] += sC[k][f * NW2 + m][i][j];
+    }
+    const size_t at = (size_t)expert_pair(T, order, i) * N + n;
+    if (SWIGLU) store_elem(out, at, sum[0] / (1.0f + __expf(-sum[0])) * sum[NW2 - 1]);
+    else T.sums[at] = sum[0];
+  }
+}
+
+// out[r][8 c ..] = residual + the token's products, weighted, in the order of its slots.  A thread has eight features of a token.
+__global__ __launch_bounds__(256) void combine_kernel(const float* sums, const int32_t* expert, const float* weights, const uint16_t* residual,
+                                                      uint16_t* out, uint32_t rows, uint32_t k, uint32_t N) {
+  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint32_t chunks = N / 8, r = (uint32_t)(i / chunks), c = (uint32_t)(i % chunks);
+  if (r >= rows) return;
+  float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (uint32_t s = 0; s < k; ++s) {
+    const size_t p = (size_t)r * k + s;
+    if (expert[p] < 0) continue;
+    const float w = weights[p];
+    const f32x4 *from = (const f32x4*)(sums + p * N + 8 * c), lo = from[0], hi = from[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      y[e] = __builtin_fmaf(w, lo[e], y[e]);
+      y[4 + e] = __builtin_fmaf(w, hi[e], y[4 + e]);
+    }
+  }
+  if (residual) {
+    float v[8];
+    unpack16<BF16>(*(const u32x4*)(residual + (size_t)r * N + 8 * c), v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] += v[e];
+  }
+  *(u32x4*)(out + (size_t)r * N + 8 * c) = pack16_round<BF16>(y);
+}
+
+// The way of a product: a list of the plan, and the kernel that goes by it.
+enum ExpertForm { kFew, kRows64, kRows128, kRows256 };
+ExpertForm expert_form(uint32_t pairs, uint32_t E) {
+  const uint32_t mean = pairs / E;
+  return mean < 24 ? kFew : mean < 96 ? kRows64 : mean < 512 ? kRows128 : kRows256;
+}
+
+bct_status check_products(const void* x, const void* w, const void* out, const void* plan, uint32_t rows, uint32_t k, uint32_t E,
+                          uint32_t K, uint32_t N) {
+  if (!x || !w || !out || K == 0 || N == 0) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
+  const bct_status st = check_expert_plan(plan, rows, k, E);
+  if (st != BCT_OK) return st;
+  if (K % 32 != 0 || N % 16 != 0) return mfail(BCT_ERR_UNSUPPORTED, "K must be a multiple of 32 and N of 16");
+  if (K > 1u << 24 || N > 1u << 24) return mfail(BCT_ERR_UNSUPPORTED, "matrix too large");
+  // grids: row tiles times feature tiles
+  if (((uint64_t)rows * k / 16 + E) * (N / 16 + 1) > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many tokens");
+  if (!al16(x) || !al16(w) || !al16(out)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
+  if (x == out) return mfail(BCT_ERR_INVALID_ARG, "out must not be x");
+  return BCT_OK;
+}
+
+template <bool SWIGLU, int MI, int NJ, int WR, int WC, int KS>
+void launch_rows_of(const void* x, const void* w, const void* w2, void* out, uint32_t K, uint32_t N, const ExpertTerm& T, hipStream_t s) {
+  const uint32_t bcols = SWIGLU ? 2 * N : N, NT = (bcols + 16 * NJ * WC - 1) / (16 * NJ * WC);
+  const dim3 grid(8 * ((T.most_tiles * NT + 7) / 8)), block(64 * WR * WC * KS);
+  const LinearOut dst = {{(uint16_t*)out, nullptr, nullptr}, {0u, N, N, N}};
+  hipLaunchKernelGGL((linear_rows_kernel<SWIGLU, false, false, MI, NJ, WR, WC, KS, ExpertTerm>), grid, block, 0, s, (const uint16_t*)x,
+                     (const u32x4*)w, (const u32x4*)w2, (const uint16_t*)nullptr, dst, 0u, K, NT, 0u, T);
+}
+
+template <bool SWIGLU>
+void launch_products(const void* x, const void* w, const void* w2, void* out, float* sums, const int32_t* plan, uint32_t rows, uint32_t k,
+                     uint32_t E, uint32_t K, uint32_t N, hipStream_t s) {
+  const ExpertPlan P = ExpertPlan::of(rows, k, E);
+  const ExpertForm form = expert_form(P.pairs, E);
+  const uint32_t list = form == kFew ? 0 : form == kRows64 ? 1 : form == kRows128 ? 2 : 3;
+  const ExpertTerm T = {(const uint4*)(plan + P.list[list]), (const uint32_t*)(plan + P.n_tiles + list), plan + P.order,
+                        ExpertPlan::most_tiles(P.pairs, E, kPlanRows[list]), P.pairs, SWIGLU ? k : 1u, E, (size_t)N * K / 8, sums};
+  switch (form) {
+    case kFew: {
+      constexpr int FT = SWIGLU ? 1 : 2, WAVES = 4, U = 8;
+      const dim3 grid((N / 16 + FT - 1) / FT, T.most_tiles);
+      hipLaunchKernelGGL((expert_few_kernel<SWIGLU, WAVES, U, FT>), grid, dim3(64 * WAVES), 0, s, (const uint16_t*)x, (const u32x4*)w,
+                         (const u32x4*)w2, (uint16_t*)out, K, N, T);
+      return;
+    }
+    case kRows64: return launch_rows_of<SWIGLU, 2, 4, 2, 2, 1>(x, w, w2, out, K, N, T, s);
+    case kRows128: return launch_rows_of<SWIGLU, 4, 4, 2, 4, 1>(x, w, w2, out, K, N, T, s);
+    case kRows256: return launch_rows_of<SWIGLU, 8, 4, 2, 4, 1>(x, w, w2, out, K, N, T, s);
+  }
+}
+
+}  // namespace
+
+}  // namespace bct
+
+using namespace bct;
+
+extern "C" {
+
+bct_status bctm_expert_swiglu(const void* x, const void* w_gate, const void* w_up, void* out, const void* plan, uint32_t rows,
+                              uint32_t k, uint32_t n_experts, uint32_t K, uint32_t N, void* hip_stream) {
+  const bct_status st = check_products(x, w_gate, out, plan, rows, k, n_experts, K, N);
+  if (st != BCT_OK) return st;
+  if (!w_up) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
+  if (!al16(w_up)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
+  launch_products<true>(x, w_gate, w_up, out, nullptr, (const int32_t*)plan, rows, k, n_experts, K, N, (hipStream_t)hip_stream);
+  return launched("expert_swiglu");
+}
+
+bct_status bctm_expert_workspace(uint32_t rows, uint32_t k, uint32_t N, size_t* bytes) {
+  if (!bytes || rows == 0 || k == 0 || N == 0) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
+  if (N % 16 != 0 || N > 1u << 24) return mfail(BCT_ERR_UNSUPPORTED, "N must be a multiple of 16, at most 16777216");
+  *bytes = (size_t)rows * k * N * 4;
+  return BCT_OK;
+}
+
+bct_status bctm_expert_linear(const void* h, const void* w_packed, const void* plan, const float* weights, const void* residual, void* out,
+                              void* workspace, size_t workspace_bytes, uint32_t rows, uint32_t k, uint32_t n_experts, uint32_t K,
+                              uint32_t N, void* hip_stream) {
+  const bct_status st = check_products(h, w_packed, out, plan, rows, k, n_experts, K, N);
+  if (st != BCT_OK) return st;
+  if (!weights || !workspace) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
+  if (!al16(residual) || !al16(workspace) || ((uintptr_t)weights & 3u)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned, weights to 4");
+  size_t need = 0;
+  bctm_expert_workspace(rows, k, N, &need);
+  if (workspace_bytes < need) return mfail(BCT_ERR_BUFFER_TOO_SMALL, "the workspace is smaller than bctm_expert_workspace says");
+  const uint64_t chunks = (uint64_t)rows * (N / 8);
+  if ((chunks + 255) / 256 > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many tokens");
+  hipStream_t s = (hipStream_t)hip_stream;
+  const ExpertPlan P = ExpertPlan::of(rows, k, n_experts);
+  launch_products<false>(h, w_packed, nullptr, nullptr, (float*)workspace, (const int32_t*)plan, rows, k, n_experts, K, N, s);
+  hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, (const float*)workspace,
+                     (const int32_t*)plan + P.expert, weights, (const uint16_t*)residual, (uint16_t*)out, rows, k, N);
+  return launched("expert_linear");
+}
+
+}  // extern "C"

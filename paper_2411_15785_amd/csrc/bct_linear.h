@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "bct_device.h"
 
 namespace bct {
@@ -21,6 +23,45 @@ struct LinearOut {
 __device__ __forceinline__ size_t tiled_chunk(uint32_t r, uint32_t k, uint32_t K) {
   return ((((size_t)(r / 32) * (K / 32) + k / 32) * 2 + (r % 32) / 16) * 64) + 16 * ((k % 32) / 8) + r % 16;
 }
+
+// Whether a kernel's terms have one of a type, and that one.
+template <typename T, typename... TERM>
+constexpr bool kHas = (std::is_same<T, TERM>::value || ... || false);
+template <typename T>
+__device__ __forceinline__ const T& only(const T& term) {
+  return term;
+}
+
+// The activations of bctm_linear_act, in fp32; act is a value of BCTM_ACT_, the same in every lane.
+__device__ __forceinline__ float activate(uint32_t act, float y) {
+  switch (act) {
+    case 1: return y < 0.f ? 0.f : y;                                      // a NaN stays one
+    case 2: return y / (1.0f + __expf(-y));
+    case 3: return 0.5f * y * erfcf(-0.70710678f * y);                     // erfc: 1 + erf would lose the small ones
+    case 4: return y / (1.0f + __expf(-1.5957691f * (y + 0.044715f * y * y * y)));   // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
+    case 5: return 1.0f / (1.0f + __expf(-y));
+    default: return y;
+  }
+}
+// Bias and activation of a projection's outputs (before its residual), bf16 or fp32 outputs.
+struct EpilogueTerm {
+  const uint16_t* bias;   // bf16 [N] or null
+  uint32_t act, out32;
+  __device__ __forceinline__ float bias_of(uint32_t n) const { return bias ? __uint_as_float((uint32_t)bias[n] << 16) : 0.f; }
+  // eight features from n on, a multiple of 8
+  __device__ __forceinline__ void apply(float (&y)[8], uint32_t n) const {
+    if (bias) {
+      float b[8];
+      unpack16<BF16>(*(const u32x4*)(bias + n), b);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] += b[k];
+    }
+    if (act) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = activate(act, y[k]);
+    }
+  }
+};
 
 // The low-rank term of a projection's rows (bct_lora.hip): out[r] += t[r] B_a^T, a = adapter[r].
 // t, for the streaming kernel: fp32 [parts][rows][width], the parts to be added up, column segment * rank + j: the rank-j input
@@ -209,6 +250,10 @@ LinearTile linear_rows_tile(uint32_t rows, uint32_t K, uint32_t N, bool swiglu, 
 hipError_t launch_linear_rows(const void* x, const void* w, const void* w2, const void* residual, const LinearOut& dst,
                               uint32_t rows, uint32_t K, uint32_t N, bool x_tiled, bool out_tiled, hipStream_t s,
                               const LoraTerm* lora = nullptr);
+
+// The same with bias and activation (bct_linear_act.hip).
+hipError_t launch_linear_rows_act(const void* x, const void* w, const void* residual, const LinearOut& dst, uint32_t rows,
+                                  uint32_t K, uint32_t N, bool x_tiled, bool out_tiled, hipStream_t s, const EpilogueTerm& term);
 
 }  // namespace bct
 

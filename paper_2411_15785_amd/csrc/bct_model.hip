@@ -169,13 +169,15 @@ __device__ __forceinline__ void lora_outputs(const LoraTerm& L, const LinearOut&
 // two row tiles, 11008 -> 4096 17.6 us (21.5), 4096 -> 4096 11.9 (12.7), 4096 -> 32000 47.9 (50.1), SwiGLU
 // 4096 -> 11008 30.0 (32.2); at 16 rows 23.1 (25.8), 11.7 (12.7), 50.2 (52.2), 33.8 (34.2).  4096 -> 12288 (three feature
 // tiles): see streaming_row_tiles.
-// LORA: none, or a LoraTerm: the rows' low-rank term is added to the outputs (lora_outputs).
-template <bool SWIGLU, bool XT, int WAVES, int U, int FT, int RT, typename... LORA>
+// TERM: none, a LoraTerm (the rows' low-rank term is added to the outputs, lora_outputs) or an EpilogueTerm (bias and activation
+// before the residual, bf16 or fp32 outputs).
+template <bool SWIGLU, bool XT, int WAVES, int U, int FT, int RT, typename... TERM>
 __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __restrict__ x,
                                                             const u32x4* __restrict__ w,
                                                             const u32x4* __restrict__ w2, const uint16_t* residual,
                                                             LinearOut dst, uint32_t rows, uint32_t K,
-                                                            uint32_t out_tiled, LORA... lora) {
+                                                            uint32_t out_tiled, TERM... term) {
+  constexpr bool kLora = kHas<LoraTerm, TERM...>, kEpilogue = kHas<EpilogueTerm, TERM...>;
   constexpr int NW2 = SWIGLU ? 2 : 1;   // weight matrices
   constexpr int NS = FT * NW2;          // weight streams of a wavefront: stream s = feature tile s / NW2 of matrix s % NW2
   constexpr int NTHR = 64 * WAVES;
@@ -201,7 +203,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __re
   constexpr size_t xstep = XT ? 128 * 8 : 32;
   constexpr int OPT = (ROWS * 16 + NTHR - 1) / NTHR;   // outputs per thread and tile
   float delta[FT][NW2][OPT];                           // the low-rank term of a thread's outputs
-  if constexpr (sizeof...(LORA) > 0) lora_outputs<SWIGLU, FT, ROWS, NTHR, OPT>(lora..., dst, r0, nt0, rows, delta);
+  if constexpr (kLora) lora_outputs<SWIGLU, FT, ROWS, NTHR, OPT>(term..., dst, r0, nt0, rows, delta);
   f32x4 acc[NS][RT];
 #pragma unroll
   for (int s = 0; s < NS; ++s)
@@ -265,7 +267,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __re
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) a += sC[k][oi][oj];
         sum[pass][q] = a;
-        if constexpr (sizeof...(LORA) > 0) sum[pass][q] += delta[f][pass][q];
+        if constexpr (kLora) sum[pass][q] += delta[f][pass][q];
       }
     }
 #pragma unroll
@@ -276,10 +278,17 @@ __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __re
         const int which = n >= dst.start[2] ? 2 : n >= dst.start[1] ? 1 : 0;
         const uint32_t width = dst.start[which + 1] - dst.start[which], col = n - dst.start[which];
         const size_t oo = (size_t)(r0 + oi) * width + col;
-        const float g = sum[0][q];
+        float g = sum[0][q];
+        if constexpr (kEpilogue) g = activate(only(term...).act, g + only(term...).bias_of(n));
         float y;
         if (SWIGLU) y = g / (1.0f + __expf(-g)) * sum[NW2 - 1][q];
         else y = residual ? g + bf16f(residual[oo]) : g;
+        if constexpr (kEpilogue) {
+          if (only(term...).out32) {
+            ((float*)dst.ptr[which])[oo] = y;
+            continue;
+          }
+        }
         // a tiled output is the input of a projection whose K is this output's width
         dst.ptr[which][out_tiled ? tiled_chunk(r0 + oi, col, width) * 8 + col % 8 : oo] = f2bf16(y);
       }
@@ -464,19 +473,16 @@ bct_status launched(const char* what, hipError_t e) {
 
 using namespace bct;
 
-template <int WV, int UN, int FT, int RT>
+template <int WV, int UN, int FT, int RT, typename... TERM>
 static void launch_linear_rt(const void* x, const void* w, const void* residual, const LinearOut& dst, uint32_t rows,
-                             uint32_t K, uint32_t N, uint32_t flags, const LoraTerm* lora, void* hip_stream) {
+                             uint32_t K, uint32_t N, uint32_t flags, void* hip_stream, TERM... term) {
   const dim3 grid(N / (16 * FT), (rows + 16 * RT - 1) / (16 * RT)), block(64 * WV);
-  auto launch = [&](auto kernel, auto... more) {
+  auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, block, 0, (hipStream_t)hip_stream, (const uint16_t*)x, (const u32x4*)w,
-                       (const u32x4*)nullptr, (const uint16_t*)residual, dst, rows, K, 0u, more...);
+                       (const u32x4*)nullptr, (const uint16_t*)residual, dst, rows, K, flags & BCTM_OUT_TILED ? 1u : 0u, term...);
   };
-  if (lora) {
-    if (flags & BCTM_X_TILED) launch(linear_kernel<false, true, WV, UN, FT, RT, LoraTerm>, *lora);
-    else launch(linear_kernel<false, false, WV, UN, FT, RT, LoraTerm>, *lora);
-  } else if (flags & BCTM_X_TILED) launch(linear_kernel<false, true, WV, UN, FT, RT>);
-  else launch(linear_kernel<false, false, WV, UN, FT, RT>);
+  if (flags & BCTM_X_TILED) launch(linear_kernel<false, true, WV, UN, FT, RT, TERM...>);
+  else launch(linear_kernel<false, false, WV, UN, FT, RT, TERM...>);
 }
 // Row tiles of a streaming launch with FT feature tiles a workgroup.
 static uint32_t streaming_row_tiles(uint32_t FT, uint32_t rows, uint32_t N, uint32_t flags) {
@@ -488,12 +494,11 @@ static uint32_t streaming_row_tiles(uint32_t FT, uint32_t rows, uint32_t N, uint
   const bool two = FT == 3 && !(flags & BCTM_X_TILED) && rows > 8 && N / (16 * FT) <= 256;
   return rows <= 16 && !two ? 1 : 2;
 }
-template <int WV, int UN, int FT>
+template <int WV, int UN, int FT, typename... TERM>
 static void launch_linear_w(const void* x, const void* w, const void* residual, const LinearOut& dst, uint32_t rows,
-                            uint32_t K, uint32_t N, uint32_t flags, const LoraTerm* lora, void* hip_stream) {
-  if (streaming_row_tiles(FT, rows, N, flags) == 1)
-    launch_linear_rt<WV, UN, FT, 1>(x, w, residual, dst, rows, K, N, flags, lora, hip_stream);
-  else launch_linear_rt<WV, UN, FT, 2>(x, w, residual, dst, rows, K, N, flags, lora, hip_stream);
+                            uint32_t K, uint32_t N, uint32_t flags, void* hip_stream, TERM... term) {
+  if (streaming_row_tiles(FT, rows, N, flags) == 1) launch_linear_rt<WV, UN, FT, 1>(x, w, residual, dst, rows, K, N, flags, hip_stream, term...);
+  else launch_linear_rt<WV, UN, FT, 2>(x, w, residual, dst, rows, K, N, flags, hip_stream, term...);
 }
 
 // The kernel of a projection shape.  Many rows (from 128 on): the matrix-core kernel (bct_linear_rows.hip); its two values
@@ -603,21 +608,32 @@ bct_status bctm_pack_weight(const void* w, void* packed, uint32_t N, uint32_t K,
   return launched("pack_weight");
 }
 
-static bct_status launch_linear(const void* x, const void* w, const void* residual, const LinearOut& dst,
-                                uint32_t rows, uint32_t K, uint32_t N, uint32_t flags, const LoraTerm* lora, void* hip_stream) {
-  const uint32_t kernel = linear_kernel_of(rows, K, N, false);
-  if (kernel == BCTM_KERNEL_TILE128 || kernel == BCTM_KERNEL_TILE256)
-    return launched("linear", launch_linear_rows(x, w, nullptr, residual, dst, rows, K, N, flags & BCTM_X_TILED, false,
-                                                 (hipStream_t)hip_stream, lora));
-  if (kernel == BCTM_KERNEL_STREAMING_WIDE) launch_linear_w<8, 4, 2>(x, w, residual, dst, rows, K, N, flags, lora, hip_stream);
-  else if (kernel == BCTM_KERNEL_STREAMING_TRIPLE) launch_linear_w<8, 4, 3>(x, w, residual, dst, rows, K, N, flags, lora, hip_stream);
-  else launch_linear_w<16, 8, 1>(x, w, residual, dst, rows, K, N, flags, lora, hip_stream);
-  return launched("linear");
-}
-
 static bool many_rows(uint32_t rows, uint32_t K, uint32_t N, bool swiglu) {   // the matrix-core kernel?
   const uint32_t kernel = linear_kernel_of(rows, K, N, swiglu);
   return kernel == BCTM_KERNEL_TILE128 || kernel == BCTM_KERNEL_TILE256;
+}
+
+}  // extern "C"
+
+template <typename... TERM>
+static void launch_linear_few(const void* x, const void* w, const void* residual, const LinearOut& dst, uint32_t rows, uint32_t K,
+                              uint32_t N, uint32_t flags, void* hip_stream, TERM... term) {
+  const uint32_t kernel = linear_kernel_of(rows, K, N, false);
+  if (kernel == BCTM_KERNEL_STREAMING_WIDE) launch_linear_w<8, 4, 2>(x, w, residual, dst, rows, K, N, flags, hip_stream, term...);
+  else if (kernel == BCTM_KERNEL_STREAMING_TRIPLE) launch_linear_w<8, 4, 3>(x, w, residual, dst, rows, K, N, flags, hip_stream, term...);
+  else launch_linear_w<16, 8, 1>(x, w, residual, dst, rows, K, N, flags, hip_stream, term...);
+}
+
+extern "C" {
+
+static bct_status launch_linear(const void* x, const void* w, const void* residual, const LinearOut& dst,
+                                uint32_t rows, uint32_t K, uint32_t N, uint32_t flags, const LoraTerm* lora, void* hip_stream) {
+  if (many_rows(rows, K, N, false))
+    return launched("linear", launch_linear_rows(x, w, nullptr, residual, dst, rows, K, N, flags & BCTM_X_TILED, false,
+                                                 (hipStream_t)hip_stream, lora));
+  if (lora) launch_linear_few(x, w, residual, dst, rows, K, N, flags, hip_stream, *lora);
+  else launch_linear_few(x, w, residual, dst, rows, K, N, flags, hip_stream);
+  return launched("linear");
 }
 
 static bct_status linear_call(const void* x, const void* w, const void* residual, void* out, uint32_t rows, uint32_t K,
@@ -645,6 +661,26 @@ bct_status bctm_linear_lora(const void* x, const void* w, const void* residual, 
                             uint32_t N, uint32_t flags, const bctm_lora* lora, void* hip_stream) {
   if (!lora) return mfail(BCT_ERR_INVALID_ARG, "NULL adapters");
   return linear_call(x, w, residual, out, rows, K, N, flags, lora, hip_stream);
+}
+
+bct_status bctm_linear_act(const void* x, const void* w, const void* bias, const void* residual, void* out, uint32_t rows,
+                           uint32_t K, uint32_t N, uint32_t act, uint32_t flags, void* hip_stream) {
+  const bct_status st = check_linear(x, w, out, rows, K, N);
+  if (st != BCT_OK) return st;
+  if (flags & ~(BCTM_X_TILED | BCTM_OUT_TILED | BCTM_OUT_F32)) return mfail(BCT_ERR_INVALID_ARG, "unknown flag");
+  if ((flags & BCTM_OUT_TILED) && (flags & BCTM_OUT_F32)) return mfail(BCT_ERR_INVALID_ARG, "tiled activations are bf16");
+  if (act > BCTM_ACT_SIGMOID) return mfail(BCT_ERR_INVALID_ARG, "unknown activation");
+  if (x == out) return mfail(BCT_ERR_INVALID_ARG, "out must not be x");
+  if (residual == out && (flags & (BCTM_OUT_TILED | BCTM_OUT_F32))) return mfail(BCT_ERR_INVALID_ARG, "only a row-major bf16 output may be the residual");
+  if ((flags & BCTM_OUT_TILED) && N % 32 != 0) return mfail(BCT_ERR_UNSUPPORTED, "tiled activations need a multiple of 32 columns");
+  if (!al16(residual) || !al16(bias)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
+  const LinearOut dst = {{(uint16_t*)out, nullptr, nullptr}, {0u, N, N, N}};
+  const EpilogueTerm term = {(const uint16_t*)bias, act, flags & BCTM_OUT_F32 ? 1u : 0u};
+  if (many_rows(rows, K, N, false))
+    return launched("linear_act", launch_linear_rows_act(x, w, residual, dst, rows, K, N, flags & BCTM_X_TILED, flags & BCTM_OUT_TILED,
+                                                         (hipStream_t)hip_stream, term));
+  launch_linear_few(x, w, residual, dst, rows, K, N, flags, hip_stream, term);
+  return launched("linear_act");
 }
 
 static bct_status linear_split_call(const void* x, const void* w, void* out0, uint32_t N0, void* out1, uint32_t N1, void* out2,

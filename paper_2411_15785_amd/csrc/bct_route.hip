@@ -1,0 +1,426 @@
+// Each token's experts from the router's logits, and the tokens in the order of their experts (gfx950):
+//
+//   p = softmax(l) or 1 / (1 + exp(-l)) over the experts a token may have (l neither NaN nor -inf)
+//   the k experts with the largest l, or with a bias p + bias; equal ones by number
+//   weight = scale * p / (sum of the chosen p, or 1)
+//
+// A wavefront has a token: lane i holds the experts i, i + 64, ..., and the choice is k times a maximum over the lanes.  With a bias,
+// scores are worked out in 64 bits, as two experts' sums may lie closer than fp32 tells them apart.
+//
+// The plan is a counting sort of the pairs (token, slot) by expert that depends on no order of atomics: blocks of tokens count
+// their experts, then each block adds up what the blocks before it counted and gives its pairs their places, a wavefront's
+// 64 at a time by comparing their experts bit by bit.  Few tokens are one block, and one launch.
+#include <math.h>
+
+#include "bct_device.h"
+#include "bct_experts.h"
+#include "bct_model_internal.h"
+
+namespace bct {
+
+namespace {
+
+typedef unsigned long long u64;
+constexpr uint32_t kThreads = 1024, kWaves = kThreads / 64;
+
+// The value of the lane that the data-parallel-primitive control names, `none` where there is none or the row is not in ROWS.
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ uint32_t other_lane(uint32_t v, uint32_t none) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xF, false);
+}
+// The largest value of the wavefront, the same in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max(v, other_lane<0x111>(v, 0));
+  v = max(v, other_lane<0x112>(v, 0));
+  v = max(v, other_lane<0x114>(v, 0));
+  v = max(v, other_lane<0x118>(v, 0));
+  v = max(v, other_lane<0x142, 0xA>(v, 0));
+  v = max(v, other_lane<0x143, 0xC>(v, 0));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ u64 wave_max(u64 v) {
+  const uint32_t hi = wave_max((uint32_t)(v >> 32));
+  return (u64)hi << 32 | wave_max((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
+}
+// What the lanes up to this one hold.
+__device__ __forceinline__ uint32_t up_to_lane(uint32_t v) {
+  v += other_lane<0x111>(v, 0);
+  v += other_lane<0x112>(v, 0);
+  v += other_lane<0x114>(v, 0);
+  v += other_lane<0x118>(v, 0);
+  v += other_lane<0x142, 0xA>(v, 0);
+  v += other_lane<0x143, 0xC>(v, 0);
+  return v;
+}
+__device__ __forceinline__ float wave_sum(float v) { return xor_sum<1, 32>(v); }
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// Keys order like the numbers, as integers; zeros of either sign are equal.  0 is no key: of a NaN or -inf.
+__device__ __forceinline__ uint32_t key_of(float v) {
+  if (!(v > -INFINITY)) return 0;
+  const int32_t b = __float_as_int(v);
+  return (uint32_t)(b < 0 ? -(b & 0x7FFFFFFF) : b) ^ 0x80000000u;
+}
+__device__ __forceinline__ u64 key_of(double v) {
+  if (!(v > -INFINITY)) return 0;
+  const long long b = __double_as_longlong(v);
+  return (u64)(b < 0 ? -(b & 0x7FFFFFFFFFFFFFFFll) : b) ^ 0x8000000000000000ull;
+}
+
+struct RouteArgs {
+  const void* logits;
+  size_t ld;
+  const float* bias;
+  int32_t* experts;
+  float* weights;
+  int32_t* plan;   // null: none is made
+  uint32_t rows, E, k;
+  float scale;
+  uint32_t sigmoid, normalise;
+};
+
+__device__ __forceinline__ float value_of(uint32_t key) {
+  const int32_t v = (int32_t)(key ^ 0x80000000u);
+  return __int_as_float(v < 0 ? (int32_t)(0x80000000u | (0u - (uint32_t)v)) : v);
+}
+
+// The choice of row r by one wavefront: its experts and weights are written, lane s < k returns that of slot s (E: none is left).
+template <typename DT, bool BIAS, int V>
+__device__ __forceinline__ uint32_t route_row(const RouteArgs& a, uint32_t r) {
+  typedef typename std::conditional<BIAS, double, float>::type F;
+  typedef typename std::conditional<BIAS, u64, uint32_t>::type Key;
+  const uint32_t lane = threadIdx.x % 64;
+  const typename DT::elem* row = (const typename DT::elem*)a.logits + (size_t)r * a.ld;
+  float l[V];
+  Key key[V];
+  float most = -INFINITY;   // with a bias: the row's largest logit
+  F all = 0;                // and the sum of exp(l - most)
+#pragma unroll
+  for (int v = 0; v < V; ++v) l[v] = load_elem(row, min(lane + 64 * v, a.E - 1));
+  if constexpr (BIAS) {
+    float bias[V];
+    uint32_t top = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      bias[v] = a.bias[min(lane + 64 * v, a.E - 1)];
+      if (lane + 64 * v >= a.E || !(l[v] > -INFINITY)) l[v] = -INFINITY;
+      top = max(top, key_of(l[v]));
+    }
+    F p[V];
+    if (a.sigmoid) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) p[v] = 1.0 / (1.0 + exp(-(double)l[v]));
+    } else {
+      top = wave_max(top);
+      if (top) most = value_of(top);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {   // infinite logits share with one another
+        p[v] = l[v] == -INFINITY ? 0.0 : l[v] == most ? 1.0 : exp((double)l[v] - (double)most);
+        all += p[v];
+      }
+      all = wave_sum(all);
+#pragma unroll
+      for (int v = 0; v < V; ++v) p[v] /= all;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = l[v] == -INFINITY ? 0 : key_of(p[v] + (double)bias[v]);
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = lane + 64 * v < a.E ? key_of(l[v]) : 0;
+  }
+  uint32_t expert = a.E;   // of slot `lane`, and its logit
+  float x = -INFINITY;
+  for (uint32_t s = 0; s < a.k; ++s) {
+    Key best = key[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) best = max(best, key[v]);
+    best = wave_max(best);
+    if (best == 0) break;   // none is left
+    bool found = false;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {   // the first expert with that key: those of a v lie before those of the next
+      const u64 has = __ballot(key[v] == best);
+      if (!found && has) {
+        const uint32_t from = __builtin_ctzll(has);
+        found = true;
+        if (lane == from) key[v] = 0;
+        const float of = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l[v]), from));
+        if (lane == s) {
+          expert = from + 64 * v;
+          x = of;
+        }
+      }
+    }
+  }
+  // The chosen scores from their logits.  To be normalised, they may have any factor in common, and are taken against the largest
+  // chosen one, so that they do not all underflow: exp(l - m), or as a sigmoid exp(min(l, 0) - min(m, 0)) / (1 + exp(-|l|)).
+  const bool has = expert < a.E;
+  F weight = 0, total = 1;
+  if (a.normalise || !(a.sigmoid || BIAS)) {
+    const uint32_t top = wave_max(key_of(x));
+    if (top) most = value_of(top);   // without a bias the first one chosen is the row's largest
+  }
+  if (a.sigmoid) {
+    if (has) weight = exp((F)fminf(x, 0.f) - (a.normalise ? (F)fminf(most, 0.f) : (F)0)) / ((F)1 + exp(-(F)fabsf(x)));
+    if (a.normalise) total = wave_sum(weight);
+  } else {
+    if (has) weight = x == most ? (F)1 : exp((F)x - (F)most);
+    if (a.normalise) {
+      total = wave_sum(weight);
+    } else if constexpr (BIAS) {
+      total = all;
+    } else {
+      total = 0;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (lane + 64 * v < a.E && l[v] > -INFINITY) total += l[v] == most ? 1.f : expf(l[v] - most);
+      total = wave_sum(total);
+    }
+  }
+  if (lane < a.k) {
+    a.experts[(size_t)r * a.k + lane] = has ? (int32_t)expert : -1;
+    a.weights[(size_t)r * a.k + lane] = has ? (float)(weight / total * (F)a.scale) : 0.f;
+  }
+  return expert;
+}
+
+struct PlanShared {
+  uint32_t wave[kWaves][kMaxExperts + 1];   // pairs of an expert in a wavefront's share, then where its next one goes
+  uint32_t total[kThreads], before[kThreads];
+  uint32_t tile[kTileLists][kMaxExperts + 1];   // an expert's first row tile
+  uint32_t scan[kTileLists + 1][kWaves];
+};
+
+// Gives the pairs of one block of tokens their places.  experts: of all pairs.
+__device__ __forceinline__ void plan_block(const int32_t* experts, int32_t* plan, const ExpertPlan& P, uint32_t rows, uint32_t k,
+                                           uint32_t block, PlanShared& s) {
+  const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), E = P.E, C = E + 1;
+  const uint32_t per_block = P.block_rows(rows) * k, p0 = min(block * per_block, P.pairs), p1 = min(p0 + per_block, P.pairs);
+  const uint32_t share = ((p1 - p0 + kWaves - 1) / kWaves + 63) / 64 * 64, w0 = min(p0 + wave * share, p1), w1 = min(w0 + share, p1);
+  for (uint32_t w = 0; w < kWaves; ++w)
+    if (threadIdx.x < C) s.wave[w][threadIdx.x] = 0;
+  __syncthreads();
+  for (uint32_t p = w0 + lane; p < w1; p += 64) {
+    const uint32_t e = min((uint32_t)experts[p], E);   // a negative one is beyond E
+    atomicAdd(&s.wave[wave][e], 1u);
+    plan[P.expert + p] = e < E ? (int32_t)e : -1;
+  }
+  // What all blocks and the blocks before this one have of each expert: thread (group, expert) adds up every groups-th block.
+  if (P.blocks > 1) {
+    const uint32_t* counts = (const uint32_t*)plan + P.counts;
+    uint32_t width = 64;
+    while (width < C) width *= 2;
+    const uint32_t groups = kThreads / width, e = threadIdx.x % width;
+    uint32_t all = 0, before = 0;
+    if (e < C) {
+#pragma unroll 8
+      for (uint32_t b = threadIdx.x / width; b < P.blocks; b += groups) {
+        const uint32_t n = counts[(size_t)b * C + e];
+        all += n;
+        before += b < block ? n : 0;
+      }
+    }
+    s.total[threadIdx.x] = all;
+    s.before[threadIdx.x] = before;
+    __syncthreads();
+    if (threadIdx.x < width) {   // only this thread reads and writes entry e of the first group
+      for (uint32_t i = 1; i < groups; ++i) {
+        all += s.total[i * width + e];
+        before += s.before[i * width + e];
+      }
+      s.total[e] = all;
+      s.before[e] = before;
+    }
+  } else {
+    __syncthreads();
+    if (threadIdx.x < C) {
+      uint32_t all = 0;
+      for (uint32_t w = 0; w < kWaves; ++w) all += s.wave[w][threadIdx.x];
+      s.total[threadIdx.x] = all;
+      s.before[threadIdx.x] = 0;
+    }
+  }
+  // Where each expert's pairs and row tiles begin; thread e has expert e, the last one the pairs without an expert.
+  const uint32_t e = threadIdx.x, n = e < C ? s.total[e] : 0;
+  uint32_t own[kTileLists + 1], run[kTileLists + 1];
+#pragma unroll
+  for (uint32_t i = 0; i <= kTileLists; ++i) {
+    const uint32_t size = kPlanRows[i % kTileLists];
+    own[i] = i == kTileLists ? n : e < E ? (n + size - 1) / size : 0;
+    run[i] = up_to_lane(own[i]);
+    if (lane == 63) s.scan[i][wave] = run[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (uint32_t i = 0; i <= kTileLists; ++i)
+    for (uint32_t w = 0; w < wave; ++w) run[i] += s.scan[i][w];
+  if (e < C) {
+    const uint32_t first = run[kTileLists] - n;
+    uint32_t at = first + s.before[e];
+    s.before[e] = first;
+    for (uint32_t w = 0; w < kWaves; ++w) {
+      const uint32_t c = s.wave[w][e];
+      s.wave[w][e] = at;
+      at += c;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kTileLists; ++i) s.tile[i][e] = run[i] - own[i];
+    if (block == 0) {
+      plan[e] = (int32_t)first;
+      if (e == E)
+#pragma unroll
+        for (uint32_t i = 0; i < kTileLists; ++i) plan[P.n_tiles + i] = (int32_t)run[i];
+    }
+  }
+  __syncthreads();
+  // the row tiles: experts are dealt out to the wavefronts of all blocks
+  for (uint32_t x = block * kWaves + wave; x < E; x += P.blocks * kWaves) {
+    const uint32_t count = s.total[x], first = s.before[x];
+#pragma unroll
+    for (uint32_t i = 0; i < kTileLists; ++i) {
+      uint4* list = (uint4*)(plan + P.list[i]) + s.tile[i][x];
+      for (uint32_t t = lane; t * kPlanRows[i] < count; t += 64)
+        list[t] = make_uint4(x, first + t * kPlanRows[i], min(kPlanRows[i], count - t * kPlanRows[i]), 0);
+    }
+  }
+  // the pairs, 64 at a time: a pair's place is its expert's next one and how many lanes before have that expert too
+  for (uint32_t p = w0; p < w1; p += 64) {
+    const bool in = p + lane < w1;
+    const uint32_t x = in ? min((uint32_t)experts[p + lane], E) : 0u;
+    u64 same = __ballot(in);
+    for (uint32_t bit = 1; bit <= E; bit *= 2) {
+      const u64 set = __ballot((x & bit) != 0);
+      same &= x & bit ? set : ~set;
+    }
+    if (!in) continue;
+    const uint32_t leader = __builtin_ctzll(same);
+    uint32_t at = 0;
+    if (lane == leader) at = atomicAdd(&s.wave[wave][x], (uint32_t)__popcll(same));
+    at = __shfl(at, leader, 64) + __popcll(same & ((1ull << lane) - 1));
+    plan[P.order + at] = (int32_t)(p + lane);
+  }
+}
+
+template <typename DT, bool BIAS, int V>
+__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a, ExpertPlan P) {
+  __shared__ union {
+    uint32_t count[kMaxExperts + 1];
+    PlanShared plan;
+  } s;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), C = a.E + 1, per = P.block_rows(a.rows);
+  const uint32_t r0 = min(blockIdx.x * per, a.rows), r1 = min(r0 + per, a.rows);
+  const bool counts = a.plan && P.blocks > 1;
+  if (counts) {
+    if (threadIdx.x < C) s.count[threadIdx.x] = 0;
+    __syncthreads();
+  }
+  for (uint32_t r = r0 + wave; r < r1; r += kWaves) {
+    const uint32_t e = route_row<DT, BIAS, V>(a, r);
+    if (counts && threadIdx.x % 64 < a.k) atomicAdd(&s.count[e], 1u);
+  }
+  __syncthreads();
+  if (counts) {
+    if (threadIdx.x < C) a.plan[P.counts + (size_t)blockIdx.x * C + threadIdx.x] = (int32_t)s.count[threadIdx.x];
+  } else if (a.plan) {
+    plan_block(a.experts, a.plan, P, a.rows, a.k, 0, s.plan);
+  }
+}
+
+// What each block of tokens has of each expert, where the experts are given.
+__global__ __launch_bounds__(kThreads) void count_kernel(const int32_t* experts, int32_t* plan, ExpertPlan P, uint32_t rows, uint32_t k) {
+  __shared__ uint32_t count[kMaxExperts + 1];
+  const uint32_t C = P.E + 1, per = P.block_rows(rows) * k, p0 = min(blockIdx.x * per, P.pairs), p1 = min(p0 + per, P.pairs);
+  if (threadIdx.x < C) count[threadIdx.x] = 0;
+  __syncthreads();
+  for (uint32_t p = p0 + threadIdx.x; p < p1; p += kThreads) atomicAdd(&count[min((uint32_t)experts[p], P.E)], 1u);
+  __syncthreads();
+  if (threadIdx.x < C) plan[P.counts + (size_t)blockIdx.x * C + threadIdx.x] = (int32_t)count[threadIdx.x];
+}
+__global__ __launch_bounds__(kThreads) void plan_kernel(const int32_t* experts, int32_t* plan, ExpertPlan P, uint32_t rows, uint32_t k) {
+  __shared__ PlanShared s;
+  plan_block(experts, plan, P, rows, k, blockIdx.x, s);
+}
+
+bct_status check_plan(uint32_t rows, uint32_t k, uint32_t E) {
+  if (rows == 0 || k == 0 || E == 0) return mfail(BCT_ERR_INVALID_ARG, "zero size");
+  if (E > kMaxExperts || k > kMaxPerToken || k > E) return mfail(BCT_ERR_UNSUPPORTED, "at most 512 experts, 16 of them and not more than there are a token");
+  if ((uint64_t)rows * k > 0x7FFFFFFFull - 0xFFFF) return mfail(BCT_ERR_UNSUPPORTED, "too many tokens");
+  return BCT_OK;
+}
+
+template <typename DT, bool BIAS>
+void launch_route(const RouteArgs& a, const ExpertPlan& P, hipStream_t s) {
+  const dim3 grid(P.blocks), block(kThreads);
+  if (a.E <= 64) hipLaunchKernelGGL((route_kernel<DT, BIAS, 1>), grid, block, 0, s, a, P);
+  else if (a.E <= 128) hipLaunchKernelGGL((route_kernel<DT, BIAS, 2>), grid, block, 0, s, a, P);
+  else if (a.E <= 256) hipLaunchKernelGGL((route_kernel<DT, BIAS, 4>), grid, block, 0, s, a, P);
+  else hipLaunchKernelGGL((route_kernel<DT, BIAS, 8>), grid, block, 0, s, a, P);
+}
+
+}  // namespace
+
+bct_status check_expert_plan(const void* plan, uint32_t rows, uint32_t k, uint32_t E) {
+  if (!plan) return mfail(BCT_ERR_INVALID_ARG, "NULL plan");
+  if (!al16(plan)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
+  return check_plan(rows, k, E);
+}
+
+}  // namespace bct
+
+using namespace bct;
+
+extern "C" {
+
+bct_status bctm_expert_plan_bytes(uint32_t rows, uint32_t k, uint32_t n_experts, size_t* bytes, size_t* order) {
+  if (!bytes) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer");
+  const bct_status st = check_plan(rows, k, n_experts);
+  if (st != BCT_OK) return st;
+  const ExpertPlan P = ExpertPlan::of(rows, k, n_experts);
+  *bytes = P.ints * 4;
+  if (order) *order = P.order;
+  return BCT_OK;
+}
+
+bct_status bctm_route(const void* logits, size_t ld, const float* bias, int32_t* experts, float* weights, void* plan,
+                      size_t plan_bytes, uint32_t rows, uint32_t n_experts, uint32_t k, float scale, int32_t dtype, uint32_t flags,
+                      void* hip_stream) {
+  if (!logits || !experts || !weights) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
+  const bct_status st = check_plan(rows, k, n_experts);
+  if (st != BCT_OK) return st;
+  if (dtype != BCT_F32 && dtype != BCT_BF16) return mfail(BCT_ERR_UNSUPPORTED, "logits are float32 or bf16");
+  if (flags & ~(BCTM_ROUTE_SIGMOID | BCTM_ROUTE_NORMALISE)) return mfail(BCT_ERR_INVALID_ARG, "unknown flag");
+  if (ld < n_experts || ld >> 56) return mfail(BCT_ERR_INVALID_ARG, "ld must be at least n_experts");
+  if (!(fabsf(scale) < INFINITY)) return mfail(BCT_ERR_INVALID_ARG, "scale must be finite");
+  if (((uintptr_t)logits & (dtype == BCT_F32 ? 3u : 1u)) || ((uintptr_t)bias & 3u) || ((uintptr_t)experts & 3u) || ((uintptr_t)weights & 3u) || !al16(plan))
+    return mfail(BCT_ERR_MISALIGNED, "pointers must be aligned to their type, the plan to 16 bytes");
+  const ExpertPlan P = ExpertPlan::of(rows, k, n_experts);
+  if (plan && plan_bytes < P.ints * 4) return mfail(BCT_ERR_BUFFER_TOO_SMALL, "the plan is smaller than bctm_expert_plan_bytes says");
+  const RouteArgs a = {logits, ld, bias, experts, weights, (int32_t*)plan, rows, n_experts, k, scale, flags & BCTM_ROUTE_SIGMOID ? 1u : 0u,
+                       flags & BCTM_ROUTE_NORMALISE ? 1u : 0u};
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (dtype == BCT_F32) bias ? launch_route<F32, true>(a, P, s) : launch_route<F32, false>(a, P, s);
+  else bias ? launch_route<BF16, true>(a, P, s) : launch_route<BF16, false>(a, P, s);
+  if (plan && P.blocks > 1)
+    hipLaunchKernelGGL(plan_kernel, dim3(P.blocks), dim3(kThreads), 0, s, (const int32_t*)experts, (int32_t*)plan, P, rows, k);
+  return launched("route");
+}
+
+bct_status bctm_expert_plan(const int32_t* experts, void* plan, size_t plan_bytes, uint32_t rows, uint32_t n_experts, uint32_t k,
+                            void* hip_stream) {
+  if (!experts || !plan) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
+  const bct_status st = check_plan(rows, k, n_experts);
+  if (st != BCT_OK) return st;
+  if (((uintptr_t)experts & 3u) || !al16(plan)) return mfail(BCT_ERR_MISALIGNED, "pointers must be aligned to their type, the plan to 16 bytes");
+  const ExpertPlan P = ExpertPlan::of(rows, k, n_experts);
+  if (plan_bytes < P.ints * 4) return mfail(BCT_ERR_BUFFER_TOO_SMALL, "the plan is smaller than bctm_expert_plan_bytes says");
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (P.blocks > 1) hipLaunchKernelGGL(count_kernel, dim3(P.blocks), dim3(kThreads), 0, s, experts, (int32_t*)plan, P, rows, k);
+  hipLaunchKernelGGL(plan_kernel, dim3(P.blocks), dim3(kThreads), 0, s, experts, (int32_t*)plan, P, rows, k);
+  return launched("expert_plan");
+}
+
+}  // extern "C"

@@ -17,7 +17,8 @@ from .binding import BCT_OK, BctCache, BctError, _dptr, _launch, _torch
 MODEL_EXPORTS = ["bctm_embed", "bctm_rmsnorm", "bctm_pack_weight", "bctm_pack_rows", "bctm_linear", "bctm_linear_split",
                  "bctm_swiglu", "bctm_linear_plan", "bctm_linear_tile", "bctm_qk_norm_rope",
                  "bctm_lora_workspace", "bctm_lora_pack", "bctm_linear_lora", "bctm_linear_split_lora", "bctm_swiglu_lora",
-                 "bctm_argmax", "bctm_sample", "bctm_last_error"]
+                 "bctm_linear_act", "bctm_expert_plan_bytes", "bctm_route", "bctm_expert_plan", "bctm_expert_swiglu",
+                 "bctm_expert_workspace", "bctm_expert_linear", "bctm_argmax", "bctm_sample", "bctm_last_error"]
 
 BCTM_KERNEL_STREAMING, BCTM_KERNEL_STREAMING_WIDE, BCTM_KERNEL_TILE128, BCTM_KERNEL_TILE256 = 0, 1, 2, 3
 BCTM_KERNEL_STREAMING_TRIPLE = 4
@@ -26,7 +27,10 @@ BCTM_X_TILED = 1
 BCTM_OUT_TILED = 2
 BCTM_HEAD_NORM = 4
 BCTM_ROPE_INTERLEAVED = 8
-
+BCTM_OUT_F32 = 16
+BCTM_ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4, "sigmoid": 5}
+BCTM_ROUTE_SIGMOID = 1
+BCTM_ROUTE_NORMALISE = 2
 
 
 class _bctm_lora(ctypes.Structure):
@@ -64,6 +68,13 @@ def mlib() -> ctypes.CDLL:
     L.bctm_linear_split_lora.argtypes = L.bctm_linear_split.argtypes[:-1] + [lora, vp]
     L.bctm_swiglu_lora.argtypes = L.bctm_swiglu.argtypes[:-1] + [lora, vp]
     L.bctm_sample.argtypes = [vp, ctypes.c_size_t] + [vp] * 7 + [u32, u32, ctypes.c_int32, vp]
+    L.bctm_linear_act.argtypes = [vp] * 5 + [u32] * 5 + [vp]
+    L.bctm_expert_plan_bytes.argtypes = [u32] * 3 + [ctypes.POINTER(sz)] * 2
+    L.bctm_route.argtypes = [vp, sz] + [vp] * 4 + [sz, u32, u32, u32, ctypes.c_float, ctypes.c_int32, u32, vp]
+    L.bctm_expert_plan.argtypes = [vp, vp, sz, u32, u32, u32, vp]
+    L.bctm_expert_swiglu.argtypes = [vp] * 5 + [u32] * 5 + [vp]
+    L.bctm_expert_workspace.argtypes = [u32] * 3 + [ctypes.POINTER(sz)]
+    L.bctm_expert_linear.argtypes = [vp] * 7 + [sz] + [u32] * 5 + [vp]
     for n in MODEL_EXPORTS[:-1]:
         getattr(L, n).restype = ctypes.c_int
     L.bctm_last_error.argtypes = []
@@ -445,6 +456,183 @@ def bctm_swiglu_lora(x, w_gate, w_up, lora, ids, out=None, tiled=False, workspac
     out, args = _swiglu_args(x, w_gate, w_up, out, tiled)
     l, keep = _lora_arg(lora, ids, workspace, args[0], args[5], args[6], args[7], 2, True)
     _ck(_launch(mlib().bctm_swiglu_lora, *args, ctypes.byref(l)), "bctm_swiglu_lora")
+    return out
+
+
+def bctm_linear_act(x, w, bias=None, act="none", residual=None, out=None, out_dtype=None, tiled=False):
+    """residual + act(x W^T + bias).  x: a [rows][K] tensor or a TiledRows; bias bf16 [N]; act: a name of BCTM_ACTS; residual bf16
+    [rows][N]; out [rows][N] of bf16 or float32 (out_dtype where it is made here), or (tiled=True) a TiledRows."""
+    torch = _torch()
+    xd, rows, K, xf = _x_arg(x)
+    _packed(w, "w", K)
+    N, device = w.N, xd.device
+    if act not in BCTM_ACTS:
+        raise ValueError(f"act: expected one of {tuple(BCTM_ACTS)}, got {act!r}")
+    if w.data.device != device:
+        raise ValueError(f"w: packed on {w.data.device}, x is on {device}")
+    if bias is not None and (bias.dtype is not torch.bfloat16 or bias.shape != (N,) or not bias.is_contiguous() or bias.device != device):
+        raise ValueError(f"bias: expected a contiguous bf16 vector of {N} on {device}")
+    if residual is not None:
+        _bf16_2d(residual, "residual", N)
+        if residual.shape[0] != rows or residual.device != device:
+            raise ValueError("residual: one row per row of x, on its device")
+    if tiled:
+        if out is None and out_dtype in (None, torch.bfloat16):
+            out = TiledRows(rows, N, device)
+        if not isinstance(out, TiledRows) or (out.rows, out.K) != (rows, N) or out.data.device != device:
+            raise ValueError("out: a TiledRows [rows][N] on x's device")
+        dst, of = out.data, BCTM_OUT_TILED
+    else:
+        if out is None:
+            out = torch.empty((rows, N), dtype=out_dtype or torch.bfloat16, device=device)
+        if not isinstance(out, torch.Tensor) or out.dtype not in (torch.bfloat16, torch.float32) or (out_dtype or out.dtype) != out.dtype \
+                or out.shape != (rows, N) or not out.is_contiguous() or out.device != device:
+            raise ValueError(f"out: expected contiguous bf16 or float32 [{rows}][{N}] on {device}")
+        dst, of = out, BCTM_OUT_F32 if out.dtype is torch.float32 else 0
+    _ck(_launch(mlib().bctm_linear_act, device, xd.data_ptr(), w.data.data_ptr(), _dptr(bias), _dptr(residual), dst.data_ptr(), rows, K, N,
+                BCTM_ACTS[act], xf | of), "bctm_linear_act")
+    return out
+
+
+class ExpertPlan:
+    """The pairs of rows tokens and their k slots (number token * k + slot) by expert: order int32 [rows * k], offsets int32
+    [n_experts + 1], views of the plan; made by bctm_route or bctm_expert_plan."""
+
+    def __init__(self, rows, k, n_experts, device):
+        torch = _torch()
+        size, order = ctypes.c_size_t(0), ctypes.c_size_t(0)
+        if rows >> 32:
+            raise ValueError("more tokens than one call takes")
+        _ck(mlib().bctm_expert_plan_bytes(rows, k, n_experts, ctypes.byref(size), ctypes.byref(order)), "bctm_expert_plan_bytes")
+        self.rows, self.k, self.n_experts, self.bytes = rows, k, n_experts, size.value
+        # zeros, not empty: a plan that has not been made has no tokens
+        self.data = torch.zeros(size.value // 4, dtype=torch.int32, device=device)
+        self.offsets = self.data[:n_experts + 1]
+        self.order = self.data[order.value:order.value + rows * k]
+
+
+def _plan(plan, rows, k, n_experts, device):
+    if not isinstance(plan, ExpertPlan) or (plan.rows, plan.k, plan.n_experts) != (rows, k, n_experts) or plan.data.device != device:
+        raise ValueError(f"plan: expected an ExpertPlan of {rows} tokens, {k} slots and {n_experts} experts on {device}")
+
+
+def bctm_route(logits, k, bias=None, sigmoid=False, normalise=True, scale=1.0, experts=None, weights=None, plan=None):
+    """Each token's k experts from its logits [rows][n_experts] (float32 or bf16, rows at any distance): those with the largest
+    logit, or with bias (float32 [n_experts]) the largest score + bias; scores are the logits' softmax or sigmoid.
+    -> (experts int32 [rows][k], weights float32 [rows][k]: scale * score, normalised over the chosen ones, plan: an ExpertPlan,
+    made here unless given).  Slots for which no expert is left have -1 and 0."""
+    torch = _torch()
+    if logits.dtype not in (torch.float32, torch.bfloat16) or logits.dim() != 2 or not logits.is_cuda or \
+            (logits.stride(1) != 1 and logits.shape[1] > 1) or logits.shape[0] >> 32:
+        raise ValueError(f"logits: expected [rows][n_experts] of float32 or bf16 on the GPU, each row contiguous, got {logits.dtype} "
+                         f"{tuple(logits.shape)} strides {logits.stride()} on {logits.device}")
+    (rows, E), device = logits.shape, logits.device
+    if plan is None:
+        plan = ExpertPlan(rows, k, E, device)
+    _plan(plan, rows, k, E, device)
+    if experts is None:
+        experts = torch.empty((rows, k), dtype=torch.int32, device=device)
+    if weights is None:
+        weights = torch.empty((rows, k), dtype=torch.float32, device=device)
+    for t, n, dtype, shape in ((experts, "experts", torch.int32, (rows, k)), (weights, "weights", torch.float32, (rows, k)),
+                               (bias, "bias", torch.float32, (E,))):
+        if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != device):
+            raise ValueError(f"{n}: expected contiguous {dtype} {shape} on {device}")
+    _ck(_launch(mlib().bctm_route, device, logits.data_ptr(), logits.stride(0) if rows > 1 else max(logits.stride(0), E), _dptr(bias),
+                experts.data_ptr(), weights.data_ptr(), plan.data.data_ptr(), plan.bytes, rows, E, k, scale,
+                binding.BCT_F32 if logits.dtype is torch.float32 else binding.BCT_BF16,
+                (BCTM_ROUTE_SIGMOID if sigmoid else 0) | (BCTM_ROUTE_NORMALISE if normalise else 0)), "bctm_route")
+    return experts, weights, plan
+
+
+def bctm_expert_plan(experts, n_experts, plan=None):
+    """The plan of experts int32 [rows][k] that the caller chose (outside [0, n_experts): none)."""
+    torch = _torch()
+    if experts.dtype is not torch.int32 or experts.dim() != 2 or not experts.is_contiguous() or not experts.is_cuda:
+        raise ValueError(f"experts: expected contiguous int32 [rows][k] on the GPU, got {experts.dtype} {tuple(experts.shape)} on {experts.device}")
+    rows, k = experts.shape
+    if plan is None:
+        plan = ExpertPlan(rows, k, n_experts, experts.device)
+    _plan(plan, rows, k, n_experts, experts.device)
+    _ck(_launch(mlib().bctm_expert_plan, experts.device, experts.data_ptr(), plan.data.data_ptr(), plan.bytes, rows, n_experts, k),
+        "bctm_expert_plan")
+    return plan
+
+
+class ExpertWeights:
+    """The matrices [n][N][K] of all experts, packed (bctm_pack_experts)."""
+
+    def __init__(self, data, n, N, K):
+        self.data, self.n, self.N, self.K = data, n, N, K
+
+
+def bctm_pack_experts(w):
+    """w bf16 [n_experts][N][K] -> ExpertWeights."""
+    torch = _torch()
+    if w.dtype is not torch.bfloat16 or w.dim() != 3 or not w.is_contiguous() or not w.is_cuda:
+        raise ValueError(f"w: expected contiguous bf16 [n_experts][N][K] on the GPU, got {w.dtype} {tuple(w.shape)} on {w.device}")
+    n, N, K = w.shape
+    if N % 16 or K % 32:
+        raise ValueError("N must be a multiple of 16 and K of 32")
+    return ExpertWeights(bctm_pack_weight(w.view(n * N, K)).data, n, N, K)
+
+
+def _expert_args(x, w, name, plan, rows):
+    if not isinstance(plan, ExpertPlan):
+        raise ValueError("plan: expected an ExpertPlan")
+    _bf16_2d(x, "x")
+    if not isinstance(w, ExpertWeights) or w.K != x.shape[1] or w.n != plan.n_experts or w.data.device != x.device:
+        raise ValueError(f"{name}: expected ExpertWeights of {plan.n_experts} experts and {x.shape[1]} inputs on {x.device} (bctm_pack_experts)")
+    if x.shape[0] != rows or plan.data.device != x.device:
+        raise ValueError(f"x: expected {rows} rows for this plan, on its device")
+
+
+def bctm_expert_swiglu(x, w_gate, w_up, plan, out=None):
+    """x bf16 [rows][K] -> [rows * k][N]: the gated product of each token with each of its experts, row token * k + slot; rows of
+    slots without an expert are left as they were (0 where out is made here)."""
+    torch = _torch()
+    _expert_args(x, w_gate, "w_gate", plan, plan.rows if isinstance(plan, ExpertPlan) else 0)
+    _expert_args(x, w_up, "w_up", plan, plan.rows)
+    if w_gate.N != w_up.N:
+        raise ValueError("w_gate and w_up: same shape")
+    if out is None:
+        out = torch.zeros((plan.rows * plan.k, w_gate.N), dtype=torch.bfloat16, device=x.device)
+    _bf16_2d(out, "out", w_gate.N)
+    if out.shape[0] != plan.rows * plan.k or out.device != x.device:
+        raise ValueError("out: one row per token and slot, on x's device")
+    _ck(_launch(mlib().bctm_expert_swiglu, x.device, x.data_ptr(), w_gate.data.data_ptr(), w_up.data.data_ptr(), out.data_ptr(),
+                plan.data.data_ptr(), plan.rows, plan.k, plan.n_experts, w_gate.K, w_gate.N), "bctm_expert_swiglu")
+    return out
+
+
+def bctm_expert_workspace(rows, k, N):
+    """Bytes of workspace that bctm_expert_linear takes."""
+    v = ctypes.c_size_t(0)
+    _ck(mlib().bctm_expert_workspace(rows, k, N, ctypes.byref(v)), "bctm_expert_workspace")
+    return v.value
+
+
+def bctm_expert_linear(h, w, plan, weights, residual=None, out=None, workspace=None):
+    """h bf16 [rows * k][K], weights float32 [rows][k] -> [rows][N]: residual + the weighted sum of each token's products with its
+    experts.  out may be the residual.  workspace: torch.uint8 of bctm_expert_workspace bytes, or None to take one from torch."""
+    torch = _torch()
+    _expert_args(h, w, "w", plan, plan.rows * plan.k if isinstance(plan, ExpertPlan) else 0)
+    rows, k, N, device = plan.rows, plan.k, w.N, h.device
+    if weights.dtype is not torch.float32 or weights.shape != (rows, k) or not weights.is_contiguous() or weights.device != device:
+        raise ValueError(f"weights: expected contiguous float32 [{rows}][{k}] on {device}")
+    if out is None:
+        out = torch.empty((rows, N), dtype=torch.bfloat16, device=device)
+    for t, n in ((out, "out"), (residual, "residual")):
+        if t is not None:
+            _bf16_2d(t, n, N)
+            if t.shape[0] != rows or t.device != device:
+                raise ValueError(f"{n}: one row per token, on h's device")
+    if workspace is None:
+        workspace = torch.empty(bctm_expert_workspace(rows, k, N), dtype=torch.uint8, device=device)
+    elif workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.device != device:
+        raise ValueError(f"workspace: expected contiguous torch.uint8 on {device}")
+    _ck(_launch(mlib().bctm_expert_linear, device, h.data_ptr(), w.data.data_ptr(), plan.data.data_ptr(), weights.data_ptr(), _dptr(residual),
+                out.data_ptr(), workspace.data_ptr(), workspace.numel(), rows, k, plan.n_experts, w.K, N), "bctm_expert_linear")
     return out
 
 
