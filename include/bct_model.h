@@ -201,9 +201,16 @@ bct_status bctm_expert_plan(const int32_t* experts, void* plan, size_t plan_byte
 bct_status bctm_expert_swiglu(const void* x, const void* w_gate_packed, const void* w_up_packed, void* out, const void* plan,
                               uint32_t rows, uint32_t k, uint32_t n_experts, uint32_t K, uint32_t N, void* hip_stream);
 
+/* Which tile of pairs x features the launch of that call or of the next one gives a workgroup (swiglu = 1: bctm_expert_swiglu, 0:
+ * bctm_expert_linear); host logic only. */
+bct_status bctm_expert_tile(uint32_t rows, uint32_t k, uint32_t n_experts, uint32_t K, uint32_t N, uint32_t swiglu, uint32_t* tile_rows,
+                            uint32_t* tile_features);
+
 /* out[r][n] = (residual ? residual[r][n] : 0) + sum over the slots s of r with an expert e of weights[r][s] * sum_j h[r k + s][j] w[e][n][j].
  * h [rows * k][K] (rows of pairs without an expert are not read), weights float32 [rows][k], out and residual [rows][N]; out may be the
- * residual.  Products, weights and sums in fp32, slots in their order, one rounding.  workspace: 16-byte aligned, at least
+ * residual.  Products, weights and sums in fp32, slots in their order, rounded at the end; tiles of more than 16 pairs
+ * (bctm_expert_tile) also leave each product off by at most 2^-14 of the largest of its eight neighbouring features (8 i .. 8 i + 7), as
+ * they wait for the sum in 16 bits.  workspace: 16-byte aligned, at least
  * bctm_expert_workspace bytes, holds nothing between calls; it must not be in use by a call on another stream. */
 bct_status bctm_expert_workspace(uint32_t rows, uint32_t k, uint32_t N, size_t* bytes);
 bct_status bctm_expert_linear(const void* h, const void* w_packed, const void* plan, const float* weights, const void* residual, void* out,

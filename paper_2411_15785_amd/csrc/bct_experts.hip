@@ -7,6 +7,8 @@
 // Few pairs an expert: bound by reading the weights of the experts in use once, so a kernel that streams them against
 // 16 rows.  Many: bound by the matrix cores, the kernel of bct_linear_rows.hip with gathered rows.  The way back leaves each
 // pair's product in fp32, and a second kernel weights and adds up those of a token in the order of its slots.
+#include <math.h>
+
 #include "bct_linear_rows.h"
 #include "bct_model_internal.h"
 
@@ -72,12 +74,14 @@ __global__ __launch_bounds__(64 * WAVES) void expert_few_kernel(const uint16_t* 
     }
     const size_t at = (size_t)expert_pair(T, order, i) * N + n;
     if (SWIGLU) store_elem(out, at, sum[0] / (1.0f + __expf(-sum[0])) * sum[NW2 - 1]);
-    else T.sums[at] = sum[0];
+    else ((float*)T.sums)[at] = sum[0];
   }
 }
 
 // out[r][8 c ..] = residual + the token's products, weighted, in the order of its slots.  A thread has eight features of a token.
-__global__ __launch_bounds__(256) void combine_kernel(const float* sums, const int32_t* expert, const float* weights, const uint16_t* residual,
+// BLOCKS: products come as blocks of eight (pack_block), else fp32.
+template <bool BLOCKS>
+__global__ __launch_bounds__(256) void combine_kernel(const void* sums, const int32_t* expert, const float* weights, const uint16_t* residual,
                                                       uint16_t* out, uint32_t rows, uint32_t k, uint32_t N) {
   const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   const uint32_t chunks = N / 8, r = (uint32_t)(i / chunks), c = (uint32_t)(i % chunks);
@@ -87,12 +91,16 @@ __global__ __launch_bounds__(256) void combine_kernel(const float* sums, const i
     const size_t p = (size_t)r * k + s;
     if (expert[p] < 0) continue;
     const float w = weights[p];
-    const f32x4 *from = (const f32x4*)(sums + p * N + 8 * c), lo = from[0], hi = from[1];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      y[e] = __builtin_fmaf(w, lo[e], y[e]);
-      y[4 + e] = __builtin_fmaf(w, hi[e], y[4 + e]);
+    float v[8];
+    if constexpr (BLOCKS) {
+      unpack_block(((const u32x4*)sums)[p * chunks + c], v);
+    } else {
+      const f32x4* from = (const f32x4*)sums + (p * chunks + c) * 2;
+      *(f32x4*)&v[0] = from[0];
+      *(f32x4*)&v[4] = from[1];
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(w, v[e], y[e]);
   }
   if (residual) {
     float v[8];
@@ -103,11 +111,37 @@ __global__ __launch_bounds__(256) void combine_kernel(const float* sums, const i
   *(u32x4*)(out + (size_t)r * N + 8 * c) = pack16_round<BF16>(y);
 }
 
-// The way of a product: a list of the plan, and the kernel that goes by it.
-enum ExpertForm { kFew, kRows64, kRows128, kRows256 };
-ExpertForm expert_form(uint32_t pairs, uint32_t E) {
-  const uint32_t mean = pairs / E;
-  return mean < 24 ? kFew : mean < 96 ? kRows64 : mean < 512 ? kRows128 : kRows256;
+// The form of a product's sizes: what a workgroup has, 16 rows of the streaming kernel or 64 x 128, 128 x 256 or 256 x 256 of
+// rows and columns (two of a SwiGLU's feature).  The host knows how many pairs an expert has in the mean, not how many each has: about
+// mean / rows + 1/2 row tiles, at least one.  Estimates in us from
+//   streaming   every row tile reads the expert's weights: 6.7 TB/s
+//   64 x 128    0.17 a K step alone on its compute unit, 0.19 for each of several
+//   128 x 256   0.34 a K step of a round of workgroups;  256 x 256  0.48;  and for all three the weights at 5.6 TB/s
+// and what begins and ends a launch.  Measured us, streaming | 64 x 128 | 128 x 256 | 256 x 256, gated K = 4096, N = 1376, 64 experts with a
+// mean of 4: 212 | 243 | 232 | 235; 8: 240 | 258 | 246 | 244; 16: 326 | 274 | 256 | 252; 48: 811 | 333 | 285 | 292; 128: - | 526 | 371 | 356; 256:
+// - | 813 | 570 | 468.  8 experts, 2048, 1024, mean 4: 15.0 | 16.2 | 23.3 | 28.7; 16: 18.9 | 17.3 | 24.6 | 30.4; 64: 45.6 | 19.5 | 27.7 | 34.0; 192:
+// - | 29.2 | 29.3 | 43.7; 256: - | 38.0 | 29.8 | 44.1.  The way back (with its sum), 12 experts, 2080 -> 2048, mean 8: 24.0 | 24.0 | 28.2 | 33.6; 32: 43.7 |
+// 26.6 | 32.2 | 38.3; 128: 127 | 41.2 | 47.3 | 59.9; 192: - | 54.8 | 49.1 | 60.6; 384: - | 87.9 | 95.3 | 76.3.
+enum ExpertForm { kFew, kRows64, kRows128, kRows256 };   // in the order of kPlanRows
+constexpr uint32_t few_features(bool swiglu) { return swiglu ? 1 : 2; }   // feature tiles of a streaming workgroup
+ExpertForm expert_form(uint32_t pairs, uint32_t E, uint32_t K, uint32_t N, bool swiglu) {
+  const double used = pairs < E ? pairs : E, mean = pairs / used, bcols = swiglu ? 2.0 * N : N, KT = K / 32, expert = 2.0 * K * bcols;
+  auto tiles = [&](double rows) { return used * (mean / rows > 0.5 ? mean / rows + 0.5 : 1.0); };
+  const double stream = 2 + used * expert / 5.6e6;
+  ExpertForm best = kFew;
+  double cost = 4 + tiles(16) * expert / 6.7e6;
+  auto take = [&](ExpertForm f, double c) {
+    c = c > stream ? c : stream;
+    if (c < cost) {
+      cost = c;
+      best = f;
+    }
+  };
+  auto groups = [&](double rows, double cols) { return tiles(rows) * ceil(bcols / cols) / 256; };   // workgroups of a compute unit
+  take(kRows64, 6 + KT * (groups(64, 128) > 0.9 ? 0.19 * groups(64, 128) : 0.17));
+  take(kRows128, 10.8 + KT * 0.34 * ceil(groups(128, 256)));
+  take(kRows256, 13.9 + KT * 0.48 * ceil(groups(256, 256)));
+  return best;
 }
 
 bct_status check_products(const void* x, const void* w, const void* out, const void* plan, uint32_t rows, uint32_t k, uint32_t E,
@@ -134,16 +168,16 @@ void launch_rows_of(const void* x, const void* w, const void* w2, void* out, uin
 }
 
 template <bool SWIGLU>
-void launch_products(const void* x, const void* w, const void* w2, void* out, float* sums, const int32_t* plan, uint32_t rows, uint32_t k,
+void launch_products(const void* x, const void* w, const void* w2, void* out, void* sums, const int32_t* plan, uint32_t rows, uint32_t k,
                      uint32_t E, uint32_t K, uint32_t N, hipStream_t s) {
   const ExpertPlan P = ExpertPlan::of(rows, k, E);
-  const ExpertForm form = expert_form(P.pairs, E);
-  const uint32_t list = form == kFew ? 0 : form == kRows64 ? 1 : form == kRows128 ? 2 : 3;
+  const ExpertForm form = expert_form(P.pairs, E, K, N, SWIGLU);
+  const uint32_t list = form;
   const ExpertTerm T = {(const uint4*)(plan + P.list[list]), (const uint32_t*)(plan + P.n_tiles + list), plan + P.order,
                         ExpertPlan::most_tiles(P.pairs, E, kPlanRows[list]), P.pairs, SWIGLU ? k : 1u, E, (size_t)N * K / 8, sums};
   switch (form) {
     case kFew: {
-      constexpr int FT = SWIGLU ? 1 : 2, WAVES = 4, U = 8;
+      constexpr int FT = few_features(SWIGLU), WAVES = 4, U = 8;
       const dim3 grid((N / 16 + FT - 1) / FT, T.most_tiles);
       hipLaunchKernelGGL((expert_few_kernel<SWIGLU, WAVES, U, FT>), grid, dim3(64 * WAVES), 0, s, (const uint16_t*)x, (const u32x4*)w,
                          (const u32x4*)w2, (uint16_t*)out, K, N, T);
@@ -173,6 +207,18 @@ bct_status bctm_expert_swiglu(const void* x, const void* w_gate, const void* w_u
   return launched("expert_swiglu");
 }
 
+bct_status bctm_expert_tile(uint32_t rows, uint32_t k, uint32_t n_experts, uint32_t K, uint32_t N, uint32_t swiglu, uint32_t* tile_rows,
+                            uint32_t* tile_features) {
+  if (!tile_rows || !tile_features || K == 0 || N == 0) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
+  const bct_status st = check_plan_sizes(rows, k, n_experts);
+  if (st != BCT_OK) return st;
+  if (K % 32 != 0 || N % 16 != 0) return mfail(BCT_ERR_UNSUPPORTED, "K must be a multiple of 32 and N of 16");
+  const ExpertForm form = expert_form(rows * k, n_experts, K, N, swiglu != 0);
+  *tile_rows = kPlanRows[form];
+  *tile_features = form == kFew ? 16 * few_features(swiglu != 0) : (form == kRows64 ? 128 : 256) / (swiglu ? 2 : 1);
+  return BCT_OK;
+}
+
 bct_status bctm_expert_workspace(uint32_t rows, uint32_t k, uint32_t N, size_t* bytes) {
   if (!bytes || rows == 0 || k == 0 || N == 0) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
   if (N % 16 != 0 || N > 1u << 24) return mfail(BCT_ERR_UNSUPPORTED, "N must be a multiple of 16, at most 16777216");
@@ -194,8 +240,9 @@ bct_status bctm_expert_linear(const void* h, const void* w_packed, const void* p
   if ((chunks + 255) / 256 > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many tokens");
   hipStream_t s = (hipStream_t)hip_stream;
   const ExpertPlan P = ExpertPlan::of(rows, k, n_experts);
-  launch_products<false>(h, w_packed, nullptr, nullptr, (float*)workspace, (const int32_t*)plan, rows, k, n_experts, K, N, s);
-  hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, (const float*)workspace,
+  launch_products<false>(h, w_packed, nullptr, nullptr, workspace, (const int32_t*)plan, rows, k, n_experts, K, N, s);
+  const auto combine = expert_form(P.pairs, n_experts, K, N, false) == kFew ? combine_kernel<false> : combine_kernel<true>;
+  hipLaunchKernelGGL(combine, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, (const void*)workspace,
                      (const int32_t*)plan + P.expert, weights, (const uint16_t*)residual, (uint16_t*)out, rows, k, N);
   return launched("expert_linear");
 }

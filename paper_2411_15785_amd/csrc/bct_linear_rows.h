@@ -14,6 +14,9 @@ RowsShape rows_shape(uint32_t rows, uint32_t bcols, uint32_t K, bool x_tiled);
 
 namespace {
 
+// Where a row's four chunks of a K step lie, with experts: chunk c of row r at place c ^ row_turn(r / 4).
+__device__ __forceinline__ int row_turn(int q) { return ((q ^ q >> 1) & 1) << 1 | q >> 1; }   // 0, 2, 3, 1
+
 // KS groups of WR x WC wavefronts; a wavefront owns 16 * MI token rows x 16 * NJ B-tile columns (SwiGLU: gate and
 // up tiles alternate, so half as many output features); group g sums the K steps [KT * g / KS, ...).
 // PAIR (row-major activations): the two K steps of a line are requested together, see request_rows.
@@ -27,7 +30,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
     const uint16_t* __restrict__ x, const u32x4* __restrict__ w, const u32x4* __restrict__ w2, const uint16_t* residual,
     LinearOut dst, uint32_t rows, uint32_t K, uint32_t NT, uint32_t out_tiled, TERM... term) {
   constexpr bool kLora = kHas<LoraTerm, TERM...>, kEpilogue = kHas<EpilogueTerm, TERM...>, kExperts = kHas<ExpertTerm, TERM...>;
-  static_assert(!kExperts || (!XT && !PAIR), "gathered rows are row-major");
+  static_assert(!kExperts || (!XT && !PAIR && 64 * WR * WC * KS >= 16 * MI * WR), "gathered rows are row-major; a thread has one");
   constexpr int NW = WR * WC;                      // wavefronts of a group
   constexpr int TA = MI * WR, TB = NJ * WC, TT = TA + TB;  // 1 KB tiles of a K step: activations, weights
   constexpr int ND = TT / NW, NA = TA / NW, NB = TB / NW;  // of them per wavefront
@@ -43,6 +46,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   __shared__ __attribute__((aligned(16))) u32x4 st1[KS * TT * 64];
   __shared__ __attribute__((aligned(16))) u32x4 st2[KS * TT * 64];
   __shared__ __attribute__((aligned(16))) u32x4 st3[KS * TT * 64];
+  __shared__ uint32_t pair_of[kExperts ? BM : 1];   // the pairs of the tile's rows
 
   uint32_t RT = (rows + BM - 1) / BM;
   if constexpr (kExperts) {   // the grid is for the most tiles there can be
@@ -82,6 +86,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
     rows = tile.rows;
     if (rows == 0) return;
     order = T.order + tile.first;
+    if (threadIdx.x < rows) pair_of[threadIdx.x] = expert_pair(T, order, threadIdx.x);   // read behind the K loop's barriers
     w += tile.expert * T.stride;
     if (SWIGLU) w2 += tile.expert * T.stride;
     r0 = 0;
@@ -89,6 +94,10 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   const uint32_t kfirst = grp ? (KT + 1) / 2 : 0u;                       // this group's K steps
   const uint32_t kcount = KS > 1 ? (grp ? KT / 2 : (KT + 1) / 2) : KT;
   const uint32_t kboth = KS > 1 ? KT / 2 : KT, kmost = KS > 1 ? (KT + 1) / 2 : KT;  // steps all groups / some group have
+
+  // An expert's last row tile is partly used: the 16-row tiles of a wavefront are every WR-th one, so that those there are divide
+  // evenly, and the others are not multiplied.
+  const int active = kExperts ? __builtin_amdgcn_readfirstlane((int)(((rows + 15) / 16 + WR - 1 - wr) / WR)) : MI;
 
   // this lane's 16 bytes of the tiles wave, wave + NW, ... of a K step
   const char* src[ND];
@@ -107,7 +116,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
         // in different banks.
         const ExpertTerm& T = only(term...);
         const uint32_t r = min(tile * 16 + lane / 4, rows - 1);
-        src[j] = (const char*)(x + (size_t)(expert_pair(T, order, r) / T.per_row) * K + (lane % 4 ^ lane / 16) * 8);
+        src[j] = (const char*)(x + (size_t)(expert_pair(T, order, r) / T.per_row) * K + (lane % 4 ^ row_turn(lane / 16)) * 8);
         step[j] = 64;
       } else {
         const uint32_t r = min(r0 + tile * 16 + jl, rows - 1);
@@ -151,7 +160,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   };
   // one index into the stage each: the compiler loses track of which array an access belongs to when the
   // address is a long chain
-  const int put0 = (grp * TT + wave) * 64, geta = (grp * TT + MI * wr) * 64 + (kExperts ? jl * 4 + (kg ^ jl / 4) : lane), getb = (grp * TT + TA + NJ * wc) * 64 + lane;
+  const int put0 = (grp * TT + wave) * 64, geta = (grp * TT + (kExperts ? wr : MI * wr)) * 64 + (kExperts ? jl * 4 + (kg ^ row_turn(jl / 4)) : lane), getb = (grp * TT + TA + NJ * wc) * 64 + lane;
   auto at = [&](uint32_t kt) { return min(kfirst + kt, KT - 1); };   // past the end: the last step again, never multiplied
   auto request = [&](auto c, uint32_t kt, auto first, auto last) {   // loads first .. last - 1 of step kt
     u32x4* s = stage(c);
@@ -181,7 +190,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
 #pragma unroll
     for (int i = 0; i < NJ; ++i) b[i] = __builtin_bit_cast(bf16x8, s[getb + 64 * i]);
 #pragma unroll
-    for (int i = 0; i < MI; ++i) a[i] = __builtin_bit_cast(bf16x8, s[geta + 64 * i]);
+    for (int i = 0; i < MI; ++i) a[i] = __builtin_bit_cast(bf16x8, s[geta + 64 * i * (kExperts ? WR : 1)]);
     constexpr bool even = decltype(c)::v % 2 == 0;   // of kt as well
     constexpr int left = (S - 2) * (PAIR && !even ? NB : ND);
     if constexpr (PAIR && even) request_rows(Int<decltype(c)::v + 2>{}, kt + 2);
@@ -194,9 +203,11 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
     auto products = [&] {
       if constexpr (PING) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
+      for (int i = 0; i < MI; ++i) {
+        if (kExperts && i >= active) break;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+      }
       if constexpr (PING) __builtin_amdgcn_s_setprio(0);
     };
     if constexpr (decltype(last)::v == 0) products();
@@ -317,10 +328,10 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const int cc = lane % CPR;
-#pragma unroll
+#pragma unroll kEpilogue ? 1 : 16 / RPP
     for (int ps = 0; ps < 16 / RPP; ++ps) {
       const int rr = ps * RPP + lane / CPR;
-      const uint32_t row = r0 + wr * (16 * MI) + (grp * MO + i) * 16 + rr;
+      const uint32_t row = kExperts ? ((grp * MO + i) * WR + wr) * 16 + rr : r0 + wr * (16 * MI) + (grp * MO + i) * 16 + rr;
       const uint32_t n = nt * BNF + wc * (BNF / WC) + 8 * cc;
       if (rr < 16 && row < rows && n < dst.start[3]) {
         float y[8];
@@ -329,7 +340,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
         const int which = n >= dst.start[2] ? 2 : n >= dst.start[1] ? 1 : 0;
         const uint32_t width = dst.start[which + 1] - dst.start[which], col = n - dst.start[which];
         size_t oo = (size_t)row * width + col;
-        if constexpr (kExperts) oo = (size_t)expert_pair(only(term...), order, row) * width + col;
+        if constexpr (kExperts) oo = (size_t)pair_of[row] * width + col;
         if constexpr (kEpilogue) only(term...).apply(y, n);
         if (SWIGLU) {
           float u[8];
@@ -344,9 +355,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
           for (int k = 0; k < 8; ++k) y[k] += rv[k];
         }
         if constexpr (kExperts && !SWIGLU) {
-          float* sums = only(term...).sums;
-          *(f32x4*)(sums + oo) = *(const f32x4*)&y[0];
-          *(f32x4*)(sums + oo + 4) = *(const f32x4*)&y[4];
+          ((u32x4*)only(term...).sums)[oo / 8] = pack_block(y);
           continue;
         }
         if constexpr (kEpilogue) {

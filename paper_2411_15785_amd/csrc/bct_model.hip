@@ -279,7 +279,11 @@ __global__ __launch_bounds__(64 * WAVES) void linear_kernel(const uint16_t* __re
         const uint32_t width = dst.start[which + 1] - dst.start[which], col = n - dst.start[which];
         const size_t oo = (size_t)(r0 + oi) * width + col;
         float g = sum[0][q];
-        if constexpr (kEpilogue) g = activate(only(term...).act, g + only(term...).bias_of(n));
+        if constexpr (kEpilogue) {
+          float v[1] = {g + only(term...).bias_of(n)};
+          activate(only(term...).act, v);
+          g = v[0];
+        }
         float y;
         if (SWIGLU) y = g / (1.0f + __expf(-g)) * sum[NW2 - 1][q];
         else y = residual ? g + bf16f(residual[oo]) : g;

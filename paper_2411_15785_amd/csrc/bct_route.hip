@@ -345,13 +345,6 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(const int32_t* experts, 
   plan_block(experts, plan, P, rows, k, blockIdx.x, s);
 }
 
-bct_status check_plan(uint32_t rows, uint32_t k, uint32_t E) {
-  if (rows == 0 || k == 0 || E == 0) return mfail(BCT_ERR_INVALID_ARG, "zero size");
-  if (E > kMaxExperts || k > kMaxPerToken || k > E) return mfail(BCT_ERR_UNSUPPORTED, "at most 512 experts, 16 of them and not more than there are a token");
-  if ((uint64_t)rows * k > 0x7FFFFFFFull - 0xFFFF) return mfail(BCT_ERR_UNSUPPORTED, "too many tokens");
-  return BCT_OK;
-}
-
 template <typename DT, bool BIAS>
 void launch_route(const RouteArgs& a, const ExpertPlan& P, hipStream_t s) {
   const dim3 grid(P.blocks), block(kThreads);
@@ -363,10 +356,17 @@ void launch_route(const RouteArgs& a, const ExpertPlan& P, hipStream_t s) {
 
 }  // namespace
 
+bct_status check_plan_sizes(uint32_t rows, uint32_t k, uint32_t E) {
+  if (rows == 0 || k == 0 || E == 0) return mfail(BCT_ERR_INVALID_ARG, "zero size");
+  if (E > kMaxExperts || k > kMaxPerToken || k > E) return mfail(BCT_ERR_UNSUPPORTED, "at most 512 experts, 16 of them and not more than there are a token");
+  if ((uint64_t)rows * k > 0x7FFFFFFFull - 0xFFFF) return mfail(BCT_ERR_UNSUPPORTED, "too many tokens");
+  return BCT_OK;
+}
+
 bct_status check_expert_plan(const void* plan, uint32_t rows, uint32_t k, uint32_t E) {
   if (!plan) return mfail(BCT_ERR_INVALID_ARG, "NULL plan");
   if (!al16(plan)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
-  return check_plan(rows, k, E);
+  return check_plan_sizes(rows, k, E);
 }
 
 }  // namespace bct
@@ -377,7 +377,7 @@ extern "C" {
 
 bct_status bctm_expert_plan_bytes(uint32_t rows, uint32_t k, uint32_t n_experts, size_t* bytes, size_t* order) {
   if (!bytes) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer");
-  const bct_status st = check_plan(rows, k, n_experts);
+  const bct_status st = check_plan_sizes(rows, k, n_experts);
   if (st != BCT_OK) return st;
   const ExpertPlan P = ExpertPlan::of(rows, k, n_experts);
   *bytes = P.ints * 4;
@@ -389,7 +389,7 @@ bct_status bctm_route(const void* logits, size_t ld, const float* bias, int32_t*
                       size_t plan_bytes, uint32_t rows, uint32_t n_experts, uint32_t k, float scale, int32_t dtype, uint32_t flags,
                       void* hip_stream) {
   if (!logits || !experts || !weights) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
-  const bct_status st = check_plan(rows, k, n_experts);
+  const bct_status st = check_plan_sizes(rows, k, n_experts);
   if (st != BCT_OK) return st;
   if (dtype != BCT_F32 && dtype != BCT_BF16) return mfail(BCT_ERR_UNSUPPORTED, "logits are float32 or bf16");
   if (flags & ~(BCTM_ROUTE_SIGMOID | BCTM_ROUTE_NORMALISE)) return mfail(BCT_ERR_INVALID_ARG, "unknown flag");
@@ -412,7 +412,7 @@ bct_status bctm_route(const void* logits, size_t ld, const float* bias, int32_t*
 bct_status bctm_expert_plan(const int32_t* experts, void* plan, size_t plan_bytes, uint32_t rows, uint32_t n_experts, uint32_t k,
                             void* hip_stream) {
   if (!experts || !plan) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
-  const bct_status st = check_plan(rows, k, n_experts);
+  const bct_status st = check_plan_sizes(rows, k, n_experts);
   if (st != BCT_OK) return st;
   if (((uintptr_t)experts & 3u) || !al16(plan)) return mfail(BCT_ERR_MISALIGNED, "pointers must be aligned to their type, the plan to 16 bytes");
   const ExpertPlan P = ExpertPlan::of(rows, k, n_experts);

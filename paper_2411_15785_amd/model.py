@@ -18,7 +18,7 @@ MODEL_EXPORTS = ["bctm_embed", "bctm_rmsnorm", "bctm_pack_weight", "bctm_pack_ro
                  "bctm_swiglu", "bctm_linear_plan", "bctm_linear_tile", "bctm_qk_norm_rope",
                  "bctm_lora_workspace", "bctm_lora_pack", "bctm_linear_lora", "bctm_linear_split_lora", "bctm_swiglu_lora",
                  "bctm_linear_act", "bctm_expert_plan_bytes", "bctm_route", "bctm_expert_plan", "bctm_expert_swiglu",
-                 "bctm_expert_workspace", "bctm_expert_linear", "bctm_argmax", "bctm_sample", "bctm_last_error"]
+                 "bctm_expert_tile", "bctm_expert_workspace", "bctm_expert_linear", "bctm_argmax", "bctm_sample", "bctm_last_error"]
 
 BCTM_KERNEL_STREAMING, BCTM_KERNEL_STREAMING_WIDE, BCTM_KERNEL_TILE128, BCTM_KERNEL_TILE256 = 0, 1, 2, 3
 BCTM_KERNEL_STREAMING_TRIPLE = 4
@@ -73,6 +73,7 @@ def mlib() -> ctypes.CDLL:
     L.bctm_route.argtypes = [vp, sz] + [vp] * 4 + [sz, u32, u32, u32, ctypes.c_float, ctypes.c_int32, u32, vp]
     L.bctm_expert_plan.argtypes = [vp, vp, sz, u32, u32, u32, vp]
     L.bctm_expert_swiglu.argtypes = [vp] * 5 + [u32] * 5 + [vp]
+    L.bctm_expert_tile.argtypes = [u32] * 6 + [ctypes.POINTER(u32)] * 2
     L.bctm_expert_workspace.argtypes = [u32] * 3 + [ctypes.POINTER(sz)]
     L.bctm_expert_linear.argtypes = [vp] * 7 + [sz] + [u32] * 5 + [vp]
     for n in MODEL_EXPORTS[:-1]:
@@ -603,6 +604,13 @@ def bctm_expert_swiglu(x, w_gate, w_up, plan, out=None):
     _ck(_launch(mlib().bctm_expert_swiglu, x.device, x.data_ptr(), w_gate.data.data_ptr(), w_up.data.data_ptr(), out.data_ptr(),
                 plan.data.data_ptr(), plan.rows, plan.k, plan.n_experts, w_gate.K, w_gate.N), "bctm_expert_swiglu")
     return out
+
+
+def bctm_expert_tile(rows, k, n_experts, K, N, swiglu):
+    """(pairs, features) that the launch of this shape gives one workgroup."""
+    v = [ctypes.c_uint32(0) for _ in range(2)]
+    _ck(mlib().bctm_expert_tile(rows, k, n_experts, K, N, 1 if swiglu else 0, *(ctypes.byref(a) for a in v)), "bctm_expert_tile")
+    return tuple(a.value for a in v)
 
 
 def bctm_expert_workspace(rows, k, N):

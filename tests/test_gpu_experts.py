@@ -273,7 +273,13 @@ def swiglu_reference(x, wg, wu, ids):
 
 SHAPES = [  # rows, k, E, K, N
     (1, 1, 1, 32, 16), (1, 2, 16, 1024, 512), (7, 3, 5, 96, 48), (32, 8, 64, 256, 176), (50, 2, 3, 2080, 32), (129, 2, 8, 128, 80),
-    (300, 4, 16, 160, 96), (400, 2, 4, 64, 272), (1300, 4, 9, 96, 144), (2000, 2, 4, 64, 528), (1, 16, 512, 32, 16), (260, 1, 2, 1376, 64)]
+    (300, 4, 16, 160, 96), (400, 2, 4, 64, 272), (1300, 4, 9, 96, 144), (2000, 2, 4, 64, 528), (1, 16, 512, 32, 16), (260, 1, 2, 1376, 64),
+    (900, 4, 4, 640, 1040), (2500, 8, 16, 192, 1040), (2600, 4, 4, 640, 2064), (5000, 2, 3, 1376, 1040)]
+
+
+def test_the_shapes_reach_every_tile(M):
+    assert {M.bctm_expert_tile(*s, True) for s in SHAPES} == {(16, 16), (64, 64), (128, 128), (256, 128)}
+    assert {M.bctm_expert_tile(*s, False) for s in SHAPES} == {(16, 32), (64, 128), (128, 256), (256, 256)}
 
 
 @pytest.mark.parametrize("rows,k,E,K,N", SHAPES)
@@ -304,12 +310,17 @@ def test_expert_linear(M, rows, k, E, K, N):
             p = torch.nonzero(flat == e)[:, 0]
             y[p], mass[p] = hd[p] @ wd[e].T, hd[p].abs() @ wd[e].abs().T
         wt = weights.double()[..., None]
+        # Products that wait for their sum in blocks of eight: multiples of 2^(e - 140), with the largest of the eight at least 2^(e - 127)
+        # (1 - 2^-12) in magnitude, so off by at most 2^(e - 141) = 2^-14 / (1 - 2^-12) of it.
+        block = y.abs().view(rows * k, N // 8, 8).max(-1, keepdim=True).values.expand(-1, -1, 8).reshape(rows, k, N)
+        blocks = (2.0 ** -14 * 1.01 * block * wt.abs()).sum(1) if M.bctm_expert_tile(rows, k, E, K, N, False)[0] > 16 else 0.0
         out, mass = (y.view(rows, k, N) * wt).sum(1), (mass.view(rows, k, N) * wt.abs()).sum(1)
         # rows without an expert may hold anything
         hp = torch.where(((flat >= 0) & (flat < E)).to(DEV)[:, None], h, torch.full_like(h, float("nan")))
         wts = weights.to(DEV)
-        close(M.bctm_expert_linear(hp, packed, plan, wts), out, 2.0 ** -20 * mass, "plain")
-        close(M.bctm_expert_linear(hp, packed, plan, wts, res), out + res.double().cpu(), 2.0 ** -20 * (mass + res.double().cpu().abs()), "residual")
+        close(M.bctm_expert_linear(hp, packed, plan, wts), out, 2.0 ** -20 * mass + blocks, "plain")
+        close(M.bctm_expert_linear(hp, packed, plan, wts, res), out + res.double().cpu(),
+              2.0 ** -20 * (mass + res.double().cpu().abs()) + blocks, "residual")
         inplace = res.clone()
         M.bctm_expert_linear(hp, packed, plan, wts, inplace, inplace)
         assert torch.equal(inplace, M.bctm_expert_linear(hp, packed, plan, wts, res))
@@ -342,3 +353,40 @@ def test_nan_and_infinity_stay_with_their_token_and_expert(M):
         want = (ids.reshape(-1) == 2) | (torch.arange(rows * k) // k == 5)
         assert torch.equal(bad, want)
         assert torch.isfinite(out[(~want).to(DEV)]).all()
+
+
+@pytest.mark.parametrize("rows,k,E,K,N", [(40, 2, 4, 64, 528), (2000, 2, 4, 64, 528), (2600, 4, 4, 640, 2064)])
+def test_products_without_a_number_leave_their_neighbours_alone(M, rows, k, E, K, N):
+    """NaN and infinities among the features of a block of eight, and numbers of very different size in one."""
+    h, w = normal(1, (rows * k, K)).abs(), normal(2, (E, N, K), K ** -0.5)
+    ids, _ = choose(4, rows, k, E, none=0)
+    weights = torch.ones((rows, k), device=DEV)
+    plan = M.bctm_expert_plan(ids.to(DEV), E)
+    base = M.bctm_expert_linear(h, M.bctm_pack_experts(w), plan, weights)
+    w2 = w.clone()
+    w2[:, 3] = float("nan")
+    w2[:, 12] = float("inf")
+    w2[:, 13] = float("-inf")
+    w2[:, 40:48] = 0
+    w2[:, 65:72] *= 2.0 ** -40   # feature 64 has the block's numbers to itself
+    w2[:, 72:80] *= 2.0 ** -100
+    w2[:, 80:88] *= 2.0 ** 100
+    got = M.bctm_expert_linear(h, M.bctm_pack_experts(w2), plan, weights)
+    zero = (h == 0).view(rows, -1).any(1)   # 0 times infinity
+    assert torch.isnan(got[:, 3]).all() and torch.isnan(got[zero][:, 12:14]).all()
+    assert (got[~zero][:, 12] == float("inf")).all() and (got[~zero][:, 13] == float("-inf")).all()
+    assert (got[:, 40:48] == 0).all()
+    same = torch.ones(N, dtype=torch.bool, device=DEV)
+    same[[3, 12, 13]] = False
+    same[40:48] = same[64:88] = False
+    same[0:16] = False
+    assert torch.equal(got[:, same], base[:, same])
+    # the neighbours of what is no number: a smaller largest one only makes them more exact
+    near = [i for i in range(16) if i not in (3, 12, 13)] + [64]
+    scale = base[:, :80].float().abs().max().item() + h.float().max().item() * K ** 0.5
+    # two roundings of sums that far apart: one spacing of the larger, which is up to 2^-7 of it, and the sums' own distance
+    g, f = got[:, near].double(), base[:, near].double()
+    off = (g - f).abs() / (spacing(torch.maximum(g.abs(), f.abs())) + k * 2.0 ** -14 * scale)
+    assert off.max().item() <= 1.0
+    assert torch.equal(got[:, 72:80].float(), base[:, 72:80].float() * 2.0 ** -100)
+    assert torch.equal(got[:, 80:88].float(), base[:, 80:88].float() * 2.0 ** 100)
