@@ -155,7 +155,9 @@ bct_status bctm_swiglu_lora(const void* x, const void* w_gate_packed, const void
 /* out[r][n] = (residual ? residual[r][n] : 0) + act((bias ? bias[n] : 0) + sum_k x[r][k] * w[n][k]), everything after the sum in fp32 and
  * rounded once.  bias: bf16 [N].  act: one of BCTM_ACT_.  flags: BCTM_X_TILED as in bctm_linear; BCTM_OUT_F32: out is float32
  * (a router's logits), else bf16; BCTM_OUT_TILED: bf16 as tiled activations (N a multiple of 32).  residual: bf16, row-major; a
- * row-major bf16 out may be the residual.  Shapes, kernels and sums as in bctm_linear. */
+ * row-major bf16 out may be the residual.  Shapes as in bctm_linear, and its kernels and sums but for N a multiple of 64 and 17 rows or
+ * more, where a kernel for few features, which sums K in eight parts, runs if one round of its workgroups (16 or 32 rows x 64
+ * features) is enough, or N is 64; up to 127 rows for N up to 256.  A tiled and a row-major x give the same bits. */
 #define BCTM_OUT_F32 16u
 #define BCTM_ACT_NONE 0u
 #define BCTM_ACT_RELU 1u

@@ -274,6 +274,9 @@ hipError_t launch_linear_rows(const void* x, const void* w, const void* w2, cons
 // The same with bias and activation (bct_linear_act.hip).
 hipError_t launch_linear_rows_act(const void* x, const void* w, const void* residual, const LinearOut& dst, uint32_t rows,
                                   uint32_t K, uint32_t N, bool x_tiled, bool out_tiled, hipStream_t s, const EpilogueTerm& term);
+// Few features: workgroups of 16 * row_tiles rows (1 or 2) and 64 features, K in eight parts; N a multiple of 64.
+hipError_t launch_linear_narrow(const void* x, const void* w, const void* residual, void* out, uint32_t rows, uint32_t K, uint32_t N,
+                                bool x_tiled, bool out_tiled, hipStream_t s, const EpilogueTerm& term, uint32_t row_tiles);
 
 }  // namespace bct
 

@@ -667,6 +667,20 @@ bct_status bctm_linear_lora(const void* x, const void* w, const void* residual, 
   return linear_call(x, w, residual, out, rows, K, N, flags, lora, hip_stream);
 }
 
+// Row tiles of a workgroup of linear_narrow_kernel, 0: another kernel runs.  It reads the rows once for 64 features and its launch is short, so it
+// is for what fits into one round of workgroups, and for 64 features in any case.  Up to 16 rows, or up to 127 of more than 256 features,
+// the streaming kernel has more workgroups for the weights.  us, K = 4096, other kernels | 16 | 32 rows a workgroup, row-major x: 64 features, 32 rows
+// 12.5 | 9.1 | 11.3, 512 13.5 | 9.4 | 11.5, 4096 34.7 | 12.9 | 15.7, 8192 64.0 | 22.2 | 20.8, 16384 122 | 50.7 | 40.9; 4096 of 128 23.5 |
+// 22.1 | 16.8, of 256 23.9 | 40.2 | 28.4; 1024 of 256 23.0 | 11.6 | 13.5, of 320 23.1 | 19.1 | 13.6; 256 of 1024 23.1 | 15.1 | 17.0; 64 of 2048 13.7 | 14.7 |
+// 14.4; 16 of 128 7.8 | 9.2 | 10.7; K = 2048, 1024 of 512 14.4 | 14.5 | 11.0, 8192 of 128 15.2 | 27.6 | 22.8.  Tiled x: 4096 of 64 24.5 | 12.0 | 14.3,
+// 1024 of 64 10.1 | 10.4 | 12.8, 256 of 1024 17.3 | 15.3 | 16.8.
+static uint32_t narrow_row_tiles(uint32_t rows, uint32_t K, uint32_t N) {
+  if (N % 64 != 0 || rows <= 16 || (rows < 128 && N > 256) || N > 16384) return 0;
+  const uint64_t columns = N / 64;
+  if ((rows + 15) / 16 * columns <= 256) return 1;
+  return (rows + 31) / 32 * columns <= 256 || !many_rows(rows, K, N, false) ? 2 : 0;
+}
+
 bct_status bctm_linear_act(const void* x, const void* w, const void* bias, const void* residual, void* out, uint32_t rows,
                            uint32_t K, uint32_t N, uint32_t act, uint32_t flags, void* hip_stream) {
   const bct_status st = check_linear(x, w, out, rows, K, N);
@@ -680,6 +694,9 @@ bct_status bctm_linear_act(const void* x, const void* w, const void* bias, const
   if (!al16(residual) || !al16(bias)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
   const LinearOut dst = {{(uint16_t*)out, nullptr, nullptr}, {0u, N, N, N}};
   const EpilogueTerm term = {(const uint16_t*)bias, act, flags & BCTM_OUT_F32 ? 1u : 0u};
+  if (const uint32_t row_tiles = narrow_row_tiles(rows, K, N))
+    return launched("linear_act", launch_linear_narrow(x, w, residual, out, rows, K, N, flags & BCTM_X_TILED, flags & BCTM_OUT_TILED,
+                                                       (hipStream_t)hip_stream, term, row_tiles));
   if (many_rows(rows, K, N, false))
     return launched("linear_act", launch_linear_rows_act(x, w, residual, dst, rows, K, N, flags & BCTM_X_TILED, flags & BCTM_OUT_TILED,
                                                          (hipStream_t)hip_stream, term));
