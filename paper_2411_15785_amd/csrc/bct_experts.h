@@ -21,7 +21,7 @@ constexpr uint32_t kTileLists = 4, kPlanRows[kTileLists] = {16, 64, 128, 256};
 //   expert    [pairs]      each pair's expert, -1 for none
 //   n_tiles   [kTileLists]
 //   lists     uint4        per row tile: expert, first place in `order`, rows, 0
-//   counts    [blocks][E + 1]  how many pairs of each expert a block of tokens has (while the plan is made)
+//   counts    [blocks][E + 1, filled up to a multiple of 4]  how many pairs of each expert a block of tokens has (while the plan is made)
 struct ExpertPlan {
   uint32_t pairs, E, blocks;
   size_t order, expert, n_tiles, list[kTileLists], counts, ints;   // in ints from the plan's begin
@@ -45,7 +45,7 @@ struct ExpertPlan {
     p.expert = take(p.pairs);
     p.n_tiles = take(kTileLists);
     for (uint32_t i = 0; i < kTileLists; ++i) p.list[i] = take(4 * (size_t)most_tiles(p.pairs, E, kPlanRows[i]));
-    p.counts = take(p.blocks > 1 ? (size_t)p.blocks * (E + 1) : 0);
+    p.counts = take(p.blocks > 1 ? (size_t)p.blocks * ((E + 4) / 4 * 4) : 0);
     p.ints = at;
     return p;
   }

@@ -88,81 +88,160 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return __int_as_float(v < 0 ? (int32_t)(0x80000000u | (0u - (uint32_t)v)) : v);
 }
 
-// The choice of row r by one wavefront: its experts and weights are written, lane s < k returns that of slot s (E: none is left).
+// A lane's V keys in descending order, equal ones as they were (neighbours are exchanged only where they have to be).
+template <typename Key, int V>
+__device__ __forceinline__ void sort_keys(Key (&key)[V], uint32_t (&id)[V]) {
+#pragma unroll
+  for (int n = V - 1; n > 0; --n)
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const bool turn = key[i] < key[i + 1];
+      const Key k = turn ? key[i] : key[i + 1];
+      const uint32_t d = turn ? id[i] : id[i + 1];
+      key[i] = turn ? key[i + 1] : key[i];
+      id[i] = turn ? id[i + 1] : id[i];
+      key[i + 1] = k;
+      id[i + 1] = d;
+    }
+}
+// Takes the largest of all lanes' first keys, which are sorted, out of them: its key, 0 where none is left, and in *expert which it
+// was.  Experts go to the lanes in runs, so of equal ones the lowest lane has the first.
+template <typename Key, int V>
+__device__ __forceinline__ Key take_largest(Key (&key)[V], uint32_t (&id)[V], uint32_t* expert) {
+  const Key best = wave_max(key[0]);
+  const uint32_t from = __builtin_ctzll(__ballot(key[0] == best));
+  *expert = (uint32_t)__builtin_amdgcn_readlane((int)id[0], from);
+  const bool mine = threadIdx.x % 64 == from;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    key[v] = mine ? (v + 1 < V ? key[v + 1] : Key(0)) : key[v];
+    id[v] = mine && v + 1 < V ? id[v + 1] : id[v];
+  }
+  return best;
+}
+__device__ __forceinline__ double lane_of(double v, uint32_t lane) {
+  const long long b = __double_as_longlong(v);
+  return __longlong_as_double((long long)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, lane));
+}
+
+// The choice of row r by one wavefront: its experts and weights are written.  A lane returns the expert that it wrote, E for none,
+// more than E if it wrote nothing.
 template <typename DT, bool BIAS, int V>
 __device__ __forceinline__ uint32_t route_row(const RouteArgs& a, uint32_t r) {
   typedef typename std::conditional<BIAS, double, float>::type F;
-  typedef typename std::conditional<BIAS, u64, uint32_t>::type Key;
   const uint32_t lane = threadIdx.x % 64;
   const typename DT::elem* row = (const typename DT::elem*)a.logits + (size_t)r * a.ld;
-  float l[V];
-  Key key[V];
-  float most = -INFINITY;   // with a bias: the row's largest logit
-  F all = 0;                // and the sum of exp(l - most)
+  float l[V], bias[V];
+  uint32_t key[V], id[V], top = 0;
 #pragma unroll
-  for (int v = 0; v < V; ++v) l[v] = load_elem(row, min(lane + 64 * v, a.E - 1));
-  if constexpr (BIAS) {
-    float bias[V];
-    uint32_t top = 0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      bias[v] = a.bias[min(lane + 64 * v, a.E - 1)];
-      if (lane + 64 * v >= a.E || !(l[v] > -INFINITY)) l[v] = -INFINITY;
-      top = max(top, key_of(l[v]));
-    }
-    F p[V];
-    if (a.sigmoid) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) p[v] = 1.0 / (1.0 + exp(-(double)l[v]));
-    } else {
-      top = wave_max(top);
-      if (top) most = value_of(top);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {   // infinite logits share with one another
-        p[v] = l[v] == -INFINITY ? 0.0 : l[v] == most ? 1.0 : exp((double)l[v] - (double)most);
-        all += p[v];
-      }
-      all = wave_sum(all);
-#pragma unroll
-      for (int v = 0; v < V; ++v) p[v] /= all;
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = l[v] == -INFINITY ? 0 : key_of(p[v] + (double)bias[v]);
-  } else {
-#pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = lane + 64 * v < a.E ? key_of(l[v]) : 0;
+  for (int v = 0; v < V; ++v) {
+    id[v] = lane * V + v;
+    const uint32_t at = min(id[v], a.E - 1);
+    l[v] = load_elem(row, at);
+    if (BIAS) bias[v] = a.bias[at];
   }
-  uint32_t expert = a.E;   // of slot `lane`, and its logit
-  float x = -INFINITY;
-  for (uint32_t s = 0; s < a.k; ++s) {
-    Key best = key[0];
 #pragma unroll
-    for (int v = 1; v < V; ++v) best = max(best, key[v]);
-    best = wave_max(best);
-    if (best == 0) break;   // none is left
-    bool found = false;
+  for (int v = 0; v < V; ++v) {
+    if (id[v] >= a.E || !(l[v] > -INFINITY)) l[v] = -INFINITY;
+    key[v] = key_of(l[v]);
+    top = max(top, key[v]);
+  }
+  uint32_t expert = a.E, slot = lane;   // what the lane has found, and the slot where it goes
+  float x = -INFINITY;                  // its logit
+  uint32_t count = 0;                   // experts found
+  float most = -INFINITY;               // of a softmax: the row's largest logit, with a bias
+  F all = 0;                            // and the sum of exp(l - most)
+  if constexpr (!BIAS) {
+    sort_keys(key, id);
+    for (; count < a.k; ++count) {
+      uint32_t e;
+      const uint32_t best = take_largest(key, id, &e);
+      if (best == 0) break;
+      if (lane == count) {
+        expert = e;
+        x = value_of(best);
+      }
+    }
+  } else {
+    // Sums p + bias have to be compared in 64 bits, but in a few instructions of 32 bits it is seen which ones may be among the first: those
+    // that do not lie below the kth by more than both may be off, 2^-21 for a sigmoid and 2^-23 of the sum.  A lane takes one of them.
+    bool whole = !a.sigmoid;
+    if (a.sigmoid) {
+      uint32_t near_key[V], near_id[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {   // the first expert with that key: those of a v lie before those of the next
-      const u64 has = __ballot(key[v] == best);
-      if (!found && has) {
-        const uint32_t from = __builtin_ctzll(has);
-        found = true;
-        if (lane == from) key[v] = 0;
-        const float of = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l[v]), from));
-        if (lane == s) {
-          expert = from + 64 * v;
-          x = of;
+      for (int v = 0; v < V; ++v) {
+        near_key[v] = l[v] == -INFINITY ? 0 : key_of(__builtin_amdgcn_rcpf(1.f + __expf(-l[v])) + bias[v]);
+        near_id[v] = id[v];
+      }
+      sort_keys(near_key, near_id);
+      uint32_t least = 1, last = 0;
+      for (; count <= 64; ++count) {
+        uint32_t e;
+        last = take_largest(near_key, near_id, &e);
+        if (last < least) break;
+        if (lane == count) expert = e;
+        if (count + 1 == a.k) {
+          const float kth = value_of(last), below = kth - (0x1p-19f + 0x1p-21f * fabsf(kth));
+          least = below == below ? max(key_of(below), 1u) : last;   // an infinite one: those
         }
       }
+      if (count > 64) {   // more than there are lanes
+        whole = true;
+        count = 0;
+      } else {
+        double sum = -INFINITY;
+        if (lane < count) {
+          x = load_elem(row, expert);
+          sum = 1.0 / (1.0 + exp(-(double)x)) + (double)a.bias[expert];
+        }
+        slot = 0;
+        for (uint32_t j = 0; j < count; ++j) {
+          const double other = lane_of(sum, j);
+          const uint32_t e = (uint32_t)__builtin_amdgcn_readlane((int)expert, j);
+          slot += other > sum || (other == sum && e < expert) ? 1 : 0;
+        }
+        if (lane >= count) slot = lane;
+        count = min(count, a.k);
+      }
+    }
+    if (whole) {
+      double p[V];
+      u64 sums[V];
+      if (a.sigmoid) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) p[v] = 1.0 / (1.0 + exp(-(double)l[v]));
+      } else {
+        top = wave_max(top);
+        if (top) most = value_of(top);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {   // infinite logits share with one another
+          p[v] = l[v] == -INFINITY ? 0.0 : l[v] == most ? 1.0 : exp((double)l[v] - (double)most);
+          all += p[v];
+        }
+        all = wave_sum(all);
+#pragma unroll
+        for (int v = 0; v < V; ++v) p[v] /= all;
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) sums[v] = l[v] == -INFINITY ? 0 : key_of(p[v] + (double)bias[v]);
+      sort_keys(sums, id);
+      expert = a.E;
+      for (; count < a.k; ++count) {
+        uint32_t e;
+        if (take_largest(sums, id, &e) == 0) break;
+        if (lane == count) expert = e;
+      }
+      slot = lane;
+      if (lane < count) x = load_elem(row, expert);
     }
   }
   // The chosen scores from their logits.  To be normalised, they may have any factor in common, and are taken against the largest
   // chosen one, so that they do not all underflow: exp(l - m), or as a sigmoid exp(min(l, 0) - min(m, 0)) / (1 + exp(-|l|)).
-  const bool has = expert < a.E;
+  const bool has = slot < a.k && expert < a.E;
   F weight = 0, total = 1;
   if (a.normalise || !(a.sigmoid || BIAS)) {
-    const uint32_t top = wave_max(key_of(x));
-    if (top) most = value_of(top);   // without a bias the first one chosen is the row's largest
+    const uint32_t first = wave_max(has ? key_of(x) : 0u);
+    if (first) most = value_of(first);   // without a bias the first one chosen is the row's largest
   }
   if (a.sigmoid) {
     if (has) weight = exp((F)fminf(x, 0.f) - (a.normalise ? (F)fminf(most, 0.f) : (F)0)) / ((F)1 + exp(-(F)fabsf(x)));
@@ -177,20 +256,22 @@ __device__ __forceinline__ uint32_t route_row(const RouteArgs& a, uint32_t r) {
       total = 0;
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (lane + 64 * v < a.E && l[v] > -INFINITY) total += l[v] == most ? 1.f : expf(l[v] - most);
+        if (l[v] > -INFINITY) total += l[v] == most ? 1.f : expf(l[v] - most);
       total = wave_sum(total);
     }
   }
-  if (lane < a.k) {
-    a.experts[(size_t)r * a.k + lane] = has ? (int32_t)expert : -1;
-    a.weights[(size_t)r * a.k + lane] = has ? (float)(weight / total * (F)a.scale) : 0.f;
+  const bool none = lane < a.k && lane >= count;   // fewer experts than slots: the last ones are empty
+  if (has || none) {
+    const size_t at = (size_t)r * a.k + (has ? slot : lane);
+    a.experts[at] = has ? (int32_t)expert : -1;
+    a.weights[at] = has ? (float)(weight / total * (F)a.scale) : 0.f;
   }
-  return expert;
+  return has ? expert : none ? a.E : a.E + 1;
 }
 
 struct PlanShared {
   uint32_t wave[kWaves][kMaxExperts + 1];   // pairs of an expert in a wavefront's share, then where its next one goes
-  uint32_t total[kThreads], before[kThreads];
+  uint32_t total[4 * kThreads], before[4 * kThreads];
   uint32_t tile[kTileLists][kMaxExperts + 1];   // an expert's first row tile
   uint32_t scan[kTileLists + 1][kWaves];
 };
@@ -201,7 +282,8 @@ __device__ __forceinline__ void plan_block(const int32_t* experts, int32_t* plan
   const uint32_t lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), E = P.E, C = E + 1;
   const uint32_t per_block = P.block_rows(rows) * k, p0 = min(block * per_block, P.pairs), p1 = min(p0 + per_block, P.pairs);
   const uint32_t share = ((p1 - p0 + kWaves - 1) / kWaves + 63) / 64 * 64, w0 = min(p0 + wave * share, p1), w1 = min(w0 + share, p1);
-  for (uint32_t w = 0; w < kWaves; ++w)
+  const uint32_t waves = share ? (p1 - p0 + share - 1) / share : 0;   // that have a share; a block behind the last token has none
+  for (uint32_t w = 0; w < waves; ++w)
     if (threadIdx.x < C) s.wave[w][threadIdx.x] = 0;
   __syncthreads();
   for (uint32_t p = w0 + lane; p < w1; p += 64) {
@@ -209,37 +291,39 @@ __device__ __forceinline__ void plan_block(const int32_t* experts, int32_t* plan
     atomicAdd(&s.wave[wave][e], 1u);
     plan[P.expert + p] = e < E ? (int32_t)e : -1;
   }
-  // What all blocks and the blocks before this one have of each expert: thread (group, expert) adds up every groups-th block.
+  // What all blocks and the blocks before this one have of each expert: a thread adds up four experts of every groups-th block.
   if (P.blocks > 1) {
-    const uint32_t* counts = (const uint32_t*)plan + P.counts;
-    uint32_t width = 64;
-    while (width < C) width *= 2;
-    const uint32_t groups = kThreads / width, e = threadIdx.x % width;
-    uint32_t all = 0, before = 0;
-    if (e < C) {
+    const uint32_t quads = (C + 3) / 4, groups = kThreads / quads, g = threadIdx.x / quads, q = threadIdx.x % quads;
+    const uint4* counts = (const uint4*)(plan + P.counts) + q;
+    uint4 all = make_uint4(0, 0, 0, 0), before = all;
+    if (g < groups) {
 #pragma unroll 8
-      for (uint32_t b = threadIdx.x / width; b < P.blocks; b += groups) {
-        const uint32_t n = counts[(size_t)b * C + e];
-        all += n;
-        before += b < block ? n : 0;
+      for (uint32_t b = g; b < P.blocks; b += groups) {
+        const uint4 n = counts[(size_t)b * quads];
+        const uint32_t m = b < block ? ~0u : 0u;
+        all = make_uint4(all.x + n.x, all.y + n.y, all.z + n.z, all.w + n.w);
+        before = make_uint4(before.x + (n.x & m), before.y + (n.y & m), before.z + (n.z & m), before.w + (n.w & m));
       }
     }
-    s.total[threadIdx.x] = all;
-    s.before[threadIdx.x] = before;
+    ((uint4*)s.total)[threadIdx.x] = all;
+    ((uint4*)s.before)[threadIdx.x] = before;
     __syncthreads();
-    if (threadIdx.x < width) {   // only this thread reads and writes entry e of the first group
-      for (uint32_t i = 1; i < groups; ++i) {
-        all += s.total[i * width + e];
-        before += s.before[i * width + e];
+    uint32_t a = 0, f = 0;
+    if (threadIdx.x < C)
+      for (uint32_t i = 0; i < groups; ++i) {
+        a += s.total[i * 4 * quads + threadIdx.x];
+        f += s.before[i * 4 * quads + threadIdx.x];
       }
-      s.total[e] = all;
-      s.before[e] = before;
+    __syncthreads();
+    if (threadIdx.x < C) {
+      s.total[threadIdx.x] = a;
+      s.before[threadIdx.x] = f;
     }
   } else {
     __syncthreads();
     if (threadIdx.x < C) {
       uint32_t all = 0;
-      for (uint32_t w = 0; w < kWaves; ++w) all += s.wave[w][threadIdx.x];
+      for (uint32_t w = 0; w < waves; ++w) all += s.wave[w][threadIdx.x];
       s.total[threadIdx.x] = all;
       s.before[threadIdx.x] = 0;
     }
@@ -262,7 +346,7 @@ __device__ __forceinline__ void plan_block(const int32_t* experts, int32_t* plan
     const uint32_t first = run[kTileLists] - n;
     uint32_t at = first + s.before[e];
     s.before[e] = first;
-    for (uint32_t w = 0; w < kWaves; ++w) {
+    for (uint32_t w = 0; w < waves; ++w) {
       const uint32_t c = s.wave[w][e];
       s.wave[w][e] = at;
       at += c;
@@ -320,11 +404,11 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a, ExpertPlan
   }
   for (uint32_t r = r0 + wave; r < r1; r += kWaves) {
     const uint32_t e = route_row<DT, BIAS, V>(a, r);
-    if (counts && threadIdx.x % 64 < a.k) atomicAdd(&s.count[e], 1u);
+    if (counts && e <= a.E) atomicAdd(&s.count[e], 1u);
   }
   __syncthreads();
   if (counts) {
-    if (threadIdx.x < C) a.plan[P.counts + (size_t)blockIdx.x * C + threadIdx.x] = (int32_t)s.count[threadIdx.x];
+    if (threadIdx.x < C) a.plan[P.counts + (size_t)blockIdx.x * ((C + 3) / 4 * 4) + threadIdx.x] = (int32_t)s.count[threadIdx.x];
   } else if (a.plan) {
     plan_block(a.experts, a.plan, P, a.rows, a.k, 0, s.plan);
   }
@@ -338,7 +422,7 @@ __global__ __launch_bounds__(kThreads) void count_kernel(const int32_t* experts,
   __syncthreads();
   for (uint32_t p = p0 + threadIdx.x; p < p1; p += kThreads) atomicAdd(&count[min((uint32_t)experts[p], P.E)], 1u);
   __syncthreads();
-  if (threadIdx.x < C) plan[P.counts + (size_t)blockIdx.x * C + threadIdx.x] = (int32_t)count[threadIdx.x];
+  if (threadIdx.x < C) plan[P.counts + (size_t)blockIdx.x * ((C + 3) / 4 * 4) + threadIdx.x] = (int32_t)count[threadIdx.x];
 }
 __global__ __launch_bounds__(kThreads) void plan_kernel(const int32_t* experts, int32_t* plan, ExpertPlan P, uint32_t rows, uint32_t k) {
   __shared__ PlanShared s;
