@@ -248,7 +248,7 @@ def make_stack_weights(shape, seed: int = 0):
             if len(shp) == 1:
                 lw[name] = draw(shp, 0.1, 1.0)
             else:
-                lw[name] = draw(shp, 1.0 / np.sqrt(shp[1]))
+                lw[name] = draw(shp, 1.0 / np.sqrt(shp[-1]))
         layers.append(lw)
     keys = [draw((shape.n_kv_heads, shape.capacity_M, shape.head_dim), 1.0) for _ in range(shape.n_layers)]
     return {"embed": draw((shape.vocab, shape.dim), 1.0), "final_norm": draw((shape.dim,), 0.1, 1.0),

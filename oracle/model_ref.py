@@ -106,6 +106,27 @@ def low_rank(x, ids, a, b, scale):
     return out
 
 
+def expert_weights(logits, ids, sigmoid, normalise, scale):
+    """scale * score of each row's experts ids [rows][k] (negative: none), over the sum of the chosen scores if normalise; scores are
+    the softmax or the sigmoids of logits [rows][E]."""
+    score = 1.0 / (1.0 + np.exp(-logits)) if sigmoid else np.exp(logits - logits.max(axis=1, keepdims=True))
+    if not sigmoid:
+        score = score / score.sum(axis=1, keepdims=True)
+    w = np.where(ids >= 0, np.take_along_axis(score, np.maximum(ids, 0), axis=1), 0.0)
+    return scale * (w / w.sum(axis=1, keepdims=True) if normalise else w)
+
+
+def experts(h, ids, weights, w_gate, w_up, w_down):
+    """Sum over each row's slots of weight * the SwiGLU MLP of its expert, in float64 (the gated product rounded to bf16)."""
+    out = np.zeros((len(h), w_down.shape[1]))
+    for e in range(len(w_gate)):
+        r, s = np.nonzero(ids == e)
+        if r.size:
+            out_e = linear_f64(swiglu(h[r], w_gate[e], w_up[e]), w_down[e])
+            np.add.at(out, r, weights[r, s][:, None] * out_e)
+    return out
+
+
 class RefStack:
     """The decoder stack on the CPU.  shape: an object with n_layers, dim, n_q_heads, n_kv_heads, head_dim,
     ffn, vocab, capacity_M, batch, eps; weights: the same dictionary layout as the GPU driver, as uint16 arrays."""
@@ -121,9 +142,29 @@ class RefStack:
             c.set_values(None)
             self.caches.append(c)
 
-    def forward(self, ids, T=1, trace=None, positions=None, adapters=None, lora=None):
+    def mlp_experts(self, h, lw, choice, margin):
+        """The experts' MLP with the choice [rows][k] that was made elsewhere; it has to be one that these logits allow: no expert that was
+        left out has a larger score (with its bias) than one that was taken, by more than margin."""
+        s = self.s
+        logits = linear_f64(h, lw["w_router"])
+        rank = logits
+        if s.router_bias or s.router_sigmoid:
+            rank = 1.0 / (1.0 + np.exp(-logits)) if s.router_sigmoid else np.exp(logits) / np.exp(logits).sum(axis=1, keepdims=True)
+            if s.router_bias:
+                rank = rank + bf16_to_f64(lw["router_bias"])
+        taken = np.take_along_axis(rank, choice, axis=1)
+        left = rank.copy()
+        np.put_along_axis(left, choice, -np.inf, axis=1)
+        assert np.all(left.max(axis=1) <= taken.min(axis=1) + margin), "experts that the logits do not allow"
+        assert all(len(set(c)) == s.experts_per_token for c in choice.tolist()), "an expert twice"
+        w = expert_weights(logits, choice, s.router_sigmoid, s.router_normalise, s.router_scale)
+        y = experts(h, choice, w, lw["w_gate"], lw["w_up"], lw["w_down"])
+        return y
+
+    def forward(self, ids, T=1, trace=None, positions=None, adapters=None, lora=None, choices=None, margin=0.0):
         """ids [B*T] -> (next ids, logits bits).  trace, if a list, receives the residual stream after each layer.
-        lora: per layer {projection: (a, b, scale)} of any projection by its weight's name; adapters: each row's."""
+        lora: per layer {projection: (a, b, scale)} of any projection by its weight's name; adapters: each row's.
+        choices: per layer each row's experts, of a shape with experts (see mlp_experts)."""
         s = self.s
         x = embed(ids, self.w["embed"])
         rope = getattr(s, "rope_base", 0.0)
@@ -157,6 +198,13 @@ class RefStack:
                               wv.reshape(s.batch, T, s.n_kv_heads, s.head_dim), T)
             x = f64_to_bf16(project(l, "w_o", a.reshape(s.batch * T, -1)) + bf16_to_f64(x))
             h = rmsnorm(x, lw["mlp_norm"], s.eps)
+            if getattr(s, "n_experts", 0):
+                if s.shared_ffn:
+                    x = linear(swiglu(h, lw["w_shared_gate"], lw["w_shared_up"]), lw["w_shared_down"], x)
+                x = f64_to_bf16(self.mlp_experts(h, lw, choices[l], margin) + bf16_to_f64(x))
+                if trace is not None:
+                    trace.append(x.copy())
+                continue
             g, u = project(l, "w_gate", h), project(l, "w_up", h)
             with np.errstate(over="ignore"):
                 f = f64_to_bf16(g / (1.0 + np.exp(-g)) * u)

@@ -703,8 +703,19 @@ class StackShape:
     rope_base: float = 0.0        # > 0: turned by their token's position, inv_freq[j] = rope_base ** (-2 j / rotary_dim)
     rotary_dim: int = 0           # how much of each head is turned (0: all of it)
     rope_interleaved: bool = False
+    n_experts: int = 0            # > 0: experts of width ffn in place of the dense MLP, experts_per_token of them for each token
+    experts_per_token: int = 0
+    router_sigmoid: bool = False  # scores are the logits' sigmoids, not their softmax
+    router_bias: bool = False     # a weight router_bias is added to the scores for the choice (not for the weights)
+    router_normalise: bool = True
+    router_scale: float = 1.0
+    shared_ffn: int = 0           # > 0: beside its experts every token goes through a dense SwiGLU of that width
 
     def __post_init__(self):
+        if self.n_experts and (not 1 <= self.experts_per_token <= min(16, self.n_experts) or self.n_experts > 512 or self.shared_ffn % 32):
+            raise ValueError("experts_per_token must be 1 to 16 of at most 512 experts, shared_ffn a multiple of 32")
+        if not self.n_experts and (self.experts_per_token or self.router_sigmoid or self.router_bias or self.shared_ffn):
+            raise ValueError("experts_per_token, router_sigmoid, router_bias and shared_ffn go with n_experts")
         if (self.head_norm or self.rope_base) and (self.head_dim % 16 or self.rotary_dim % 16 or
                                                    not 0 <= self.rotary_dim <= self.head_dim or self.rope_base < 0):
             raise ValueError("head_dim and rotary_dim must be multiples of 16, rotary_dim at most head_dim, rope_base not negative")
@@ -723,10 +734,19 @@ class StackShape:
 
     def weight_shapes(self):
         """name -> shape of every per-layer weight, in the order load_layer expects."""
-        return {"attn_norm": (self.dim,), "w_q": (self.q_width, self.dim), "w_wq": (self.kv_width, self.dim),
-                "w_wv": (self.kv_width, self.dim), "w_o": (self.dim, self.q_width), "mlp_norm": (self.dim,),
-                "w_gate": (self.ffn, self.dim), "w_up": (self.ffn, self.dim), "w_down": (self.dim, self.ffn),
-                **({"q_norm": (self.head_dim,), "wq_norm": (self.head_dim,)} if self.head_norm else {})}
+        E = (self.n_experts,) if self.n_experts else ()
+        shapes = {"attn_norm": (self.dim,), "w_q": (self.q_width, self.dim), "w_wq": (self.kv_width, self.dim),
+                  "w_wv": (self.kv_width, self.dim), "w_o": (self.dim, self.q_width), "mlp_norm": (self.dim,),
+                  "w_gate": (*E, self.ffn, self.dim), "w_up": (*E, self.ffn, self.dim), "w_down": (*E, self.dim, self.ffn),
+                  **({"q_norm": (self.head_dim,), "wq_norm": (self.head_dim,)} if self.head_norm else {})}
+        if E:
+            shapes["w_router"] = (self.n_experts, self.dim)
+            if self.router_bias:
+                shapes["router_bias"] = (self.n_experts,)
+            if self.shared_ffn:
+                shapes.update(w_shared_gate=(self.shared_ffn, self.dim), w_shared_up=(self.shared_ffn, self.dim),
+                              w_shared_down=(self.dim, self.shared_ffn))
+        return shapes
 
     def weight_bytes(self):
         per_layer = sum(math.prod(s) for s in self.weight_shapes().values())
@@ -753,6 +773,8 @@ class BctStack:
               "layers": [ {name: tensor} per layer, names of StackShape.weight_shapes() ],
               "keys": [ MK per layer, [Hkv][M][d] ]}  -- all bf16 device tensors.
     With shape.head_norm and / or shape.rope_base, q and wq pass bctm_qk_norm_rope before the cache.
+    With shape.n_experts each token's MLP is that of the experts a router chooses for it (bctm_linear_act, bctm_route,
+    bctm_expert_swiglu, bctm_expert_linear), beside a shared one with shape.shared_ffn.
     """
 
     def __init__(self, shape: StackShape, weights, max_prefill_T=0, device="cuda:0"):
@@ -776,8 +798,14 @@ class BctStack:
             for n, shp in s.weight_shapes().items():
                 if tuple(lw[n].shape) != shp or lw[n].dtype != torch.bfloat16:
                     raise ValueError(f"layer {l} {n}: expected bf16 {shp}")
-                if len(shp) == 1:
+                if n == "router_bias":
+                    pl[n] = lw[n].float()
+                elif len(shp) == 1:
                     pl[n] = lw[n]
+                elif len(shp) == 3:
+                    pl[n] = bctm_pack_experts(lw[n])
+                elif n == "w_router":   # features are packed by 16, and a multiple of 64 has a kernel of its own
+                    pl[n] = bctm_pack_weight(torch.nn.functional.pad(lw[n], (0, 0, 0, -shp[0] % 64)))
                 elif n not in ("w_q", "w_wq", "w_wv"):
                     pl[n] = bctm_pack_weight(lw[n])
             # the three projections of the attention input run as one launch with three outputs
@@ -802,8 +830,9 @@ class BctStack:
             if len(layers) != self.shape.n_layers:
                 raise ValueError(f"adapters: expected {self.shape.n_layers} layers")
             s = self.shape
-            want = {"qkv": (s.dim, s.q_width + 2 * s.kv_width, 3, False), "o": (s.q_width, s.dim, 1, False),
-                    "gate_up": (s.dim, s.ffn, 2, True), "down": (s.ffn, s.dim, 1, False)}
+            want = {"qkv": (s.dim, s.q_width + 2 * s.kv_width, 3, False), "o": (s.q_width, s.dim, 1, False)}
+            if not s.n_experts:   # experts have no adapters
+                want.update(gate_up=(s.dim, s.ffn, 2, True), down=(s.ffn, s.dim, 1, False))
             for l, d in enumerate(layers):
                 for n, a in d.items():
                     if n not in want or not isinstance(a, LoraWeights) or (a.K, a.N, a.segments, a.b_up is not None) != want[n] \
@@ -838,6 +867,29 @@ class BctStack:
         if k not in self._bufs:
             self._bufs[k] = TiledRows(rows, cols, self.device)
         return self._bufs[k]
+
+    def _experts(self, x, lw, rows):
+        """x += the experts' (and the shared) MLP of its norm."""
+        torch = _torch()
+        s = self.shape
+        k = ("experts", rows)
+        if k not in self._bufs:   # the layers run one after the other and share them
+            dev = self.device
+            self._bufs[k] = (torch.empty((rows, (s.n_experts + 63) // 64 * 64), dtype=torch.float32, device=dev),
+                             torch.empty((rows, s.experts_per_token), dtype=torch.int32, device=dev),
+                             torch.empty((rows, s.experts_per_token), dtype=torch.float32, device=dev),
+                             ExpertPlan(rows, s.experts_per_token, s.n_experts, dev),
+                             torch.empty(bctm_expert_workspace(rows, s.experts_per_token, s.dim), dtype=torch.uint8, device=dev))
+        logits, experts, weights, plan, workspace = self._bufs[k]
+        h = bctm_rmsnorm(x, lw["mlp_norm"], s.eps, self._buf("h", rows, s.dim))
+        bctm_linear_act(h, lw["w_router"], out=logits)
+        bctm_route(logits[:, :s.n_experts], s.experts_per_token, lw.get("router_bias"), s.router_sigmoid, s.router_normalise, s.router_scale,
+                   experts, weights, plan)
+        if s.shared_ffn:
+            f = bctm_swiglu(h, lw["w_shared_gate"], lw["w_shared_up"], self._tiled("shared", rows, s.shared_ffn), tiled=True)
+            bctm_linear(f, lw["w_shared_down"], x, x)
+        g = bctm_expert_swiglu(h, lw["w_gate"], lw["w_up"], plan, self._buf("g", rows * s.experts_per_token, s.ffn))
+        bctm_expert_linear(g, lw["w_down"], plan, weights, x, x, workspace)
 
     def forward(self, ids, T=1, next_ids=None, head="all", positions=None, adapters=None, sampling=None):
         """ids int32 [B*T] (sequence-major: row b*T + t) -> (next ids, logits).
@@ -908,6 +960,9 @@ class BctStack:
                 bctm_linear_lora(ax, lw["w_o"], lora["o"], adapters, x, x, lora_ws)
             else:
                 bctm_linear(ax, lw["w_o"], x, x)
+            if s.n_experts:
+                self._experts(x, lw, rows)
+                continue
             bctm_rmsnorm(x, lw["mlp_norm"], s.eps, h, tiled=True)
             if "gate_up" in lora:
                 bctm_swiglu_lora(h, lw["w_gate"], lw["w_up"], lora["gate_up"], adapters, f, True, lora_ws)
