@@ -33,7 +33,10 @@ struct ExpertPlan {
     ExpertPlan p;
     p.pairs = rows * k;
     p.E = E;
-    p.blocks = rows <= kOneBlock ? 1 : (rows + kBlockRows - 1) / kBlockRows;
+    // One block is one launch, several are two; but a compute unit takes long over many tokens of many experts.  us in a graph, all in one | 64 | 16
+    // | 4 tokens a block, 8 of 64 experts: 32 tokens 10.8 | - | 12.7 | -, 128 15.7 | 13.9 | 12.7 | 12.7, 1024 - | 14.1 | 13.1 | 14.2; 8 of 256 with a
+    // bias: 32 24.2 | - | 20.6 | 17.6, 64 32.6 | - | 20.1 | 17.7, 1024 - | 31.4 | 21.4 | 23.5.
+    p.blocks = rows <= 64 && rows * E <= 4096 ? 1 : (rows + 15) / 16;
     if (p.blocks > kMostBlocks) p.blocks = kMostBlocks;
     size_t at = (E + 4) / 4 * 4;
     auto take = [&](size_t n) {
@@ -51,7 +54,7 @@ struct ExpertPlan {
   }
   // tokens of a block, the last one may have fewer
   __host__ __device__ uint32_t block_rows(uint32_t rows) const { return (rows + blocks - 1) / blocks; }
-  static constexpr uint32_t kOneBlock = 64, kBlockRows = 64, kMostBlocks = 256;
+  static constexpr uint32_t kMostBlocks = 256;
 };
 
 // The checks of a plan's sizes and pointer.
@@ -69,56 +72,74 @@ struct ExpertTerm {
 };
 
 // Eight sums in 16 bytes: whole numbers of 15 bits, multiples of a power of two that they share, each in the upper bits of a
-// half word; the lowest bits of the eight are that power's exponent.  Between the products of the way back and their weighted
-// sum, halves a pass over memory and back that is a third of the call with fp32 (4096 tokens of 8 experts, 1376 -> 4096).  A number is off by at
-// most 2^-14 of the largest of its eight (which is 2^13 steps at least), where the bf16 result is rounded to 2^-9 of itself.  Sums below 2^-126 are 0; NaN
-// and the infinities have numbers of their own, so their neighbours are as exact as others.
-constexpr int kBlockMost = 16382, kBlockInf = 16383, kBlockNan = -16384;
+// half word; the lowest bits of the eight are that power's exponent, word w has its bits w and w + 4.  Between the products of the way back
+// and their weighted sum, halves a pass over memory and back that is a third of the call with fp32 (4096 tokens of 8 experts, 1376 ->
+// 4096).  A number is off by at most 2^-14 of the largest of its eight (which is 2^13 steps at least, as long as a step is not below
+// 2^-126), where the bf16 result is rounded to 2^-9 of itself.  NaN and the infinities have numbers of their own, so their
+// neighbours are as exact as others.
+constexpr int kBlockMost = 16382, kBlockInf = 16383, kBlockNan = -16384, kBlockLeast = 14;
+__device__ __forceinline__ uint32_t block_bits(uint32_t e, int w) { return (e | e << 12) >> w & 0x00010001u; }
+// The largest magnitude below 2^(e - 126) / (1 + 2^-12), so times 2^(140 - e) it is below kBlockMost, and 2^13 (1 - 2^-12) at least.
+__device__ __forceinline__ uint32_t block_exponent(float top) {
+  return max(__float_as_uint(top * (1.f + 1.f / 4096)) >> 23, (uint32_t)kBlockLeast);
+}
 __device__ __forceinline__ u32x4 pack_block(const float (&y)[8]) {
   float top = 0.f;
+  bool number = true;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(y[i]));   // of a NaN and a number, the number
-  bool odd = false;
-  if (!(top < INFINITY)) {
-    odd = true;
-    top = 0.f;
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(y[i]));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fabsf(y[i]) < INFINITY ? fmaxf(top, fabsf(y[i])) : top;
-  }
-  // the largest is below 2^(e - 126) / (1 + 2^-12), so times 2^(140 - e) below kBlockMost, and 2^13 (1 - 2^-12) at least
-  const uint32_t e = __float_as_uint(top * (1.f + 1.f / 4096)) >> 23;
-  const int shift = 140 - (int)e;
+  for (int i = 0; i < 8; ++i) number = number && y[i] == y[i];   // fmaxf passes over a NaN
   u32x4 v;
+  if (number && top < INFINITY) {
+    const uint32_t e = block_exponent(top);
+    const float scale = __uint_as_float((140 + 127 - e) << 23);   // 2^(140 - e)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      // 1.5 2^23 + q has q in its lower bits, rounded to the nearest by the addition
+      const uint32_t lo = __float_as_uint(__builtin_fmaf(y[2 * w], scale, 12582912.f)), hi = __float_as_uint(__builtin_fmaf(y[2 * w + 1], scale, 12582912.f));
+      v[w] = (__builtin_amdgcn_perm(hi, lo, 0x05040100u) << 1 & 0xFFFEFFFEu) | block_bits(e, w);
+    }
+    return v;
+  }
+  top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fabsf(y[i]) < INFINITY ? fmaxf(top, fabsf(y[i])) : top;
+  const uint32_t e = block_exponent(top);
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     uint32_t half[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int i = 2 * w + h;
-      float f = __builtin_amdgcn_ldexpf(y[i], shift);
-      int q = (int)rintf(__builtin_amdgcn_fmed3f(f, -(float)kBlockMost, (float)kBlockMost));
-      if (odd || y[i] != y[i]) q = y[i] != y[i] ? kBlockNan : y[i] == INFINITY ? kBlockInf : y[i] == -INFINITY ? -kBlockInf : q;
-      half[h] = ((uint32_t)q << 1 | (e >> i & 1)) & 0xFFFFu;
+      const float f = y[2 * w + h];
+      const int q = f != f ? kBlockNan : f == INFINITY ? kBlockInf : f == -INFINITY ? -kBlockInf : (int)rintf(__builtin_amdgcn_ldexpf(f, 140 - (int)e));
+      half[h] = (uint32_t)q << 1 & 0xFFFEu;
     }
-    v[w] = half[0] | half[1] << 16;
+    v[w] = half[0] | half[1] << 16 | block_bits(e, w);
   }
   return v;
 }
-__device__ __forceinline__ void unpack_block(const u32x4 v, float (&y)[8]) {
-  uint32_t e = 0;
+// y += weight * the block's sums.
+__device__ __forceinline__ void add_block(const u32x4 v, float weight, float (&y)[8]) {
+  uint32_t x = 0;
   int q[8], most = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int half = i % 2 ? (int)v[i / 2] >> 16 : (int)(int16_t)v[i / 2];
-    e |= (uint32_t)(half & 1) << i;
-    q[i] = half >> 1;
-    most = max(most, max(q[i], -q[i]));
+  for (int w = 0; w < 4; ++w) {
+    x |= (v[w] & 0x00010001u) << w;
+    q[2 * w] = (int)(v[w] << 16) >> 17;
+    q[2 * w + 1] = (int)v[w] >> 17;
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = __builtin_amdgcn_ldexpf((float)q[i], (int)e - 140);
-  if (most > kBlockMost) {
+  for (int i = 0; i < 8; ++i) most = max(most, max(q[i], -q[i]));
+  const int e = (int)((x | x >> 12) & 0xFFu);
+  const float scale = __builtin_amdgcn_ldexpf(1.f, e - 140);
+  if (most <= kBlockMost) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = q[i] == kBlockNan ? __builtin_nanf("") : q[i] == kBlockInf ? INFINITY : q[i] == -kBlockInf ? -INFINITY : y[i];
+    for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(weight, (float)q[i] * scale, y[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      y[i] = __builtin_fmaf(weight, q[i] == kBlockNan ? __builtin_nanf("") : q[i] == kBlockInf ? INFINITY : q[i] == -kBlockInf ? -INFINITY : (float)q[i] * scale, y[i]);
   }
 }
 

@@ -91,16 +91,16 @@ __global__ __launch_bounds__(256) void combine_kernel(const void* sums, const in
     const size_t p = (size_t)r * k + s;
     if (expert[p] < 0) continue;
     const float w = weights[p];
-    float v[8];
     if constexpr (BLOCKS) {
-      unpack_block(((const u32x4*)sums)[p * chunks + c], v);
+      add_block(((const u32x4*)sums)[p * chunks + c], w, y);
     } else {
-      const f32x4* from = (const f32x4*)sums + (p * chunks + c) * 2;
-      *(f32x4*)&v[0] = from[0];
-      *(f32x4*)&v[4] = from[1];
-    }
+      const f32x4 *from = (const f32x4*)sums + (p * chunks + c) * 2, lo = from[0], hi = from[1];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(w, v[e], y[e]);
+      for (int e = 0; e < 4; ++e) {
+        y[e] = __builtin_fmaf(w, lo[e], y[e]);
+        y[4 + e] = __builtin_fmaf(w, hi[e], y[4 + e]);
+      }
+    }
   }
   if (residual) {
     float v[8];

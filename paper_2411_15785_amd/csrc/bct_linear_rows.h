@@ -347,7 +347,10 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
           *(f32x4*)&u[0] = *(const f32x4*)&e[rr][CW / 2 + 8 * cc];
           *(f32x4*)&u[4] = *(const f32x4*)&e[rr][CW / 2 + 8 * cc + 4];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] = y[k] / (1.0f + __expf(-y[k])) * u[k];
+          for (int k = 0; k < 8; ++k) {
+            if constexpr (kExperts) y[k] = y[k] * __builtin_amdgcn_rcpf(1.0f + __expf(-y[k])) * u[k];
+            else y[k] = y[k] / (1.0f + __expf(-y[k])) * u[k];
+          }
         } else if (residual) {
           float rv[8];
           unpack16<BF16>(*(const u32x4*)(residual + oo), rv);

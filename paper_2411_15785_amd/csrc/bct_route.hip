@@ -4,8 +4,10 @@
 //   the k experts with the largest l, or with a bias p + bias; equal ones by number
 //   weight = scale * p / (sum of the chosen p, or 1)
 //
-// A wavefront has a token: lane i holds the experts i, i + 64, ..., and the choice is k times a maximum over the lanes.  With a bias,
-// scores are worked out in 64 bits, as two experts' sums may lie closer than fp32 tells them apart.
+// Sixteen lanes have a token, each a run of its experts, and the choice is k times a maximum: over a lane's keys, then over the sixteen
+// by the data-parallel primitives, so four tokens share the instructions of a wavefront, which is what bounds it.  With a bias, scores
+// are worked out in 64 bits, as two experts' sums may lie closer than fp32 tells them apart: of sigmoids only those of the few that fp32 leaves
+// near the border, of a softmax all, by a whole wavefront for a token.
 //
 // The plan is a counting sort of the pairs (token, slot) by expert that depends on no order of atomics: blocks of tokens count
 // their experts, then each block adds up what the blocks before it counted and gives its pairs their places, a wavefront's
@@ -119,154 +121,202 @@ __device__ __forceinline__ Key take_largest(Key (&key)[V], uint32_t (&id)[V], ui
   }
   return best;
 }
-__device__ __forceinline__ double lane_of(double v, uint32_t lane) {
+
+// The value of the lane that is `distance` 1, 2, 4 or 8 away among sixteen that have their own, or one for every 2, 4, 8.
+template <int CTRL>
+__device__ __forceinline__ uint32_t of_sixteen(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+}
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+  v = max(v, of_sixteen<0xB1>(v));    // the other of a pair
+  v = max(v, of_sixteen<0x4E>(v));    // the other pair of four
+  v = max(v, of_sixteen<0x141>(v));   // mirrored in eight
+  return max(v, of_sixteen<0x140>(v));   // in sixteen
+}
+__device__ __forceinline__ float sum16(float v) { return xor_sum<1, 8>(v); }
+template <int L>
+__device__ __forceinline__ double row_lane(double v) {
   const long long b = __double_as_longlong(v);
-  return __longlong_as_double((long long)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, lane));
+  return __longlong_as_double((long long)of_sixteen<0x150 + L>((uint32_t)(b >> 32)) << 32 | of_sixteen<0x150 + L>((uint32_t)b));
 }
 
-// The choice of row r by one wavefront: its experts and weights are written.  A lane returns the expert that it wrote, E for none,
-// more than E if it wrote nothing.
-template <typename DT, bool BIAS, int V>
-__device__ __forceinline__ uint32_t route_row(const RouteArgs& a, uint32_t r) {
-  typedef typename std::conditional<BIAS, double, float>::type F;
+// Writes what was chosen for a token: a lane with has has the expert, its logit x and the slot where it goes; `empty`: the slot of a lane
+// that has none, if it is one of the k.  most: of a softmax without normalising, the row's largest logit, and all the sum of exp(l - most).
+// MAX, SUM: over the token's lanes.
+// The scores come from the logits.  To be normalised, they may have any factor in common, and are taken against the largest chosen one,
+// so that they do not all underflow: exp(l - m), or as a sigmoid exp(min(l, 0) - min(m, 0)) / (1 + exp(-|l|)).
+template <typename MAX, typename SUM>
+__device__ __forceinline__ void write_choice(const RouteArgs& a, uint32_t r, bool has, uint32_t expert, float x, uint32_t slot, bool empty,
+                                             uint32_t lane, float most, float all, uint32_t* counts, MAX max_of, SUM sum_of) {
+  if (a.normalise) {
+    const uint32_t first = max_of(has ? key_of(x) : 0u);
+    most = value_of(first);
+  }
+  float weight = 0.f, total = 1.f;
+  if (a.sigmoid) {
+    if (has) weight = expf(fminf(x, 0.f) - (a.normalise ? fminf(most, 0.f) : 0.f)) / (1.f + expf(-fabsf(x)));
+  } else {
+    if (has) weight = x == most ? 1.f : expf(x - most);
+    total = all;
+  }
+  if (a.normalise) total = sum_of(weight);
+  if (has || empty) {
+    const size_t at = (size_t)r * a.k + (has ? slot : lane);
+    a.experts[at] = has ? (int32_t)expert : -1;
+    a.weights[at] = has ? weight / total * a.scale : 0.f;
+    if (counts) atomicAdd(&counts[has ? expert : a.E], 1u);
+  }
+}
+
+// The choice with a bias in 64 bits throughout, by a whole wavefront.
+template <typename DT, int V>
+__device__ __forceinline__ void route_whole(const RouteArgs& a, uint32_t r, uint32_t* counts) {
   const uint32_t lane = threadIdx.x % 64;
   const typename DT::elem* row = (const typename DT::elem*)a.logits + (size_t)r * a.ld;
-  float l[V], bias[V];
-  uint32_t key[V], id[V], top = 0;
+  float l[V], most = -INFINITY;
+  uint32_t id[V], top = 0;
+  u64 sums[V];
+  double p[V], all = 0;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     id[v] = lane * V + v;
-    const uint32_t at = min(id[v], a.E - 1);
+    l[v] = load_elem(row, min(id[v], a.E - 1));
+    asm("" : "+v"(l[v]));
+    if (id[v] >= a.E || !(l[v] > -INFINITY)) l[v] = -INFINITY;
+    top = max(top, key_of(l[v]));
+  }
+  if (a.sigmoid) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) p[v] = 1.0 / (1.0 + exp(-(double)l[v]));
+  } else {
+    top = wave_max(top);
+    if (top) most = value_of(top);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {   // infinite logits share with one another
+      p[v] = l[v] == -INFINITY ? 0.0 : l[v] == most ? 1.0 : exp((double)l[v] - (double)most);
+      all += p[v];
+    }
+    all = wave_sum(all);
+#pragma unroll
+    for (int v = 0; v < V; ++v) p[v] /= all;
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) sums[v] = l[v] == -INFINITY ? 0 : key_of(p[v] + (double)a.bias[min(id[v], a.E - 1)]);
+  sort_keys(sums, id);
+  uint32_t expert = a.E, count = 0;
+  for (; count < a.k; ++count) {
+    uint32_t e;
+    if (take_largest(sums, id, &e) == 0) break;
+    if (lane == count) expert = e;
+  }
+  const bool has = lane < count;
+  const float x = has ? load_elem(row, expert) : -INFINITY;
+  write_choice(a, r, has, expert, x, lane, !has && lane < a.k, lane, most, (float)all, counts,
+               [](uint32_t v) { return wave_max(v); }, [](float v) { return wave_sum(v); });
+}
+
+// The choice for four tokens from r on (those below r1) by a wavefront, V of a token's experts to each of its sixteen lanes: four side by
+// side, so that four lanes read 64 bytes, and the four that are 64 further.  counts: how many of each expert there are is added to
+// it, if it is not null.
+template <typename DT, bool BIAS, int V>
+__device__ __forceinline__ void route_four(const RouteArgs& a, uint32_t r, uint32_t r1, uint32_t* counts) {
+  const uint32_t lane = threadIdx.x % 16, group = threadIdx.x % 64 / 16, mine = r + group;
+  if (BIAS && !a.sigmoid) {
+    for (uint32_t i = r; i < min(r + 4, r1); ++i) route_whole<DT, V / 4>(a, i, counts);
+    return;
+  }
+  const bool there = mine < r1;
+  const typename DT::elem* row = (const typename DT::elem*)a.logits + (size_t)min(mine, r1 - 1) * a.ld;
+  uint32_t key[V];
+  float most = -INFINITY, all = 1.f;
+  float l[V], bias[V];
+  auto expert_of = [&](uint32_t v) -> uint32_t { return 4 * lane + v / 4 * 64 + v % 4; };
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const uint32_t at = min(expert_of(v), a.E - 1);
     l[v] = load_elem(row, at);
     if (BIAS) bias[v] = a.bias[at];
   }
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    if (id[v] >= a.E || !(l[v] > -INFINITY)) l[v] = -INFINITY;
-    key[v] = key_of(l[v]);
-    top = max(top, key[v]);
+    // requested all at once: behind the branch that the compiler makes of what follows, they would be waited for one by one
+    asm("" : "+v"(l[v]));
+    if (BIAS) asm("" : "+v"(bias[v]));
   }
-  uint32_t expert = a.E, slot = lane;   // what the lane has found, and the slot where it goes
-  float x = -INFINITY;                  // its logit
-  uint32_t count = 0;                   // experts found
-  float most = -INFINITY;               // of a softmax: the row's largest logit, with a bias
-  F all = 0;                            // and the sum of exp(l - most)
-  if constexpr (!BIAS) {
-    sort_keys(key, id);
-    for (; count < a.k; ++count) {
-      uint32_t e;
-      const uint32_t best = take_largest(key, id, &e);
-      if (best == 0) break;
-      if (lane == count) {
-        expert = e;
-        x = value_of(best);
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    key[v] = expert_of(v) < a.E ? key_of(l[v]) : 0;
+    if constexpr (BIAS) key[v] = key[v] ? key_of(__builtin_amdgcn_rcpf(1.f + __expf(-l[v])) + bias[v]) : 0;
+  }
+  if (!BIAS && !a.sigmoid && !a.normalise) {   // the softmax' sum over all experts
+    uint32_t top = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) top = max(top, key[v]);
+    top = max16(top);
+    most = value_of(top);
+    all = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (key[v]) all += key[v] == top ? 1.f : expf(value_of(key[v]) - most);
+    all = sum16(all);
+  }
+  // With a bias the rounds go on, to the last lane, as long as a sum does not lie below the kth by more than both may be off: 2^-21 for a
+  // sigmoid of fp32, 2^-23 of the sum.
+  uint32_t count = 0, least = 1, expert = a.E;   // found; no smaller key is; what is in this lane's place
+  bool more = false;
+  for (uint32_t s = 0; s < (BIAS ? 17u : a.k); ++s) {
+    uint32_t best = key[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) best = max(best, key[v]);
+    best = max16(best);
+    if (BIAS && s >= a.k && __ballot(best >= least && there) == 0) break;
+    // the first expert that has it
+    uint32_t at = V;
+#pragma unroll
+    for (int v = V - 1; v >= 0; --v) at = key[v] == best ? v : at;
+    const uint32_t e = at < V ? expert_of(at) : ~0u, first = ~max16(~e);
+    at = e == first ? at : V;
+#pragma unroll
+    for (int v = 0; v < V; ++v) key[v] = at == v ? 0 : key[v];
+    if (best >= least) {
+      if (lane == s) expert = first;
+      ++count;
+      more = BIAS && s == 16;
+    }
+    if constexpr (BIAS) {
+      if (s + 1 == a.k) {
+        const float kth = value_of(best), below = kth - (0x1p-19f + 0x1p-21f * fabsf(kth));
+        least = best < least ? ~0u : below == below ? max(key_of(below), 1u) : best;   // none left; an infinite one: those
       }
     }
+  }
+  uint32_t slot = lane;
+  const bool listed = lane < count && there;
+  if (!listed) expert = a.E;
+  const float x = listed ? load_elem(row, expert) : -INFINITY;
+  if constexpr (BIAS) {
+    double sum = -INFINITY;
+    if (listed) sum = 1.0 / (1.0 + exp(-(double)x)) + (double)a.bias[expert];
+    slot = 0;
+    auto against = [&](auto j) {   // how many come before this one; equal sums were found in the order of their numbers or not at all
+      const double other = row_lane<decltype(j)::v>(sum);
+      const uint32_t e = of_sixteen<0x150 + decltype(j)::v>(expert);
+      slot += other > sum || (other == sum && e < expert) ? 1 : 0;
+    };
+    against(Int<0>{}), against(Int<1>{}), against(Int<2>{}), against(Int<3>{}), against(Int<4>{}), against(Int<5>{}), against(Int<6>{});
+    against(Int<7>{}), against(Int<8>{}), against(Int<9>{}), against(Int<10>{}), against(Int<11>{}), against(Int<12>{}), against(Int<13>{});
+    against(Int<14>{}), against(Int<15>{});
+    const u64 whole = __ballot(more && there && lane == 0);   // more near the border than there are lanes
+    count = min(count, a.k);
+    const bool mine_done = there && !more;
+    write_choice(a, mine, listed && !more && slot < a.k, expert, x, slot, mine_done && lane >= count && lane < a.k, lane, most, all, counts,
+                 [](uint32_t v) { return max16(v); }, [](float v) { return sum16(v); });
+    for (uint32_t g = 0; g < 4; ++g)
+      if (whole >> (16 * g) & 1) route_whole<DT, V / 4>(a, r + g, counts);
   } else {
-    // Sums p + bias have to be compared in 64 bits, but in a few instructions of 32 bits it is seen which ones may be among the first: those
-    // that do not lie below the kth by more than both may be off, 2^-21 for a sigmoid and 2^-23 of the sum.  A lane takes one of them.
-    bool whole = !a.sigmoid;
-    if (a.sigmoid) {
-      uint32_t near_key[V], near_id[V];
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        near_key[v] = l[v] == -INFINITY ? 0 : key_of(__builtin_amdgcn_rcpf(1.f + __expf(-l[v])) + bias[v]);
-        near_id[v] = id[v];
-      }
-      sort_keys(near_key, near_id);
-      uint32_t least = 1, last = 0;
-      for (; count <= 64; ++count) {
-        uint32_t e;
-        last = take_largest(near_key, near_id, &e);
-        if (last < least) break;
-        if (lane == count) expert = e;
-        if (count + 1 == a.k) {
-          const float kth = value_of(last), below = kth - (0x1p-19f + 0x1p-21f * fabsf(kth));
-          least = below == below ? max(key_of(below), 1u) : last;   // an infinite one: those
-        }
-      }
-      if (count > 64) {   // more than there are lanes
-        whole = true;
-        count = 0;
-      } else {
-        double sum = -INFINITY;
-        if (lane < count) {
-          x = load_elem(row, expert);
-          sum = 1.0 / (1.0 + exp(-(double)x)) + (double)a.bias[expert];
-        }
-        slot = 0;
-        for (uint32_t j = 0; j < count; ++j) {
-          const double other = lane_of(sum, j);
-          const uint32_t e = (uint32_t)__builtin_amdgcn_readlane((int)expert, j);
-          slot += other > sum || (other == sum && e < expert) ? 1 : 0;
-        }
-        if (lane >= count) slot = lane;
-        count = min(count, a.k);
-      }
-    }
-    if (whole) {
-      double p[V];
-      u64 sums[V];
-      if (a.sigmoid) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) p[v] = 1.0 / (1.0 + exp(-(double)l[v]));
-      } else {
-        top = wave_max(top);
-        if (top) most = value_of(top);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {   // infinite logits share with one another
-          p[v] = l[v] == -INFINITY ? 0.0 : l[v] == most ? 1.0 : exp((double)l[v] - (double)most);
-          all += p[v];
-        }
-        all = wave_sum(all);
-#pragma unroll
-        for (int v = 0; v < V; ++v) p[v] /= all;
-      }
-#pragma unroll
-      for (int v = 0; v < V; ++v) sums[v] = l[v] == -INFINITY ? 0 : key_of(p[v] + (double)bias[v]);
-      sort_keys(sums, id);
-      expert = a.E;
-      for (; count < a.k; ++count) {
-        uint32_t e;
-        if (take_largest(sums, id, &e) == 0) break;
-        if (lane == count) expert = e;
-      }
-      slot = lane;
-      if (lane < count) x = load_elem(row, expert);
-    }
+    write_choice(a, mine, listed, expert, x, slot, there && lane >= count && lane < a.k, lane, most, all, counts,
+                 [](uint32_t v) { return max16(v); }, [](float v) { return sum16(v); });
   }
-  // The chosen scores from their logits.  To be normalised, they may have any factor in common, and are taken against the largest
-  // chosen one, so that they do not all underflow: exp(l - m), or as a sigmoid exp(min(l, 0) - min(m, 0)) / (1 + exp(-|l|)).
-  const bool has = slot < a.k && expert < a.E;
-  F weight = 0, total = 1;
-  if (a.normalise || !(a.sigmoid || BIAS)) {
-    const uint32_t first = wave_max(has ? key_of(x) : 0u);
-    if (first) most = value_of(first);   // without a bias the first one chosen is the row's largest
-  }
-  if (a.sigmoid) {
-    if (has) weight = exp((F)fminf(x, 0.f) - (a.normalise ? (F)fminf(most, 0.f) : (F)0)) / ((F)1 + exp(-(F)fabsf(x)));
-    if (a.normalise) total = wave_sum(weight);
-  } else {
-    if (has) weight = x == most ? (F)1 : exp((F)x - (F)most);
-    if (a.normalise) {
-      total = wave_sum(weight);
-    } else if constexpr (BIAS) {
-      total = all;
-    } else {
-      total = 0;
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (l[v] > -INFINITY) total += l[v] == most ? 1.f : expf(l[v] - most);
-      total = wave_sum(total);
-    }
-  }
-  const bool none = lane < a.k && lane >= count;   // fewer experts than slots: the last ones are empty
-  if (has || none) {
-    const size_t at = (size_t)r * a.k + (has ? slot : lane);
-    a.experts[at] = has ? (int32_t)expert : -1;
-    a.weights[at] = has ? (float)(weight / total * (F)a.scale) : 0.f;
-  }
-  return has ? expert : none ? a.E : a.E + 1;
 }
 
 struct PlanShared {
@@ -402,10 +452,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a, ExpertPlan
     if (threadIdx.x < C) s.count[threadIdx.x] = 0;
     __syncthreads();
   }
-  for (uint32_t r = r0 + wave; r < r1; r += kWaves) {
-    const uint32_t e = route_row<DT, BIAS, V>(a, r);
-    if (counts && e <= a.E) atomicAdd(&s.count[e], 1u);
-  }
+  for (uint32_t r = r0 + 4 * wave; r < r1; r += 4 * kWaves) route_four<DT, BIAS, V>(a, r, r1, counts ? s.count : nullptr);
   __syncthreads();
   if (counts) {
     if (threadIdx.x < C) a.plan[P.counts + (size_t)blockIdx.x * ((C + 3) / 4 * 4) + threadIdx.x] = (int32_t)s.count[threadIdx.x];
@@ -432,10 +479,10 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(const int32_t* experts, 
 template <typename DT, bool BIAS>
 void launch_route(const RouteArgs& a, const ExpertPlan& P, hipStream_t s) {
   const dim3 grid(P.blocks), block(kThreads);
-  if (a.E <= 64) hipLaunchKernelGGL((route_kernel<DT, BIAS, 1>), grid, block, 0, s, a, P);
-  else if (a.E <= 128) hipLaunchKernelGGL((route_kernel<DT, BIAS, 2>), grid, block, 0, s, a, P);
-  else if (a.E <= 256) hipLaunchKernelGGL((route_kernel<DT, BIAS, 4>), grid, block, 0, s, a, P);
-  else hipLaunchKernelGGL((route_kernel<DT, BIAS, 8>), grid, block, 0, s, a, P);
+  if (a.E <= 64) hipLaunchKernelGGL((route_kernel<DT, BIAS, 4>), grid, block, 0, s, a, P);
+  else if (a.E <= 128) hipLaunchKernelGGL((route_kernel<DT, BIAS, 8>), grid, block, 0, s, a, P);
+  else if (a.E <= 256) hipLaunchKernelGGL((route_kernel<DT, BIAS, 16>), grid, block, 0, s, a, P);
+  else hipLaunchKernelGGL((route_kernel<DT, BIAS, 32>), grid, block, 0, s, a, P);
 }
 
 }  // namespace
