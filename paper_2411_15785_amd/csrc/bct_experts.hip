@@ -79,26 +79,35 @@ __global__ __launch_bounds__(64 * WAVES) void expert_few_kernel(const uint16_t* 
 }
 
 // out[r][8 c ..] = residual + the token's products, weighted, in the order of its slots.  A thread has eight features of a token.
-// BLOCKS: products come as blocks of eight (pack_block), else fp32.
-template <bool BLOCKS>
+// BLOCKS: products come as blocks of eight (pack_block), else fp32.  S slots are requested at once, whether they have an expert or not: behind a
+// branch they would be waited for one by one.
+template <bool BLOCKS, int S>
 __global__ __launch_bounds__(256) void combine_kernel(const void* sums, const int32_t* expert, const float* weights, const uint16_t* residual,
                                                       uint16_t* out, uint32_t rows, uint32_t k, uint32_t N) {
   const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   const uint32_t chunks = N / 8, r = (uint32_t)(i / chunks), c = (uint32_t)(i % chunks);
   if (r >= rows) return;
   float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (uint32_t s = 0; s < k; ++s) {
-    const size_t p = (size_t)r * k + s;
-    if (expert[p] < 0) continue;
-    const float w = weights[p];
-    if constexpr (BLOCKS) {
-      add_block(((const u32x4*)sums)[p * chunks + c], w, y);
-    } else {
-      const f32x4 *from = (const f32x4*)sums + (p * chunks + c) * 2, lo = from[0], hi = from[1];
+  for (uint32_t s = 0; s < k; s += S) {
+    u32x4 v[S][BLOCKS ? 1 : 2];
+    int32_t id[S];
+    float w[S];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        y[e] = __builtin_fmaf(w, lo[e], y[e]);
-        y[4 + e] = __builtin_fmaf(w, hi[e], y[4 + e]);
+    for (int u = 0; u < S; ++u) {
+      const size_t p = (size_t)r * k + min(s + u, k - 1);
+      id[u] = s + u < k ? expert[p] : -1;
+      w[u] = weights[p];
+#pragma unroll
+      for (int h = 0; h < (BLOCKS ? 1 : 2); ++h) v[u][h] = ((const u32x4*)sums)[(p * chunks + c) * (BLOCKS ? 1 : 2) + h];
+    }
+#pragma unroll
+    for (int u = 0; u < S; ++u) {
+      if (id[u] < 0) continue;   // its product was not computed
+      if constexpr (BLOCKS) {
+        add_block(v[u][0], w[u], y);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(w[u], __uint_as_float(v[u][e / 4][e % 4]), y[e]);
       }
     }
   }
@@ -241,7 +250,10 @@ bct_status bctm_expert_linear(const void* h, const void* w_packed, const void* p
   hipStream_t s = (hipStream_t)hip_stream;
   const ExpertPlan P = ExpertPlan::of(rows, k, n_experts);
   launch_products<false>(h, w_packed, nullptr, nullptr, workspace, (const int32_t*)plan, rows, k, n_experts, K, N, s);
-  const auto combine = expert_form(P.pairs, n_experts, K, N, false) == kFew ? combine_kernel<false> : combine_kernel<true>;
+  const bool blocks = expert_form(P.pairs, n_experts, K, N, false) != kFew;
+  const auto combine = k <= 2   ? (blocks ? combine_kernel<true, 2> : combine_kernel<false, 2>)
+                       : k <= 4 ? (blocks ? combine_kernel<true, 4> : combine_kernel<false, 4>)
+                                : (blocks ? combine_kernel<true, 8> : combine_kernel<false, 8>);
   hipLaunchKernelGGL(combine, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, (const void*)workspace,
                      (const int32_t*)plan + P.expert, weights, (const uint16_t*)residual, (uint16_t*)out, rows, k, N);
   return launched("expert_linear");
