@@ -83,7 +83,8 @@ __device__ __forceinline__ uint32_t block_bits(uint32_t e, int w) { return (e | 
 __device__ __forceinline__ uint32_t block_exponent(float top) {
   return max(__float_as_uint(top * (1.f + 1.f / 4096)) >> 23, (uint32_t)kBlockLeast);
 }
-__device__ __forceinline__ u32x4 pack_block(const float (&y)[8]) {
+// lds: the same eight, for those that are not all numbers: a loop, so that this, which stands in an epilogue many times, stays short.
+__device__ __forceinline__ u32x4 pack_block(const float (&y)[8], const float* lds) {
   float top = 0.f;
   bool number = true;
 #pragma unroll
@@ -103,20 +104,20 @@ __device__ __forceinline__ u32x4 pack_block(const float (&y)[8]) {
     return v;
   }
   top = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = fabsf(y[i]) < INFINITY ? fmaxf(top, fabsf(y[i])) : top;
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) top = fabsf(lds[i]) < INFINITY ? fmaxf(top, fabsf(lds[i])) : top;
   const uint32_t e = block_exponent(top);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    uint32_t half[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float f = y[2 * w + h];
-      const int q = f != f ? kBlockNan : f == INFINITY ? kBlockInf : f == -INFINITY ? -kBlockInf : (int)rintf(__builtin_amdgcn_ldexpf(f, 140 - (int)e));
-      half[h] = (uint32_t)q << 1 & 0xFFFEu;
-    }
-    v[w] = half[0] | half[1] << 16 | block_bits(e, w);
+  unsigned long long low = 0, high = 0;
+#pragma unroll 1
+  for (int i = 7; i >= 0; --i) {
+    const float f = lds[i];
+    const int q = f != f ? kBlockNan : f == INFINITY ? kBlockInf : f == -INFINITY ? -kBlockInf : (int)rintf(__builtin_amdgcn_ldexpf(f, 140 - (int)e));
+    high = high << 16 | low >> 48;
+    low = low << 16 | ((uint32_t)q << 1 & 0xFFFEu);
   }
+  v = u32x4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) v[w] |= block_bits(e, w);
   return v;
 }
 // y += weight * the block's sums.

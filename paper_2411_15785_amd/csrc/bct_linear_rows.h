@@ -36,7 +36,9 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   constexpr int ND = TT / NW, NA = TA / NW, NB = TB / NW;  // of them per wavefront
   static_assert(TA % NW == 0 && TB % NW == 0, "tiles must divide among the wavefronts");
   static_assert(!PAIR || !XT, "tiled activations have no half lines");
-  constexpr int S = 4;                             // LDS stages
+  // LDS stages.  Three leave room for two workgroups of 128 x 256 on a compute unit, and one begins and ends under the other's
+  // products: with experts, whose tiles are many, 4096 tokens of 8 in 64 1376 -> 4096 618 -> 550 us, gated 4096 -> 1376 910 -> 858.
+  constexpr int S = kExperts && MI == 4 && NW == 8 ? 3 : 4;
   constexpr bool PING = NW * KS == 8;              // two wavefronts per SIMD that take turns
   constexpr uint32_t HB = 4;                       // row tiles of a band
   constexpr uint32_t BM = 16 * MI * WR;            // token rows of a workgroup
@@ -45,7 +47,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   __shared__ __attribute__((aligned(16))) u32x4 st0[KS * TT * 64];
   __shared__ __attribute__((aligned(16))) u32x4 st1[KS * TT * 64];
   __shared__ __attribute__((aligned(16))) u32x4 st2[KS * TT * 64];
-  __shared__ __attribute__((aligned(16))) u32x4 st3[KS * TT * 64];
+  __shared__ __attribute__((aligned(16))) u32x4 st3[S > 3 ? KS * TT * 64 : 1];
   __shared__ uint32_t pair_of[kExperts ? BM : 1];   // the pairs of the tile's rows
 
   uint32_t RT = (rows + BM - 1) / BM;
@@ -227,7 +229,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
   __builtin_amdgcn_sched_barrier(0);
   request(Int<1>{}, 1, Int<PAIR ? NA : 0>{}, Int<ND>{});
   __builtin_amdgcn_sched_barrier(0);
-  request(Int<2>{}, 2, Int<PAIR ? NA : 0>{}, Int<ND>{});
+  if constexpr (S > 3) request(Int<2>{}, 2, Int<PAIR ? NA : 0>{}, Int<ND>{});
   __builtin_amdgcn_sched_barrier(0);
   // The low-rank term first, while the stages fill: what it loads is waited for together with them.  With two groups, the first
   // takes that of the first half of the row tiles.
@@ -261,12 +263,13 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
     k_step(Int<0>{}, kt, Int<0>{});
     k_step(Int<1>{}, kt + 1, Int<0>{});
     k_step(Int<2>{}, kt + 2, Int<0>{});
-    k_step(Int<3>{}, kt + 3, Int<0>{});
+    if constexpr (S > 3) k_step(Int<3>{}, kt + 3, Int<0>{});
   }
   if (kt < kmost) k_step(Int<0>{}, kt, Int<1>{});
   if (kt + 1 < kmost) k_step(Int<1>{}, kt + 1, Int<1>{});
-  if (kt + 2 < kmost) k_step(Int<2>{}, kt + 2, Int<1>{});
-  if (KS > 1 && kt + 3 < kmost) k_step(Int<3>{}, kt + 3, Int<1>{});
+  if ((S > 3 || KS > 1) && kt + 2 < kmost) k_step(Int<2>{}, kt + 2, Int<1>{});
+  if constexpr (S > 3)
+    if (KS > 1 && kt + 3 < kmost) k_step(Int<3>{}, kt + 3, Int<1>{});
   if (PING && !second) bare_barrier();   // every wavefront passes the same number of barriers
   __builtin_amdgcn_s_waitcnt(wait_vm(0));   // the stages are free once the last requests have arrived
   __syncthreads();
@@ -328,7 +331,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const int cc = lane % CPR;
-#pragma unroll kEpilogue ? 1 : 16 / RPP
+#pragma unroll kEpilogue || kExperts ? 1 : 16 / RPP
     for (int ps = 0; ps < 16 / RPP; ++ps) {
       const int rr = ps * RPP + lane / CPR;
       const uint32_t row = kExperts ? ((grp * MO + i) * WR + wr) * 16 + rr : r0 + wr * (16 * MI) + (grp * MO + i) * 16 + rr;
@@ -358,7 +361,7 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
           for (int k = 0; k < 8; ++k) y[k] += rv[k];
         }
         if constexpr (kExperts && !SWIGLU) {
-          ((u32x4*)only(term...).sums)[oo / 8] = pack_block(y);
+          ((u32x4*)only(term...).sums)[oo / 8] = pack_block(y, &e[rr][8 * cc]);
           continue;
         }
         if constexpr (kEpilogue) {
