@@ -18,7 +18,7 @@ constexpr uint32_t kTileLists = 4, kPlanRows[kTileLists] = {16, 64, 128, 256};
 // A plan in memory, int32 unless said otherwise; a pair is token * k + slot.
 //   offsets   [E + 1]      where each expert's pairs begin in `order`; the last one: how many pairs have an expert
 //   order     [pairs]      the pairs by expert, equal ones by number; those without an expert last
-//   expert    [pairs]      each pair's expert, -1 for none
+//   expert    [pairs]      1 + each pair's expert, 0 for none: a plan of zeros has no tokens
 //   n_tiles   [kTileLists]
 //   lists     uint4        per row tile: expert, first place in `order`, rows, 0
 //   counts    [blocks][E + 1, filled up to a multiple of 4]  how many pairs of each expert a block of tokens has (while the plan is made)

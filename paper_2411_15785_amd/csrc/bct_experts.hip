@@ -95,14 +95,14 @@ __global__ __launch_bounds__(256) void combine_kernel(const void* sums, const in
 #pragma unroll
     for (int u = 0; u < S; ++u) {
       const size_t p = (size_t)r * k + min(s + u, k - 1);
-      id[u] = s + u < k ? expert[p] : -1;
+      id[u] = s + u < k ? expert[p] : 0;
       w[u] = weights[p];
 #pragma unroll
       for (int h = 0; h < (BLOCKS ? 1 : 2); ++h) v[u][h] = ((const u32x4*)sums)[(p * chunks + c) * (BLOCKS ? 1 : 2) + h];
     }
 #pragma unroll
     for (int u = 0; u < S; ++u) {
-      if (id[u] < 0) continue;   // its product was not computed
+      if (id[u] == 0) continue;   // its product was not computed
       if constexpr (BLOCKS) {
         add_block(v[u][0], w[u], y);
       } else {

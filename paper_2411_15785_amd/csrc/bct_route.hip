@@ -339,7 +339,7 @@ __device__ __forceinline__ void plan_block(const int32_t* experts, int32_t* plan
   for (uint32_t p = w0 + lane; p < w1; p += 64) {
     const uint32_t e = min((uint32_t)experts[p], E);   // a negative one is beyond E
     atomicAdd(&s.wave[wave][e], 1u);
-    plan[P.expert + p] = e < E ? (int32_t)e : -1;
+    plan[P.expert + p] = e < E ? (int32_t)e + 1 : 0;
   }
   // What all blocks and the blocks before this one have of each expert: a thread adds up four experts of every groups-th block.
   if (P.blocks > 1) {

@@ -390,3 +390,123 @@ def test_products_without_a_number_leave_their_neighbours_alone(M, rows, k, E, K
     assert off.max().item() <= 1.0
     assert torch.equal(got[:, 72:80].float(), base[:, 72:80].float() * 2.0 ** -100)
     assert torch.equal(got[:, 80:88].float(), base[:, 80:88].float() * 2.0 ** 100)
+
+
+# ------------------------------------------------------------------ together, as a layer uses them
+
+
+class Layer:
+    """Router, experts and their way back on buffers of their own."""
+
+    def __init__(self, M, rows, E, k, dim, ffn, seed=1):
+        self.M, self.k, self.E = M, k, E
+        self.x = normal(seed, (rows, dim))
+        self.router = M.bctm_pack_weight(normal(seed + 1, (64 * ((E + 63) // 64), dim), dim ** -0.5))
+        self.gate, self.up = (M.bctm_pack_experts(normal(seed + i, (E, ffn, dim), dim ** -0.5)) for i in (2, 3))
+        self.down = M.bctm_pack_experts(normal(seed + 4, (E, dim, ffn), ffn ** -0.5))
+        self.bias = normal(seed + 5, (E,), 0.05, F32)
+        self.logits = torch.empty((rows, 64 * ((E + 63) // 64)), device=DEV)
+        self.experts, self.weights = torch.empty((rows, k), dtype=torch.int32, device=DEV), torch.empty((rows, k), device=DEV)
+        self.plan = M.ExpertPlan(rows, k, E, DEV)
+        self.h = torch.zeros((rows * k, ffn), dtype=BF16, device=DEV)
+        self.out = torch.empty((rows, dim), dtype=BF16, device=DEV)
+        self.workspace = torch.empty(M.bctm_expert_workspace(rows, k, dim), dtype=torch.uint8, device=DEV)
+
+    def __call__(self):
+        M = self.M
+        M.bctm_linear_act(self.x, self.router, out=self.logits)
+        M.bctm_route(self.logits[:, :self.E], self.k, self.bias, True, experts=self.experts, weights=self.weights, plan=self.plan)
+        M.bctm_expert_swiglu(self.x, self.gate, self.up, self.plan, self.h)
+        return M.bctm_expert_linear(self.h, self.down, self.plan, self.weights, self.x, self.out, self.workspace)
+
+
+@pytest.mark.parametrize("rows,E,k,dim,ffn", [(1, 8, 2, 256, 96), (40, 12, 3, 128, 64), (700, 70, 6, 512, 160), (3000, 4, 2, 1056, 2080)])
+def test_captured_layers_follow_their_inputs(M, rows, E, k, dim, ffn):
+    """Replays with other tokens, and so other experts and another plan, eager work of a second layer in between."""
+    a, b = Layer(M, rows, E, k, dim, ffn), Layer(M, rows, E, k, dim, ffn)
+    a()
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        a()
+    for step in range(4):
+        x = normal(100 + step, (rows, dim))
+        if step == 2:
+            x[rows // 2:] = x[0]   # many tokens for the same experts
+        a.x.copy_(x)
+        b.x.copy_(x)
+        g.replay()
+        b()
+        torch.cuda.synchronize()
+        assert torch.equal(a.experts, b.experts) and torch.equal(a.plan.order, b.plan.order) and torch.equal(a.plan.offsets, b.plan.offsets)
+        assert torch.equal(a.weights, b.weights) and torch.equal(a.out.view(torch.int16), b.out.view(torch.int16)), step
+        check_plan(b.plan, b.experts.cpu().numpy(), E)
+
+
+def test_two_streams_at_once(M):
+    """Two layers that share weights and nothing else, each on a stream of its own, many times: the bits of the same calls one after the other."""
+    a, b = Layer(M, 300, 16, 4, 512, 160), Layer(M, 300, 16, 4, 512, 160)
+    for n in ("router", "gate", "up", "down", "bias"):
+        setattr(b, n, getattr(a, n))
+    b.x = normal(77, (300, 512))
+    want = [a().clone(), b().clone()]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(20):
+        for i, layer in enumerate((a, b)):
+            with torch.cuda.stream(streams[i]):
+                layer()
+                got[i].append(layer.out.clone())
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o.view(torch.int16), want[i].view(torch.int16)) for o in got[i])
+
+
+def test_a_plan_that_was_not_made_has_no_tokens(M):
+    """Products by a plan of zeros write nothing; the weighted sum of nothing is the residual."""
+    x, w = normal(1, (20, 64)), M.bctm_pack_experts(normal(2, (4, 32, 64)))
+    plan = M.ExpertPlan(20, 2, 4, DEV)
+    out = torch.full((40, 32), 3.0, dtype=BF16, device=DEV)
+    assert (M.bctm_expert_swiglu(x, w, w, plan, out) == 3.0).all()
+    res, workspace = normal(3, (20, 32)), torch.full((M.bctm_expert_workspace(20, 2, 32),), 255, dtype=torch.uint8, device=DEV)
+    got = M.bctm_expert_linear(normal(4, (40, 64)), w, plan, torch.ones((20, 2), device=DEV), res, workspace=workspace)
+    assert torch.equal(got, res)
+
+
+def test_refusals_of_the_wrappers(M):
+    x, w = normal(1, (20, 64)), M.bctm_pack_experts(normal(2, (4, 32, 64)))
+    ids = torch.zeros((20, 2), dtype=torch.int32, device=DEV)
+    plan, weights = M.bctm_expert_plan(ids, 4), torch.ones((20, 2), device=DEV)
+    logits, h = torch.zeros((20, 4), device=DEV), normal(3, (40, 64))
+    p = M.bctm_pack_weight(normal(4, (32, 64)))
+    bad = [
+        lambda: M.bctm_route(logits.double(), 2), lambda: M.bctm_route(logits.t(), 2), lambda: M.bctm_route(logits[0], 2),
+        lambda: M.bctm_route(logits, 2, bias=torch.zeros(3, device=DEV)), lambda: M.bctm_route(logits, 2, bias=torch.zeros(4, device=DEV).half()),
+        lambda: M.bctm_route(logits, 3, plan=plan), lambda: M.bctm_route(logits[:10], 2, plan=plan),
+        lambda: M.bctm_route(logits, 2, experts=ids[:, :1]), lambda: M.bctm_route(logits, 2, weights=weights.double()),
+        lambda: M.bctm_route(logits, 2, experts=ids.long()),
+        lambda: M.bctm_expert_plan(ids.long(), 4), lambda: M.bctm_expert_plan(ids.t(), 4), lambda: M.bctm_expert_plan(ids[0], 4),
+        lambda: M.bctm_expert_plan(ids, 5, plan), lambda: M.bctm_pack_experts(normal(5, (2, 24, 64))), lambda: M.bctm_pack_experts(normal(5, (32, 64))),
+        lambda: M.bctm_expert_swiglu(x[:10], w, w, plan), lambda: M.bctm_expert_swiglu(x[:, :32].contiguous(), w, w, plan),
+        lambda: M.bctm_expert_swiglu(x, w, p, plan), lambda: M.bctm_expert_swiglu(x, w, M.bctm_pack_experts(normal(6, (4, 48, 64))), plan),
+        lambda: M.bctm_expert_swiglu(x, w, w, plan, out=normal(7, (20, 32))), lambda: M.bctm_expert_swiglu(x, w, w, plan.data),
+        lambda: M.bctm_expert_linear(x, w, plan, weights), lambda: M.bctm_expert_linear(h, w, plan, weights.double()),
+        lambda: M.bctm_expert_linear(h, w, plan, weights[:10]), lambda: M.bctm_expert_linear(h, w, plan, weights, residual=normal(8, (20, 64))),
+        lambda: M.bctm_expert_linear(h, w, plan, weights, out=normal(8, (40, 32))),
+        lambda: M.bctm_expert_linear(h, w, plan, weights, workspace=torch.empty(9999, device=DEV)),
+        lambda: M.bctm_linear_act(x, p, act="tanh"), lambda: M.bctm_linear_act(x, p, bias=torch.zeros(32, device=DEV)),
+        lambda: M.bctm_linear_act(x, p, residual=normal(9, (19, 32))), lambda: M.bctm_linear_act(x, p, out=torch.empty((20, 32), device=DEV).half()),
+        lambda: M.bctm_linear_act(x, p, out=torch.empty((20, 32), device=DEV), out_dtype=BF16),
+        lambda: M.bctm_linear_act(x, p, out=torch.empty((20, 32), device=DEV), tiled=True), lambda: M.bctm_linear_act(x, p, out_dtype=F32, tiled=True),
+        lambda: M.bctm_linear_act(x, p, out=M.TiledRows(20, 32, DEV)), lambda: M.bctm_linear_act(x, w),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail(f"call {i} was taken")
+    for f in (lambda: M.bctm_route(logits, 5), lambda: M.bctm_route(logits, 0), lambda: M.bctm_route(logits, 2, scale=float("nan")),
+              lambda: M.bctm_expert_linear(h, w, plan, weights, workspace=torch.empty(64, dtype=torch.uint8, device=DEV)),
+              lambda: M.bctm_route(torch.zeros((0, 4), device=DEV), 2)):
+        with pytest.raises(M.BctModelError):
+            f()
