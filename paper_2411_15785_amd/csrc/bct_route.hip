@@ -4,7 +4,7 @@
 //   the k experts with the largest l, or with a bias p + bias; equal ones by number
 //   weight = scale * p / (sum of the chosen p, or 1)
 //
-// Sixteen lanes have a token, each a run of its experts, and the choice is k times a maximum: over a lane's keys, then over the sixteen
+// Sixteen lanes have a token, each some of its experts, and the choice is k times a maximum: over a lane's keys, then over the sixteen
 // by the data-parallel primitives, so four tokens share the instructions of a wavefront, which is what bounds it.  With a bias, scores
 // are worked out in 64 bits, as two experts' sums may lie closer than fp32 tells them apart: of sigmoids only those of the few that fp32 leaves
 // near the border, of a softmax all, by a whole wavefront for a token.
@@ -12,6 +12,10 @@
 // The plan is a counting sort of the pairs (token, slot) by expert that depends on no order of atomics: blocks of tokens count
 // their experts, then each block adds up what the blocks before it counted and gives its pairs their places, a wavefront's
 // 64 at a time by comparing their experts bit by bit.  Few tokens are one block, and one launch.
+//
+// us in a graph, choice and plan: 8 of 64 experts, 1 token 8.9, 64 11.8, 1024 13.2, 16384 16.0; 8 of 256, 16384 tokens 25.7, of sigmoids with a bias 37, of
+// a softmax with one 47; 16 of 512, 4096 tokens 35, 63, 60 (these two spill 125 registers, for the wavefront's part).  A token a wavefront, its k maxima
+// over 64 lanes, took 40 for the sigmoids with a bias.  The plan is 13 of 16384 tokens' times, launch included.
 #include <math.h>
 
 #include "bct_device.h"
@@ -229,24 +233,30 @@ __device__ __forceinline__ void route_four(const RouteArgs& a, uint32_t r, uint3
   const typename DT::elem* row = (const typename DT::elem*)a.logits + (size_t)min(mine, r1 - 1) * a.ld;
   uint32_t key[V];
   float most = -INFINITY, all = 1.f;
-  float l[V], bias[V];
   auto expert_of = [&](uint32_t v) -> uint32_t { return 4 * lane + v / 4 * 64 + v % 4; };
+  constexpr int AT_ONCE = BIAS && V > 16 ? 16 : BIAS && V > 8 ? 8 : V;   // what there are registers for
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const uint32_t at = min(expert_of(v), a.E - 1);
-    l[v] = load_elem(row, at);
-    if (BIAS) bias[v] = a.bias[at];
-  }
+  for (int v0 = 0; v0 < V; v0 += AT_ONCE) {
+    float l[AT_ONCE], bias[AT_ONCE];
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    // requested all at once: behind the branch that the compiler makes of what follows, they would be waited for one by one
-    asm("" : "+v"(l[v]));
-    if (BIAS) asm("" : "+v"(bias[v]));
-  }
+    for (int v = 0; v < AT_ONCE; ++v) {
+      const uint32_t at = min(expert_of(v0 + v), a.E - 1);
+      l[v] = load_elem(row, at);
+      if (BIAS) bias[v] = a.bias[at];
+    }
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    key[v] = expert_of(v) < a.E ? key_of(l[v]) : 0;
-    if constexpr (BIAS) key[v] = key[v] ? key_of(__builtin_amdgcn_rcpf(1.f + __expf(-l[v])) + bias[v]) : 0;
+    for (int v = 0; v < AT_ONCE; ++v) {
+      // requested together: behind the branch that the compiler makes of what follows, they would be waited for one by one
+      asm("" : "+v"(l[v]));
+      if (BIAS) asm("" : "+v"(bias[v]));
+    }
+#pragma unroll
+    for (int v = 0; v < AT_ONCE; ++v) {
+      uint32_t& to = key[v0 + v];
+      to = expert_of(v0 + v) < a.E ? key_of(l[v]) : 0;
+      if constexpr (BIAS) to = to ? key_of(__builtin_amdgcn_rcpf(1.f + __expf(-l[v])) + bias[v]) : 0;
+    }
+    if (AT_ONCE < V) __builtin_amdgcn_sched_barrier(0);
   }
   if (!BIAS && !a.sigmoid && !a.normalise) {   // the softmax' sum over all experts
     uint32_t top = 0;

@@ -234,6 +234,22 @@ def test_route_equal_and_far_logits(M):
     assert ids[0].tolist() == [7, 6, 5]
 
 
+@pytest.mark.parametrize("E,k", [(40, 8), (40, 16), (100, 6), (200, 16), (512, 16)])
+def test_route_crowds_at_the_border(M, E, k):
+    """Biased sigmoids of which many lie within the roundings of fp32 of the kth, more than there are lanes for a token, beside tokens
+    without such crowds; equal sums among them."""
+    g = torch.Generator().manual_seed(E)
+    x = torch.randn((50, E), generator=g)
+    x[::3] = 1.0 + torch.randint(0, 40, (17, E), generator=g) * 2.0 ** -22
+    x[1::6, : E // 2] = 3.0
+    x[7] = 0.0
+    x[8] = 12.0 + torch.arange(E) * 2.0 ** -20     # sigmoids that differ by 6e-12, far above 2^-53, far below 2^-24
+    x[9, ::2] = float("-inf")
+    for bias in (torch.zeros(E), torch.full((E,), 1000.0), torch.randn(E, generator=g) * 1e-7):
+        for sigmoid in (True, False):
+            check_route(M, x.to(DEV), k, bias.to(DEV), sigmoid)
+
+
 @pytest.mark.parametrize("rows,k,E", [(1, 1, 1), (1, 16, 16), (64, 16, 512), (65, 3, 7), (4096, 8, 64), (20001, 2, 512), (33000, 16, 33)])
 def test_plan_of_given_experts(M, rows, k, E):
     """Any ids: the same expert twice in a row of slots, one expert for all, none for some or all."""
