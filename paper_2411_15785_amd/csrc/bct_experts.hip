@@ -121,15 +121,15 @@ __global__ __launch_bounds__(256) void combine_kernel(const void* sums, const in
 }
 
 // The form of a product's sizes: what a workgroup has, 16 rows of the streaming kernel or 64 x 128, 128 x 256 or 256 x 256 of
-// rows and columns (two of a SwiGLU's feature).  The host knows how many pairs an expert has in the mean, not how many each has: about
-// mean / rows + 1/2 row tiles, at least one.  Estimates in us from
+// rows and columns (two of a SwiGLU's feature).  The host knows how many pairs there are, not how many each expert has: as many experts
+// are taken to be used as if all were as likely, and about mean / rows + 1/2 row tiles each, at least one.  Estimates in us from
 //   streaming   every row tile reads the expert's weights: 6.7 TB/s
 //   64 x 128    0.17 a K step alone on its compute unit, 0.21 for each of several
-//   128 x 256   0.36 a K step where one round of workgroups is enough, else 0.30 for each of a compute unit, as much again for the part of its rows that
+//   128 x 256   0.40 a K step where one round of workgroups is enough, else 0.30 for each of a compute unit, as much again for the part of its rows that
 //               is used, and 3 for its ends, which a second workgroup covers in part
 //   256 x 256   0.48; 0.45 and as much again, 9 for its ends, and half a round that is not full
-// and for the last three the weights at 5.6 TB/s.  60 and 110 drawn shapes take 1.1 and 1.5 % longer than in their best form, in the geometric
-// mean.  Measured us, streaming | 64 x 128 | 128 x 256 | 256 x 256, gated K = 4096, N = 1376, 64 experts with a mean of 4: 212 | 243 | 232 | 235; 8: 240 |
+// and for the last three the weights at 5.6 TB/s.  90 drawn shapes take 0.6 % longer than in their best form, in the geometric
+// mean, with weights from memory.  Measured us, streaming | 64 x 128 | 128 x 256 | 256 x 256, gated K = 4096, N = 1376, 64 experts with a mean of 4: 212 | 243 | 232 | 235; 8: 240 |
 // 258 | 246 | 244; 16: 326 | 274 | 256 | 252; 48: 811 | 333 | 285 | 292; 128: - | 526 | 363 | 354; 512: - | - | 861 | 742.  8 experts, 2048, 1024,
 // mean 4: 15.0 | 16.2 | 23.3 | 28.7; 16: 18.9 | 17.3 | 24.6 | 30.4; 64: 45.6 | 19.5 | 27.7 | 34.0; 192: - | 29.2 | 29.3 | 43.7; 384: - | 47.9 | 31 | 42.
 // The way back (with its sum), 12 experts, 2080 -> 2048, mean 8: 24.0 | 24.0 | 28.2 | 33.6; 32: 43.7 | 26.6 | 32.2 | 38.3; 128: 127 | 41.2 | 47.3 |
@@ -137,9 +137,9 @@ __global__ __launch_bounds__(256) void combine_kernel(const void* sums, const in
 enum ExpertForm { kFew, kRows64, kRows128, kRows256 };   // in the order of kPlanRows
 constexpr uint32_t few_features(bool swiglu) { return swiglu ? 1 : 2; }   // feature tiles of a streaming workgroup
 ExpertForm expert_form(uint32_t pairs, uint32_t E, uint32_t K, uint32_t N, bool swiglu) {
-  const double used = pairs < E ? pairs : E, mean = pairs / used, bcols = swiglu ? 2.0 * N : N, KT = K / 32, expert = 2.0 * K * bcols;
+  const double used = E * -expm1(-(double)pairs / E), mean = pairs / used, bcols = swiglu ? 2.0 * N : N, KT = K / 32, expert = 2.0 * K * bcols;
   auto tiles = [&](double rows) { return used * (mean / rows > 0.5 ? mean / rows + 0.5 : 1.0); };
-  const double stream = 2 + used * expert / 5.6e6;
+  const double stream = 4 + used * expert / 5.6e6;
   ExpertForm best = kFew;
   double cost = 4 + tiles(16) * expert / 6.7e6;
   auto take = [&](ExpertForm f, double c) {
@@ -153,8 +153,8 @@ ExpertForm expert_form(uint32_t pairs, uint32_t E, uint32_t K, uint32_t N, bool 
   auto full = [&](double rows, double cols) { return pairs / rows * ceil(bcols / cols) / 256; };   // of them, were all of their rows used
   auto most = [](double a, double b) { return a > b ? a : b; };
   const double g64 = groups(64, 128), g128 = groups(128, 256), g256 = groups(256, 256);
-  take(kRows64, 6 + KT * (g64 > 0.8 ? 0.21 * g64 : 0.17));
-  take(kRows128, most(8 + KT * 0.36, 3 * g128 + KT * 0.30 * (g128 + full(128, 256))));
+  take(kRows64, 7 + KT * (g64 > 0.8 ? 0.21 * g64 : 0.17));
+  take(kRows128, most(8 + KT * 0.40, 3 * g128 + KT * 0.30 * (g128 + full(128, 256))));
   take(kRows256, most(13.9 + KT * 0.48, 9 * g256 + KT * 0.45 * (g256 + full(256, 256) + 0.6)));
   return best;
 }
