@@ -20,7 +20,7 @@ constexpr uint32_t kTileLists = 4, kPlanRows[kTileLists] = {16, 64, 128, 256};
 //   order     [pairs]      the pairs by expert, equal ones by number; those without an expert last
 //   expert    [pairs]      1 + each pair's expert, 0 for none: a plan of zeros has no tokens
 //   n_tiles   [kTileLists]
-//   lists     uint4        per row tile: expert, first place in `order`, rows, 0
+//   lists     uint4        per row tile: expert, where its pairs begin in `order`, how many it has, which of its tiles this is
 //   counts    [blocks][E + 1, filled up to a multiple of 4]  how many pairs of each expert a block of tokens has (while the plan is made)
 struct ExpertPlan {
   uint32_t pairs, E, blocks;
@@ -144,14 +144,15 @@ __device__ __forceinline__ void add_block(const u32x4 v, float weight, float (&y
   }
 }
 
+// An expert by one of its row tiles.  One of no pairs where the plan holds something else than a tile for these sizes: no read leaves the
+// buffers by it.
 struct ExpertTile {
-  uint32_t expert, first, rows;
+  uint32_t expert, begin, pairs, tile;
 };
-// A tile of no rows where the plan holds something else than one for these sizes: no read leaves the buffers by it.
 __device__ __forceinline__ ExpertTile expert_tile(const ExpertTerm& T, uint32_t i) {
   const uint4 t = T.tiles[i];
-  const bool good = t.x < T.n_experts && t.y < T.pairs && t.z <= T.pairs - t.y;
-  return {good ? t.x : 0u, good ? t.y : 0u, good ? t.z : 0u};
+  const bool good = t.x < T.n_experts && t.y < T.pairs && t.z <= T.pairs - t.y && t.w <= i;
+  return {good ? t.x : 0u, good ? t.y : 0u, good ? t.z : 0u, good ? t.w : 0u};
 }
 __device__ __forceinline__ uint32_t expert_pair(const ExpertTerm& T, const int32_t* order, uint32_t row) {
   return min((uint32_t)order[row], T.pairs - 1);

@@ -25,15 +25,16 @@ __global__ __launch_bounds__(64 * WAVES) void expert_few_kernel(const uint16_t* 
   __shared__ float sC[WAVES][NS][16][17];
   if (blockIdx.y >= *T.n_tiles) return;
   const ExpertTile tile = expert_tile(T, blockIdx.y);
-  if (tile.rows == 0) return;
+  if (tile.tile * 16 >= tile.pairs) return;
+  const uint32_t rows = min(tile.pairs - tile.tile * 16, 16u);
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, jl = lane % 16, kg = lane / 16, KT = K / 32, NT = N / 16;
   const uint32_t kt0 = (uint32_t)((uint64_t)wave * KT / WAVES), kt1 = (uint32_t)((uint64_t)(wave + 1) * KT / WAVES);
-  const int32_t* order = T.order + tile.first;
+  const int32_t* order = T.order + tile.begin + tile.tile * 16;
   const u32x4* wt[NS];
 #pragma unroll
   for (int s = 0; s < NS; ++s)   // a feature tile past the end: the last one again, not stored
     wt[s] = ((s % NW2) ? w2 : w) + tile.expert * T.stride + ((size_t)min(blockIdx.x * FT + s / NW2, NT - 1) * KT + kt0) * 64 + lane;
-  const bool there = jl < tile.rows;   // lanes of rows that are not there load nothing
+  const bool there = jl < rows;   // lanes of rows that are not there load nothing
   const uint16_t* xr = x + (size_t)(expert_pair(T, order, there ? jl : 0u) / T.per_row) * K + (size_t)kt0 * 32 + kg * 8;
   f32x4 acc[NS];
 #pragma unroll
@@ -64,7 +65,7 @@ __global__ __launch_bounds__(64 * WAVES) void expert_few_kernel(const uint16_t* 
   __syncthreads();
   for (uint32_t o = threadIdx.x; o < FT * 256; o += NTHR) {
     const uint32_t f = o / 256, i = o % 256 / 16, j = o % 16, n = (blockIdx.x * FT + f) * 16 + j;
-    if (i >= tile.rows || n >= N) continue;
+    if (i >= rows || n >= N) continue;
     float sum[NW2];
 #pragma unroll
     for (int m = 0; m < NW2; ++m) {

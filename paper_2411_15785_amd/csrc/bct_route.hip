@@ -428,7 +428,7 @@ __device__ __forceinline__ void plan_block(const int32_t* experts, int32_t* plan
     for (uint32_t i = 0; i < kTileLists; ++i) {
       uint4* list = (uint4*)(plan + P.list[i]) + s.tile[i][x];
       for (uint32_t t = lane; t * kPlanRows[i] < count; t += 64)
-        list[t] = make_uint4(x, first + t * kPlanRows[i], min(kPlanRows[i], count - t * kPlanRows[i]), 0);
+        list[t] = make_uint4(x, first, count, t);
     }
   }
   // the pairs, 64 at a time: a pair's place is its expert's next one and how many lanes before have that expert too
