@@ -10,7 +10,10 @@
  * itself stays bct_decode_step / bct_prefill (include/bct.h).  For what each
  * request of a batch brings of its own: head norms with the rotation by its
  * position (bctm_qk_norm_rope), low-rank adapters beside the projections
- * (bctm_lora) and sampled instead of greedy tokens (bctm_sample).
+ * (bctm_lora) and sampled instead of greedy tokens (bctm_sample).  For layers with
+ * experts in place of the dense MLP: the router's product (bctm_linear_act), its
+ * choice (bctm_route) and the experts' products (bctm_expert_swiglu,
+ * bctm_expert_linear).
  *
  * All data pointers are DEVICE memory owned by the caller, bf16, row-major,
  * 16-byte aligned, unless a call says otherwise; token ids are int32.  Calls enqueue on the given stream and

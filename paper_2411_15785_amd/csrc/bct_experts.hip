@@ -5,8 +5,17 @@
 //
 // Pairs come by expert (the plan of bct_route.hip), in row tiles that belong to one expert each; rows are gathered where they lie.
 // Few pairs an expert: bound by reading the weights of the experts in use once, so a kernel that streams them against
-// 16 rows.  Many: bound by the matrix cores, the kernel of bct_linear_rows.hip with gathered rows.  The way back leaves each
-// pair's product in fp32, and a second kernel weights and adds up those of a token in the order of its slots.
+// 16 rows.  Many: bound by the matrix cores, the kernel of bct_linear_rows.hip with gathered rows, the tiles of an expert side by side
+// on an XCD and of the same size.  The way back leaves each pair's product in fp32, or from tiles of many rows in blocks of eight in 16 bytes
+// (pack_block), and a second kernel weights and adds up those of a token in the order of its slots.
+//
+// us in a graph, weights from memory: 32 tokens of 8 in 64 experts, gated 4096 -> 1376 208 (1.42 GB, 6.8 TB/s), back 115 (6.2); 4096 tokens 700 (1.06
+// PFLOP/s; clock 1.6 GHz, matrix cores busy 69 % of the cycles, 2.2 GB from memory; with the weights of one expert for all 607) and 503 (0.73, the sum 65 of
+// them); 777 of 2 in 12, 2080 -> 2048 back 46.  Measured and not kept: lines of weights read ahead into the L2, 4 to 16 K steps (4096 tokens
+// 4 to 13 % slower: each line is one more request), six stages of 64 x 128 or 128 x 256 (the same times), weights side by side by groups of 2 to 8 feature
+// tiles (the same), past the caches (4 % slower), rows past the caches (a third slower), four wavefronts of 64 x 128 or 128 x 64 each (the
+// same, 10 % slower), 128 x 128, 64 x 64 and 128 x 64 with K in two parts (slower but for 5 to 15 % at 24 to 64 rows an expert of small matrices), all 16-row tiles
+// multiplied whether they hold rows or not (2 to 4 % slower).
 #include <math.h>
 
 #include "bct_linear_rows.h"

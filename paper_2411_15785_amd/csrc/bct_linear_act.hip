@@ -1,6 +1,7 @@
 // The matrix-core projections of many token rows with bias, activation, residual and fp32 outputs in their epilogue: the kernel of
 // bct_linear_rows.hip with an EpilogueTerm.  It is applied to the fp32 sums where they are written out, so it costs no pass
-// over memory of its own.
+// over memory of its own.  4096 x 4096 x 11008, tiled x: 249 us without bias and activation (bctm_linear), 256 with a bias, 266 into fp32, 277 with bias
+// and gelu_tanh.
 //
 // Few features of many rows (a router's logits) are neither: no tile of it is wide enough for the matrix cores to be busy, and the streaming
 // kernel, a workgroup per 16 features, reads every row once for each of them.  linear_narrow_kernel has all 64 features in a
@@ -14,7 +15,8 @@ namespace {
 // 16 * RT rows and 64 features of a workgroup; its wavefronts share K, each with row tiles of its own in LDS.  Bound by the address
 // unit of a compute unit: a kilobyte of weights or rows takes 16 cycles of it, but rows read as operands lie, 16 side by side, take
 // 64; so a row's 256 bytes of four K tiles come to LDS whole (chunk c of row r at place c ^ r of its 16, so that an operand read
-// finds its rows in different banks), a round of four ahead of the products.
+// finds its rows in different banks), a round of four ahead of the products.  4096 rows, 4096 -> 64: 12.9 us (33.5 MB of rows are 5.5 at the rate of a
+// copy); rows as operands lie, the weights straight to registers all the same: 18.
 template <bool XT, int RT>
 __global__ __launch_bounds__(512) void linear_narrow_kernel(const uint16_t* __restrict__ x, const u32x4* __restrict__ w,
                                                             const uint16_t* residual, void* out, uint32_t rows, uint32_t K, uint32_t N,
