@@ -32,17 +32,18 @@ __global__ __launch_bounds__(64 * WAVES) void expert_few_kernel(const uint16_t* 
                                                                 ExpertTerm T) {
   constexpr int NW2 = SWIGLU ? 2 : 1, NS = FT * NW2, NTHR = 64 * WAVES;
   __shared__ float sC[WAVES][NS][16][17];
-  if (blockIdx.y >= *T.n_tiles) return;
-  const ExpertTile tile = expert_tile(T, blockIdx.y);
+  const uint32_t NT = N / 16, features = (NT + FT - 1) / FT, nt0 = blockIdx.x % features * FT, t = blockIdx.x / features;
+  if (t >= *T.n_tiles) return;
+  const ExpertTile tile = expert_tile(T, t);
   if (tile.tile * 16 >= tile.pairs) return;
   const uint32_t rows = min(tile.pairs - tile.tile * 16, 16u);
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, jl = lane % 16, kg = lane / 16, KT = K / 32, NT = N / 16;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, jl = lane % 16, kg = lane / 16, KT = K / 32;
   const uint32_t kt0 = (uint32_t)((uint64_t)wave * KT / WAVES), kt1 = (uint32_t)((uint64_t)(wave + 1) * KT / WAVES);
   const int32_t* order = T.order + tile.begin + tile.tile * 16;
   const u32x4* wt[NS];
 #pragma unroll
   for (int s = 0; s < NS; ++s)   // a feature tile past the end: the last one again, not stored
-    wt[s] = ((s % NW2) ? w2 : w) + tile.expert * T.stride + ((size_t)min(blockIdx.x * FT + s / NW2, NT - 1) * KT + kt0) * 64 + lane;
+    wt[s] = ((s % NW2) ? w2 : w) + tile.expert * T.stride + ((size_t)min(nt0 + s / NW2, NT - 1) * KT + kt0) * 64 + lane;
   const bool there = jl < rows;   // lanes of rows that are not there load nothing
   const uint16_t* xr = x + (size_t)(expert_pair(T, order, there ? jl : 0u) / T.per_row) * K + (size_t)kt0 * 32 + kg * 8;
   f32x4 acc[NS];
@@ -50,15 +51,15 @@ __global__ __launch_bounds__(64 * WAVES) void expert_few_kernel(const uint16_t* 
   for (int s = 0; s < NS; ++s) acc[s] = f32x4{0.f, 0.f, 0.f, 0.f};
   const uint32_t n_t = kt1 - kt0;
   // Rounds of U tiles, all requested before the first product; the missing tiles of the last round are not loaded and count as 0.
-  for (uint32_t t = 0; t < n_t; t += U) {
+  for (uint32_t k = 0; k < n_t; k += U) {
     u32x4 b[U][NS], a[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool is = t + u < n_t;
+      const bool is = k + u < n_t;
       a[u] = u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int s = 0; s < NS; ++s) b[u][s] = is ? __builtin_nontemporal_load(wt[s] + (size_t)(t + u) * 64) : u32x4{0u, 0u, 0u, 0u};
-      if (is && there) a[u] = *(const u32x4*)(xr + (size_t)(t + u) * 32);
+      for (int s = 0; s < NS; ++s) b[u][s] = is ? __builtin_nontemporal_load(wt[s] + (size_t)(k + u) * 64) : u32x4{0u, 0u, 0u, 0u};
+      if (is && there) a[u] = *(const u32x4*)(xr + (size_t)(k + u) * 32);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -73,7 +74,7 @@ __global__ __launch_bounds__(64 * WAVES) void expert_few_kernel(const uint16_t* 
     for (int v = 0; v < 4; ++v) sC[wave][s][4 * kg + v][jl] = acc[s][v];
   __syncthreads();
   for (uint32_t o = threadIdx.x; o < FT * 256; o += NTHR) {
-    const uint32_t f = o / 256, i = o % 256 / 16, j = o % 16, n = (blockIdx.x * FT + f) * 16 + j;
+    const uint32_t f = o / 256, i = o % 256 / 16, j = o % 16, n = (nt0 + f) * 16 + j;
     if (i >= rows || n >= N) continue;
     float sum[NW2];
 #pragma unroll
@@ -94,8 +95,7 @@ __global__ __launch_bounds__(64 * WAVES) void expert_few_kernel(const uint16_t* 
 template <bool BLOCKS, int S>
 __global__ __launch_bounds__(256) void combine_kernel(const void* sums, const int32_t* expert, const float* weights, const uint16_t* residual,
                                                       uint16_t* out, uint32_t rows, uint32_t k, uint32_t N) {
-  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  const uint32_t chunks = N / 8, r = (uint32_t)(i / chunks), c = (uint32_t)(i % chunks);
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x, chunks = N / 8, r = i / chunks, c = i % chunks;
   if (r >= rows) return;
   float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (uint32_t s = 0; s < k; s += S) {
@@ -169,15 +169,25 @@ ExpertForm expert_form(uint32_t pairs, uint32_t E, uint32_t K, uint32_t N, bool 
   return best;
 }
 
+// What a workgroup of a form has of the features.
+uint32_t form_features(ExpertForm form, bool swiglu) {
+  return form == kFew ? 16 * few_features(swiglu) : (form == kRows64 ? 128 : 256) / (swiglu ? 2 : 1);
+}
+uint64_t form_groups(ExpertForm form, uint32_t pairs, uint32_t E, uint32_t N, bool swiglu) {   // workgroups of the launch
+  const uint32_t features = form_features(form, swiglu);
+  return (uint64_t)ExpertPlan::most_tiles(pairs, E, kPlanRows[form]) * ((N + features - 1) / features);
+}
+constexpr uint64_t kMostThreads = 0xFFFFF000u;   // of a launch
+
 bct_status check_products(const void* x, const void* w, const void* out, const void* plan, uint32_t rows, uint32_t k, uint32_t E,
-                          uint32_t K, uint32_t N) {
+                          uint32_t K, uint32_t N, bool swiglu) {
   if (!x || !w || !out || K == 0 || N == 0) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
   const bct_status st = check_expert_plan(plan, rows, k, E);
   if (st != BCT_OK) return st;
   if (K % 32 != 0 || N % 16 != 0) return mfail(BCT_ERR_UNSUPPORTED, "K must be a multiple of 32 and N of 16");
   if (K > 1u << 24 || N > 1u << 24) return mfail(BCT_ERR_UNSUPPORTED, "matrix too large");
-  // grids: row tiles times feature tiles
-  if (((uint64_t)rows * k / 16 + E) * (N / 16 + 1) > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many tokens");
+  if ((form_groups(expert_form(rows * k, E, K, N, swiglu), rows * k, E, N, swiglu) + 8) * 512 > kMostThreads || (!swiglu && (uint64_t)rows * (N / 8) > kMostThreads))
+    return mfail(BCT_ERR_UNSUPPORTED, "too many tokens");
   if (!al16(x) || !al16(w) || !al16(out)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
   if (x == out) return mfail(BCT_ERR_INVALID_ARG, "out must not be x");
   return BCT_OK;
@@ -203,7 +213,7 @@ void launch_products(const void* x, const void* w, const void* w2, void* out, vo
   switch (form) {
     case kFew: {
       constexpr int FT = few_features(SWIGLU), WAVES = 4, U = 8;
-      const dim3 grid((N / 16 + FT - 1) / FT, T.most_tiles);
+      const dim3 grid((unsigned)form_groups(kFew, P.pairs, E, N, SWIGLU));
       hipLaunchKernelGGL((expert_few_kernel<SWIGLU, WAVES, U, FT>), grid, dim3(64 * WAVES), 0, s, (const uint16_t*)x, (const u32x4*)w,
                          (const u32x4*)w2, (uint16_t*)out, K, N, T);
       return;
@@ -224,7 +234,7 @@ extern "C" {
 
 bct_status bctm_expert_swiglu(const void* x, const void* w_gate, const void* w_up, void* out, const void* plan, uint32_t rows,
                               uint32_t k, uint32_t n_experts, uint32_t K, uint32_t N, void* hip_stream) {
-  const bct_status st = check_products(x, w_gate, out, plan, rows, k, n_experts, K, N);
+  const bct_status st = check_products(x, w_gate, out, plan, rows, k, n_experts, K, N, true);
   if (st != BCT_OK) return st;
   if (!w_up) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
   if (!al16(w_up)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned");
@@ -240,12 +250,14 @@ bct_status bctm_expert_tile(uint32_t rows, uint32_t k, uint32_t n_experts, uint3
   if (K % 32 != 0 || N % 16 != 0) return mfail(BCT_ERR_UNSUPPORTED, "K must be a multiple of 32 and N of 16");
   const ExpertForm form = expert_form(rows * k, n_experts, K, N, swiglu != 0);
   *tile_rows = kPlanRows[form];
-  *tile_features = form == kFew ? 16 * few_features(swiglu != 0) : (form == kRows64 ? 128 : 256) / (swiglu ? 2 : 1);
+  *tile_features = form_features(form, swiglu != 0);
   return BCT_OK;
 }
 
 bct_status bctm_expert_workspace(uint32_t rows, uint32_t k, uint32_t N, size_t* bytes) {
-  if (!bytes || rows == 0 || k == 0 || N == 0) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
+  if (!bytes || N == 0) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
+  const bct_status st = check_plan_sizes(rows, k, k);
+  if (st != BCT_OK) return st;
   if (N % 16 != 0 || N > 1u << 24) return mfail(BCT_ERR_UNSUPPORTED, "N must be a multiple of 16, at most 16777216");
   *bytes = (size_t)rows * k * N * 4;
   return BCT_OK;
@@ -254,15 +266,13 @@ bct_status bctm_expert_workspace(uint32_t rows, uint32_t k, uint32_t N, size_t* 
 bct_status bctm_expert_linear(const void* h, const void* w_packed, const void* plan, const float* weights, const void* residual, void* out,
                               void* workspace, size_t workspace_bytes, uint32_t rows, uint32_t k, uint32_t n_experts, uint32_t K,
                               uint32_t N, void* hip_stream) {
-  const bct_status st = check_products(h, w_packed, out, plan, rows, k, n_experts, K, N);
+  const bct_status st = check_products(h, w_packed, out, plan, rows, k, n_experts, K, N, false);
   if (st != BCT_OK) return st;
   if (!weights || !workspace) return mfail(BCT_ERR_INVALID_ARG, "NULL pointer or zero size");
   if (!al16(residual) || !al16(workspace) || ((uintptr_t)weights & 3u)) return mfail(BCT_ERR_MISALIGNED, "pointers must be 16-byte aligned, weights to 4");
   size_t need = 0;
   bctm_expert_workspace(rows, k, N, &need);
   if (workspace_bytes < need) return mfail(BCT_ERR_BUFFER_TOO_SMALL, "the workspace is smaller than bctm_expert_workspace says");
-  const uint64_t chunks = (uint64_t)rows * (N / 8);
-  if ((chunks + 255) / 256 > 0x7FFFFFFFu) return mfail(BCT_ERR_UNSUPPORTED, "too many tokens");
   hipStream_t s = (hipStream_t)hip_stream;
   const ExpertPlan P = ExpertPlan::of(rows, k, n_experts);
   launch_products<false>(h, w_packed, nullptr, nullptr, workspace, (const int32_t*)plan, rows, k, n_experts, K, N, s);
@@ -270,7 +280,7 @@ bct_status bctm_expert_linear(const void* h, const void* w_packed, const void* p
   const auto combine = k <= 2   ? (blocks ? combine_kernel<true, 2> : combine_kernel<false, 2>)
                        : k <= 4 ? (blocks ? combine_kernel<true, 4> : combine_kernel<false, 4>)
                                 : (blocks ? combine_kernel<true, 8> : combine_kernel<false, 8>);
-  hipLaunchKernelGGL(combine, dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, s, (const void*)workspace,
+  hipLaunchKernelGGL(combine, dim3((unsigned)(((uint64_t)rows * (N / 8) + 255) / 256)), dim3(256), 0, s, (const void*)workspace,
                      (const int32_t*)plan + P.expert, weights, (const uint16_t*)residual, (uint16_t*)out, rows, k, N);
   return launched("expert_linear");
 }

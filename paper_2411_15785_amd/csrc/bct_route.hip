@@ -126,16 +126,17 @@ __device__ __forceinline__ Key take_largest(Key (&key)[V], uint32_t (&id)[V], ui
   return best;
 }
 
-// The value of the lane that is `distance` 1, 2, 4 or 8 away among sixteen that have their own, or one for every 2, 4, 8.
+// The value of the lane of the same sixteen that the data-parallel-primitive control names, and what that makes of all sixteen: the other
+// of a pair, the other pair of four, mirrored in eight and in sixteen.
 template <int CTRL>
 __device__ __forceinline__ uint32_t of_sixteen(uint32_t v) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
 }
 __device__ __forceinline__ uint32_t max16(uint32_t v) {
-  v = max(v, of_sixteen<0xB1>(v));    // the other of a pair
-  v = max(v, of_sixteen<0x4E>(v));    // the other pair of four
-  v = max(v, of_sixteen<0x141>(v));   // mirrored in eight
-  return max(v, of_sixteen<0x140>(v));   // in sixteen
+  v = max(v, of_sixteen<0xB1>(v));
+  v = max(v, of_sixteen<0x4E>(v));
+  v = max(v, of_sixteen<0x141>(v));
+  return max(v, of_sixteen<0x140>(v));
 }
 __device__ __forceinline__ float sum16(float v) { return xor_sum<1, 8>(v); }
 template <int L>
@@ -172,7 +173,7 @@ __device__ __forceinline__ void write_choice(const RouteArgs& a, uint32_t r, boo
   }
 }
 
-// The choice with a bias in 64 bits throughout, by a whole wavefront.
+// The choice with a bias in 64 bits throughout, by a whole wavefront: a lane has V experts one after the other.
 template <typename DT, int V>
 __device__ __forceinline__ void route_whole(const RouteArgs& a, uint32_t r, uint32_t* counts) {
   const uint32_t lane = threadIdx.x % 64;
@@ -308,7 +309,7 @@ __device__ __forceinline__ void route_four(const RouteArgs& a, uint32_t r, uint3
     double sum = -INFINITY;
     if (listed) sum = 1.0 / (1.0 + exp(-(double)x)) + (double)a.bias[expert];
     slot = 0;
-    auto against = [&](auto j) {   // how many come before this one; equal sums were found in the order of their numbers or not at all
+    auto against = [&](auto j) {   // the slot is how many come before this one
       const double other = row_lane<decltype(j)::v>(sum);
       const uint32_t e = of_sixteen<0x150 + decltype(j)::v>(expert);
       slot += other > sum || (other == sum && e < expert) ? 1 : 0;

@@ -88,7 +88,7 @@ def test_plan_refusals(ML, kw, status):
 PRODUCTS = SIZES + [(dict(x=None), INVALID), (dict(w=None), INVALID), (dict(out=None), INVALID), (dict(plan=None), INVALID), (dict(K=0), INVALID),
                     (dict(N=0), INVALID), (dict(K=16), UNSUPPORTED), (dict(N=8), UNSUPPORTED), (dict(out=A), INVALID), (dict(x=odd), MISALIGNED),
                     (dict(w=odd), MISALIGNED), (dict(out=odd), MISALIGNED), (dict(plan=odd), MISALIGNED), (dict(K=1 << 25), UNSUPPORTED),
-                    (dict(N=1 << 25), UNSUPPORTED), (dict(rows=1 << 30, k=1, N=1 << 20), UNSUPPORTED)]
+                    (dict(N=1 << 25), UNSUPPORTED), (dict(rows=1 << 30, k=1, N=1 << 20), UNSUPPORTED), (dict(rows=100 << 20, k=1, K=4096, N=4096), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("kw,status", PRODUCTS + [(dict(up=None), INVALID), (dict(up=odd), MISALIGNED)])
@@ -113,6 +113,8 @@ def test_workspace(ML):
     assert ML.bctm_expert_workspace(0, 2, 48, ctypes.byref(v)) == INVALID
     assert ML.bctm_expert_workspace(4, 2, 40, ctypes.byref(v)) == UNSUPPORTED
     assert ML.bctm_expert_workspace(4, 2, 48, None) == INVALID
+    assert ML.bctm_expert_workspace(4, 17, 48, ctypes.byref(v)) == UNSUPPORTED
+    assert ML.bctm_expert_workspace(0xFFFFFFFF, 16, 48, ctypes.byref(v)) == UNSUPPORTED
 
 
 def test_python_wrappers_refuse_what_is_not_on_the_gpu():

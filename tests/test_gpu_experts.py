@@ -342,6 +342,23 @@ def test_expert_linear(M, rows, k, E, K, N):
         assert torch.equal(inplace, M.bctm_expert_linear(hp, packed, plan, wts, res))
 
 
+def test_expert_linear_of_more_tiles_than_a_grid_is_high(M):
+    """Tiny matrices have tiles of 16 rows at any number of tokens: more than 65535 of them."""
+    rows, k, E, K, N = 140000, 8, 8, 32, 16
+    assert M.bctm_expert_tile(rows, k, E, K, N, False) == (16, 32) and rows * k / 16 > 65535
+    h, w = normal(1, (rows * k, K)), normal(2, (E, N, K), K ** -0.5)
+    ids, weights = choose(5, rows, k, E)
+    plan = M.bctm_expert_plan(ids.to(DEV), E)
+    flat, y, mass = ids.reshape(-1).to(DEV), torch.zeros((rows * k, N), dtype=torch.float64, device=DEV), torch.zeros((rows * k, N), dtype=torch.float64, device=DEV)
+    for e in range(E):
+        p = torch.nonzero(flat == e)[:, 0]
+        hd, wd = h[p].double(), w[e].double()
+        y[p], mass[p] = (hd[:, None] * wd).sum(-1), (hd[:, None] * wd).abs().sum(-1)
+    wt = weights.to(DEV).double()[..., None]
+    out, slack = (y.view(rows, k, N) * wt).sum(1), 2.0 ** -20 * (mass.view(rows, k, N) * wt.abs()).sum(1)
+    close(M.bctm_expert_linear(h, M.bctm_pack_experts(w), plan, weights.to(DEV)), out.cpu(), slack.cpu(), "many tiles")
+
+
 @pytest.mark.parametrize("rows,E", [(40, 8), (400, 8), (2500, 8)])
 def test_a_tokens_bits_do_not_depend_on_the_others(M, rows, E):
     """The same tokens with other companions, another order and the experts' other tokens gone."""
