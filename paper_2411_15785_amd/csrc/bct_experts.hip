@@ -138,21 +138,21 @@ __global__ __launch_bounds__(256) void combine_kernel(const void* sums, const in
 //   128 x 256   0.40 a K step where one round of workgroups is enough, else 0.30 for each of a compute unit, as much again for the part of its rows that
 //               is used, and 3 for its ends, which a second workgroup covers in part
 //   256 x 256   0.48; 0.45 and as much again, 9 for its ends, and half a round that is not full
-// and for the last three the weights at 5.6 TB/s.  90 drawn shapes take 0.6 % longer than in their best form, in the geometric
-// mean, with weights from memory.  Measured us, streaming | 64 x 128 | 128 x 256 | 256 x 256, gated K = 4096, N = 1376, 64 experts with a mean of 4: 212 | 243 | 232 | 235; 8: 240 |
-// 258 | 246 | 244; 16: 326 | 274 | 256 | 252; 48: 811 | 333 | 285 | 292; 128: - | 526 | 363 | 354; 512: - | - | 861 | 742.  8 experts, 2048, 1024,
-// mean 4: 15.0 | 16.2 | 23.3 | 28.7; 16: 18.9 | 17.3 | 24.6 | 30.4; 64: 45.6 | 19.5 | 27.7 | 34.0; 192: - | 29.2 | 29.3 | 43.7; 384: - | 47.9 | 31 | 42.
-// The way back (with its sum), 12 experts, 2080 -> 2048, mean 8: 24.0 | 24.0 | 28.2 | 33.6; 32: 43.7 | 26.6 | 32.2 | 38.3; 128: 127 | 41.2 | 47.3 |
-// 59.9; 64 experts, 1376 -> 4096, 128: - | 290 | 235 | 256; 512: - | - | 549 | 525.
+// and for the last three the weights at 5.6, 5.6 and 5.9 TB/s.  90 drawn shapes take 0.5 % longer than in their best form, in the geometric
+// mean, with weights from memory.  Measured us, streaming | 64 x 128 | 128 x 256 | 256 x 256, gated K = 4096, N = 1376, 64 experts with a mean
+// of 4: 209 | 240 | 260 | 234; 8: 237 | 251 | 272 | 245; 16: 325 | 260 | 280 | 247; 48: 806 | 297 | 295 | 278; 128: - | 439 | 330 | 332; 512: - | 1232 |
+// 779 | 677.  8 experts, 2048, 1024, mean 4: 12.6 | 19.3 | 32.2 | 29.7; 16: 18.1 | 19.6 | 32.5 | 30.2; 64: 43.0 | 22.2 | 36.8 | 37.4; 192: 110 | 34.1 | 38.6 |
+// 51.0; 384: 208 | 55.5 | 39.0 | 50.4.  The way back (with its sum), 12 experts, 2080 -> 2048, mean 8: 23.2 | 27.1 | 40.2 | 37.9; 32: 42.6 | 30.6 | 43.1 | 43.0;
+// 128: 124 | 46.6 | 51.8 | 62.4; 64 experts, 1376 -> 4096, 128: - | 256 | 212 | 223; 512: - | 715 | 511 | 494.
 enum ExpertForm { kFew, kRows64, kRows128, kRows256 };   // in the order of kPlanRows
 constexpr uint32_t few_features(bool swiglu) { return swiglu ? 1 : 2; }   // feature tiles of a streaming workgroup
 ExpertForm expert_form(uint32_t pairs, uint32_t E, uint32_t K, uint32_t N, bool swiglu) {
   const double used = E * -expm1(-(double)pairs / E), mean = pairs / used, bcols = swiglu ? 2.0 * N : N, KT = K / 32, expert = 2.0 * K * bcols;
   auto tiles = [&](double rows) { return used * (mean / rows > 0.5 ? mean / rows + 0.5 : 1.0); };
-  const double stream = 4 + used * expert / 5.6e6;
   ExpertForm best = kFew;
   double cost = 4 + tiles(16) * expert / 6.7e6;
   auto take = [&](ExpertForm f, double c) {
+    const double stream = 4 + used * expert / (f == kRows256 ? 5.9e6 : 5.6e6);
     c = c > stream ? c : stream;
     if (c < cost) {
       cost = c;
