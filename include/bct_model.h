@@ -213,9 +213,7 @@ bct_status bctm_expert_tile(uint32_t rows, uint32_t k, uint32_t n_experts, uint3
 
 /* out[r][n] = (residual ? residual[r][n] : 0) + sum over the slots s of r with an expert e of weights[r][s] * sum_j h[r k + s][j] w[e][n][j].
  * h [rows * k][K] (rows of pairs without an expert are not read), weights float32 [rows][k], out and residual [rows][N]; out may be the
- * residual.  Products, weights and sums in fp32, slots in their order, rounded at the end; tiles of more than 16 pairs
- * (bctm_expert_tile) also leave each product off by at most 2^-14 of the largest of its eight neighbouring features (8 i .. 8 i + 7), as
- * they wait for the sum in 16 bits.  workspace: 16-byte aligned, at least
+ * residual.  Products, weights and sums in fp32, slots in their order, rounded once at the end.  workspace: 16-byte aligned, at least
  * bctm_expert_workspace bytes, holds nothing between calls; it must not be in use by a call on another stream. */
 bct_status bctm_expert_workspace(uint32_t rows, uint32_t k, uint32_t N, size_t* bytes);
 bct_status bctm_expert_linear(const void* h, const void* w_packed, const void* plan, const float* weights, const void* residual, void* out,

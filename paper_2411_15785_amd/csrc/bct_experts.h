@@ -68,81 +68,8 @@ struct ExpertTerm {
   const int32_t* order;
   uint32_t most_tiles, pairs, per_row, n_experts;
   size_t stride;   // 16-byte chunks of one expert's matrix
-  void* sums;      // outputs of the plain product, [pairs][N]: blocks of eight (pack_block), from the streaming kernel fp32
+  float* sums;     // outputs of the plain product, [pairs][N]
 };
-
-// Eight sums in 16 bytes: whole numbers of 15 bits, multiples of a power of two that they share, each in the upper bits of a
-// half word; the lowest bits of the eight are that power's exponent, word w has its bits w and w + 4.  Between the products of the way back
-// and their weighted sum, halves a pass over memory and back that is a third of the call with fp32 (4096 tokens of 8 experts, 1376 ->
-// 4096).  A number is off by at most 2^-14 of the largest of its eight (which is 2^13 steps at least, as long as a step is not below
-// 2^-126), where the bf16 result is rounded to 2^-9 of itself.  NaN and the infinities have numbers of their own, so their
-// neighbours are as exact as others.
-constexpr int kBlockMost = 16382, kBlockInf = 16383, kBlockNan = -16384, kBlockLeast = 14;
-__device__ __forceinline__ uint32_t block_bits(uint32_t e, int w) { return (e | e << 12) >> w & 0x00010001u; }
-// The largest magnitude below 2^(e - 126) / (1 + 2^-12), so times 2^(140 - e) it is below kBlockMost, and 2^13 (1 - 2^-12) at least.
-__device__ __forceinline__ uint32_t block_exponent(float top) {
-  return max(__float_as_uint(top * (1.f + 1.f / 4096)) >> 23, (uint32_t)kBlockLeast);
-}
-// lds: the same eight, for those that are not all numbers: a loop, so that this, which stands in an epilogue many times, stays short.
-__device__ __forceinline__ u32x4 pack_block(const float (&y)[8], const float* lds) {
-  float top = 0.f;
-  bool number = true;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(y[i]));
-#pragma unroll
-  for (int i = 0; i < 8; ++i) number = number && y[i] == y[i];   // fmaxf passes over a NaN
-  u32x4 v;
-  if (number && top < INFINITY) {
-    const uint32_t e = block_exponent(top);
-    const float scale = __uint_as_float((140 + 127 - e) << 23);   // 2^(140 - e)
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      // 1.5 2^23 + q has q in its lower bits, rounded to the nearest by the addition
-      const uint32_t lo = __float_as_uint(__builtin_fmaf(y[2 * w], scale, 12582912.f)), hi = __float_as_uint(__builtin_fmaf(y[2 * w + 1], scale, 12582912.f));
-      v[w] = (__builtin_amdgcn_perm(hi, lo, 0x05040100u) << 1 & 0xFFFEFFFEu) | block_bits(e, w);
-    }
-    return v;
-  }
-  top = 0.f;
-#pragma unroll 1
-  for (int i = 0; i < 8; ++i) top = fabsf(lds[i]) < INFINITY ? fmaxf(top, fabsf(lds[i])) : top;
-  const uint32_t e = block_exponent(top);
-  unsigned long long low = 0, high = 0;
-#pragma unroll 1
-  for (int i = 7; i >= 0; --i) {
-    const float f = lds[i];
-    const int q = f != f ? kBlockNan : f == INFINITY ? kBlockInf : f == -INFINITY ? -kBlockInf : (int)rintf(__builtin_amdgcn_ldexpf(f, 140 - (int)e));
-    high = high << 16 | low >> 48;
-    low = low << 16 | ((uint32_t)q << 1 & 0xFFFEu);
-  }
-  v = u32x4{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
-#pragma unroll
-  for (int w = 0; w < 4; ++w) v[w] |= block_bits(e, w);
-  return v;
-}
-// y += weight * the block's sums.
-__device__ __forceinline__ void add_block(const u32x4 v, float weight, float (&y)[8]) {
-  uint32_t x = 0;
-  int q[8], most = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    x |= (v[w] & 0x00010001u) << w;
-    q[2 * w] = (int)(v[w] << 16) >> 17;
-    q[2 * w + 1] = (int)v[w] >> 17;
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) most = max(most, max(q[i], -q[i]));
-  const int e = (int)((x | x >> 12) & 0xFFu);
-  const float scale = __builtin_amdgcn_ldexpf(1.f, e - 140);
-  if (most <= kBlockMost) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(weight, (float)q[i] * scale, y[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      y[i] = __builtin_fmaf(weight, q[i] == kBlockNan ? __builtin_nanf("") : q[i] == kBlockInf ? INFINITY : q[i] == -kBlockInf ? -INFINITY : (float)q[i] * scale, y[i]);
-  }
-}
 
 // An expert by one of its row tiles.  One of no pairs where the plan holds something else than a tile for these sizes: no read leaves the
 // buffers by it.

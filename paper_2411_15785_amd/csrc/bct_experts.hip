@@ -6,12 +6,13 @@
 // Pairs come by expert (the plan of bct_route.hip), in row tiles that belong to one expert each; rows are gathered where they lie.
 // Few pairs an expert: bound by reading the weights of the experts in use once, so a kernel that streams them against
 // 16 rows.  Many: bound by the matrix cores, the kernel of bct_linear_rows.hip with gathered rows, the tiles of an expert side by side
-// on an XCD and of the same size.  The way back leaves each pair's product in fp32, or from tiles of many rows in blocks of eight in 16 bytes
-// (pack_block), and a second kernel weights and adds up those of a token in the order of its slots.
+// on an XCD and of the same size.  The way back leaves each pair's product in fp32, and a second kernel weights and adds up those of a token in
+// the order of its slots.  (Products in 16 bits with a power of two for every eight features took half of that traffic, 4096 tokens below 498 us,
+// but left a feature a thousand times smaller than its neighbour 3 % off.)
 //
 // us in a graph, weights from memory: 32 tokens of 8 in 64 experts, gated 4096 -> 1376 208 (1.42 GB, 6.8 TB/s), back 115 (6.2); 4096 tokens 700 (1.06
-// PFLOP/s; clock 1.6 GHz, matrix cores busy 69 % of the cycles, 2.2 GB from memory; with the weights of one expert for all 607) and 503 (0.73, the sum 65 of
-// them); 777 of 2 in 12, 2080 -> 2048 back 46.  Measured and not kept: lines of weights read ahead into the L2, 4 to 16 K steps (4096 tokens
+// PFLOP/s; clock 1.6 GHz, matrix cores busy 69 % of the cycles, 2.2 GB from memory; with the weights of one expert for all 607) and 586 (0.63, the sum 120 of
+// them); 777 of 2 in 12, 2080 -> 2048 back 47.  Measured and not kept: lines of weights read ahead into the L2, 4 to 16 K steps (4096 tokens
 // 4 to 13 % slower: each line is one more request), six stages of 64 x 128 or 128 x 256 (the same times), weights side by side by groups of 2 to 8 feature
 // tiles (the same), past the caches (4 % slower), rows past the caches (a third slower), four wavefronts of 64 x 128 or 128 x 64 each (the
 // same, 10 % slower), 128 x 128, 64 x 64 and 128 x 64 with K in two parts (slower but for 5 to 15 % at 24 to 64 rows an expert of small matrices), all 16-row tiles
@@ -85,21 +86,20 @@ __global__ __launch_bounds__(64 * WAVES) void expert_few_kernel(const uint16_t* 
     }
     const size_t at = (size_t)expert_pair(T, order, i) * N + n;
     if (SWIGLU) store_elem(out, at, sum[0] / (1.0f + __expf(-sum[0])) * sum[NW2 - 1]);
-    else ((float*)T.sums)[at] = sum[0];
+    else T.sums[at] = sum[0];
   }
 }
 
 // out[r][8 c ..] = residual + the token's products, weighted, in the order of its slots.  A thread has eight features of a token.
-// BLOCKS: products come as blocks of eight (pack_block), else fp32.  S slots are requested at once, whether they have an expert or not: behind a
-// branch they would be waited for one by one.
-template <bool BLOCKS, int S>
-__global__ __launch_bounds__(256) void combine_kernel(const void* sums, const int32_t* expert, const float* weights, const uint16_t* residual,
+// S slots are requested at once, whether they have an expert or not: behind a branch they would be waited for one by one.
+template <int S>
+__global__ __launch_bounds__(256) void combine_kernel(const float* sums, const int32_t* expert, const float* weights, const uint16_t* residual,
                                                       uint16_t* out, uint32_t rows, uint32_t k, uint32_t N) {
   const uint32_t i = blockIdx.x * 256 + threadIdx.x, chunks = N / 8, r = i / chunks, c = i % chunks;
   if (r >= rows) return;
   float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   for (uint32_t s = 0; s < k; s += S) {
-    u32x4 v[S][BLOCKS ? 1 : 2];
+    f32x4 v[S][2];
     int32_t id[S];
     float w[S];
 #pragma unroll
@@ -108,17 +108,13 @@ __global__ __launch_bounds__(256) void combine_kernel(const void* sums, const in
       id[u] = s + u < k ? expert[p] : 0;
       w[u] = weights[p];
 #pragma unroll
-      for (int h = 0; h < (BLOCKS ? 1 : 2); ++h) v[u][h] = ((const u32x4*)sums)[(p * chunks + c) * (BLOCKS ? 1 : 2) + h];
+      for (int h = 0; h < 2; ++h) v[u][h] = ((const f32x4*)sums)[(p * chunks + c) * 2 + h];
     }
 #pragma unroll
     for (int u = 0; u < S; ++u) {
       if (id[u] == 0) continue;   // its product was not computed
-      if constexpr (BLOCKS) {
-        add_block(v[u][0], w[u], y);
-      } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(w[u], __uint_as_float(v[u][e / 4][e % 4]), y[e]);
-      }
+      for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(w[u], v[u][e / 4][e % 4], y[e]);
     }
   }
   if (residual) {
@@ -142,8 +138,9 @@ __global__ __launch_bounds__(256) void combine_kernel(const void* sums, const in
 // mean, with weights from memory.  Measured us, streaming | 64 x 128 | 128 x 256 | 256 x 256, gated K = 4096, N = 1376, 64 experts with a mean
 // of 4: 209 | 240 | 260 | 234; 8: 237 | 251 | 272 | 245; 16: 325 | 260 | 280 | 247; 48: 806 | 297 | 295 | 278; 128: - | 439 | 330 | 332; 512: - | 1232 |
 // 779 | 677.  8 experts, 2048, 1024, mean 4: 12.6 | 19.3 | 32.2 | 29.7; 16: 18.1 | 19.6 | 32.5 | 30.2; 64: 43.0 | 22.2 | 36.8 | 37.4; 192: 110 | 34.1 | 38.6 |
-// 51.0; 384: 208 | 55.5 | 39.0 | 50.4.  The way back (with its sum), 12 experts, 2080 -> 2048, mean 8: 23.2 | 27.1 | 40.2 | 37.9; 32: 42.6 | 30.6 | 43.1 | 43.0;
-// 128: 124 | 46.6 | 51.8 | 62.4; 64 experts, 1376 -> 4096, 128: - | 256 | 212 | 223; 512: - | 715 | 511 | 494.
+// 51.0; 384: 208 | 55.5 | 39.0 | 50.4.  The way back (with its sum), 12 experts, 2080 -> 2048, mean 8: 23.3 | 26.8 | 40.0 | 37.6; 32: 42.7 | 30.2 | 42.8 | 42.3;
+// 128: 124 | 47.9 | 52.8 | 62.1; 64 experts, 1376 -> 4096, 8: 133 | 143 | 142 | 147; 32: 295 | 170 | 161 | 165; 128: - | 274 | 231 | 236; 512: - | 839 | 630 | 586.  8
+// experts, 1376 -> 4096, 750: - | 156 | 131 | 116, where the estimate takes 128 x 256, the most that it is off in 15 shapes of the way back.
 enum ExpertForm { kFew, kRows64, kRows128, kRows256 };   // in the order of kPlanRows
 constexpr uint32_t few_features(bool swiglu) { return swiglu ? 1 : 2; }   // feature tiles of a streaming workgroup
 ExpertForm expert_form(uint32_t pairs, uint32_t E, uint32_t K, uint32_t N, bool swiglu) {
@@ -203,7 +200,7 @@ void launch_rows_of(const void* x, const void* w, const void* w2, void* out, uin
 }
 
 template <bool SWIGLU>
-void launch_products(const void* x, const void* w, const void* w2, void* out, void* sums, const int32_t* plan, uint32_t rows, uint32_t k,
+void launch_products(const void* x, const void* w, const void* w2, void* out, float* sums, const int32_t* plan, uint32_t rows, uint32_t k,
                      uint32_t E, uint32_t K, uint32_t N, hipStream_t s) {
   const ExpertPlan P = ExpertPlan::of(rows, k, E);
   const ExpertForm form = expert_form(P.pairs, E, K, N, SWIGLU);
@@ -275,12 +272,9 @@ bct_status bctm_expert_linear(const void* h, const void* w_packed, const void* p
   if (workspace_bytes < need) return mfail(BCT_ERR_BUFFER_TOO_SMALL, "the workspace is smaller than bctm_expert_workspace says");
   hipStream_t s = (hipStream_t)hip_stream;
   const ExpertPlan P = ExpertPlan::of(rows, k, n_experts);
-  launch_products<false>(h, w_packed, nullptr, nullptr, workspace, (const int32_t*)plan, rows, k, n_experts, K, N, s);
-  const bool blocks = expert_form(P.pairs, n_experts, K, N, false) != kFew;
-  const auto combine = k <= 2   ? (blocks ? combine_kernel<true, 2> : combine_kernel<false, 2>)
-                       : k <= 4 ? (blocks ? combine_kernel<true, 4> : combine_kernel<false, 4>)
-                                : (blocks ? combine_kernel<true, 8> : combine_kernel<false, 8>);
-  hipLaunchKernelGGL(combine, dim3((unsigned)(((uint64_t)rows * (N / 8) + 255) / 256)), dim3(256), 0, s, (const void*)workspace,
+  launch_products<false>(h, w_packed, nullptr, nullptr, (float*)workspace, (const int32_t*)plan, rows, k, n_experts, K, N, s);
+  const auto combine = k <= 2 ? combine_kernel<2> : k <= 4 ? combine_kernel<4> : combine_kernel<8>;
+  hipLaunchKernelGGL(combine, dim3((unsigned)(((uint64_t)rows * (N / 8) + 255) / 256)), dim3(256), 0, s, (const float*)workspace,
                      (const int32_t*)plan + P.expert, weights, (const uint16_t*)residual, (uint16_t*)out, rows, k, N);
   return launched("expert_linear");
 }

@@ -30,14 +30,14 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
     const uint16_t* __restrict__ x, const u32x4* __restrict__ w, const u32x4* __restrict__ w2, const uint16_t* residual,
     LinearOut dst, uint32_t rows, uint32_t K, uint32_t NT, uint32_t out_tiled, TERM... term) {
   constexpr bool kLora = kHas<LoraTerm, TERM...>, kEpilogue = kHas<EpilogueTerm, TERM...>, kExperts = kHas<ExpertTerm, TERM...>;
-  static_assert(!kExperts || (!XT && !PAIR && 64 * WR * WC * KS >= 16 * MI * WR), "gathered rows are row-major; a thread has one");
+  static_assert(!kExperts || (!XT && !PAIR && 64 * WR * WC * KS >= 16 * MI * WR && NJ == 4), "gathered rows are row-major; a thread has one");
   constexpr int NW = WR * WC;                      // wavefronts of a group
   constexpr int TA = MI * WR, TB = NJ * WC, TT = TA + TB;  // 1 KB tiles of a K step: activations, weights
   constexpr int ND = TT / NW, NA = TA / NW, NB = TB / NW;  // of them per wavefront
   static_assert(TA % NW == 0 && TB % NW == 0, "tiles must divide among the wavefronts");
   static_assert(!PAIR || !XT, "tiled activations have no half lines");
   // LDS stages.  Three leave room for two workgroups of 128 x 256 on a compute unit, and one begins and ends under the other's
-  // products: with experts, whose tiles are many, 4096 tokens of 8 in 64 1376 -> 4096 618 -> 550 us, gated 4096 -> 1376 910 -> 858.
+  // products: with experts, whose tiles are many, 4096 tokens of 8 in 64 1376 -> 4096 670 -> 630 us, gated 4096 -> 1376 827 -> 792.
   constexpr int S = kExperts && MI == 4 && NW == 8 ? 3 : 4;
   constexpr bool PING = NW * KS == 8;              // two wavefronts per SIMD that take turns
   constexpr uint32_t HB = 4;                       // row tiles of a band
@@ -343,6 +343,17 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+    if constexpr (kExperts && !SWIGLU) {
+      // Products that wait for their weighted sum stay fp32; sixteen lanes have a row's 256 bytes, so a store fills whole lines.
+#pragma unroll
+      for (int ps = 0; ps < 4; ++ps) {
+        const int rr = ps * 4 + lane / 16;
+        const uint32_t row = ((grp * MO + i) * WR + wr) * 16 + rr, n = nt * BNF + wc * CW + 4 * (lane % 16);
+        if (row < rows && n < dst.start[3])
+          *(f32x4*)(only(term...).sums + (size_t)pair_of[row] * dst.start[3] + n) = *(const f32x4*)&e[rr][4 * (lane % 16)];
+      }
+      continue;
+    }
     const int cc = lane % CPR;
 #pragma unroll kEpilogue || kExperts ? 1 : 16 / RPP
     for (int ps = 0; ps < 16 / RPP; ++ps) {
@@ -372,10 +383,6 @@ __global__ __launch_bounds__(64 * WR * WC * KS, 2) void linear_rows_kernel(
           unpack16<BF16>(*(const u32x4*)(residual + oo), rv);
 #pragma unroll
           for (int k = 0; k < 8; ++k) y[k] += rv[k];
-        }
-        if constexpr (kExperts && !SWIGLU) {
-          ((u32x4*)only(term...).sums)[oo / 8] = pack_block(y, &e[rr][8 * cc]);
-          continue;
         }
         if constexpr (kEpilogue) {
           if (only(term...).out32) {
