@@ -151,7 +151,8 @@ class RefStack:
         if s.router_bias or s.router_sigmoid:
             rank = 1.0 / (1.0 + np.exp(-logits)) if s.router_sigmoid else np.exp(logits) / np.exp(logits).sum(axis=1, keepdims=True)
             if s.router_bias:
-                rank = rank + bf16_to_f64(lw["router_bias"])
+                b = lw["router_bias"]
+                rank = rank + (bf16_to_f64(b) if b.dtype == np.uint16 else b.astype(np.float64))
         taken = np.take_along_axis(rank, choice, axis=1)
         left = rank.copy()
         np.put_along_axis(left, choice, -np.inf, axis=1)

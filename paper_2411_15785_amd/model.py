@@ -771,7 +771,8 @@ class BctStack:
 
     weights: {"embed": [vocab][dim], "final_norm": [dim], "head": [vocab][dim],
               "layers": [ {name: tensor} per layer, names of StackShape.weight_shapes() ],
-              "keys": [ MK per layer, [Hkv][M][d] ]}  -- all bf16 device tensors.
+              "keys": [ MK per layer, [Hkv][M][d] ]}  -- all bf16 device tensors, but router_bias may be float32 (its steps
+              decide between scores closer than bf16 tells apart).
     With shape.head_norm and / or shape.rope_base, q and wq pass bctm_qk_norm_rope before the cache.
     With shape.n_experts each token's MLP is that of the experts a router chooses for it (bctm_linear_act, bctm_route,
     bctm_expert_swiglu, bctm_expert_linear), beside a shared one with shape.shared_ffn.
@@ -796,10 +797,11 @@ class BctStack:
         for l, lw in enumerate(weights["layers"]):
             pl = {}
             for n, shp in s.weight_shapes().items():
-                if tuple(lw[n].shape) != shp or lw[n].dtype != torch.bfloat16:
-                    raise ValueError(f"layer {l} {n}: expected bf16 {shp}")
+                types = (torch.float32, torch.bfloat16) if n == "router_bias" else (torch.bfloat16,)
+                if tuple(lw[n].shape) != shp or lw[n].dtype not in types:
+                    raise ValueError(f"layer {l} {n}: expected {' or '.join(str(t) for t in types)} {shp}")
                 if n == "router_bias":
-                    pl[n] = lw[n].float()
+                    pl[n] = lw[n].float().contiguous()
                 elif len(shp) == 1:
                     pl[n] = lw[n]
                 elif len(shp) == 3:
