@@ -864,6 +864,15 @@ class BctStack:
             self._bufs[k] = torch.empty((rows, cols), dtype=torch.bfloat16, device=self.device)
         return self._bufs[k]
 
+    def _shared(self, name, n, dtype):
+        """n values that calls of any number of rows share, so that prompts of many lengths do not keep a buffer each.  One that has become
+        too small stays with the calls that have it, as a captured step has its address; each is twice the one before it at least, so all
+        together are four times the largest call's at most."""
+        kept = self._bufs.setdefault(("shared", name), [])
+        if not kept or kept[-1].numel() < n:
+            kept.append(_torch().empty(max(n, 2 * kept[-1].numel()) if kept else n, dtype=dtype, device=self.device))
+        return kept[-1][:n]
+
     def _tiled(self, name, rows, cols):
         k = ("tiled", name, rows, cols)
         if k not in self._bufs:
@@ -881,8 +890,10 @@ class BctStack:
                              torch.empty((rows, s.experts_per_token), dtype=torch.int32, device=dev),
                              torch.empty((rows, s.experts_per_token), dtype=torch.float32, device=dev),
                              ExpertPlan(rows, s.experts_per_token, s.n_experts, dev),
-                             torch.empty(bctm_expert_workspace(rows, s.experts_per_token, s.dim), dtype=torch.uint8, device=dev))
-        logits, experts, weights, plan, workspace = self._bufs[k]
+                             # each pair's products on the way back and its gated ones: far more than the rest
+                             self._shared("workspace", bctm_expert_workspace(rows, s.experts_per_token, s.dim), torch.uint8),
+                             self._shared("g", rows * s.experts_per_token * s.ffn, torch.bfloat16).view(rows * s.experts_per_token, s.ffn))
+        logits, experts, weights, plan, workspace, g = self._bufs[k]
         h = bctm_rmsnorm(x, lw["mlp_norm"], s.eps, self._buf("h", rows, s.dim))
         bctm_linear_act(h, lw["w_router"], out=logits)
         bctm_route(logits[:, :s.n_experts], s.experts_per_token, lw.get("router_bias"), s.router_sigmoid, s.router_normalise, s.router_scale,
@@ -890,7 +901,7 @@ class BctStack:
         if s.shared_ffn:
             f = bctm_swiglu(h, lw["w_shared_gate"], lw["w_shared_up"], self._tiled("shared", rows, s.shared_ffn), tiled=True)
             bctm_linear(f, lw["w_shared_down"], x, x)
-        g = bctm_expert_swiglu(h, lw["w_gate"], lw["w_up"], plan, self._buf("g", rows * s.experts_per_token, s.ffn))
+        bctm_expert_swiglu(h, lw["w_gate"], lw["w_up"], plan, g)
         bctm_expert_linear(g, lw["w_down"], plan, weights, x, x, workspace)
 
     def forward(self, ids, T=1, next_ids=None, head="all", positions=None, adapters=None, sampling=None):
@@ -931,7 +942,7 @@ class BctStack:
         lora_ws = self._lora_workspace(rows) if adapters is not None else None
         x = bctm_embed(ids, self.embed, self._buf("x", rows, s.dim))
         # every input of a projection is kept tiled, so that the projections read it in whole kilobytes
-        h, f = self._tiled("h", rows, s.dim), self._tiled("f", rows, s.ffn)
+        h, f = self._tiled("h", rows, s.dim), None if s.n_experts else self._tiled("f", rows, s.ffn)
         q, wq, wv = self._buf("q", rows, s.q_width), self._buf("wq", rows, s.kv_width), self._buf("wv", rows, s.kv_width)
         a = self._buf("a", rows, s.q_width)
         # a chunk's attention output is re-tiled for W_o (the matrix-core kernel reads whole tiles); for the

@@ -1,4 +1,4 @@
-"""Settings of a stack with experts beyond those of test_gpu_expert_stack.py: a selection bias in float32."""
+"""Settings of a stack with experts beyond those of test_gpu_expert_stack.py: a selection bias in float32, and many lengths of chunks."""
 import numpy as np
 import pytest
 import torch
@@ -85,3 +85,58 @@ def test_other_types_of_a_bias_are_refused(M):
         wd["layers"][1]["router_bias"] = torch.zeros(s.n_experts, dtype=bad, device="cuda")
         with pytest.raises(ValueError, match="router_bias"):
             M.BctStack(s, wd)
+
+
+def test_chunks_of_many_lengths_share_the_large_buffers(M):
+    """After a chunk of the longest length, shorter ones take no workspace and no gated rows of their own."""
+    s = M.StackShape(**{**SHAPE, "batch": 8, "ffn": 256})
+    _, wd = weights_of(s)
+    gpu = M.BctStack(s, wd, max_prefill_T=64)
+    run = lambda T: gpu.forward(torch.from_numpy(syn.make_token_ids(31, T, s.batch * T, s.vocab)).cuda(), T=T, head="last")
+    run(64)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    lengths = range(33, 64)
+    for T in lengths:
+        run(T)
+    torch.cuda.synchronize()
+    own = sum(M.bctm_expert_workspace(s.batch * T, s.experts_per_token, s.dim) + 2 * s.batch * T * s.experts_per_token * s.ffn for T in lengths)
+    # seven bf16 rows of a token as wide as the stream and its heads, one tiled, plan, logits and choice: a fifth of the two
+    assert torch.cuda.memory_allocated() - before < own / 2
+
+
+def test_longer_chunks_take_at_most_four_times_the_largest(M):
+    s = M.StackShape(**{**SHAPE, "batch": 8})
+    gpu = M.BctStack(s, weights_of(s)[1], max_prefill_T=64)
+    for T in range(2, 65):
+        gpu.forward(torch.from_numpy(syn.make_token_ids(31, T, s.batch * T, s.vocab)).cuda(), T=T, head="last")
+    kept = gpu._bufs[("shared", "workspace")]
+    assert sum(t.numel() for t in kept) <= 4 * M.bctm_expert_workspace(s.batch * 64, s.experts_per_token, s.dim)
+
+
+def test_a_captured_step_goes_on_after_longer_chunks(M):
+    """The buffers grow between the replays of a decode step, which has the addresses of the smaller ones."""
+    s = M.StackShape(**SHAPE)
+    _, wd = weights_of(s)
+    a, b = M.BctStack(s, wd, max_prefill_T=40), M.BctStack(s, wd, max_prefill_T=40)
+    ids = torch.from_numpy(syn.make_token_ids(31, 0, s.batch, s.vocab)).cuda()
+    eager = ids.clone()
+    step = lambda stack, i: stack.forward(i, next_ids=i)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(a, ids)
+    torch.cuda.current_stream().wait_stream(side)
+    step(b, eager)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        _, logits = step(a, ids)
+    for T in (3, 40, 17, 29):
+        chunk = torch.from_numpy(syn.make_token_ids(31, T, s.batch * T, s.vocab)).cuda()
+        for stack in (a, b):
+            stack.forward(chunk, T=T, head="last")
+        for _ in range(2):
+            g.replay()
+            _, want = step(b, eager)
+            torch.cuda.synchronize()
+            assert torch.equal(logits.view(torch.int16), want.view(torch.int16)) and torch.equal(ids, eager), T
