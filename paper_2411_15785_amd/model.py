@@ -879,8 +879,8 @@ class BctStack:
             self._bufs[k] = TiledRows(rows, cols, self.device)
         return self._bufs[k]
 
-    def _experts(self, x, lw, rows):
-        """x += the experts' (and the shared) MLP of its norm."""
+    def _expert_bufs(self, rows):
+        """(logits, experts, weights, plan, workspace, gated rows) of a step of that many rows."""
         torch = _torch()
         s = self.shape
         k = ("experts", rows)
@@ -893,7 +893,12 @@ class BctStack:
                              # each pair's products on the way back and its gated ones: far more than the rest
                              self._shared("workspace", bctm_expert_workspace(rows, s.experts_per_token, s.dim), torch.uint8),
                              self._shared("g", rows * s.experts_per_token * s.ffn, torch.bfloat16).view(rows * s.experts_per_token, s.ffn))
-        logits, experts, weights, plan, workspace, g = self._bufs[k]
+        return self._bufs[k]
+
+    def _experts(self, x, lw, rows):
+        """x += the experts' (and the shared) MLP of its norm."""
+        s = self.shape
+        logits, experts, weights, plan, workspace, g = self._expert_bufs(rows)
         h = bctm_rmsnorm(x, lw["mlp_norm"], s.eps, self._buf("h", rows, s.dim))
         bctm_linear_act(h, lw["w_router"], out=logits)
         bctm_route(logits[:, :s.n_experts], s.experts_per_token, lw.get("router_bias"), s.router_sigmoid, s.router_normalise, s.router_scale,
@@ -940,6 +945,8 @@ class BctStack:
             if t is not None and (t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous() or t.device != dev):
                 raise ValueError(f"{name}: expected a contiguous {dtype} vector of {n} on {dev}")
         lora_ws = self._lora_workspace(rows) if adapters is not None else None
+        if s.n_experts:
+            self._expert_bufs(rows)
         x = bctm_embed(ids, self.embed, self._buf("x", rows, s.dim))
         # every input of a projection is kept tiled, so that the projections read it in whole kilobytes
         h, f = self._tiled("h", rows, s.dim), None if s.n_experts else self._tiled("f", rows, s.ffn)

@@ -140,3 +140,25 @@ def test_a_captured_step_goes_on_after_longer_chunks(M):
             _, want = step(b, eager)
             torch.cuda.synchronize()
             assert torch.equal(logits.view(torch.int16), want.view(torch.int16)) and torch.equal(ids, eager), T
+
+
+@pytest.mark.parametrize("what", ["ExpertPlan", "bctm_expert_workspace"])
+def test_a_step_whose_buffers_are_not_to_be_had_changes_nothing(M, what, monkeypatch):
+    """The caches take a step's tokens layer by layer: a plan or workspace that is refused has to be refused before."""
+    s = M.StackShape(**SHAPE)
+    _, wd = weights_of(s)
+    a, b = M.BctStack(s, wd, max_prefill_T=9), M.BctStack(s, wd, max_prefill_T=9)
+    chunk = torch.from_numpy(syn.make_token_ids(31, 0, s.batch * 9, s.vocab)).cuda()
+    ids = torch.from_numpy(syn.make_token_ids(31, 1, s.batch, s.vocab)).cuda()
+
+    def refuse(*args):
+        raise MemoryError
+
+    with monkeypatch.context() as m:
+        m.setattr(M, what, refuse)
+        with pytest.raises(MemoryError):
+            a.forward(chunk, T=9)
+    for stack in (a, b):
+        stack.forward(ids)
+    (_, got), (_, want) = a.forward(chunk, T=9), b.forward(chunk, T=9)
+    assert torch.equal(got.view(torch.int16), want.view(torch.int16))
