@@ -714,6 +714,8 @@ class StackShape:
     def __post_init__(self):
         if self.n_experts and (not 1 <= self.experts_per_token <= min(16, self.n_experts) or self.n_experts > 512 or self.shared_ffn % 32):
             raise ValueError("experts_per_token must be 1 to 16 of at most 512 experts, shared_ffn a multiple of 32")
+        if not math.isfinite(ctypes.c_float(self.router_scale).value):
+            raise ValueError("router_scale must be finite in float32")
         if not self.n_experts and (self.experts_per_token or self.router_sigmoid or self.router_bias or self.shared_ffn):
             raise ValueError("experts_per_token, router_sigmoid, router_bias and shared_ffn go with n_experts")
         if (self.head_norm or self.rope_base) and (self.head_dim % 16 or self.rotary_dim % 16 or

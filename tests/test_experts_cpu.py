@@ -128,3 +128,12 @@ def test_python_wrappers_refuse_what_is_not_on_the_gpu():
             f()
     with pytest.raises(model.BctModelError):
         model.ExpertPlan(4, 3, 2, "cpu")
+
+
+@pytest.mark.parametrize("scale", [float("inf"), float("-inf"), float("nan"), 1e39])
+def test_a_stack_refuses_a_scale_that_the_router_would(scale):
+    """With the shape, not in the middle of a step."""
+    shape = dict(n_layers=1, dim=64, n_q_heads=1, n_kv_heads=1, head_dim=64, ffn=64, vocab=64, capacity_M=64, batch=1, n_experts=4, experts_per_token=2)
+    model.StackShape(**shape, router_scale=-2.5)
+    with pytest.raises(ValueError, match="router_scale"):
+        model.StackShape(**shape, router_scale=scale)
