@@ -165,7 +165,7 @@ bct_status bctm_swiglu_lora(const void* x, const void* w_gate_packed, const void
 #define BCTM_ACT_NONE 0u
 #define BCTM_ACT_RELU 1u
 #define BCTM_ACT_SILU 2u      /* y / (1 + exp(-y)) */
-#define BCTM_ACT_GELU 3u      /* y (1 + erf(y / sqrt 2)) / 2 */
+#define BCTM_ACT_GELU 3u      /* y (1 + erf(y / sqrt 2)) / 2, the factor of y within 2e-7 */
 #define BCTM_ACT_GELU_TANH 4u /* y (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))) / 2 */
 #define BCTM_ACT_SIGMOID 5u   /* 1 / (1 + exp(-y)) */
 bct_status bctm_linear_act(const void* x, const void* w_packed, const void* bias, const void* residual, void* out, uint32_t rows,

@@ -140,7 +140,11 @@ __global__ __launch_bounds__(256) void combine_kernel(const float* sums, const i
 // 779 | 677.  8 experts, 2048, 1024, mean 4: 12.6 | 19.3 | 32.2 | 29.7; 16: 18.1 | 19.6 | 32.5 | 30.2; 64: 43.0 | 22.2 | 36.8 | 37.4; 192: 110 | 34.1 | 38.6 |
 // 51.0; 384: 208 | 55.5 | 39.0 | 50.4.  The way back (with its sum), 12 experts, 2080 -> 2048, mean 8: 23.3 | 26.8 | 40.0 | 37.6; 32: 42.7 | 30.2 | 42.8 | 42.3;
 // 128: 124 | 47.9 | 52.8 | 62.1; 64 experts, 1376 -> 4096, 8: 133 | 143 | 142 | 147; 32: 295 | 170 | 161 | 165; 128: - | 274 | 231 | 236; 512: - | 839 | 630 | 586.  8
-// experts, 1376 -> 4096, 750: - | 156 | 131 | 116, where the estimate takes 128 x 256, the most that it is off in 15 shapes of the way back.
+// experts, 1376 -> 4096, 750: - | 156 | 131 | 116, of which the estimate takes 131.  Beyond the sizes of the estimate, 8 experts, gated 4096 -> 14336, mean 8: 291 |
+// 312 | 319 | 322; 64: 1412 | 428 | 367 | 367; 256: - | 964 | 621 | 591; back 8: 147 | 159 | 229 | 202; 64: 659 | 270 | 258 | 257; 256: - | 541 | 468 | 377, of which it
+// takes 468, the most that it was off; 256 experts, gated 7168 -> 2048, mean 8: 2345 | 2364 | 2372 | 2340; 128: - | 4566 | 3366 | 3190.
+// Tokens that share their experts: the streaming kernel reads an expert's weights once for 16 of them, 64 tokens of the same 8 in 64
+// 4096 -> 1376 in 124 us (two forms on, 128 tokens, in 80), where 64 that choose theirs apart take 240.
 enum ExpertForm { kFew, kRows64, kRows128, kRows256 };   // in the order of kPlanRows
 constexpr uint32_t few_features(bool swiglu) { return swiglu ? 1 : 2; }   // feature tiles of a streaming workgroup
 ExpertForm expert_form(uint32_t pairs, uint32_t E, uint32_t K, uint32_t N, bool swiglu) {

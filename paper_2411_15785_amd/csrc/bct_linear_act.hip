@@ -15,7 +15,8 @@ namespace {
 // 16 * RT rows and 64 features of a workgroup; its wavefronts share K, each with row tiles of its own in LDS.  Bound by the address
 // unit of a compute unit: a kilobyte of weights or rows takes 16 cycles of it, but rows read as operands lie, 16 side by side, take
 // 64; so a row's 256 bytes of four K tiles come to LDS whole (chunk c of row r at place c ^ r of its 16, so that an operand read
-// finds its rows in different banks), a round of four ahead of the products.  4096 rows, 4096 -> 64: 12.9 us (33.5 MB of rows are 5.5 at the rate of a
+// finds its rows in different banks), a round of four ahead of the products.  Every second round only: on the path from the loop's break its second
+// half's registers count as unfinished, so at its head the compiler waits for all loads in flight before the next are requested.  4096 rows, 4096 -> 64: 12.9 us (33.5 MB of rows are 5.5 at the rate of a
 // copy); rows as operands lie, the weights straight to registers all the same: 18.
 template <bool XT, int RT>
 __global__ __launch_bounds__(512) void linear_narrow_kernel(const uint16_t* __restrict__ x, const u32x4* __restrict__ w,

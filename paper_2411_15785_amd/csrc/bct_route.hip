@@ -14,7 +14,8 @@
 // 64 at a time by comparing their experts bit by bit.  Few tokens are one block, and one launch.
 //
 // us in a graph, choice and plan: 8 of 64 experts, 1 token 8.9, 64 11.8, 1024 13.2, 16384 16.0; 8 of 256, 16384 tokens 25.7, of sigmoids with a bias 37, of
-// a softmax with one 47; 16 of 512, 4096 tokens 35, 63, 60 (these two spill 125 registers, for the wavefront's part).  A token a wavefront, its k maxima
+// a softmax with one 47; 16 of 512, 4096 tokens 35, 63, 60.  The forms with a bias hold the wavefront's part too and spill: up to
+// 512 experts 193 registers (192 of bf16 logits), up to 256 14 (8).  A token a wavefront, its k maxima
 // over 64 lanes, took 40 for the sigmoids with a bias.  The plan is 13 of 16384 tokens' times, launch included.
 #include <math.h>
 
